@@ -521,6 +521,195 @@ int ifq_wait_selftest(int limit_us, void* stream);
  */
 int ifq_device_status(void* stream, int* status);
 
+/*
+ * ---------------------------------------------------------------------------
+ * The attention block of a quantised decoder.
+ *
+ * The same conventions hold for these calls (status, ownership, streams, no
+ * allocation).  Types of 16- and 32-bit tensors:
+ */
+enum { IFQ_F16 = 1, IFQ_BF16 = 2, IFQ_F32 = 3 };
+
+/*
+ * A paged key/value cache whose entries are held in 4 bits.  A page holds
+ * page_size tokens (a multiple of 16) of every key/value head; the buffer is
+ *   [pages][kv_heads][page_size / 16] groups of 16 tokens,
+ * and a group of head size D (64, 128 or 256) has 16 * D + 128 bytes:
+ *   K codes (8 * D bytes), V codes (8 * D bytes),
+ *   K parameters, V parameters: 16 pairs (scale, min) of IEEE half each.
+ * The value of a code is code * scale + min, with one pair per token and head.
+ * Codes are 4-bit fields as everywhere in the library, the lower-numbered of
+ * two in the low half of their byte.  With DB = min(D, 128), K codes are
+ * [D / DB][16 tokens][DB]; V codes are [D / DB][2][8][4][DB / 32][2][4] with
+ * token = 8 * (2nd axis) + 2 * (4th) + (6th) and dimension = DB / 8 * (3rd) +
+ * 4 * (5th) + (7th) of its block, so that a 32-bit word holds the same four
+ * dimensions of two neighbouring tokens.
+ * The caller owns the buffer (16-byte aligned); a page is contiguous, so pages
+ * can be copied or moved as bytes.  A slot is page * page_size + offset.
+ */
+typedef struct {
+  int pages;
+  int page_size;
+  int kv_heads;
+  int head_dim;
+} ifq_kv4_cache;
+
+/* Bytes of the cache's buffer (host, pure). */
+int ifq_kv4_cache_bytes(const ifq_kv4_cache* c, size_t* bytes);
+
+/* Rotation of the positions: none, pairs (i, i + rot_dim/2), or pairs (2i, 2i + 1). */
+enum { IFQ_ROPE_NONE = 0, IFQ_ROPE_HALVES = 1, IFQ_ROPE_PAIRS = 2 };
+
+/*
+ * New tokens of ifq_kv4_append and ifq_kv4_read.  Rows of q, k, v and q_out
+ * are tokens; within a row the heads are contiguous, [heads][head_dim]; the
+ * strides count elements from row to row (0: rows are dense), so that q, k and
+ * v may be parts of one projection's rows.  dtype is IFQ_F16 or IFQ_BF16.
+ * rot_dim: the rotated dimensions of a head, the first ones, a multiple of 16
+ * (<= head_dim; ignored for IFQ_ROPE_NONE); positions: rows of the cos and sin
+ * tables.  tokens may be 0.  Strides are multiples of 8 elements and at least
+ * a row's width (IFQ_EINVAL otherwise).
+ */
+typedef struct {
+  ifq_kv4_cache cache;
+  int tokens;
+  int q_heads;
+  int dtype;
+  int rope;
+  int rot_dim;
+  int positions;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+} ifq_kv4_append_desc;
+
+/*
+ * ifq_kv4_append -- rotate q and k by their positions, quantise k and v to 4
+ * bits and write them into the cache.  For a token at position p with table
+ * rows cos[p], sin[p] (float [positions][rot_dim/2]), each rotated pair (a, b)
+ * becomes (a*cos - b*sin, b*cos + a*sin); q is rounded to dtype and written to
+ * q_out (which may be q).  Each head's row of k (rotated) and of v is
+ * quantised by itself: with the row clamped to +-65504,
+ *   min = half(smallest), scale = half((largest - smallest) * single(1/15)),
+ *   code = clamp(rint((x - min) / scale), 0, 15), or 0 where scale is 0.
+ * All of it in IEEE single, rounded operation by operation in the order
+ * written (no fused multiply-add), so the codes are those of any program that
+ * does the same.  A NaN in a row makes both its parameters NaN.
+ * q (device): may be NULL, then q_out is not written.  positions (device):
+ * int32 [tokens] (not read for IFQ_ROPE_NONE).  slots (device): int64
+ * [tokens]; a negative slot leaves the cache as it is (padding tokens).  No
+ * two tokens of a call may have the same slot.
+ * Device-side checks: a slot past the cache or a position outside the tables
+ * sets IFQ_ERANGE (ifq_device_status) and that token is skipped.
+ * Pointers are 16-byte aligned (positions and tables 4, slots 8).
+ */
+int ifq_kv4_append(const ifq_kv4_append_desc* d, const void* q, const void* k, const void* v, const float* cos,
+                   const float* sin, const int32_t* positions, const int64_t* slots, void* q_out, void* cache,
+                   void* stream);
+
+/*
+ * ifq_kv4_read -- the values that the cache holds at `slots` (device, int64
+ * [tokens]): code * scale + min in IEEE single, rounded to dtype, into k_out
+ * and v_out (device, dense rows [tokens][kv_heads][head_dim]; either may be
+ * NULL).  Uses cache, tokens and dtype of the descriptor.  A negative slot
+ * reads as zeros; one past the cache too, and sets IFQ_ERANGE.
+ */
+int ifq_kv4_read(const ifq_kv4_append_desc* d, const void* cache, const int64_t* slots, void* k_out, void* v_out,
+                 void* stream);
+
+/*
+ * Attention of new tokens' queries over the cache.  seqs sequences; sequence s
+ * has lens[s] tokens in the cache (its new ones included), token j of it in
+ * page page_table[s][j / page_size], row j % page_size.  Its queries are rows
+ * q_starts[s] .. q_starts[s+1]-1 of q (n_s of them; q_starts NULL: row s
+ * alone) and sit at its last n_s positions.  Query head h reads key/value head
+ * h / (q_heads / kv_heads).  A query at position p sees the tokens j <= p, or
+ * with window > 0 those with j > p - window or j < sinks.
+ * q_tokens: rows of q; max_q: no sequence has more queries than this;
+ * max_pages: entries of a row of page_table; max_len: no sequence is longer
+ * (0: max_pages * page_size).  max_q and max_len choose the kernel and its
+ * launch shape.  Strides of q and out as in ifq_kv4_append_desc.
+ */
+typedef struct {
+  ifq_kv4_cache cache;
+  int seqs;
+  int q_tokens;
+  int max_q;
+  int max_pages;
+  int max_len;
+  int q_heads;
+  int dtype;
+  float scale;
+  int window;
+  int sinks;
+  int64_t q_stride, out_stride;
+} ifq_kv4_attention_desc;
+
+/* Device workspace of ifq_kv4_attention for `d` (host; the current device's, or a full GB300's where there is none). */
+int ifq_kv4_attention_workspace_bytes(const ifq_kv4_attention_desc* d, size_t* bytes);
+
+/*
+ * ifq_kv4_attention -- out = softmax(scale * q K^T) V over the visible tokens,
+ * with K and V the values the cache holds.  Codes enter the products as exact
+ * numbers; scales, minima, sums and the softmax are in IEEE single.
+ * out (device): [q_tokens] rows of [q_heads][head_dim], dtype.  lse (device,
+ * may be NULL): float [q_tokens][q_heads], the log of the softmax's sum.  A
+ * query that sees nothing gives zeros and -infinity.
+ * page_table (device): int32 [seqs][max_pages]; lens (device): int32 [seqs];
+ * q_starts (device): int32 [seqs + 1], ascending, or NULL.  Entries of
+ * page_table past a sequence's length are not read, nor are tokens past it.
+ * Device-side checks: a length that is negative or past the table's row,
+ * q_starts out of order or past q_tokens, or more queries than max_q set
+ * IFQ_ERANGE and leave that sequence's rows unwritten; a page past the cache
+ * sets IFQ_ERANGE and its values are undefined.
+ * ws (device): ifq_kv4_attention_workspace_bytes bytes, 16-byte aligned; calls
+ * in flight at the same time must not share it.  Results do not depend on
+ * what it holds, nor on timing.
+ */
+int ifq_kv4_attention(const ifq_kv4_attention_desc* d, const void* q, const void* cache, const int32_t* page_table,
+                      const int32_t* lens, const int32_t* q_starts, void* out, float* lse, void* ws, size_t ws_bytes,
+                      void* stream);
+
+/*
+ * Product with operands in e4m3 and a float scale for each block of 128:
+ *   out[i][j] = sum over blocks b of  x_scale[b][i] * w_scale[j / 128][b] *
+ *               sum over k in block b of x[i][k] * w[j][k]
+ * x: [m][k] e4m3, w: [n][k] e4m3 (dense rows), x_scale: float [ceil(k/128)][m],
+ * w_scale: float [ceil(n/128)][ceil(k/128)].  The last block may hold fewer
+ * than 128.  k is a multiple of 16 (IFQ_ESHAPE otherwise); m may be 0.
+ * dtype: type of the activations that ifq_fp8_quantize reads (IFQ_F16 or
+ * IFQ_BF16), with x_stride elements from row to row (0: dense; a multiple of
+ * 8).  out_dtype: IFQ_F16, IFQ_BF16 or IFQ_F32, with out_stride elements from
+ * row to row (0: dense).
+ */
+typedef struct {
+  int m, n, k;
+  int dtype;
+  int out_dtype;
+  int64_t x_stride, out_stride;
+} ifq_fp8_desc;
+
+/*
+ * ifq_fp8_quantize -- activations to e4m3 with a scale per row and block of
+ * 128 along k: scale = largest |x| of the block * single(1/448), code =
+ * e4m3(x / scale) (nearest even), 0 where scale is 0, in IEEE single.  x (device): [m][k]
+ * dtype; codes (device): [m][k] bytes; scales (device): float
+ * [ceil(k/128)][m].  A NaN or an infinity in a block makes its scale NaN or
+ * infinite, and with it the products of that row's block.
+ */
+int ifq_fp8_quantize(const ifq_fp8_desc* d, const void* x, void* codes, float* scales, void* stream);
+
+/* Device workspace of ifq_fp8_matmul for `d` (host); may be 0. */
+int ifq_fp8_workspace_bytes(const ifq_fp8_desc* d, size_t* bytes);
+
+/*
+ * ifq_fp8_matmul -- the product above.  Products and their sums within a block
+ * are the tensor cores' in IEEE single, the scaled blocks are added in IEEE
+ * single, and the sum is rounded once to out_dtype.  All pointers are device
+ * pointers, 16-byte aligned (scales 4; out 16, and out rows start on a multiple
+ * of their element).
+ */
+int ifq_fp8_matmul(const ifq_fp8_desc* d, const void* x, const float* x_scale, const void* w, const float* w_scale,
+                   void* out, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

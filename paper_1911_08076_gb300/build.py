@@ -2,7 +2,7 @@
 
     python -m paper_1911_08076_gb300.build        # or build() from Python
 
-The two translation units compile in parallel; the result is
+The translation units compile in parallel; the result is
 paper_1911_08076_gb300/_build/libifq.so.
 """
 from __future__ import annotations
@@ -32,7 +32,8 @@ def _nvcc() -> str:
 
 
 def _sources():
-    return [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC))] + [os.path.join(INCLUDE, "ifq.h")]
+    return [os.path.join(d, f) for d, _, names in sorted(os.walk(CSRC)) for f in sorted(names)] + \
+        [os.path.join(INCLUDE, "ifq.h")]
 
 
 def _stale() -> bool:
@@ -68,10 +69,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = _nvcc()
     tag = f"{os.getpid()}"
     o_cu = os.path.join(OUT, f"ifq_api.{tag}.o")
+    o_lm = os.path.join(OUT, f"lm_api.{tag}.o")
     o_cpp = os.path.join(OUT, f"ifq_host.{tag}.o")
+    cu = [nvcc, *ARCH, "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC,
+          "-Xptxas", "-v", "-c"]
     cmds = [
-        [nvcc, *ARCH, "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC,
-         "-Xptxas", "-v", "-c", os.path.join(CSRC, "ifq_api.cu"), "-o", o_cu],
+        [*cu, os.path.join(CSRC, "ifq_api.cu"), "-o", o_cu],
+        [*cu, os.path.join(CSRC, "lm", "lm_api.cu"), "-o", o_lm],
         ["g++", "-O2", "-std=c++17", "-fPIC", "-ffp-contract=off", "-fno-fast-math", "-I", INCLUDE, "-c",
          os.path.join(CSRC, "ifq_host.cpp"), "-o", o_cpp],
     ]
@@ -82,16 +86,16 @@ def build(force: bool = False, verbose: bool = False) -> str:
             raise RuntimeError(f"build failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
         return r.stdout + r.stderr
 
-    with ThreadPoolExecutor(2) as ex:
+    with ThreadPoolExecutor(len(cmds)) as ex:
         logs = list(ex.map(run, cmds))
-    spilled = spilling_kernels(logs[0])
+    spilled = spilling_kernels(logs[0] + logs[1])
     if spilled:
         raise RuntimeError("tensor-core kernels spill registers to local memory: " + ", ".join(spilled))
     tmp = LIB + f".{tag}.tmp"
     cudalib = os.path.join(os.path.dirname(os.path.dirname(nvcc)), "lib64")
-    run([nvcc, *ARCH, "-shared", "-cudart", "shared", o_cu, o_cpp, "-Xlinker", f"-rpath={cudalib}", "-o", tmp])
+    run([nvcc, *ARCH, "-shared", "-cudart", "shared", o_cu, o_lm, o_cpp, "-Xlinker", f"-rpath={cudalib}", "-o", tmp])
     os.replace(tmp, LIB)
-    for o in (o_cu, o_cpp):
+    for o in (o_cu, o_lm, o_cpp):
         os.remove(o)
     if verbose:
         sys.stdout.write("".join(logs))

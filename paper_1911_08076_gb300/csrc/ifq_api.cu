@@ -24,6 +24,8 @@
 #include "conv_warp.cuh"
 #include "conv_win.cuh"
 #include "ifq.h"
+#include "launch.cuh"
+#include "lm/lm_api.h"
 #include "pool_pack.cuh"
 #include "selftest.cuh"
 #include "stack_tc.cuh"
@@ -38,83 +40,12 @@ constexpr int kMaxK = 65536;
 // largest magnitude at which exactness has been checked on GB300 with adversarial inputs
 // (accumulators near the bound with odd addends all along K).
 constexpr int kTcMaxAcc = 3 * 65536;
-constexpr int kMaxDevices = 64;
-
-inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
-inline size_t round_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
-inline cudaStream_t S(void* s) { return (cudaStream_t)s; }
 
 // Guards the per-device state below (kernel attributes, SM count, occupancy lookups, the address
 // of the no-allocation scratch array).
 std::mutex g_dev_mu;
 
-// ---------------------------------------------------------------- driver entry point for TMA descriptors
-
-PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
-std::once_flag g_encode_once;
-
-bool get_encode() {
-  std::call_once(g_encode_once, [] {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) ==
-            cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      g_encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
-  });
-  return g_encode != nullptr;
-}
-
 // ---------------------------------------------------------------- kernel instances
-
-// Programmatic dependent launch (on unless IFQ_PDL=0): a kernel may start its
-// prologue while the previous kernel in the stream finishes; every kernel here
-// waits (griddepcontrol.wait) before it touches global memory.
-bool pdl_enabled() {
-  static const bool on = [] {
-    const char* v = getenv("IFQ_PDL");
-    return !(v && v[0] == '0');
-  }();
-  return on;
-}
-
-template <typename... Exp, typename... Act>
-cudaError_t launch_k(void (*kern)(Exp...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Act&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, std::forward<Act>(args)...);
-}
-
-// A launch in clusters of `cluster` CTAs along x (grid.x a multiple of it), with programmatic
-// dependent launch as in launch_k.
-template <typename... Exp, typename... Act>
-cudaError_t launch_k_cluster(void (*kern)(Exp...), int cluster, dim3 grid, dim3 block, size_t smem, cudaStream_t st,
-                             Act&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = (unsigned)cluster;
-  at[1].val.clusterDim.y = 1;
-  at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kern, std::forward<Act>(args)...);
-}
 
 // One instance of the tensor-core kernel.  KS > 1 (split K over clusters of KS CTAs): the grid is
 // as many clusters as can be resident at once (cudaOccupancyMaxActiveClusters), at most one per
@@ -2150,9 +2081,11 @@ int ifq_wait_selftest(int limit_us, void* stream) {
 int ifq_device_status(void* stream, int* status) {
   if (!status) return IFQ_EINVAL;
   if (cudaStreamSynchronize(S(stream)) != cudaSuccess) return IFQ_ECUDA;
-  int v = 0, zero = 0;
+  int v = 0, lm = 0, zero = 0;
   if (cudaMemcpyFromSymbol(&v, ifq::g_status, sizeof(int)) != cudaSuccess) return IFQ_ECUDA;
   if (v != 0 && cudaMemcpyToSymbol(ifq::g_status, &zero, sizeof(int)) != cudaSuccess) return IFQ_ECUDA;
+  if (lm_take_status(&lm) != IFQ_OK) return IFQ_ECUDA;
+  if (v == 0) v = lm;
   *status = v;
   return IFQ_OK;
 }

@@ -1,0 +1,283 @@
+// C ABI entry points of the attention block of a quantised decoder: the paged 4-bit key/value cache,
+// attention over it, and products in e4m3 with block scales.
+#include "lm_api.h"
+
+#include <cmath>
+#include <climits>
+
+#include "../launch.cuh"
+#include "fp8.cuh"
+#include "ifq.h"
+#include "kv4.cuh"
+#include "kv4_attention.cuh"
+
+namespace {
+
+using namespace ifq;
+
+inline bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+inline int done(cudaError_t e) { return e == cudaSuccess ? IFQ_OK : IFQ_ECUDA; }
+inline bool is16(int dtype) { return dtype == IFQ_F16 || dtype == IFQ_BF16; }
+
+// The kernel instance of a head size and type: f(head size, bfloat16) with both as types.
+template <int D, typename F>
+int by_type(int dtype, F&& f) {
+  return dtype == IFQ_BF16 ? f(std::integral_constant<int, D>(), std::true_type())
+                           : f(std::integral_constant<int, D>(), std::false_type());
+}
+template <typename F>
+int by_head(int head_dim, int dtype, F&& f) {
+  switch (head_dim) {
+    case 64: return by_type<64>(dtype, f);
+    case 128: return by_type<128>(dtype, f);
+    default: return by_type<256>(dtype, f);
+  }
+}
+
+int check_cache(const ifq_kv4_cache* c, size_t* bytes) {
+  if (c->pages < 1 || c->page_size < 1 || c->kv_heads < 1 || c->head_dim < 1) return IFQ_EINVAL;
+  if (c->page_size % kKvGroup != 0) return IFQ_ESHAPE;
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return IFQ_EUNSUPPORTED;
+  // (sizes are ints: the product of three, and of the fourth, is checked against overflow)
+  const double b = (double)c->pages * c->page_size * c->kv_heads * (c->head_dim + 8);
+  if (b > 4e18 || (double)c->pages * c->page_size > 4e18 || c->kv_heads > 65536) return IFQ_ERANGE;
+  *bytes = (size_t)c->pages * c->kv_heads * (c->page_size / kKvGroup) * kv4_group_bytes(c->head_dim);
+  return IFQ_OK;
+}
+
+// A row stride in elements (0: dense): at least a row, in units of 16 bytes of a 16-bit type.
+int stride_of(int64_t given, long long width, long long* out) {
+  if (given < 0 || (given != 0 && (given < width || given % 8 != 0))) return IFQ_EINVAL;
+  *out = given ? given : width;
+  return IFQ_OK;
+}
+
+KvCacheArgs cache_args(const ifq_kv4_cache& c, const void* p) {
+  KvCacheArgs a;
+  a.p = (uint8_t*)p;
+  a.slots = (long long)c.pages * c.page_size;
+  a.page_size = c.page_size;
+  a.kv_heads = c.kv_heads;
+  return a;
+}
+
+}  // namespace
+
+namespace ifq {
+
+int lm_take_status(int* status) {
+  int v = 0, zero = 0;
+  if (cudaMemcpyFromSymbol(&v, g_status, sizeof(int)) != cudaSuccess) return IFQ_ECUDA;
+  if (v != 0 && cudaMemcpyToSymbol(g_status, &zero, sizeof(int)) != cudaSuccess) return IFQ_ECUDA;
+  *status = v;
+  return IFQ_OK;
+}
+
+}  // namespace ifq
+
+extern "C" {
+
+int ifq_kv4_cache_bytes(const ifq_kv4_cache* c, size_t* bytes) {
+  if (!c || !bytes) return IFQ_EINVAL;
+  return check_cache(c, bytes);
+}
+
+int ifq_kv4_append(const ifq_kv4_append_desc* d, const void* q, const void* k, const void* v, const float* cos,
+                   const float* sin, const int32_t* positions, const int64_t* slots, void* q_out, void* cache,
+                   void* stream) {
+  if (!d) return IFQ_EINVAL;
+  size_t bytes;
+  int rc = check_cache(&d->cache, &bytes);
+  if (rc) return rc;
+  const int D = d->cache.head_dim;
+  if (d->tokens < 0 || d->q_heads < 0 || !is16(d->dtype)) return IFQ_EINVAL;
+  if (d->q_heads > 65536) return IFQ_ERANGE;
+  if (d->rope != IFQ_ROPE_NONE && d->rope != IFQ_ROPE_HALVES && d->rope != IFQ_ROPE_PAIRS) return IFQ_EINVAL;
+  if (d->rope != IFQ_ROPE_NONE && (d->rot_dim < 16 || d->rot_dim > D || d->rot_dim % 16 != 0)) return IFQ_ESHAPE;
+  if (d->rope != IFQ_ROPE_NONE && d->positions < 1) return IFQ_EINVAL;
+  KvAppendArgs a = {};
+  if ((rc = stride_of(d->q_stride, (long long)d->q_heads * D, &a.q_stride))) return rc;
+  if ((rc = stride_of(d->q_out_stride, (long long)d->q_heads * D, &a.q_out_stride))) return rc;
+  if ((rc = stride_of(d->k_stride, (long long)d->cache.kv_heads * D, &a.k_stride))) return rc;
+  if ((rc = stride_of(d->v_stride, (long long)d->cache.kv_heads * D, &a.v_stride))) return rc;
+  if (!k || !v || !slots || !cache || (q && (!q_out || d->q_heads < 1))) return IFQ_EINVAL;
+  if (d->rope != IFQ_ROPE_NONE && (!cos || !sin || !positions)) return IFQ_EINVAL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q ? q_out : nullptr) || !aligned16(cache) ||
+      !aligned(slots, 8) || !aligned(cos, 4) || !aligned(sin, 4) || !aligned(positions, 4))
+    return IFQ_EALIGN;
+  a.cache = cache_args(d->cache, cache);
+  a.q = (const uint16_t*)q;
+  a.k = (const uint16_t*)k;
+  a.v = (const uint16_t*)v;
+  a.q_out = (uint16_t*)q_out;
+  a.cos = cos;
+  a.sin = sin;
+  a.pos = positions;
+  a.slots = slots;
+  a.tokens = d->tokens;
+  a.q_heads = q ? d->q_heads : 0;
+  a.rope = d->rope;
+  a.rot = d->rot_dim;
+  a.positions = d->positions;
+  const long long items = (long long)d->tokens * (a.q_heads + 2 * d->cache.kv_heads);
+  const long long blocks = (items + kAppendWarps - 1) / kAppendWarps;
+  if (blocks > INT_MAX) return IFQ_ERANGE;
+  if (!blocks) return IFQ_OK;
+  return by_head(D, d->dtype, [&](auto dim, auto bf) {
+    return done(launch_k(kv4_append_kernel<decltype(dim)::value, decltype(bf)::value>, dim3((unsigned)blocks),
+                         dim3(32 * kAppendWarps), 0, S(stream), a));
+  });
+}
+
+int ifq_kv4_read(const ifq_kv4_append_desc* d, const void* cache, const int64_t* slots, void* k_out, void* v_out,
+                 void* stream) {
+  if (!d) return IFQ_EINVAL;
+  size_t bytes;
+  int rc = check_cache(&d->cache, &bytes);
+  if (rc) return rc;
+  if (d->tokens < 0 || !is16(d->dtype) || !cache || !slots) return IFQ_EINVAL;
+  if (!aligned16(cache) || !aligned16(k_out) || !aligned16(v_out) || !aligned(slots, 8)) return IFQ_EALIGN;
+  const long long blocks = ((long long)d->tokens * 2 * d->cache.kv_heads + kAppendWarps - 1) / kAppendWarps;
+  if (blocks > INT_MAX) return IFQ_ERANGE;
+  if (!blocks || (!k_out && !v_out)) return IFQ_OK;
+  KvReadArgs a;
+  a.cache = cache_args(d->cache, cache);
+  a.slots = slots;
+  a.k_out = (uint16_t*)k_out;
+  a.v_out = (uint16_t*)v_out;
+  a.tokens = d->tokens;
+  return by_head(d->cache.head_dim, d->dtype, [&](auto dim, auto bf) {
+    return done(launch_k(kv4_read_kernel<decltype(dim)::value, decltype(bf)::value>, dim3((unsigned)blocks),
+                         dim3(32 * kAppendWarps), 0, S(stream), a));
+  });
+}
+
+static int check_attention(const ifq_kv4_attention_desc* d, KvAttnArgs* a) {
+  if (!d) return IFQ_EINVAL;
+  size_t bytes;
+  int rc = check_cache(&d->cache, &bytes);
+  if (rc) return rc;
+  if (d->seqs < 0 || d->q_tokens < 0 || d->max_q < 0 || d->max_pages < 0 || d->max_len < 0 || d->q_heads < 1 ||
+      d->window < 0 || d->sinks < 0 || !is16(d->dtype) || !std::isfinite(d->scale))
+    return IFQ_EINVAL;
+  if (d->q_heads % d->cache.kv_heads != 0) return IFQ_ESHAPE;
+  if (d->q_heads > 65536 || (long long)d->max_pages * d->cache.page_size > INT_MAX) return IFQ_ERANGE;
+  const long long width = (long long)d->q_heads * d->cache.head_dim;
+  if ((rc = stride_of(d->q_stride, width, &a->q_stride))) return rc;
+  if ((rc = stride_of(d->out_stride, width, &a->out_stride))) return rc;
+  a->pages = d->cache.pages;
+  a->page_size = d->cache.page_size;
+  a->kv_heads = d->cache.kv_heads;
+  a->seqs = d->seqs;
+  a->q_tokens = d->q_tokens;
+  a->max_q = d->max_q;
+  a->max_pages = d->max_pages;
+  a->q_heads = d->q_heads;
+  a->group = d->q_heads / d->cache.kv_heads;
+  a->window = d->window;
+  a->sinks = d->sinks;
+  a->scale = d->scale;
+  return IFQ_OK;
+}
+
+int ifq_kv4_attention_workspace_bytes(const ifq_kv4_attention_desc* d, size_t* bytes) {
+  if (!bytes) return IFQ_EINVAL;
+  KvAttnArgs a = {};
+  const int rc = check_attention(d, &a);
+  if (rc) return rc;
+  *bytes = 0;
+  return IFQ_OK;
+}
+
+int ifq_kv4_attention(const ifq_kv4_attention_desc* d, const void* q, const void* cache, const int32_t* page_table,
+                      const int32_t* lens, const int32_t* q_starts, void* out, float* lse, void* ws, size_t ws_bytes,
+                      void* stream) {
+  KvAttnArgs a = {};
+  const int rc = check_attention(d, &a);
+  if (rc) return rc;
+  if (!q || !cache || !lens || !out || (!page_table && d->max_pages > 0)) return IFQ_EINVAL;
+  if (!q_starts && (d->q_tokens != d->seqs)) return IFQ_ESHAPE;
+  if (!aligned16(q) || !aligned16(cache) || !aligned16(out) || !aligned(page_table, 4) || !aligned(lens, 4) ||
+      !aligned(q_starts, 4) || !aligned(lse, 4) || !aligned16(ws))
+    return IFQ_EALIGN;
+  a.q = (const uint16_t*)q;
+  a.cache = (const uint8_t*)cache;
+  a.table = page_table;
+  a.lens = lens;
+  a.starts = q_starts;
+  a.out = (uint16_t*)out;
+  a.lse = lse;
+  (void)ws_bytes;
+  const long long blocks = ((long long)d->q_tokens * d->q_heads + kAttnWarps - 1) / kAttnWarps;
+  if (blocks > INT_MAX) return IFQ_ERANGE;
+  if (!blocks || !d->seqs) return IFQ_OK;
+  return by_head(d->cache.head_dim, d->dtype, [&](auto dim, auto bf) {
+    return done(launch_k(kv4_attention_kernel<decltype(dim)::value, decltype(bf)::value>, dim3((unsigned)blocks),
+                         dim3(32 * kAttnWarps), 0, S(stream), a));
+  });
+}
+
+static int check_fp8(const ifq_fp8_desc* d) {
+  if (!d) return IFQ_EINVAL;
+  if (d->m < 0 || d->n < 1 || d->k < 1) return IFQ_EINVAL;
+  if (d->k % 16 != 0) return IFQ_ESHAPE;
+  return IFQ_OK;
+}
+
+int ifq_fp8_quantize(const ifq_fp8_desc* d, const void* x, void* codes, float* scales, void* stream) {
+  int rc = check_fp8(d);
+  if (rc) return rc;
+  Fp8QuantArgs a;
+  if (!is16(d->dtype)) return IFQ_EINVAL;
+  if ((rc = stride_of(d->x_stride, d->k, &a.x_stride))) return rc;
+  if (!x || !codes || !scales) return IFQ_EINVAL;
+  if (!aligned16(x) || !aligned16(codes) || !aligned(scales, 4)) return IFQ_EALIGN;
+  a.x = (const uint16_t*)x;
+  a.codes = (uint8_t*)codes;
+  a.scales = scales;
+  a.m = d->m;
+  a.k = d->k;
+  a.kb = ceil_div(d->k, kFp8Block);
+  const long long blocks = ((long long)a.m * a.kb + kFp8QuantWarps - 1) / kFp8QuantWarps;
+  if (blocks > INT_MAX) return IFQ_ERANGE;
+  if (!blocks) return IFQ_OK;
+  return done(d->dtype == IFQ_BF16 ? launch_k(fp8_quantize_kernel<true>, dim3((unsigned)blocks), dim3(32 * kFp8QuantWarps), 0, S(stream), a)
+                                   : launch_k(fp8_quantize_kernel<false>, dim3((unsigned)blocks), dim3(32 * kFp8QuantWarps), 0, S(stream), a));
+}
+
+int ifq_fp8_workspace_bytes(const ifq_fp8_desc* d, size_t* bytes) {
+  if (!bytes) return IFQ_EINVAL;
+  const int rc = check_fp8(d);
+  if (rc) return rc;
+  *bytes = 0;
+  return IFQ_OK;
+}
+
+int ifq_fp8_matmul(const ifq_fp8_desc* d, const void* x, const float* x_scale, const void* w, const float* w_scale,
+                   void* out, void* ws, size_t ws_bytes, void* stream) {
+  const int rc = check_fp8(d);
+  if (rc) return rc;
+  if (!is16(d->out_dtype) && d->out_dtype != IFQ_F32) return IFQ_EINVAL;
+  if (d->out_stride < 0 || (d->out_stride != 0 && d->out_stride < d->n)) return IFQ_EINVAL;
+  if (!x || !x_scale || !w || !w_scale || !out) return IFQ_EINVAL;
+  if (!aligned16(x) || !aligned16(w) || !aligned16(out) || !aligned16(ws) || !aligned(x_scale, 4) || !aligned(w_scale, 4))
+    return IFQ_EALIGN;
+  (void)ws_bytes;
+  Fp8Args a;
+  a.x = (const uint8_t*)x;
+  a.w = (const uint8_t*)w;
+  a.xs = x_scale;
+  a.ws = w_scale;
+  a.out = out;
+  a.out_stride = d->out_stride ? d->out_stride : d->n;
+  a.m = d->m;
+  a.n = d->n;
+  a.k = d->k;
+  a.kb = ceil_div(d->k, kFp8Block);
+  a.out_type = d->out_dtype;
+  if (ceil_div(d->m, 64) > 65535) return IFQ_ERANGE;
+  if (!d->m) return IFQ_OK;
+  return done(launch_k(fp8_matmul_kernel, dim3(ceil_div(d->n, 64), ceil_div(d->m, 64)), dim3(256), 0, S(stream), a));
+}
+
+}  // extern "C"

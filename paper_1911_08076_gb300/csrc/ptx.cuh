@@ -9,8 +9,8 @@
 
 namespace ifq {
 
-// Device status word (first error wins).  Read and cleared by ifq_device_status.
-__device__ int g_status;
+// Device status word of the translation unit (first error wins).  Read and cleared by ifq_device_status.
+static __device__ int g_status;
 
 __device__ __forceinline__ void set_status(int s) { atomicCAS(&g_status, 0, s); }
 

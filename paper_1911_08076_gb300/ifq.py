@@ -24,6 +24,8 @@ IFQ_OUT_CODES, IFQ_OUT_ACC, IFQ_OUT_BOTH = 1, 2, 3
 IFQ_PATH_AUTO, IFQ_PATH_TC, IFQ_PATH_BITSERIAL, IFQ_PATH_DIRECT, IFQ_PATH_WIN, IFQ_PATH_WARP = 0, 1, 2, 3, 4, 5
 IFQ_LAYER_CONV, IFQ_LAYER_POOL, IFQ_LAYER_FIXED = 1, 2, 3
 IFQ_FORWARD_LAYERS, IFQ_FORWARD_PERSISTENT = 1, 2
+IFQ_F16, IFQ_BF16, IFQ_F32 = 1, 2, 3
+IFQ_ROPE_NONE, IFQ_ROPE_HALVES, IFQ_ROPE_PAIRS = 0, 1, 2
 
 
 class IfqError(RuntimeError):
@@ -51,6 +53,28 @@ class Layer(ctypes.Structure):
                 ("w_prep", ctypes.c_void_p), ("thr", ctypes.c_void_p), ("sign", ctypes.c_void_p),
                 ("y_codes", ctypes.c_void_p), ("y_acc", ctypes.c_void_p), ("fixed", FixedDesc),
                 ("fx_mul", ctypes.c_void_p), ("fx_add", ctypes.c_void_p)]
+
+
+class KV4Cache(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int) for f in ("pages", "page_size", "kv_heads", "head_dim")]
+
+
+class KV4AppendDesc(ctypes.Structure):
+    _fields_ = [("cache", KV4Cache)] + [(f, ctypes.c_int) for f in
+                                        ("tokens", "q_heads", "dtype", "rope", "rot_dim", "positions")] + \
+        [(f, ctypes.c_int64) for f in ("q_stride", "k_stride", "v_stride", "q_out_stride")]
+
+
+class KV4AttentionDesc(ctypes.Structure):
+    _fields_ = [("cache", KV4Cache)] + [(f, ctypes.c_int) for f in
+                                        ("seqs", "q_tokens", "max_q", "max_pages", "max_len", "q_heads", "dtype")] + \
+        [("scale", ctypes.c_float), ("window", ctypes.c_int), ("sinks", ctypes.c_int),
+         ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
+
+
+class Fp8Desc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int) for f in ("m", "n", "k", "dtype", "out_dtype")] + \
+        [("x_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
 
 
 _P = ctypes.c_void_p
@@ -91,6 +115,14 @@ _SIGS = {
     "ifq_unpack_codes_kbits": ([_P, _P, _SZ, _I, _P], _I),
     "ifq_pack_signs": ([_P, _P, _I, _I, _P], _I),
     "ifq_copy_bytes": ([_P, _P, _SZ, _P], _I),
+    "ifq_kv4_cache_bytes": ([ctypes.POINTER(KV4Cache), ctypes.POINTER(_SZ)], _I),
+    "ifq_kv4_append": ([ctypes.POINTER(KV4AppendDesc), _P, _P, _P, _P, _P, _P, _P, _P, _P, _P], _I),
+    "ifq_kv4_read": ([ctypes.POINTER(KV4AppendDesc), _P, _P, _P, _P, _P], _I),
+    "ifq_kv4_attention_workspace_bytes": ([ctypes.POINTER(KV4AttentionDesc), ctypes.POINTER(_SZ)], _I),
+    "ifq_kv4_attention": ([ctypes.POINTER(KV4AttentionDesc), _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P], _I),
+    "ifq_fp8_quantize": ([ctypes.POINTER(Fp8Desc), _P, _P, _P, _P], _I),
+    "ifq_fp8_workspace_bytes": ([ctypes.POINTER(Fp8Desc), ctypes.POINTER(_SZ)], _I),
+    "ifq_fp8_matmul": ([ctypes.POINTER(Fp8Desc), _P, _P, _P, _P, _P, _P, _SZ, _P], _I),
     "ifq_wait_selftest": ([_I, _P], _I),
     "ifq_device_status": ([_P, ctypes.POINTER(_I)], _I),
 }
@@ -364,6 +396,79 @@ def ifq_pack_signs(w, bits, rows: int, K: int, stream=None):
 
 def ifq_copy_bytes(dst, src, n: int, stream=None):
     _ok(lib().ifq_copy_bytes(_ptr(dst), _ptr(src), n, _stream(stream)), "ifq_copy_bytes")
+
+
+def kv4_cache(pages: int, page_size: int, kv_heads: int, head_dim: int) -> KV4Cache:
+    return KV4Cache(pages, page_size, kv_heads, head_dim)
+
+
+def ifq_kv4_cache_bytes(c: KV4Cache) -> int:
+    out = _SZ()
+    _ok(lib().ifq_kv4_cache_bytes(ctypes.byref(c), ctypes.byref(out)), "ifq_kv4_cache_bytes")
+    return out.value
+
+
+def kv4_append_desc(cache: KV4Cache, tokens: int, q_heads: int, dtype: int, rope: int = IFQ_ROPE_HALVES,
+                    rot_dim: Optional[int] = None, positions: int = 0, q_stride: int = 0, k_stride: int = 0,
+                    v_stride: int = 0, q_out_stride: int = 0) -> KV4AppendDesc:
+    return KV4AppendDesc(cache, tokens, q_heads, dtype, rope, cache.head_dim if rot_dim is None else rot_dim, positions,
+                         q_stride, k_stride, v_stride, q_out_stride)
+
+
+def ifq_kv4_append(d: KV4AppendDesc, q, k, v, cos, sin, positions, slots, q_out, cache, stream=None):
+    """Rotate q and k, quantise k and v to 4 bits and write them into the cache at `slots`."""
+    _ok(lib().ifq_kv4_append(ctypes.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(cos), _ptr(sin), _ptr(positions),
+                             _ptr(slots), _ptr(q_out), _ptr(cache), _stream(stream)), "ifq_kv4_append")
+
+
+def ifq_kv4_read(d: KV4AppendDesc, cache, slots, k_out=None, v_out=None, stream=None):
+    """The values that the cache holds at `slots`."""
+    _ok(lib().ifq_kv4_read(ctypes.byref(d), _ptr(cache), _ptr(slots), _ptr(k_out), _ptr(v_out), _stream(stream)),
+        "ifq_kv4_read")
+
+
+def kv4_attention_desc(cache: KV4Cache, seqs: int, q_tokens: int, max_q: int, max_pages: int, q_heads: int, dtype: int,
+                       scale: float, window: int = 0, sinks: int = 0, max_len: int = 0, q_stride: int = 0,
+                       out_stride: int = 0) -> KV4AttentionDesc:
+    return KV4AttentionDesc(cache, seqs, q_tokens, max_q, max_pages, max_len, q_heads, dtype, scale, window, sinks,
+                            q_stride, out_stride)
+
+
+def ifq_kv4_attention_workspace_bytes(d: KV4AttentionDesc) -> int:
+    out = _SZ()
+    _ok(lib().ifq_kv4_attention_workspace_bytes(ctypes.byref(d), ctypes.byref(out)),
+        "ifq_kv4_attention_workspace_bytes")
+    return out.value
+
+
+def ifq_kv4_attention(d: KV4AttentionDesc, q, cache, page_table, lens, q_starts, out, lse=None, ws=None,
+                      ws_bytes: int = 0, stream=None):
+    """Attention of the queries over the tokens that the cache holds."""
+    _ok(lib().ifq_kv4_attention(ctypes.byref(d), _ptr(q), _ptr(cache), _ptr(page_table), _ptr(lens), _ptr(q_starts),
+                                _ptr(out), _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)), "ifq_kv4_attention")
+
+
+def fp8_desc(m: int, n: int, k: int, dtype: int = IFQ_BF16, out_dtype: int = IFQ_BF16, x_stride: int = 0,
+             out_stride: int = 0) -> Fp8Desc:
+    return Fp8Desc(m, n, k, dtype, out_dtype, x_stride, out_stride)
+
+
+def ifq_fp8_quantize(d: Fp8Desc, x, codes, scales, stream=None):
+    """Activations [m][k] to e4m3 with a scale per row and block of 128."""
+    _ok(lib().ifq_fp8_quantize(ctypes.byref(d), _ptr(x), _ptr(codes), _ptr(scales), _stream(stream)),
+        "ifq_fp8_quantize")
+
+
+def ifq_fp8_workspace_bytes(d: Fp8Desc) -> int:
+    out = _SZ()
+    _ok(lib().ifq_fp8_workspace_bytes(ctypes.byref(d), ctypes.byref(out)), "ifq_fp8_workspace_bytes")
+    return out.value
+
+
+def ifq_fp8_matmul(d: Fp8Desc, x, x_scale, w, w_scale, out, ws=None, ws_bytes: int = 0, stream=None):
+    """out = x w^T with e4m3 operands and block scales."""
+    _ok(lib().ifq_fp8_matmul(ctypes.byref(d), _ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(out), _ptr(ws),
+                             ws_bytes, _stream(stream)), "ifq_fp8_matmul")
 
 
 def ifq_wait_selftest(limit_us: int, stream=None):
