@@ -3,13 +3,17 @@
 #include "lm_api.h"
 
 #include <cmath>
+#include <algorithm>
 #include <climits>
+#include <mutex>
+#include <type_traits>
 
 #include "../launch.cuh"
 #include "fp8.cuh"
 #include "ifq.h"
 #include "kv4.cuh"
 #include "kv4_attention.cuh"
+#include "kv4_rows.cuh"
 
 namespace {
 
@@ -18,6 +22,8 @@ using namespace ifq;
 inline bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 inline int done(cudaError_t e) { return e == cudaSuccess ? IFQ_OK : IFQ_ECUDA; }
 inline bool is16(int dtype) { return dtype == IFQ_F16 || dtype == IFQ_BF16; }
+
+std::mutex g_lm_mu;   // guards the per-device state below
 
 // The kernel instance of a head size and type: f(head size, bfloat16) with both as types.
 template <int D, typename F>
@@ -59,6 +65,110 @@ KvCacheArgs cache_args(const ifq_kv4_cache& c, const void* p) {
   a.page_size = c.page_size;
   a.kv_heads = c.kv_heads;
   return a;
+}
+
+// ---------------------------------------------------------------- attention
+
+KvDiv make_div(uint32_t d) {
+  KvDiv f;
+  f.d = d;
+  f.shift = 0;
+  while ((1ull << f.shift) < d) ++f.shift;
+  f.mul = (uint32_t)(((1ull << 32) * ((1ull << f.shift) - d)) / d + 1ull);
+  return f;
+}
+
+int check_attention(const ifq_kv4_attention_desc* d, KvAttnArgs* a) {
+  if (!d) return IFQ_EINVAL;
+  size_t bytes;
+  int rc = check_cache(&d->cache, &bytes);
+  if (rc) return rc;
+  if (d->seqs < 0 || d->q_tokens < 0 || d->max_q < 0 || d->max_pages < 0 || d->max_len < 0 || d->q_heads < 1 ||
+      d->window < 0 || d->sinks < 0 || !is16(d->dtype) || !std::isfinite(d->scale))
+    return IFQ_EINVAL;
+  if (d->q_heads % d->cache.kv_heads != 0) return IFQ_ESHAPE;
+  if (d->q_heads > 65536 || (long long)d->max_pages * d->cache.page_size > INT_MAX ||
+      (long long)d->max_q * d->q_heads > INT_MAX)
+    return IFQ_ERANGE;
+  const long long width = (long long)d->q_heads * d->cache.head_dim;
+  if ((rc = stride_of(d->q_stride, width, &a->q_stride))) return rc;
+  if ((rc = stride_of(d->out_stride, width, &a->out_stride))) return rc;
+  a->pages = d->cache.pages;
+  a->page_size = d->cache.page_size;
+  a->kv_heads = d->cache.kv_heads;
+  a->seqs = d->seqs;
+  a->q_tokens = d->q_tokens;
+  a->max_q = d->max_q;
+  a->max_pages = d->max_pages;
+  a->q_heads = d->q_heads;
+  a->group = d->q_heads / d->cache.kv_heads;
+  a->window = d->window;
+  a->sinks = d->sinks;
+  a->scale = d->scale;
+  return IFQ_OK;
+}
+
+struct AttnPlan {
+  int nt;          // row tiles of an item
+  int direct;      // a block an item
+  int blocks;      // of a sequence's rows (direct), or ranges
+  size_t ws;
+};
+
+// SM count of the current device, or a full GB300's where there is none.
+int sm_count() {
+  static int known[kMaxDevices];
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 152;
+  std::lock_guard<std::mutex> lk(g_lm_mu);
+  if (!known[dev] && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) known[dev] = n;
+  return known[dev] ? known[dev] : 152;
+}
+
+int plan_attention(const ifq_kv4_attention_desc* d, const KvAttnArgs& a, AttnPlan* p) {
+  const int D = d->cache.head_dim;
+  const long long rows = (long long)d->max_q * a.group;
+  long long reach = (long long)d->max_pages * d->cache.page_size;   // tokens that a sequence's queries read at most
+  if (d->max_len > 0) reach = std::min<long long>(reach, d->max_len);
+  if (d->window > 0) reach = std::min<long long>(reach, (long long)d->window + d->sinks + d->max_q + 2 * kKvGroup);
+  p->nt = rows > 8 && D < 256 ? 2 : 1;   // (two tiles of size 256 do not fit the registers)
+  const int R = 8 * p->nt;
+  const long long blocks = std::max<long long>(1, (rows + R - 1) / R);   // (the device checks max_q = 0 too)
+  p->direct = reach <= 64 * kKvGroup && blocks <= 65535 && d->seqs <= 65535;
+  p->blocks = p->direct ? (int)blocks : sm_count() * (p->nt == 1 ? 2 : 1);
+  p->ws = p->direct ? 0 : round_up((size_t)p->blocks * (2 * R * (D * 4 + 8) + 16), 256);
+  return IFQ_OK;
+}
+
+template <int D, bool BF, int NT>
+int run_rows(const KvAttnArgs& a, const AttnPlan& p, void* ws, cudaStream_t st) {
+  constexpr int R = 8 * NT, smem = kv_rows_smem<D>(R);
+  static_assert(smem <= 232448, "shared memory budget");
+  static bool set[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return IFQ_ECUDA;
+  {
+    std::lock_guard<std::mutex> lk(g_lm_mu);
+    if (!set[dev]) {
+      if (cudaFuncSetAttribute(kv4_rows_kernel<D, BF, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+        return IFQ_ECUDA;
+      set[dev] = true;
+    }
+  }
+  KvRowsArgs r = {};
+  r.a = a;
+  r.by_gpp = make_div(a.page_size / kKvGroup);
+  r.by_group = make_div(a.group);
+  r.direct = p.direct;
+  if (!p.direct) {
+    r.cut = (int4*)ws;
+    r.part_ml = (float2*)(r.cut + p.blocks);
+    r.part = (float*)(r.part_ml + (size_t)p.blocks * 2 * R);
+  }
+  const dim3 grid = p.direct ? dim3(a.kv_heads, p.blocks, a.seqs) : dim3(p.blocks);
+  const cudaError_t e = launch_k(kv4_rows_kernel<D, BF, NT>, grid, dim3(32 * KvRowsShape<D>::W), smem, st, r);
+  if (e != cudaSuccess || p.direct) return done(e);
+  return done(launch_k(kv4_join_kernel<D, BF, NT>, dim3(p.blocks, R), dim3(128), 0, st, r));
 }
 
 }  // namespace
@@ -152,40 +262,13 @@ int ifq_kv4_read(const ifq_kv4_append_desc* d, const void* cache, const int64_t*
   });
 }
 
-static int check_attention(const ifq_kv4_attention_desc* d, KvAttnArgs* a) {
-  if (!d) return IFQ_EINVAL;
-  size_t bytes;
-  int rc = check_cache(&d->cache, &bytes);
-  if (rc) return rc;
-  if (d->seqs < 0 || d->q_tokens < 0 || d->max_q < 0 || d->max_pages < 0 || d->max_len < 0 || d->q_heads < 1 ||
-      d->window < 0 || d->sinks < 0 || !is16(d->dtype) || !std::isfinite(d->scale))
-    return IFQ_EINVAL;
-  if (d->q_heads % d->cache.kv_heads != 0) return IFQ_ESHAPE;
-  if (d->q_heads > 65536 || (long long)d->max_pages * d->cache.page_size > INT_MAX) return IFQ_ERANGE;
-  const long long width = (long long)d->q_heads * d->cache.head_dim;
-  if ((rc = stride_of(d->q_stride, width, &a->q_stride))) return rc;
-  if ((rc = stride_of(d->out_stride, width, &a->out_stride))) return rc;
-  a->pages = d->cache.pages;
-  a->page_size = d->cache.page_size;
-  a->kv_heads = d->cache.kv_heads;
-  a->seqs = d->seqs;
-  a->q_tokens = d->q_tokens;
-  a->max_q = d->max_q;
-  a->max_pages = d->max_pages;
-  a->q_heads = d->q_heads;
-  a->group = d->q_heads / d->cache.kv_heads;
-  a->window = d->window;
-  a->sinks = d->sinks;
-  a->scale = d->scale;
-  return IFQ_OK;
-}
-
 int ifq_kv4_attention_workspace_bytes(const ifq_kv4_attention_desc* d, size_t* bytes) {
   if (!bytes) return IFQ_EINVAL;
   KvAttnArgs a = {};
-  const int rc = check_attention(d, &a);
-  if (rc) return rc;
-  *bytes = 0;
+  AttnPlan p;
+  int rc = check_attention(d, &a);
+  if (rc || (rc = plan_attention(d, a, &p))) return rc;
+  *bytes = p.ws;
   return IFQ_OK;
 }
 
@@ -193,13 +276,17 @@ int ifq_kv4_attention(const ifq_kv4_attention_desc* d, const void* q, const void
                       const int32_t* lens, const int32_t* q_starts, void* out, float* lse, void* ws, size_t ws_bytes,
                       void* stream) {
   KvAttnArgs a = {};
-  const int rc = check_attention(d, &a);
+  AttnPlan p;
+  int rc = check_attention(d, &a);
   if (rc) return rc;
   if (!q || !cache || !lens || !out || (!page_table && d->max_pages > 0)) return IFQ_EINVAL;
   if (!q_starts && (d->q_tokens != d->seqs)) return IFQ_ESHAPE;
   if (!aligned16(q) || !aligned16(cache) || !aligned16(out) || !aligned(page_table, 4) || !aligned(lens, 4) ||
       !aligned(q_starts, 4) || !aligned(lse, 4) || !aligned16(ws))
     return IFQ_EALIGN;
+  if ((rc = plan_attention(d, a, &p))) return rc;
+  if (p.ws && (!ws || ws_bytes < p.ws)) return IFQ_EWORKSPACE;
+  if (!d->q_tokens || !d->seqs) return IFQ_OK;
   a.q = (const uint16_t*)q;
   a.cache = (const uint8_t*)cache;
   a.table = page_table;
@@ -207,13 +294,12 @@ int ifq_kv4_attention(const ifq_kv4_attention_desc* d, const void* q, const void
   a.starts = q_starts;
   a.out = (uint16_t*)out;
   a.lse = lse;
-  (void)ws_bytes;
-  const long long blocks = ((long long)d->q_tokens * d->q_heads + kAttnWarps - 1) / kAttnWarps;
-  if (blocks > INT_MAX) return IFQ_ERANGE;
-  if (!blocks || !d->seqs) return IFQ_OK;
   return by_head(d->cache.head_dim, d->dtype, [&](auto dim, auto bf) {
-    return done(launch_k(kv4_attention_kernel<decltype(dim)::value, decltype(bf)::value>, dim3((unsigned)blocks),
-                         dim3(32 * kAttnWarps), 0, S(stream), a));
+    constexpr int D = decltype(dim)::value;
+    constexpr bool BF = decltype(bf)::value;
+    if constexpr (D < 256)
+      if (p.nt == 2) return run_rows<D, BF, 2>(a, p, ws, S(stream));
+    return run_rows<D, BF, 1>(a, p, ws, S(stream));
   });
 }
 
