@@ -201,35 +201,42 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
     cur.base = -first[2];
   }
 
-  // the producer's side: the next group to fetch, in order
+  // the producer's side: the next group to fetch, in order; its page is looked up one fetch ahead
   KvCursor pro = cur;
   int po = warp;          // its offset
-  int issued = 0;
-  auto fetch = [&]() {
+  int issued = 0, page = 0, where = 0, pro_head = 0;
+  bool there = false;
+  auto look_up = [&]() {
     if (po < n) {
       kv_advance<R>(A, pro, po);
       const int g = po - pro.base, gi = g < pro.sg ? g : g + pro.skip;
+      const int pi = kv_div(gi, A.by_gpp);
+      where = gi - pi * A.by_gpp.d;
+      pro_head = pro.it % a.kv_heads;
+      there = gi * kKvGroup < pro.q.len;
+      if (there) page = a.table[(long long)pro.s * a.max_pages + pi];
+    }
+  };
+  auto fetch = [&]() {
+    if (po < n) {
       const int st = issued % ST;
       if (lane == 0) {
-        const uint32_t pi = kv_div(gi, A.by_gpp);
-        int page = -1;
-        if (gi * kKvGroup < pro.q.len) {
-          page = a.table[(long long)pro.s * a.max_pages + pi];
-          if (page < 0 || page >= a.pages) set_status(IFQ_ERANGE), page = -1;
-        }
-        if (page >= 0) {
-          const int head = pro.it % a.kv_heads;
-          const uint8_t* src = a.cache + (((long long)page * a.kv_heads + head) * A.by_gpp.d + (gi - pi * A.by_gpp.d)) * GB;
+        const bool good = there && page >= 0 && page < a.pages;
+        if (good) {
+          const uint8_t* src = a.cache + (((long long)page * a.kv_heads + pro_head) * A.by_gpp.d + where) * GB;
           mbar_arrive_expect_tx(bar0 + 8 * st, GB);
           bulk_copy_g2s(smem_u32(ring + st * GB), src, GB, bar0 + 8 * st);
         } else {
+          if (there) set_status(IFQ_ERANGE);
           mbar_arrive(bar0 + 8 * st);
         }
       }
       ++issued;
       po += W;
+      look_up();
     }
   };
+  look_up();
 #pragma unroll
   for (int i = 0; i < ST; ++i) fetch();
 
@@ -303,6 +310,12 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 4; ++c) o[i][nt][c] = 0.0f;
+    float ow[NT][4];   // 8 sum w, as the products have it: values are taken about code 8, so that what rounding the
+                       // weights changes goes with the values' spread and not with their distance from code 0
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) ow[nt][c] = 0.0f;
     float vmul = 1.0f, vtop = 0.0f;   // factor of the value scales, and the scale that raises it
 
     for (; co < o1; co += W) {
@@ -311,11 +324,11 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
       ++used;
       const uint8_t* g = ring + st * GB;
       const int gg = co - cur.base, gi = gg < cur.sg ? gg : gg + cur.skip, j0 = gi * kKvGroup;
-      float s[NT][4];
+      float s[NT][4], s2[NT][4];   // two chains of products
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) s[nt][c] = 0.0f;
+        for (int c = 0; c < 4; ++c) s[nt][c] = s2[nt][c] = 0.0f;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         uint32_t ka[WPL], kb[WPL];
@@ -329,7 +342,7 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
             const int k = (b * WPL + i) * 2 + h;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
-              mma_f16(s[nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][k][0], qf[nt][k][1]);
+              mma_f16(h ? s2[nt] : s[nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][k][0], qf[nt][k][1]);
           }
       }
       const uint32_t* par = (const uint32_t*)(g + 16 * D);
@@ -343,8 +356,8 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          s[nt][c] = (s[nt][c] * fa[nt][c]) * ks0 + fb[nt][c] * k0.y;
-          s[nt][2 + c] = (s[nt][2 + c] * fa[nt][c]) * ks1 + fb[nt][c] * k1.y;
+          s[nt][c] = ((s[nt][c] + s2[nt][c]) * fa[nt][c]) * ks0 + fb[nt][c] * k0.y;
+          s[nt][2 + c] = ((s[nt][2 + c] + s2[nt][2 + c]) * fa[nt][c]) * ks1 + fb[nt][c] * k1.y;
         }
       if (!full) {
 #pragma unroll
@@ -389,6 +402,7 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
             m[nt][c] = now;
             l[nt][c] *= f;
             z[nt][c] *= f;
+            ow[nt][c] *= f * vf;
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
               o[i][nt][c] *= f * vf;
@@ -397,6 +411,8 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
           }
       }
       const float w0 = v0.x * vmul, w1 = v1.x * vmul;
+      v0.y += 8.0f * v0.x;   // the value of code 8
+      v1.y += 8.0f * v1.x;
       uint32_t wf[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -419,6 +435,7 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
         }
         wf[nt][0] = transpose8x8(pack16<false>(w[0], w[1]));
         wf[nt][1] = transpose8x8(pack16<false>(w[2], w[3]));
+        mma_f16(ow[nt], 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, wf[nt][0], wf[nt][1]);
       }
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
@@ -477,7 +494,8 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const float* v = o[(b * WPL + i) * 2 + h][nt];
-              *(float2*)(dst + b * DB + gid * (DB / 8) + 4 * i + 2 * h) = make_float2(v[c] * f, v[2 + c] * f * 0.0625f);
+              *(float2*)(dst + b * DB + gid * (DB / 8) + 4 * i + 2 * h) =
+                  make_float2((v[c] - ow[nt][c]) * f, (v[2 + c] * 0.0625f - ow[nt][c]) * f);
             }
       }
       __syncthreads();
