@@ -14,11 +14,12 @@
 // seen, so that w < 2^15 and weights keep their 11 bits down to 2^-20 of the largest.  p in the denominator and in
 // the sum with the minima stays fp32.
 //
-// Work: the groups of all items in a row are cut into as many equal ranges as there are blocks, whatever the lengths
-// (an item cut by a range's end leaves partial sums in the workspace, joined by kv4_join_kernel); or, where no
-// sequence is long, one block an item.  Each warp takes every W-th group of its block's range, with a ring of its own
-// filled by bulk copies (one contiguous block a group), across the ends of items; at an item's end the warps' sums
-// are joined in shared memory.
+// Work: an item's groups are taken in units of U; the units of all items in a row are cut into as many equal ranges as
+// there are blocks, whatever the lengths (an item cut by a range's end leaves partial sums in the workspace, joined by
+// kv4_join_kernel); or, where no sequence is long, one block an item.  Each warp takes every W-th unit of its block's
+// range.  One more warp fetches for all of them, a lane a group (page lookup and one bulk copy of the group's
+// contiguous bytes), two units ahead and across the ends of items.  At an item's end the warps' sums are joined in
+// shared memory.
 #pragma once
 #include "kv4_attention.cuh"
 
@@ -45,13 +46,18 @@ struct KvRowsArgs {
 
 template <int D>
 struct KvRowsShape {
-  static constexpr int W = D == 256 ? 4 : 8;        // warps
-  static constexpr int stages = D == 64 ? 6 : 4;    // groups in flight a warp
+  static constexpr int W = 7;                       // computing warps; with the fetching one, two a scheduler
+  static constexpr int U = D == 64 ? 4 : 2;         // groups a unit
+  static constexpr int stages = 2;                  // units in flight a warp
+  static constexpr int threads = 32 * (W + 1);
+  static_assert(W * U <= 32, "a fetching lane a group");
 };
+// Blocks an SM: two of 128 registers a thread where those do, else one.
+__host__ __device__ constexpr int kv_rows_per_sm(int D, int NT) { return D < 256 && NT == 1 ? 2 : 1; }
 template <int D>
 __host__ __device__ constexpr int kv_rows_smem(int R) {
   using C = KvRowsShape<D>;
-  return C::W * C::stages * (kv4_group_bytes(D) + 8) + C::W * 8 * (D + 4) * 4 + 3 * C::W * R * 4 + 64 * 8 + 64;
+  return C::W * C::stages * (C::U * kv4_group_bytes(D) + 16) + C::W * 8 * (D + 4) * 4 + 3 * C::W * R * 4 + 16 * 8;
 }
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -78,11 +84,11 @@ struct KvCursor {
   int s;           // sequence
   KvSeq q;
   int it, nit;     // item of the sequence (block of rows * key heads + key head), items
-  int ng, sg, skip;
-  int base;        // where the item starts, relative to the block's range
+  int ng, sg, skip, nu;   // groups, of those at its start, groups left out after them, units
+  int base;        // the unit at which the item starts, relative to the block's range
 };
 
-template <int R>
+template <int R, int U>
 __device__ __forceinline__ void kv_shape(const KvRowsArgs& A, KvCursor& c) {
   const KvAttnArgs& a = A.a;
   c.q = kv_seq(a, c.s);
@@ -95,67 +101,71 @@ __device__ __forceinline__ void kv_shape(const KvRowsArgs& A, KvCursor& c) {
   c.sg = c.sg < lo ? c.sg : lo;
   c.skip = lo - c.sg;
   c.ng = all - c.skip;
+  c.nu = (c.ng + U - 1) / U;
 }
-// Move on to the item that holds offset o of the range.
-template <int R>
+// Move on to the item that holds unit o of the range.
+template <int R, int U>
 __device__ __forceinline__ void kv_advance(const KvRowsArgs& A, KvCursor& c, int o) {
-  while (o >= c.base + c.ng) {
-    c.base += c.ng;
+  while (o >= c.base + c.nu) {
+    c.base += c.nu;
     if (++c.it >= c.nit) {
       c.it = 0;
       do {
         ++c.s;
-        kv_shape<R>(A, c);
+        kv_shape<R, U>(A, c);
       } while (c.nit == 0);
     }
   }
 }
 
 template <int D, bool BF, int NT>
-__global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_rows_kernel(const __grid_constant__ KvRowsArgs A) {
+__global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)) kv4_rows_kernel(const __grid_constant__ KvRowsArgs A) {
   using C = KvRowsShape<D>;
-  constexpr int W = C::W, ST = C::stages, R = 8 * NT, GB = kv4_group_bytes(D);
+  constexpr int W = C::W, U = C::U, ST = C::stages, R = 8 * NT, GB = kv4_group_bytes(D);
   constexpr int DB = kv4_block(D), NB = D / DB, WPL = DB / 32;   // blocks of dimensions, words a lane and row
   constexpr int KS = D / 16, MT = D / 16;                        // steps along d of S, tiles along d of O
+  static_assert(4 * U * NT <= 32, "a bit a score");
   extern __shared__ __align__(128) uint8_t smem[];
   const KvAttnArgs& a = A.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
-  uint8_t* ring = smem + warp * ST * GB;
-  float* jO = (float*)(smem + W * ST * GB);                 // [W][8][D + 4]
+  float* jO = (float*)(smem + W * ST * U * GB);             // [W][8][D + 4]
   float* jm = jO + W * 8 * (D + 4);                         // [W][R] each
   float *jl = jm + W * R, *jz = jl + W * R;
-  uint64_t* bars = (uint64_t*)(jz + W * R);                 // [W][ST]
-  long long* scan = (long long*)(bars + W * ST);            // [W + 1]
-  __shared__ int first[4];
-  const uint32_t bar0 = smem_u32(bars + warp * ST);
-  if (lane == 0) {
-    for (int i = 0; i < ST; ++i) mbar_init(bar0 + 8 * i, 1);
+  uint64_t* bars = (uint64_t*)(jz + W * R);                 // full [W][ST], empty [W][ST]
+  long long* scan = (long long*)(bars + 2 * W * ST);        // [W + 1]
+  __shared__ int first[3];
+  const uint32_t bar_full = smem_u32(bars), bar_empty = smem_u32(bars + W * ST);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < W * ST; ++i) {
+      mbar_init(bar_full + 8 * i, U);
+      mbar_init(bar_empty + 8 * i, 1);
+    }
     fence_mbar_init();
   }
-  __syncwarp();
+  __syncthreads();
   grid_dep_wait();
   grid_dep_launch();
 
   KvCursor cur;
-  int n;        // groups of this block
+  int n;        // units of this block
   if (A.direct) {
     cur.s = blockIdx.z;
-    kv_shape<R>(A, cur);
+    kv_shape<R, U>(A, cur);
     if (!cur.q.ok && threadIdx.x == 0) set_status(IFQ_ERANGE);
     cur.it = blockIdx.y * a.kv_heads + blockIdx.x;
     cur.base = 0;
     if (cur.it >= cur.nit) return;
-    n = cur.ng;
+    n = cur.nu;
   } else {
-    // the groups of every sequence, summed over the block's threads' shares of the sequences
-    const int per = (a.seqs + 32 * W - 1) / (32 * W), s0 = threadIdx.x * per, s1 = min(a.seqs, s0 + per);
+    // the units of every sequence, summed over the block's threads' shares of the sequences
+    const int per = (a.seqs + C::threads - 1) / C::threads, s0 = threadIdx.x * per, s1 = min(a.seqs, s0 + per);
     long long mine = 0;
     for (int s = s0; s < s1; ++s) {
       KvCursor t;
       t.s = s;
-      kv_shape<R>(A, t);
+      kv_shape<R, U>(A, t);
       if (!t.q.ok && blockIdx.x == 0) set_status(IFQ_ERANGE);
-      mine += (long long)t.nit * t.ng;
+      mine += (long long)t.nit * t.nu;
     }
     long long incl = mine;
 #pragma unroll
@@ -167,12 +177,12 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
     __syncthreads();
     long long before = incl - mine, total = 0;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
+    for (int w = 0; w <= W; ++w) {
       if (w < warp) before += scan[w];
       total += scan[w];
     }
     long long share = (total + gridDim.x - 1) / gridDim.x;
-    if (share < 2 * W) share = 2 * W;
+    if (share < W) share = W;
     const long long start = share * blockIdx.x;
     if (start >= total) {
       if (threadIdx.x == 0) A.cut[blockIdx.x] = make_int4(0, 0, 0, 0);
@@ -184,67 +194,60 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
       KvCursor t;
       t.s = s0;
       for (;; ++t.s) {
-        kv_shape<R>(A, t);
-        const long long c = (long long)t.nit * t.ng;
+        kv_shape<R, U>(A, t);
+        const long long c = (long long)t.nit * t.nu;
         if (start < at + c) break;
         at += c;
       }
       const long long in = start - at;
       first[0] = t.s;
-      first[1] = (int)(in / t.ng);
-      first[2] = (int)(in % t.ng);
+      first[1] = (int)(in / t.nu);
+      first[2] = (int)(in % t.nu);
     }
     __syncthreads();
     cur.s = first[0];
-    kv_shape<R>(A, cur);
+    kv_shape<R, U>(A, cur);
     cur.it = first[1];
     cur.base = -first[2];
   }
 
-  // the producer's side: the next group to fetch, in order; its page is looked up one fetch ahead
-  KvCursor pro = cur;
-  int po = warp;          // its offset
-  int issued = 0, page = 0, where = 0, pro_head = 0;
-  bool there = false;
-  auto look_up = [&]() {
-    if (po < n) {
-      kv_advance<R>(A, pro, po);
-      const int g = po - pro.base, gi = g < pro.sg ? g : g + pro.skip;
-      const int pi = kv_div(gi, A.by_gpp);
-      where = gi - pi * A.by_gpp.d;
-      pro_head = pro.it % a.kv_heads;
-      there = gi * kKvGroup < pro.q.len;
-      if (there) page = a.table[(long long)pro.s * a.max_pages + pi];
-    }
-  };
-  auto fetch = [&]() {
-    if (po < n) {
-      const int st = issued % ST;
-      if (lane == 0) {
-        const bool good = there && page >= 0 && page < a.pages;
-        if (good) {
-          const uint8_t* src = a.cache + (((long long)page * a.kv_heads + pro_head) * A.by_gpp.d + where) * GB;
-          mbar_arrive_expect_tx(bar0 + 8 * st, GB);
-          bulk_copy_g2s(smem_u32(ring + st * GB), src, GB, bar0 + 8 * st);
+  if (warp == W) {
+    // fetch: lane (w, u) the u-th group of warp w's units
+    const int w = lane / U, u = lane % U;
+    if (w < W) {
+      const uint32_t ring = smem_u32(smem + w * ST * U * GB + u * GB);
+      int k = 0;
+      for (int o = w; o < n; o += W, ++k) {
+        kv_advance<R, U>(A, cur, o);
+        const int g = (o - cur.base) * U + u, gi = g < cur.sg ? g : g + cur.skip;
+        const bool there = g < cur.ng && gi * kKvGroup < cur.q.len;
+        const int pi = kv_div(gi, A.by_gpp);
+        int page = 0;
+        if (there) {
+          page = a.table[(long long)cur.s * a.max_pages + pi];
+          if (page < 0 || page >= a.pages) set_status(IFQ_ERANGE);
+        }
+        const int st = k % ST, head = cur.it % a.kv_heads;
+        if (k >= ST && !mbar_wait(bar_empty + 8 * (w * ST + st), (k / ST - 1) & 1)) break;
+        const uint32_t bar = bar_full + 8 * (w * ST + st);
+        if (there && page >= 0 && page < a.pages) {
+          const uint8_t* src = a.cache + (((long long)page * a.kv_heads + head) * A.by_gpp.d + (gi - pi * A.by_gpp.d)) * GB;
+          mbar_arrive_expect_tx(bar, GB);
+          bulk_copy_g2s(ring + st * U * GB, src, GB, bar);
         } else {
-          if (there) set_status(IFQ_ERANGE);
-          mbar_arrive(bar0 + 8 * st);
+          mbar_arrive(bar);
         }
       }
-      ++issued;
-      po += W;
-      look_up();
     }
-  };
-  look_up();
-#pragma unroll
-  for (int i = 0; i < ST; ++i) fetch();
+    return;
+  }
 
+  const uint8_t* ring = smem + warp * ST * U * GB;
   int used = 0, co = warp;
   bool alive = true;
   for (int o0 = 0; o0 < n;) {
-    kv_advance<R>(A, cur, o0);
-    const int o1 = min(n, cur.base + cur.ng);
+    kv_advance<R, U>(A, cur, o0);
+    const int o1 = min(n, cur.base + cur.nu);
     const int rb = cur.it / a.kv_heads, head = cur.it - rb * a.kv_heads, nrows = cur.q.n * a.group;
     const int p_lo = cur.q.len - cur.q.n + (int)kv_div(rb * R, A.by_group);
     const int p_hi = cur.q.len - cur.q.n + (int)kv_div(min(nrows, rb * R + R) - 1, A.by_group);
@@ -296,7 +299,7 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
       for (int c = 0; c < 2; ++c) {
         fa[nt][c] = __shfl_sync(0xffffffffu, va, 8 * tig + 4 * c);
         fb[nt][c] = __shfl_sync(0xffffffffu, vb, 8 * tig + 4 * c);
-        m[nt][c] = kNoMax;
+        m[nt][c] = 0.0f;
         l[nt][c] = 0.0f;
         z[nt][c] = 0.0f;
         const int rc = rb * R + nt * 8 + 2 * tig + c;
@@ -316,75 +319,99 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int c = 0; c < 4; ++c) ow[nt][c] = 0.0f;
+    uint32_t fresh = 0;   // columns that have no score yet, a bit each (theirs that are no rows never count)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) fresh |= (rb * R + nt * 8 + 2 * tig + c < nrows ? 1u : 0u) << (2 * nt + c);
     float vmul = 1.0f, vtop = 0.0f;   // factor of the value scales, and the scale that raises it
 
     for (; co < o1; co += W) {
       const int st = used % ST;
-      if (alive) alive = mbar_wait(bar0 + 8 * st, (used / ST) & 1);
+      if (alive) alive = mbar_wait(bar_full + 8 * (warp * ST + st), (used / ST) & 1);
       ++used;
-      const uint8_t* g = ring + st * GB;
-      const int gg = co - cur.base, gi = gg < cur.sg ? gg : gg + cur.skip, j0 = gi * kKvGroup;
-      float s[NT][4], s2[NT][4];   // two chains of products
+      const uint8_t* unit = ring + st * U * GB;
+      float s[U][NT][4];
+      float2 v[U][2];
+      uint32_t hidden = 0;   // of the lane's scores, 4 a tile
+      float most = -INFINITY, wide = 0.0f;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) s[nt][c] = s2[nt][c] = 0.0f;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        uint32_t ka[WPL], kb[WPL];
-        load_words(ka, g + b * 8 * DB + gid * (DB / 2) + tig * (DB / 8));
-        load_words(kb, g + b * 8 * DB + (gid + 8) * (DB / 2) + tig * (DB / 8));
-#pragma unroll
-        for (int i = 0; i < WPL; ++i)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t x = h ? ka[i] >> 8 : ka[i], y = h ? kb[i] >> 8 : kb[i];
-            const int k = (b * WPL + i) * 2 + h;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              mma_f16(h ? s2[nt] : s[nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][k][0], qf[nt][k][1]);
-          }
-      }
-      const uint32_t* par = (const uint32_t*)(g + 16 * D);
-      const float2 k0 = unpack16<false>(par[gid]), k1 = unpack16<false>(par[gid + 8]);
-      float2 v0 = unpack16<false>(par[16 + gid]), v1 = unpack16<false>(par[16 + gid + 8]);
-      const float ks0 = k0.x * 16777216.0f, ks1 = k1.x * 16777216.0f;
-      const bool full = j0 + kKvGroup - 1 <= p_lo && (a.window == 0 || j0 > p_hi - a.window || j0 + kKvGroup <= a.sinks);
-      uint32_t hidden = 0;   // of the lane's four scores a tile
-      bool up = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          s[nt][c] = ((s[nt][c] + s2[nt][c]) * fa[nt][c]) * ks0 + fb[nt][c] * k0.y;
-          s[nt][2 + c] = ((s[nt][2 + c] + s2[nt][2 + c]) * fa[nt][c]) * ks1 + fb[nt][c] * k1.y;
-        }
-      if (!full) {
+      for (int u = 0; u < U; ++u) {
+        const uint8_t* g = unit + u * GB;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (!kv_sees(a, prow[nt][c & 1], j0 + gid + (c & 2) * 4)) {
-              hidden |= 1u << (4 * nt + c);
-              s[nt][c] = -INFINITY;
+          for (int c = 0; c < 4; ++c) s[u][nt][c] = 0.0f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          uint32_t ka[WPL], kb[WPL];
+          load_words(ka, g + b * 8 * DB + gid * (DB / 2) + tig * (DB / 8));
+          load_words(kb, g + b * 8 * DB + (gid + 8) * (DB / 2) + tig * (DB / 8));
+#pragma unroll
+          for (int i = 0; i < WPL; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t x = h ? ka[i] >> 8 : ka[i], y = h ? kb[i] >> 8 : kb[i];
+              const int k = (b * WPL + i) * 2 + h;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+                mma_f16(s[u][nt], x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, qf[nt][k][0],
+                        qf[nt][k][1]);
             }
-          }
-        // scales of tokens that no row sees must not raise the factor
-        if (j0 + gid > p_hi) v0 = make_float2(0.0f, 0.0f);
-        if (j0 + gid + 8 > p_hi) v1 = make_float2(0.0f, 0.0f);
+        }
       }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int u = 0; u < U; ++u) {   // the exponents t - m
+        const uint32_t* par = (const uint32_t*)(unit + u * GB + 16 * D);
+        float2 k0 = unpack16<false>(par[gid]), k1 = unpack16<false>(par[gid + 8]);
+        k0.x *= 16777216.0f;   // the codes are in units of 2^-24
+        k1.x *= 16777216.0f;
+        v[u][0] = unpack16<false>(par[16 + gid]), v[u][1] = unpack16<false>(par[16 + gid + 8]);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) up |= fmaxf(s[nt][c], s[nt][2 + c]) > m[nt][c] + 8.0f;
-      up |= fmaxf(v0.x, v1.x) > vtop;
-      if (__any_sync(0xffffffffu, up)) {
-        float vm = fmaxf(v0.x, v1.x);
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int k = 4; k <= 16; k <<= 1) vm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, k));
+          for (int c = 0; c < 2; ++c) {
+            s[u][nt][c] = s[u][nt][c] * (fa[nt][c] * k0.x) + (fb[nt][c] * k0.y - m[nt][c]);
+            s[u][nt][2 + c] = s[u][nt][2 + c] * (fa[nt][c] * k1.x) + (fb[nt][c] * k1.y - m[nt][c]);
+          }
+      }
+      const int g0 = (co - cur.base) * U;
+      // all the unit's groups there, in reach of every row (and none of them past a gap)
+      const int i0 = g0 < cur.sg ? g0 : g0 + cur.skip, j0 = i0 * kKvGroup, jn = j0 + U * kKvGroup;
+      const bool full = jn - 1 <= p_lo && (g0 + U <= cur.sg || g0 >= cur.sg) &&
+                        (a.window == 0 || j0 > p_hi - a.window || jn <= a.sinks);
+      if (!full) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int gu = g0 + u, ju = (gu < cur.sg ? gu : gu + cur.skip) * kKvGroup + gid;
+          const bool out0 = gu >= cur.ng || ju > p_hi, out1 = gu >= cur.ng || ju + 8 > p_hi;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if ((c < 2 ? out0 : out1) || !kv_sees(a, prow[nt][c & 1], ju + (c & 2) * 4)) {
+                hidden |= 1u << ((u * NT + nt) * 4 + c);
+                s[u][nt][c] = -INFINITY;
+              }
+          // what no row sees may hold anything
+          if (out0) v[u][0] = make_float2(0.0f, 0.0f);
+          if (out1) v[u][1] = make_float2(0.0f, 0.0f);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) most = fmaxf(most, s[u][nt][c]);
+        wide = fmaxf(wide, fmaxf(v[u][0].x, v[u][1].x));
+      }
+      if (__any_sync(0xffffffffu, most > 8.0f || wide > vtop || fresh)) {
+#pragma unroll
+        for (int k = 4; k <= 16; k <<= 1) wide = fmaxf(wide, __shfl_xor_sync(0xffffffffu, wide, k));
         float vf = 1.0f;
-        if (vm > vtop) {   // the largest scale to [2^5, 2^6); it may grow to 2^7 before the next time
-          const uint32_t e = __float_as_uint(vm) >> 23;
+        if (wide > vtop) {   // the largest scale to [2^5, 2^6); it may grow to 2^7 before the next time
+          const uint32_t e = __float_as_uint(wide) >> 23;
           const float now = __uint_as_float((254u + 5u - e) << 23);
           vf = vtop == 0.0f ? 1.0f : now / vmul;
           vmul = now;
@@ -394,12 +421,21 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float t = fmaxf(s[nt][c], s[nt][2 + c]);
+            float t = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < U; ++u) t = fmaxf(t, fmaxf(s[u][nt][c], s[u][nt][2 + c]));
 #pragma unroll
             for (int k = 4; k <= 16; k <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, k));
-            const float now = t > m[nt][c] + 8.0f ? t : m[nt][c];
-            const float f = exp2_fast(m[nt][c] - now);
-            m[nt][c] = now;
+            const uint32_t bit = 1u << (2 * nt + c);
+            const bool begin = (fresh & bit) && t > -INFINITY;
+            const float rise = begin || t > 8.0f ? t : 0.0f, f = begin ? 1.0f : exp2_fast(-rise);
+            if (begin) fresh &= ~bit;
+            m[nt][c] += rise;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              s[u][nt][c] -= rise;
+              s[u][nt][2 + c] -= rise;
+            }
             l[nt][c] *= f;
             z[nt][c] *= f;
             ow[nt][c] *= f * vf;
@@ -410,51 +446,54 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
             }
           }
       }
-      const float w0 = v0.x * vmul, w1 = v1.x * vmul;
-      v0.y += 8.0f * v0.x;   // the value of code 8
-      v1.y += 8.0f * v1.x;
-      uint32_t wf[NT][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float p[4], w[4];
+      for (int u = 0; u < U; ++u) {
+        const float w0 = v[u][0].x * vmul, w1 = v[u][1].x * vmul;
+        const float c0 = v[u][0].y + 8.0f * v[u][0].x, c1 = v[u][1].y + 8.0f * v[u][1].x;   // the values of code 8
+        uint32_t wf[NT][2];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          p[c] = exp2_fast(s[nt][c] - m[nt][c & 1]);
-          w[c] = p[c] * (c < 2 ? w0 : w1);
-        }
-        if (!full) {
+        for (int nt = 0; nt < NT; ++nt) {
+          float p[4], w[4], y[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (hidden >> (4 * nt + c) & 1u) w[c] = 0.0f;
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          l[nt][c] += p[c] + p[2 + c];
-          const bool h0 = !full && (hidden >> (4 * nt + c) & 1u), h1 = !full && (hidden >> (4 * nt + 2 + c) & 1u);
-          z[nt][c] += (h0 ? 0.0f : p[c] * v0.y) + (h1 ? 0.0f : p[2 + c] * v1.y);
-        }
-        wf[nt][0] = transpose8x8(pack16<false>(w[0], w[1]));
-        wf[nt][1] = transpose8x8(pack16<false>(w[2], w[3]));
-        mma_f16(ow[nt], 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, wf[nt][0], wf[nt][1]);
-      }
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        uint32_t x[WPL], y[WPL];
-        load_words(x, g + 8 * D + b * 8 * DB + lane * (DB / 8));
-        load_words(y, g + 8 * D + b * 8 * DB + 4 * DB + lane * (DB / 8));
-#pragma unroll
-        for (int i = 0; i < WPL; ++i)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t u = h ? x[i] >> 8 : x[i], v = h ? y[i] >> 8 : y[i];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              mma_f16(o[(b * WPL + i) * 2 + h][nt], u & 0x000f000fu, u & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u,
-                      wf[nt][0], wf[nt][1]);
+          for (int c = 0; c < 4; ++c) {
+            p[c] = exp2_fast(s[u][nt][c]);
+            w[c] = p[c] * (c < 2 ? w0 : w1);
+            y[c] = p[c] * (c < 2 ? c0 : c1);
           }
+          if (!full) {   // (a hidden token's parameters need not be numbers)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (hidden >> ((u * NT + nt) * 4 + c) & 1u) w[c] = y[c] = 0.0f;
+          }
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            l[nt][c] += p[c] + p[2 + c];
+            z[nt][c] += y[c] + y[2 + c];
+          }
+          wf[nt][0] = transpose8x8(pack16<false>(w[0], w[1]));
+          wf[nt][1] = transpose8x8(pack16<false>(w[2], w[3]));
+          mma_f16(ow[nt], 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, wf[nt][0], wf[nt][1]);
+        }
+        const uint8_t* g = unit + u * GB + 8 * D;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          uint32_t x[WPL], y[WPL];
+          load_words(x, g + b * 8 * DB + lane * (DB / 8));
+          load_words(y, g + b * 8 * DB + 4 * DB + lane * (DB / 8));
+#pragma unroll
+          for (int i = 0; i < WPL; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t p = h ? x[i] >> 8 : x[i], q = h ? y[i] >> 8 : y[i];
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+                mma_f16(o[(b * WPL + i) * 2 + h][nt], p & 0x000f000fu, p & 0x00f000f0u, q & 0x000f000fu, q & 0x00f000f0u,
+                        wf[nt][0], wf[nt][1]);
+            }
+        }
       }
       __syncwarp();
-      fetch();
+      if (lane == 0) mbar_arrive(bar_empty + 8 * (warp * ST + st));
     }
 
     // join the warps' sums: of each row the maximum, then everything relative to it
@@ -467,6 +506,7 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
           l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], k);
           z[nt][c] += __shfl_xor_sync(0xffffffffu, z[nt][c], k);
         }
+        if (fresh >> (2 * nt + c) & 1u) m[nt][c] = kNoMax;
         if (gid == 0) {
           const int r = warp * R + nt * 8 + 2 * tig + c;
           jm[r] = m[nt][c];
@@ -474,8 +514,8 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
           jz[r] = z[nt][c];
         }
       }
-    __syncthreads();
-    const bool whole = o0 - cur.base == 0 && o1 - cur.base == cur.ng;
+    named_bar(1, 32 * W);
+    const bool whole = o0 == cur.base && o1 - cur.base == cur.nu;
     const float back = 16777216.0f / vmul;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -498,57 +538,43 @@ __global__ void __launch_bounds__(32 * KvRowsShape<D>::W, NT == 1 ? 2 : 1) kv4_r
                   make_float2((v[c] - ow[nt][c]) * f, (v[2 + c] * 0.0625f - ow[nt][c]) * f);
             }
       }
-      __syncthreads();
-      constexpr int kPer = 8 * D / (32 * W);          // consecutive dimensions of a row a thread
-      const int row = threadIdx.x / (D / kPer), d0 = (threadIdx.x % (D / kPer)) * kPer;
-      const int r = rb * R + nt * 8 + row;
-      if (r < nrows) {
-        float top = kNoMax, sum = 0.0f, zs = 0.0f, v[kPer];
+      named_bar(1, 32 * W);
+      for (int i = threadIdx.x; i < 8 * D / 4; i += 32 * W) {   // four dimensions of a row each
+        const int row = i / (D / 4), d0 = i % (D / 4) * 4, r = rb * R + nt * 8 + row;
+        if (r >= nrows) break;
+        float top = kNoMax, sum = 0.0f, zs = 0.0f;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
         for (int w = 0; w < W; ++w) top = fmaxf(top, jm[w * R + nt * 8 + row]);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) v[i] = 0.0f;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
           const float f = exp2_fast(jm[w * R + nt * 8 + row] - top);
           sum += jl[w * R + nt * 8 + row] * f;
           zs += jz[w * R + nt * 8 + row] * f;
-#pragma unroll
-          for (int i = 0; i < kPer; i += 2) {
-            const float2 t = *(const float2*)(jO + (w * 8 + row) * (D + 4) + d0 + i);
-            v[i] += t.x;
-            v[i + 1] += t.y;
-          }
+          const float4 x = *(const float4*)(jO + (w * 8 + row) * (D + 4) + d0);
+          v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
         }
         if (whole) {
           const int qi = kv_div(r, A.by_group), hq = head * a.group + r - qi * a.group;
           const long long t = cur.q.first + qi;
           const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-          constexpr int kW = kPer / 2 < 4 ? kPer / 2 : 4;   // words a store
-#pragma unroll
-          for (int i = 0; i < kPer / 2; i += kW) {
-            uint32_t w[kW];
-#pragma unroll
-            for (int k = 0; k < kW; ++k)
-              w[k] = pack16<BF>((v[2 * (i + k)] + zs) * inv, (v[2 * (i + k) + 1] + zs) * inv);
-            store_words(a.out + t * a.out_stride + (long long)hq * D + d0 + 2 * i, w);
-          }
+          const uint32_t w[2] = {pack16<BF>((v.x + zs) * inv, (v.y + zs) * inv), pack16<BF>((v.z + zs) * inv, (v.w + zs) * inv)};
+          store_words(a.out + t * a.out_stride + (long long)hq * D + d0, w);
           if (a.lse && d0 == 0)
             a.lse[t * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
         } else {
           const int slot = o0 == cur.base ? 1 : 0;   // an item left open by the range's end, or one begun before it
           const long long at = ((long long)blockIdx.x * 2 + slot) * R + nt * 8 + row;
-#pragma unroll
-          for (int i = 0; i < kPer; i += 2) *(float2*)(A.part + at * D + d0 + i) = make_float2(v[i] + zs, v[i + 1] + zs);
+          *(float4*)(A.part + at * D + d0) = make_float4(v.x + zs, v.y + zs, v.z + zs, v.w + zs);
           if (d0 == 0) A.part_ml[at] = make_float2(top, sum);
         }
       }
-      __syncthreads();
+      named_bar(1, 32 * W);
     }
     if (!A.direct && o1 == n && threadIdx.x == 0) {
       const bool open = o0 == cur.base && !whole;
-      // the ranges that the item's groups reach into: each has n groups, the last one or fewer
-      const int rest = cur.ng - (o1 - o0);
+      // the ranges that the item's units reach into: each has n of them, the last one or fewer
+      const int rest = cur.nu - (o1 - o0);
       A.cut[blockIdx.x] = make_int4(cur.s, cur.it, open ? 1 + (rest + n - 1) / n : 0, 0);
     }
     o0 = o1;
@@ -569,7 +595,7 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const __grid_constant__ K
   if (parts == 0) return;
   KvCursor c;
   c.s = cut.x;
-  kv_shape<R>(A, c);
+  kv_shape<R, KvRowsShape<D>::U>(A, c);
   const int rb = cut.y / a.kv_heads, head = cut.y - rb * a.kv_heads, r = rb * R + blockIdx.y;
   if (r >= c.q.n * a.group) return;
   auto at = [&](int i) { return ((long long)(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * R + blockIdx.y; };

@@ -135,7 +135,7 @@ int plan_attention(const ifq_kv4_attention_desc* d, const KvAttnArgs& a, AttnPla
   const int R = 8 * p->nt;
   const long long blocks = std::max<long long>(1, (rows + R - 1) / R);   // (the device checks max_q = 0 too)
   p->direct = reach <= 64 * kKvGroup && blocks <= 65535 && d->seqs <= 65535;
-  p->blocks = p->direct ? (int)blocks : sm_count() * (p->nt == 1 ? 2 : 1);
+  p->blocks = p->direct ? (int)blocks : sm_count() * kv_rows_per_sm(D, p->nt);
   p->ws = p->direct ? 0 : round_up((size_t)p->blocks * (2 * R * (D * 4 + 8) + 16), 256);
   return IFQ_OK;
 }
@@ -166,7 +166,7 @@ int run_rows(const KvAttnArgs& a, const AttnPlan& p, void* ws, cudaStream_t st) 
     r.part = (float*)(r.part_ml + (size_t)p.blocks * 2 * R);
   }
   const dim3 grid = p.direct ? dim3(a.kv_heads, p.blocks, a.seqs) : dim3(p.blocks);
-  const cudaError_t e = launch_k(kv4_rows_kernel<D, BF, NT>, grid, dim3(32 * KvRowsShape<D>::W), smem, st, r);
+  const cudaError_t e = launch_k(kv4_rows_kernel<D, BF, NT>, grid, dim3(KvRowsShape<D>::threads), smem, st, r);
   if (e != cudaSuccess || p.direct) return done(e);
   return done(launch_k(kv4_join_kernel<D, BF, NT>, dim3(p.blocks, R), dim3(128), 0, st, r));
 }
