@@ -1,7 +1,7 @@
 // Products in e4m3 with a float scale for each block of 128 along k, and the quantiser of their
 // activations.
 #pragma once
-#include <cuda_fp8.h>
+#include <cuda.h>
 
 #include "kv4.cuh"
 
@@ -46,61 +46,302 @@ __global__ void __launch_bounds__(32 * kFp8QuantWarps) fp8_quantize_kernel(const
   if (lane == 0) a.scales[(long long)b * a.m + r] = s;
 }
 
+// ---------------------------------------------------------------- the product
+//
+// One tcgen05.mma tile: 128 rows of operand A (tensor-memory lanes) x BN rows of operand B (columns).
+// Where there are many rows of x, A is x and B is w; with few (SWAP) A is w, so that the weights, which
+// are then what is read, fill the lanes, and the rows of x are as few columns as 16.
+//
+// A block of 128 along k is one pipeline stage and one tensor-memory accumulator (two take turns): its
+// sum has scales of its own, so it leaves tensor memory for registers, where the tile's sum is kept:
+//   acc += (x_scale w_scale) * block      (one fma an element; the factor is a lane's own, or with SWAP
+//                                          a column's).
+// Warps: eight that promote and store (32 lanes x half the columns each), one that loads (TMA, 128-byte
+// swizzle), one that issues MMAs.
+//
+// A tile's k may be split over a cluster of ks blocks: each sends its partial columns to the block that
+// owns them through distributed shared memory, which adds them in the order of the ranks.
 struct Fp8Args {
-  const uint8_t *x, *w;
   const float *xs, *ws;
   void* out;
   long long out_stride;
-  int m, n, k, kb, out_type;
+  int m, n, kb, out_type, vec;   // vec: 16-byte stores are aligned
+  int tiles, tiles_a, ks;        // tiles of A
 };
 
-__device__ __forceinline__ float e4m3_value(uint8_t b) {
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)b, __NV_E4M3)));
+constexpr int kFp8Promote = 8;
+constexpr int kFp8Threads = 32 * (kFp8Promote + 2);
+
+template <int BN, bool SWAP>
+struct Fp8Shape {
+  static constexpr int stage = 16384 + BN * 128;
+  static constexpr bool split = BN < 256;
+  // a receive slot a rank: the owner's columns, 129 floats each
+  static constexpr int recv = split ? (BN + 8) * 129 * 4 : 0;
+  static constexpr int fit = (232448 - 1024 - 1024 - recv) / stage;
+  static constexpr int stages = fit < 8 ? fit : 8;
+  static constexpr int bytes = 1024 + stages * stage + recv + 256;
+  static constexpr int cols = 2 * BN < 32 ? 32 : 2 * BN;   // tensor memory
+  static_assert(bytes <= 232448 && stages >= 3, "shared memory budget");
+};
+
+template <int X>
+__device__ __forceinline__ void tmem_ld(uint32_t t, uint32_t (&v)[X]) {
+  static_assert(X == 8 || X == 16 || X == 32, "columns a load");
+  if constexpr (X == 8)
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(t)
+                 : "memory");
+  else if constexpr (X == 16)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(t)
+        : "memory");
+  else
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+          "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+          "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(t)
+        : "memory");
+}
+__device__ __forceinline__ void fma2(uint64_t& c, uint32_t a0, uint32_t a1, float f0, float f1) {
+  uint64_t a, f;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(a) : "r"(a0), "r"(a1));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(f) : "f"(f0), "f"(f1));
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(c) : "l"(a), "l"(f));
+}
+__device__ __forceinline__ float2 halves2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ void fp8_store(const Fp8Args& a, long long at, float v) {
+  if (a.out_type == IFQ_F32) ((float*)a.out)[at] = v;
+  else if (a.out_type == IFQ_F16) ((__half*)a.out)[at] = __float2half_rn(v);
+  else ((__nv_bfloat16*)a.out)[at] = __float2bfloat16_rn(v);
+}
+__device__ __forceinline__ uint32_t fp8_pack(int type, float a, float b) {
+  return type == IFQ_F16 ? pack16<false>(a, b) : pack16<true>(a, b);
 }
 
-// 64 x 64 outputs a block of 256 threads, 4 x 4 a thread.
-__global__ void __launch_bounds__(256) fp8_matmul_kernel(const Fp8Args a) {
-  __shared__ float sx[32][65], sw[32][65];
-  grid_dep_wait();
-  const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, ti = threadIdx.x / 16, tj = threadIdx.x % 16;
-  float acc[4][4] = {}, part[4][4] = {};
-  for (int k0 = 0; k0 < a.k; k0 += 32) {
-    for (int e = threadIdx.x; e < 64 * 32; e += 256) {
-      const int r = e / 32, c = e % 32;
-      const bool in = k0 + c < a.k;
-      sx[c][r] = in && i0 + r < a.m ? e4m3_value(a.x[(long long)(i0 + r) * a.k + k0 + c]) : 0.0f;
-      sw[c][r] = in && j0 + r < a.n ? e4m3_value(a.w[(long long)(j0 + r) * a.k + k0 + c]) : 0.0f;
+template <int BN, bool SWAP>
+__global__ void __launch_bounds__(kFp8Threads, 1)
+    fp8_matmul_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const __grid_constant__ Fp8Args a) {
+  using C = Fp8Shape<BN, SWAP>;
+  constexpr int ST = C::stages, HC = BN / 2;   // columns a thread
+  constexpr int LD = HC < 32 ? HC : HC > 64 ? 16 : 32;       // columns a load (few registers are left beside 128 sums)
+  extern __shared__ uint8_t raw[];
+  uint8_t* smem = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+  const uint32_t base = smem_u32(smem);
+  float* recv = (float*)(smem + ST * C::stage);
+  const uint32_t bars = base + ST * C::stage + C::recv;
+  auto full = [&](int s) { return bars + 8 * s; };
+  auto empty = [&](int s) { return bars + 8 * (ST + s); };
+  auto dfull = [&](int b) { return bars + 8 * (2 * ST + b); };
+  auto dempty = [&](int b) { return bars + 8 * (2 * ST + 2 + b); };
+  uint32_t* tptr = (uint32_t*)(smem + ST * C::stage + C::recv + 8 * (2 * ST + 4));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int ks = a.ks, rank = ks > 1 ? (int)cluster_ctarank() : 0;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < ST; ++i) {
+      mbar_init(full(i), 1);
+      mbar_init(empty(i), 1);
     }
-    __syncthreads();
-    for (int c = 0; c < 32; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) part[i][j] += sx[c][ti + 16 * i] * sw[c][tj + 16 * j];
-    __syncthreads();
-    if ((k0 + 32) % kFp8Block == 0 || k0 + 32 >= a.k) {
-      const int b = k0 / kFp8Block;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = i0 + ti + 16 * i, c = j0 + tj + 16 * j;
-          if (r < a.m && c < a.n) acc[i][j] += a.xs[(long long)b * a.m + r] * a.ws[(long long)(c / 128) * a.kb + b] * part[i][j];
-          part[i][j] = 0.0f;
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(dfull(b), 1);
+      mbar_init(dempty(b), kFp8Promote);
+    }
+    fence_mbar_init();
+    prefetch_tmap(&ta);
+    prefetch_tmap(&tb);
+  }
+  if (warp == 0) {
+    tmem_alloc(smem_u32(tptr), C::cols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tptr;
+  if (ks > 1) cluster_sync_all();   // the partners' shared memory is there
+  grid_dep_wait();
+  grid_dep_launch();
+
+  const int k0 = (int)((long long)rank * a.kb / ks), k1 = (int)((long long)(rank + 1) * a.kb / ks);
+  const int first = blockIdx.x / ks, step = gridDim.x / ks;
+  // tiles in groups of 16 tiles of A, within a group along A first
+  auto tile = [&](int t, int& ia, int& ib) {
+    const int tb_n = a.tiles / a.tiles_a, g = t / (16 * tb_n), in = t - g * 16 * tb_n, wide = min(16, a.tiles_a - 16 * g);
+    ib = in / wide;
+    ia = 16 * g + in - ib * wide;
+  };
+
+  if (warp == kFp8Promote) {
+    int it = 0;
+    bool ok = true;
+    for (int t = first; t < a.tiles && ok; t += step) {
+      int ia, ib;
+      tile(t, ia, ib);
+      for (int k = k0; k < k1; ++k, ++it) {
+        const int s = it % ST;
+        if (it >= ST && !__all_sync(0xffffffffu, mbar_wait(empty(s), (it / ST - 1) & 1))) { ok = false; break; }
+        if (elect_one()) {
+          mbar_arrive_expect_tx(full(s), C::stage);
+          tma_load_2d(base + s * C::stage, &ta, full(s), k * kFp8Block, ia * 128);
+          tma_load_2d(base + s * C::stage + 16384, &tb, full(s), k * kFp8Block, ib * BN);
         }
+        __syncwarp();
+      }
+    }
+    if (!ok)   // what was loaded has landed before the block may exit
+      for (int i = it - ST < 0 ? 0 : it - ST; i < it; ++i) mbar_wait(full(i % ST), (i / ST) & 1);
+  } else if (warp == kFp8Promote + 1) {
+    constexpr uint32_t idesc = idesc_e4m3_f32(128, BN);
+    int it = 0;
+    bool ok = true;
+    for (int t = first; t < a.tiles && ok; t += step)
+      for (int k = k0; k < k1; ++k, ++it) {
+        const int s = it % ST, b = it & 1;
+        if (!__all_sync(0xffffffffu, mbar_wait(full(s), (it / ST) & 1)) ||
+            (it >= 2 && !__all_sync(0xffffffffu, mbar_wait(dempty(b), (it / 2 - 1) & 1)))) { ok = false; break; }
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t da = sdesc_sw128(base + s * C::stage), db = sdesc_sw128(base + s * C::stage + 16384);
+#pragma unroll
+          for (int j = 0; j < kFp8Block / 32; ++j)   // 32 bytes along k: two 16-byte units of the descriptors' address
+            mma_e4m3(tmem + b * BN, da + 2 * j, db + 2 * j, idesc, j > 0);
+          mma_commit(empty(s));
+          mma_commit(dfull(b));
+        }
+        __syncwarp();
+      }
+  } else {
+    const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane, c0 = half * HC;
+    const uint32_t tl = tmem + ((uint32_t)(quad * 32) << 16) + c0;
+    int it = 0;
+    bool ok = true;
+    for (int t = first; t < a.tiles && ok; t += step) {
+      int ia, ib;
+      tile(t, ia, ib);
+      uint64_t acc[HC / 2];
+#pragma unroll
+      for (int i = 0; i < HC / 2; ++i) acc[i] = 0;
+      // the factors of block k: a thread's own row of x and its columns' 128 rows of w; with SWAP its row of w, and
+      // lane c of a warp has column c0 + c's (and c0 + 32 + c's) of x
+      const int wb = SWAP ? ia : (ib * BN + c0) / 128;
+      const int xr = SWAP ? ib * BN + c0 + lane : ia * 128 + row;
+      const bool have = xr < a.m && (!SWAP || lane < HC) && (SWAP || wb * 128 < a.n);
+      const float* xp = a.xs + xr;
+      const float* wp = a.ws + (long long)wb * a.kb;
+      float fn = have ? xp[(long long)k0 * a.m] * wp[k0] : 0.0f;
+      for (int k = k0; k < k1; ++k, ++it) {
+        const float f = fn;
+        if (k + 1 < k1 && have) fn = xp[(long long)(k + 1) * a.m] * wp[k + 1];
+        const int b = it & 1;
+        if (!__all_sync(0xffffffffu, mbar_wait(dfull(b), (it / 2) & 1))) { ok = false; break; }
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < HC; c += LD) {
+          uint32_t v[LD];
+          tmem_ld<LD>(tl + b * BN + c, v);
+          if (c + LD == HC) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(dempty(b));
+          }
+#pragma unroll
+          for (int i = 0; i < LD; i += 2) {
+            if constexpr (SWAP)
+              fma2(acc[(c + i) / 2], v[i], v[i + 1], __shfl_sync(0xffffffffu, f, i), __shfl_sync(0xffffffffu, f, i + 1));
+            else
+              fma2(acc[(c + i) / 2], v[i], v[i + 1], f, f);
+          }
+        }
+      }
+      if (!ok) break;
+      if (C::split && ks > 1) {
+#pragma unroll
+        for (int i = 0; i < HC / 2; ++i) {
+          const float2 v = halves2(acc[i]);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int c = c0 + 2 * i + e, own = ((c + 1) * ks - 1) / BN, lo = own * BN / ks, per = (BN + ks - 1) / ks;
+            const uint32_t at = mapa_shared(smem_u32(recv + (rank * per + c - lo) * 129 + row), own);
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(e ? v.y : v.x) : "memory");
+          }
+        }
+        break;
+      }
+      if constexpr (SWAP) {
+        const int n = ia * 128 + row;
+        if (n < a.n) {
+#pragma unroll
+          for (int i = 0; i < HC / 2; ++i) {
+            const float2 v = halves2(acc[i]);
+            const int m = ib * BN + c0 + 2 * i;
+            if (m < a.m) fp8_store(a, (long long)m * a.out_stride + n, v.x);
+            if (m + 1 < a.m) fp8_store(a, (long long)(m + 1) * a.out_stride + n, v.y);
+          }
+        }
+      } else {
+        const int m = ia * 128 + row, n = ib * BN + c0;
+        if (m < a.m) {
+#pragma unroll
+          for (int i = 0; i < HC; i += 8) {
+            const long long at = (long long)m * a.out_stride + n + i;
+            float2 v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = halves2(acc[i / 2 + j]);
+            if (a.vec && n + i + 8 <= a.n) {
+              if (a.out_type == IFQ_F32) {
+                *(float4*)((float*)a.out + at) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+                *(float4*)((float*)a.out + at + 4) = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+              } else {
+                *(uint4*)((uint16_t*)a.out + at) =
+                    make_uint4(fp8_pack(a.out_type, v[0].x, v[0].y), fp8_pack(a.out_type, v[1].x, v[1].y),
+                               fp8_pack(a.out_type, v[2].x, v[2].y), fp8_pack(a.out_type, v[3].x, v[3].y));
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                if (n + i + 2 * j < a.n) fp8_store(a, at + 2 * j, v[j].x);
+                if (n + i + 2 * j + 1 < a.n) fp8_store(a, at + 2 * j + 1, v[j].y);
+              }
+            }
+          }
+        }
+      }
     }
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = i0 + ti + 16 * i, c = j0 + tj + 16 * j;
-      if (r >= a.m || c >= a.n) continue;
-      const long long at = r * a.out_stride + c;
-      if (a.out_type == IFQ_F32) ((float*)a.out)[at] = acc[i][j];
-      else if (a.out_type == IFQ_F16) ((__half*)a.out)[at] = __float2half_rn(acc[i][j]);
-      else ((__nv_bfloat16*)a.out)[at] = __float2bfloat16_rn(acc[i][j]);
+  if (C::split && ks > 1) {
+    __syncwarp();
+    cluster_sync_all();   // every partial sum has arrived
+    if (warp < kFp8Promote) {
+      int ia, ib;
+      tile(first, ia, ib);
+      const int lo = rank * BN / ks, hi = (rank + 1) * BN / ks, wide = hi - lo, per = (BN + ks - 1) / ks;
+      for (int i = threadIdx.x; i < 128 * wide; i += 32 * kFp8Promote) {
+        // out rows are contiguous along w's rows: those are the lanes (SWAP) or the columns
+        const int r = SWAP ? i % 128 : i / wide, c = SWAP ? i / 128 : i - r * wide;
+        float v = 0.0f;
+        for (int p = 0; p < ks; ++p) v += recv[(p * per + c) * 129 + r];
+        const int m = SWAP ? ib * BN + lo + c : ia * 128 + r, n = SWAP ? ia * 128 + r : ib * BN + lo + c;
+        if (m < a.m && n < a.n) fp8_store(a, (long long)m * a.out_stride + n, v);
+      }
     }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tmem, C::cols);
 }
 
 }  // namespace ifq

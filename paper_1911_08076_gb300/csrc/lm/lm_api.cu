@@ -171,6 +171,103 @@ int run_rows(const KvAttnArgs& a, const AttnPlan& p, void* ws, cudaStream_t st) 
   return done(launch_k(kv4_join_kernel<D, BF, NT>, dim3(p.blocks, R), dim3(128), 0, st, r));
 }
 
+// ---------------------------------------------------------------- products in e4m3
+
+struct Fp8Operands {
+  const void* x;
+  const float* xs;
+  const void* w;
+  const float* ws;
+  void* out;
+  cudaStream_t st;
+};
+
+// TMA descriptor of an e4m3 operand: [rows][k] bytes, boxes of `box` rows x 128 bytes in the 128-byte swizzle; rows and
+// columns past the end read as zeros.
+bool encode_e4m3(const void* p, int rows, int k, int box, CUtensorMap* tm) {
+  const cuuint64_t gdim[2] = {(cuuint64_t)k, (cuuint64_t)rows}, gstride[1] = {(cuuint64_t)k};
+  const cuuint32_t bdim[2] = {(cuuint32_t)kFp8Block, (cuuint32_t)box}, estr[2] = {1, 1};
+  return g_encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p), gdim, gstride, bdim, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int kFp8MaxSplit = 8;
+
+// One-time setup of an instance on the current device: its shared memory, and how many clusters of each size run at
+// once (in `slots`; a plain launch is size 1).
+template <int BN, bool SWAP>
+int fp8_setup(const int** slots) {
+  static int known[kMaxDevices][kFp8MaxSplit + 1];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return IFQ_ECUDA;
+  const int sms = sm_count();
+  std::lock_guard<std::mutex> lk(g_lm_mu);
+  int* s = known[dev];
+  if (!s[1]) {
+    using C = Fp8Shape<BN, SWAP>;
+    auto kern = fp8_matmul_kernel<BN, SWAP>;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::bytes) != cudaSuccess) return IFQ_ECUDA;
+    for (int ks = 2; C::split && ks <= kFp8MaxSplit; ++ks) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3((unsigned)(sms / ks * ks));
+      cfg.blockDim = dim3(kFp8Threads);
+      cfg.dynamicSmemBytes = C::bytes;
+      cudaLaunchAttribute at[1];
+      at[0].id = cudaLaunchAttributeClusterDimension;
+      at[0].val.clusterDim.x = (unsigned)ks;
+      at[0].val.clusterDim.y = 1;
+      at[0].val.clusterDim.z = 1;
+      cfg.attrs = at;
+      cfg.numAttrs = 1;
+      int n = 0;
+      s[ks] = cudaOccupancyMaxActiveClusters(&n, kern, &cfg) == cudaSuccess ? n : 0;
+    }
+    cudaGetLastError();   // (a cluster size that does not fit is no error of this call)
+    s[1] = sms;
+  }
+  *slots = s;
+  return IFQ_OK;
+}
+
+template <int BN, bool SWAP>
+int run_fp8(const ifq_fp8_desc* d, const Fp8Operands& o) {
+  using C = Fp8Shape<BN, SWAP>;
+  const int* slots;
+  const int rc = fp8_setup<BN, SWAP>(&slots);
+  if (rc) return rc;
+  Fp8Args a;
+  a.xs = o.xs;
+  a.ws = o.ws;
+  a.out = o.out;
+  a.out_stride = d->out_stride ? d->out_stride : d->n;
+  a.m = d->m;
+  a.n = d->n;
+  a.kb = ceil_div(d->k, kFp8Block);
+  a.out_type = d->out_dtype;
+  a.vec = a.out_stride * (d->out_dtype == IFQ_F32 ? 4 : 2) % 16 == 0;
+  a.tiles_a = ceil_div(SWAP ? d->n : d->m, 128);
+  const long long tiles = (long long)a.tiles_a * ceil_div(SWAP ? d->m : d->n, BN);
+  if (tiles > INT_MAX / kFp8MaxSplit) return IFQ_ERANGE;
+  a.tiles = (int)tiles;
+  // the split of k with the fewest blocks of k in a row, each launch or cluster also costing as much as a few blocks
+  a.ks = 1;
+  double best = (double)ceil_div(a.tiles, slots[1]) * (a.kb + 6);
+  for (int ks = 2; C::split && ks <= kFp8MaxSplit && ks <= a.kb; ++ks) {
+    if (slots[ks] < 1) continue;
+    const double c = (double)ceil_div(a.tiles, slots[ks]) * (ceil_div(a.kb, ks) + 6) + 4;
+    if (c < best) best = c, a.ks = ks;
+  }
+  CUtensorMap tx, tw;
+  if (!encode_e4m3(o.x, d->m, d->k, SWAP ? BN : 128, &tx) || !encode_e4m3(o.w, d->n, d->k, SWAP ? 128 : BN, &tw)) return IFQ_ECUDA;
+  const CUtensorMap &ta = SWAP ? tw : tx, &tb = SWAP ? tx : tw;
+  if (a.ks > 1)
+    return done(launch_k_cluster(fp8_matmul_kernel<BN, SWAP>, a.ks, dim3((unsigned)(a.tiles * a.ks)), dim3(kFp8Threads), C::bytes,
+                                 o.st, ta, tb, a));
+  return done(launch_k(fp8_matmul_kernel<BN, SWAP>, dim3((unsigned)std::min(a.tiles, slots[1])), dim3(kFp8Threads), C::bytes, o.st,
+                       ta, tb, a));
+}
+
 }  // namespace
 
 namespace ifq {
@@ -349,21 +446,15 @@ int ifq_fp8_matmul(const ifq_fp8_desc* d, const void* x, const float* x_scale, c
   if (!aligned16(x) || !aligned16(w) || !aligned16(out) || !aligned16(ws) || !aligned(x_scale, 4) || !aligned(w_scale, 4))
     return IFQ_EALIGN;
   (void)ws_bytes;
-  Fp8Args a;
-  a.x = (const uint8_t*)x;
-  a.w = (const uint8_t*)w;
-  a.xs = x_scale;
-  a.ws = w_scale;
-  a.out = out;
-  a.out_stride = d->out_stride ? d->out_stride : d->n;
-  a.m = d->m;
-  a.n = d->n;
-  a.k = d->k;
-  a.kb = ceil_div(d->k, kFp8Block);
-  a.out_type = d->out_dtype;
-  if (ceil_div(d->m, 64) > 65535) return IFQ_ERANGE;
   if (!d->m) return IFQ_OK;
-  return done(launch_k(fp8_matmul_kernel, dim3(ceil_div(d->n, 64), ceil_div(d->m, 64)), dim3(256), 0, S(stream), a));
+  if (!get_encode()) return IFQ_ECUDA;
+  const Fp8Operands o = {x, x_scale, w, w_scale, out, S(stream)};
+  if (d->m <= 16) return run_fp8<16, true>(d, o);
+  if (d->m <= 32) return run_fp8<32, true>(d, o);
+  if (d->m <= 64) return run_fp8<64, true>(d, o);
+  // wide tiles where they fill the SMs
+  if ((long long)ceil_div(d->m, 128) * ceil_div(d->n, 256) >= sm_count()) return run_fp8<256, false>(d, o);
+  return run_fp8<128, false>(d, o);
 }
 
 }  // extern "C"
