@@ -1,0 +1,583 @@
+// Attention of many query rows per sequence over the paged 4-bit cache (chunks of a prompt), on tcgen05.
+//
+// A block takes 128 RT rows of a key head (query tokens x the heads that share it) and their keys in tiles of 128:
+//   S[row][key] = sum_d q[row][d] c[key][d]    (half x half, both operands in shared memory),
+//   O[row][d]  += sum_key p[row][key] v[key][d] (p from tensor memory, over S's columns; v in shared memory).
+// Bound by the tensor cores' half rate in the limit, by the softmax's instructions beside them as measured.
+//
+// Keys: codes are expanded to halves as the subnormals c 2^-24 and 16 c 2^-24 (masks alone, as in kv4_rows.cuh; q's
+// elements stand in the order that leaves the codes of a word in, with the factors 1/16 in them).  Products with them
+// are exact, sums fp32; the scale and the minimum of a key are applied to the sum,
+//   t = s (q . c) + m sum(q),   two packed fma a pair of keys, with the softmax's reference in the second.
+// Values: v = half((s' c' + m') / 2), one fma of halves: as fine as the minimum that the cache holds (a half), and
+// within the half's range where s' c' + m' would leave it.  Weights p are halves of 2^(t - m) with the reference m of a
+// row raised only when a score passes it by 8, in whole powers of two; their sum is that of the unrounded p.
+// A value that is not a number must reach only the rows that see it: its operand is 0 and its key's minimum NaN.
+//
+// Warps: one or two groups of four run the softmax, a thread a row, so that no value crosses threads; four expand codes
+// (global memory to registers a tile ahead, then to swizzled shared memory); one issues MMAs.  Two S buffers: with
+// RT = 2 one a row tile; else the key tiles alternate, and with two groups each has an O of its own, joined at the end.
+// A block's keys may be split over `splits` blocks, joined by kv4_chunk_join_kernel.
+#pragma once
+#include "kv4_rows.cuh"
+
+namespace ifq {
+
+struct KvChunkArgs {
+  KvAttnArgs a;
+  KvDiv by_gpp, by_group;
+  int blocks, splits;        // blocks of rows of a (sequence, head) at most; blocks a block's keys are split over
+  float* part;               // [seqs][heads][blocks][splits][rows][D]
+  float2* part_ml;           // the same without D: reference and sum
+};
+
+constexpr int kChunkKeys = 128, kChunkPar = 4;   // keys a tile; tiles whose parameters are held
+
+template <int D, int RT>
+struct KvChunkShape {
+  static constexpr int NG = D == 256 ? 1 : 2;               // softmax groups
+  static constexpr int NB = D == 256 ? 1 : 2;               // key and value buffers
+  static constexpr int threads = 32 * (4 * NG + 5);
+  static constexpr int q_bytes = RT * 128 * D * 2, kv_bytes = 128 * D * 2;
+  static constexpr int par_bytes = kChunkPar * kChunkKeys * 8;
+  static constexpr int bytes = 1024 + q_bytes + 2 * NB * kv_bytes + par_bytes + 512;
+  static_assert(RT == 1 || NG == 2, "a group a row tile");
+  static_assert(bytes <= 232448, "shared memory budget");
+};
+
+// Instruction descriptor, kind::f16, half operands, fp32 accumulator, both K-major.
+__host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N) {
+  return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(d),
+               "l"(a), "l"(b), "r"(idesc), "r"(acc)
+               : "memory");
+}
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;}" ::"r"(d),
+               "r"(a), "l"(b), "r"(idesc), "r"(acc)
+               : "memory");
+}
+// 16 / 32 registers of a lane to consecutive columns of its row.
+__device__ __forceinline__ void tmem_st16(uint32_t t, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(t),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ uint64_t pair2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2v(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// The key tiles that a block of rows reads: those with the first tokens (sinks), then those in reach.
+struct KvTiles {
+  int n, sg, skip;
+};
+__device__ __forceinline__ KvTiles kv_tiles(const KvAttnArgs& a, int len, int p_lo, int p_hi) {
+  KvTiles t;
+  const int all = p_hi < 0 ? 0 : p_hi / kChunkKeys + 1;
+  const int lo = a.window > 0 && p_lo >= a.window ? (p_lo - a.window + 1) / kChunkKeys : 0;
+  const int sinks = min(a.sinks, len);
+  t.sg = min((sinks + kChunkKeys - 1) / kChunkKeys, lo);
+  t.skip = lo - t.sg;
+  t.n = max(0, all - t.skip);
+  return t;
+}
+
+template <int D, bool BF, int RT>
+__global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_kernel(const __grid_constant__ KvChunkArgs A) {
+  using C = KvChunkShape<D, RT>;
+  constexpr int NG = C::NG, NB = C::NB, DB = kv4_block(D), NBLK = D / DB, WPB = DB / 32, GB = kv4_group_bytes(D);
+  extern __shared__ uint8_t raw[];
+  uint8_t* smem = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+  uint8_t *sQ = smem, *sK = sQ + C::q_bytes, *sV = sK + NB * C::kv_bytes;
+  float4* sPar = (float4*)(sV + NB * C::kv_bytes);          // [kChunkPar][64 pairs of keys]: s, s, m, m
+  const uint32_t bars = smem_u32(sPar) + C::par_bytes;
+  auto kfull = [&](int b) { return bars + 8 * b; };          // expanded keys
+  auto kempty = [&](int b) { return bars + 16 + 8 * b; };
+  auto vfull = [&](int b) { return bars + 32 + 8 * b; };
+  auto vempty = [&](int b) { return bars + 48 + 8 * b; };
+  auto sfull = [&](int b) { return bars + 64 + 8 * b; };     // a finished S, its weights, a finished O
+  auto pready = [&](int b) { return bars + 80 + 8 * b; };
+  auto odone = [&](int r) { return bars + 96 + 8 * r; };
+  auto pfull = [&](int b) { return bars + 112 + 8 * b; };    // parameters
+  auto pempty = [&](int b) { return bars + 112 + 8 * kChunkPar + 8 * b; };
+  const uint32_t qready = bars + 112 + 16 * kChunkPar;
+  uint32_t* tptr = (uint32_t*)((uint8_t*)sPar + C::par_bytes + 112 + 16 * kChunkPar + 8);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(kfull(b), 4);
+      mbar_init(kempty(b), 1);
+      mbar_init(vfull(b), 4);
+      mbar_init(vempty(b), 1);
+      mbar_init(sfull(b), 1);
+      mbar_init(pready(b), 4);
+      mbar_init(odone(b), 1);
+    }
+    for (int b = 0; b < kChunkPar; ++b) {
+      mbar_init(pfull(b), 4);
+      mbar_init(pempty(b), 4 * RT);
+    }
+    mbar_init(qready, 4 * RT);
+    fence_mbar_init();
+  }
+  if (warp == 4 * NG + 4) {
+    tmem_alloc(smem_u32(tptr), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tptr;
+  grid_dep_wait();
+  grid_dep_launch();
+
+  const KvAttnArgs& a = A.a;
+  const int s = blockIdx.z / A.splits, sp = blockIdx.z - s * A.splits, head = blockIdx.y;
+  const KvSeq q = kv_seq(a, s);
+  const int rows = q.ok ? q.n * a.group : 0, r0 = (A.blocks - 1 - (int)blockIdx.x) * 128 * RT;   // the longest first
+  if (!q.ok && threadIdx.x == 0) set_status(IFQ_ERANGE);
+  const bool work = r0 < rows;
+  const int p_lo = q.len - q.n + (work ? (int)kv_div(r0, A.by_group) : 0);
+  const int p_hi = q.len - q.n + (work ? (int)kv_div(min(rows, r0 + 128 * RT) - 1, A.by_group) : 0);
+  const KvTiles tiles = kv_tiles(a, q.len, p_lo, p_hi);
+  const int t0 = work ? (int)((long long)tiles.n * sp / A.splits) : 0, t1 = work ? (int)((long long)tiles.n * (sp + 1) / A.splits) : 0;
+  const int nt = t1 - t0, steps = nt * RT;   // step x: tile x / RT, S buffer x % 2, softmax group x % NG
+  auto first_key = [&](int i) { return (t0 + i < tiles.sg ? t0 + i : t0 + i + tiles.skip) * kChunkKeys; };
+
+  if (warp < 4 * NG) {
+    // ------------------------------------------------------------ softmax: a thread a row
+    const int grp = warp >> 2, row = threadIdx.x & 127, rt = RT == 2 ? grp : 0, r = r0 + rt * 128 + row;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, tO = tmem + lanes + 256 + grp * D;
+    const bool have = work && r < rows;
+    const int qi = have ? (int)kv_div(r, A.by_group) : 0, hq = head * a.group + (have ? r - qi * a.group : 0);
+    const int p = q.len - q.n + qi, p_first = a.window > 0 ? p - a.window + 1 : 0;
+    float fa = 0.0f, fb = 0.0f;
+    if (work) {
+      // the row of q, brought to half by a power of two; with one row tile the second group only needs the factors
+      const uint16_t* src = a.q + (long long)(q.first + qi) * a.q_stride + (long long)hq * D;
+      float top = 0.0f, sum = 0.0f;
+#pragma unroll 4
+      for (int i = 0; i < D / 8; ++i) {
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (have) load_words(w, src + 8 * i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 f = unpack16<BF>(w[k]);
+          top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+          sum += f.x + f.y;
+        }
+      }
+      int e = (int)(__float_as_uint(top) >> 23) - 127 - 14;
+      e = max(-100, min(113, e));
+      const float down = __uint_as_float((uint32_t)(127 - e) << 23), low = down * 0.0625f, sc = a.scale * 1.44269504f;
+      fa = sc * __uint_as_float((uint32_t)(127 + e) << 23);
+      fb = sc * sum;
+      if (RT == 2 || grp == 0) {
+#pragma unroll 4
+        for (int i = 0; i < D / 8; ++i) {
+          uint32_t w[4] = {0, 0, 0, 0};
+          if (have) load_words(w, src + 8 * i);
+          const float2 f0 = unpack16<BF>(w[0]), f1 = unpack16<BF>(w[1]), f2 = unpack16<BF>(w[2]), f3 = unpack16<BF>(w[3]);
+          const uint4 v = make_uint4(pack16<false>(f0.x * down, f2.x * down), pack16<false>(f0.y * low, f2.y * low),
+                                     pack16<false>(f1.x * down, f3.x * down), pack16<false>(f1.y * low, f3.y * low));
+          *(uint4*)(sQ + rt * 128 * D * 2 + (i >> 3) * 16384 + row * 128 + (((i & 7) ^ (row & 7)) << 4)) = v;
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(qready);
+      }
+    }
+    float m = 0.0f;
+    uint64_t l2 = 0;
+    bool fresh = have, ok = true;
+    int mine = 0;   // steps of this group so far
+    for (int x = grp; x < steps && ok; x += NG, ++mine) {
+      const int i = x / RT, b = x & 1, pb = i % kChunkPar, j0 = first_key(i);
+      const uint32_t tS = tmem + lanes + b * 128;
+      ok = __all_sync(0xffffffffu, mbar_wait(pfull(pb), (i / kChunkPar) & 1) && mbar_wait(sfull(b), (x >> 1) & 1));
+      if (!ok) break;
+      tc_fence_after();
+      const float4* par = sPar + pb * (kChunkKeys / 2);
+      const bool full = j0 + kChunkKeys - 1 <= p_lo && (a.window == 0 || j0 > p_hi - a.window || j0 + kChunkKeys <= a.sinks);
+      const uint64_t fa2 = pair2(fa, fa), fb2 = pair2(fb, fb);
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        uint32_t v[32];
+        tmem_ld<32>(tS + 32 * c, v);
+        float t[32];
+        const uint64_t m2 = pair2(-m, -m);
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const float4 kp = par[16 * c + k];
+          const float2 z = halves2(fma2v(pair2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])),
+                                         mul2(pair2(kp.x, kp.y), fa2), fma2v(pair2(kp.z, kp.w), fb2, m2)));
+          t[2 * k] = z.x;
+          t[2 * k + 1] = z.y;
+        }
+        if (!full) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            const int j = j0 + 32 * c + k;
+            if (j > p || (j < p_first && j >= a.sinks)) t[k] = -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) top = fmaxf(top, fmaxf(t[k], t[k + 1]));
+        if (__any_sync(0xffffffffu, top > 8.0f || (fresh && top > -INFINITY))) {
+          const bool begin = fresh && top > -INFINITY;
+          const float rise = begin || top > 8.0f ? ceilf(top) : 0.0f, f = begin ? 1.0f : exp2_fast(-rise);
+          if (begin) fresh = false;
+          m += rise;
+          l2 = mul2(l2, pair2(f, f));
+#pragma unroll
+          for (int k = 0; k < 32; ++k) t[k] -= rise;
+          // what this tile's columns and the sum already hold
+          const uint32_t fh = pack16<false>(f, f);
+          tmem_wait_st();
+          for (int d = 0; d < c; ++d) {
+            uint32_t w[16];
+            tmem_ld<16>(tS + 16 * d, w);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const __half2 y = __hmul2(*(const __half2*)&w[k], *(const __half2*)&fh);
+              w[k] = *(const uint32_t*)&y;
+            }
+            tmem_st16(tS + 16 * d, w);
+          }
+          if (mine > 0) {
+            ok = __all_sync(0xffffffffu, mbar_wait(odone(grp), (mine - 1) & 1));
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int d = 0; d < D; d += 16) {
+              uint32_t w[16];
+              tmem_ld<16>(tO + d, w);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * f);
+              tmem_st16(tO + d, w);
+            }
+          }
+        }
+        uint32_t w[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const float u0 = exp2_fast(t[2 * k]), u1 = exp2_fast(t[2 * k + 1]);
+          l2 = add2(l2, pair2(u0, u1));
+          w[k] = pack16<false>(u0, u1);
+        }
+        tmem_st16(tS + 16 * c, w);
+      }
+      if (!ok) break;
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(pready(b));
+        mbar_arrive(pempty(pb));
+      }
+    }
+    if (mine > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(odone(grp), (mine - 1) & 1));
+    tc_fence_after();
+    const float2 lh = halves2(l2);
+    float sum = lh.x + lh.y, top = fresh || !have ? kNoMax : m;
+    float other_top = kNoMax, other_f = 0.0f, my_f = 1.0f;
+    float* xo = (float*)sK;   // [128][D + 4], and the second group's references and sums
+    float2* xml = (float2*)(xo + 128 * (D + 4));
+    if (NG == 2 && RT == 1 && work) {
+      // the other half of the keys; all products are done once both groups have passed their waits
+      named_bar(1, 256);
+      if (grp == 1) {
+        xml[row] = make_float2(top, sum);
+#pragma unroll 1
+        for (int d = 0; d < D; d += 16) {
+          uint32_t w[16];
+          if (mine > 0) tmem_ld<16>(tO + d, w);
+#pragma unroll
+          for (int k = 0; k < 16; k += 4)
+            *(float4*)(xo + row * (D + 4) + d + k) =
+                mine > 0 ? make_float4(__uint_as_float(w[k]), __uint_as_float(w[k + 1]), __uint_as_float(w[k + 2]), __uint_as_float(w[k + 3]))
+                         : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+      }
+      named_bar(1, 256);
+      if (grp == 0) {
+        const float2 o = xml[row];
+        other_top = o.x;
+        const float all = fmaxf(top, other_top);
+        my_f = exp2_fast(top - all);
+        other_f = exp2_fast(other_top - all);
+        sum = sum * my_f + o.y * other_f;
+        top = all;
+      }
+    }
+    if (work && (RT == 2 || grp == 0)) {
+      const bool parts = A.splits > 1;
+      const long long at = ((((long long)s * a.kv_heads + head) * A.blocks + r0 / (128 * RT)) * A.splits + sp) * (128 * RT) + rt * 128 + row;
+      const float inv = parts ? 2.0f : sum == 0.0f ? 0.0f : 2.0f / sum;
+#pragma unroll 1
+      for (int d = 0; d < D; d += 16) {
+        uint32_t w[16];
+        if (mine > 0) tmem_ld<16>(tO + d, w);
+        float o[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) o[k] = mine > 0 ? __uint_as_float(w[k]) : 0.0f;
+        if (NG == 2 && RT == 1) {
+#pragma unroll
+          for (int k = 0; k < 16; k += 4) {
+            const float4 y = *(const float4*)(xo + row * (D + 4) + d + k);
+            o[k] = o[k] * my_f + y.x * other_f, o[k + 1] = o[k + 1] * my_f + y.y * other_f;
+            o[k + 2] = o[k + 2] * my_f + y.z * other_f, o[k + 3] = o[k + 3] * my_f + y.w * other_f;
+          }
+        }
+        if (have && parts) {
+#pragma unroll
+          for (int k = 0; k < 16; k += 4)
+            *(float4*)(A.part + at * D + d + k) = make_float4(o[k] * inv, o[k + 1] * inv, o[k + 2] * inv, o[k + 3] * inv);
+        } else if (have) {
+          uint16_t* dst = a.out + (long long)(q.first + qi) * a.out_stride + (long long)hq * D + d;
+#pragma unroll
+          for (int k = 0; k < 16; k += 8) {
+            const uint32_t y[4] = {pack16<BF>(o[k] * inv, o[k + 1] * inv), pack16<BF>(o[k + 2] * inv, o[k + 3] * inv),
+                                   pack16<BF>(o[k + 4] * inv, o[k + 5] * inv), pack16<BF>(o[k + 6] * inv, o[k + 7] * inv)};
+            store_words(dst + k, y);
+          }
+        }
+        __syncwarp();
+      }
+      if (have) {
+        if (parts) A.part_ml[at] = make_float2(top, sum);
+        else if (a.lse)
+          a.lse[(long long)(q.first + qi) * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
+      }
+    }
+  } else if (warp < 4 * NG + 4) {
+    // ------------------------------------------------------------ expansion: a thread a key, and 8 keys x D/8 values
+    const int tid = threadIdx.x - 128 * NG, w = warp - 4 * NG;
+    const int kg = tid >> 4, krow = tid & 15;                                  // the key's group of the tile, row of it
+    const int c8 = lane & 7, vg = (w >> 1) * 4 + (c8 >> 1), vh = c8 & 1, slice = (lane >> 3) | (w & 1) << 2;
+    uint32_t kw[NBLK * WPB * 4], vw[NBLK * WPB * 4], kpar = 0, vpar = 0, vp[8];
+    auto group = [&](int i, int g) -> const uint8_t* {   // group g of tile i, if it holds tokens
+      const int gi = first_key(i) / kKvGroup + g;
+      if (gi * kKvGroup >= q.len) return nullptr;
+      const int pi = kv_div(gi, A.by_gpp), page = a.table[(long long)s * a.max_pages + pi];
+      if (page < 0 || page >= a.pages) {
+        set_status(IFQ_ERANGE);
+        return nullptr;
+      }
+      return a.cache + (((long long)page * a.kv_heads + head) * A.by_gpp.d + (gi - pi * A.by_gpp.d)) * GB;
+    };
+    auto load_k = [&](const uint8_t* g) {
+#pragma unroll
+      for (int b = 0; b < NBLK; ++b)
+#pragma unroll
+        for (int k = 0; k < WPB; ++k) {
+          uint4 y = make_uint4(0, 0, 0, 0);
+          if (g) y = *(const uint4*)(g + b * 8 * DB + krow * (DB / 2) + 16 * k);
+          const int o = (b * WPB + k) * 4;
+          kw[o] = y.x, kw[o + 1] = y.y, kw[o + 2] = y.z, kw[o + 3] = y.w;
+        }
+      kpar = g ? *(const uint32_t*)(g + 16 * D + 4 * krow) : 0u;
+      vpar = g ? *(const uint32_t*)(g + 16 * D + 64 + 4 * krow) : 0u;
+    };
+    auto load_v = [&](const uint8_t* g) {
+#pragma unroll
+      for (int b = 0; b < NBLK; ++b)
+#pragma unroll
+        for (int k = 0; k < WPB; ++k) {
+          uint4 y = make_uint4(0, 0, 0, 0);
+          if (g) y = *(const uint4*)(g + 8 * D + b * 8 * DB + vh * 4 * DB + slice * 4 * (DB / 8) + 16 * k);
+          const int o = (b * WPB + k) * 4;
+          vw[o] = y.x, vw[o + 1] = y.y, vw[o + 2] = y.z, vw[o + 3] = y.w;
+        }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint4 y = make_uint4(0, 0, 0, 0);
+        if (g) y = *(const uint4*)(g + 16 * D + 64 + 32 * vh + 16 * k);
+        vp[4 * k] = y.x, vp[4 * k + 1] = y.y, vp[4 * k + 2] = y.z, vp[4 * k + 3] = y.w;
+      }
+    };
+    // a key's parameters that are numbers (neither an infinity nor a NaN in either half)
+    auto finite = [](uint32_t par) { return (par & 0x7c00u) != 0x7c00u && (par & 0x7c000000u) != 0x7c000000u; };
+    bool ok = true;
+    if (nt > 0) {
+      load_k(group(0, kg));
+      load_v(group(0, vg));
+    }
+    for (int i = 0; i < nt && ok; ++i) {
+      const int b = i % NB, pb = i % kChunkPar, j0 = first_key(i);
+      const uint8_t *gk = nullptr, *gv = nullptr;
+      if (i + 1 < nt) gk = group(i + 1, kg), gv = group(i + 1, vg);
+      ok = (i < kChunkPar || mbar_wait(pempty(pb), (i / kChunkPar - 1) & 1)) &&
+           (i < NB || mbar_wait(kempty(b), (i / NB - 1) & 1));
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      {
+        const bool there = j0 + tid < q.len;
+        float2 f = unpack16<false>(there ? kpar : 0u);
+        if (there && !finite(vpar)) f.y = __uint_as_float(0x7fc00000u);   // NaN to the rows that see it
+        float* dst = (float*)(sPar + pb * (kChunkKeys / 2) + tid / 2) + (tid & 1);
+        dst[0] = f.x * 16777216.0f;
+        dst[2] = f.y;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(pfull(pb));
+      }
+      uint8_t* dk = sK + b * C::kv_bytes + tid * 128;
+#pragma unroll
+      for (int k = 0; k < NBLK * WPB * 4; ++k) {
+        const uint32_t u = kw[k], h = u >> 8;
+        *(uint4*)(dk + (k >> 3) * 16384 + (((k & 7) ^ (tid & 7)) << 4)) =
+            make_uint4(u & 0x000f000fu, u & 0x00f000f0u, h & 0x000f000fu, h & 0x00f000f0u);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(kfull(b));
+      if (i + 1 < nt) load_k(gk);
+      ok = __all_sync(0xffffffffu, i < NB || mbar_wait(vempty(b), (i / NB - 1) & 1));
+      if (!ok) break;
+      uint8_t* dv = sV + b * C::kv_bytes + (w >> 1) * (D * 128);
+      __half2 vs[4], vm[4];   // pairs of tokens: scales and minima, halved
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int j = j0 + vg * kKvGroup + 8 * vh + 2 * t;
+        const uint32_t y0 = j < q.len && finite(vp[2 * t]) ? vp[2 * t] : 0u;
+        const uint32_t y1 = j + 1 < q.len && finite(vp[2 * t + 1]) ? vp[2 * t + 1] : 0u;
+        const uint32_t sc = __byte_perm(y0, y1, 0x5410), mn = __byte_perm(y0, y1, 0x7632);
+        vs[t] = __hmul2(*(const __half2*)&sc, __float2half2_rn(0.5f));
+        vm[t] = __hmul2(*(const __half2*)&mn, __float2half2_rn(0.5f));
+      }
+#pragma unroll
+      for (int blk = 0; blk < NBLK; ++blk)
+#pragma unroll
+        for (int k = 0; k < WPB; ++k) {      // word k of each pair of tokens: four dimensions
+          const int d0 = blk * DB + slice * (DB / 8) + 4 * k;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            uint32_t y[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const uint32_t u = vw[blk * WPB * 4 + t * WPB + k] >> (n & 2 ? 8 : 0);
+              const uint32_t g = (u & (n & 1 ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;   // 1024 + c, 1024 + 16 c
+              const __half2 code = n & 1 ? __hfma2(*(const __half2*)&g, __float2half2_rn(0.0625f), __float2half2_rn(-64.0f))
+                                         : __hadd2(*(const __half2*)&g, __float2half2_rn(-1024.0f));
+              const __half2 v = __hfma2(code, vs[t], vm[t]);
+              y[t] = *(const uint32_t*)&v;
+            }
+            const int d = d0 + n;
+            *(uint4*)(dv + d * 128 + ((c8 ^ (d & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+          }
+        }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(vfull(b));
+      if (i + 1 < nt) load_v(gv);
+    }
+  } else {
+    // ------------------------------------------------------------ MMA
+    constexpr uint32_t is = idesc_f16_f32(128, kChunkKeys), io = idesc_f16_f32(128, D);
+    bool ok = steps > 0 && __all_sync(0xffffffffu, mbar_wait(qready, 0));
+    auto scores = [&](int x) {   // S of step x
+      const int i = x / RT, b = i % NB;
+      if (x % RT == 0 && !__all_sync(0xffffffffu, mbar_wait(kfull(b), (i / NB) & 1))) return false;
+      tc_fence_after();
+      if (elect_one()) {
+        const uint32_t q0 = smem_u32(sQ) + (RT == 2 ? (x & 1) * 128 * D * 2 : 0), k0 = smem_u32(sK) + b * C::kv_bytes;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          mma_f16_ss(tmem + (x & 1) * 128, sdesc_sw128(q0 + (k >> 2) * 16384 + (k & 3) * 32),
+                     sdesc_sw128(k0 + (k >> 2) * 16384 + (k & 3) * 32), is, k > 0);
+        mma_commit(sfull(x & 1));
+        if (x % RT == RT - 1) mma_commit(kempty(b));
+      }
+      __syncwarp();
+      return true;
+    };
+    for (int x = 0; x < 2 && x < steps && ok; ++x) ok = scores(x);
+    for (int x = 0; x < steps && ok; ++x) {
+      const int i = x / RT, b = i % NB;
+      ok = __all_sync(0xffffffffu, mbar_wait(pready(x & 1), (x >> 1) & 1)) &&
+           (x % RT != 0 || __all_sync(0xffffffffu, mbar_wait(vfull(b), (i / NB) & 1)));
+      if (!ok) break;
+      tc_fence_after();
+      if (elect_one()) {
+        const uint32_t v0 = smem_u32(sV) + b * C::kv_bytes;
+#pragma unroll
+        for (int k = 0; k < kChunkKeys / 16; ++k)
+          mma_f16_ts(tmem + 256 + (x % NG) * D, tmem + (x & 1) * 128 + 8 * k, sdesc_sw128(v0 + (k >> 2) * (D * 128) + (k & 3) * 32),
+                     io, x >= NG || k > 0);
+        mma_commit(odone(x % NG));
+        if (x % RT == RT - 1) mma_commit(vempty(b));
+      }
+      __syncwarp();
+      if (x + 2 < steps) ok = scores(x + 2);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 4 * NG + 4) tmem_dealloc(tmem, 512);
+}
+
+// The parts of a block's split keys: a warp a row.
+template <int D, bool BF>
+__global__ void __launch_bounds__(256) kv4_chunk_join_kernel(const __grid_constant__ KvChunkArgs A, int block_rows) {
+  grid_dep_wait();
+  grid_dep_launch();
+  const KvAttnArgs& a = A.a;
+  const int lane = threadIdx.x & 31, s = blockIdx.z, head = blockIdx.y, r = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const KvSeq q = kv_seq(a, s);
+  if (!q.ok || r >= q.n * a.group) return;
+  const int blk = r / block_rows, in = r - blk * block_rows;
+  const long long at = (((long long)s * a.kv_heads + head) * A.blocks + blk) * A.splits * block_rows + in;
+  float top = kNoMax, sum = 0.0f;
+  for (int i = 0; i < A.splits; ++i) top = fmaxf(top, A.part_ml[at + (long long)i * block_rows].x);
+  constexpr int N = D > 128 ? 2 : 1;
+  float4 v[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int i = 0; i < A.splits; ++i) {
+    const float2 ml = A.part_ml[at + (long long)i * block_rows];
+    const float f = exp2_fast(ml.x - top);
+    sum += ml.y * f;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (lane * 4 + 128 * k < D) {
+        const float4 x = *(const float4*)(A.part + (at + (long long)i * block_rows) * D + lane * 4 + 128 * k);
+        v[k].x += x.x * f, v[k].y += x.y * f, v[k].z += x.z * f, v[k].w += x.w * f;
+      }
+  }
+  const int qi = kv_div(r, A.by_group), hq = head * a.group + r - qi * a.group;
+  const long long t = q.first + qi;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (lane * 4 + 128 * k < D) {
+      const uint32_t w[2] = {pack16<BF>(v[k].x * inv, v[k].y * inv), pack16<BF>(v[k].z * inv, v[k].w * inv)};
+      store_words(a.out + t * a.out_stride + (long long)hq * D + lane * 4 + 128 * k, w);
+    }
+  if (a.lse && lane == 0) a.lse[t * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
+}
+
+}  // namespace ifq

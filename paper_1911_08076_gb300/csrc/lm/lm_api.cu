@@ -13,6 +13,7 @@
 #include "ifq.h"
 #include "kv4.cuh"
 #include "kv4_attention.cuh"
+#include "kv4_chunk.cuh"
 #include "kv4_rows.cuh"
 
 namespace {
@@ -108,10 +109,15 @@ int check_attention(const ifq_kv4_attention_desc* d, KvAttnArgs* a) {
   return IFQ_OK;
 }
 
+// More rows of a key head than this take the kernel for many.
+constexpr int kChunkRows = 32;
+
 struct AttnPlan {
-  int nt;          // row tiles of an item
+  int chunk;       // the kernel for many rows (kv4_chunk.cuh): row tiles of 128 a block; 0: that for few
+  int splits;      // chunk: blocks that a block's keys are split over
+  int nt;          // few rows: row tiles of an item
   int direct;      // a block an item
-  int blocks;      // of a sequence's rows (direct), or ranges
+  int blocks;      // of a sequence's rows (chunk, direct), or ranges
   size_t ws;
 };
 
@@ -131,6 +137,16 @@ int plan_attention(const ifq_kv4_attention_desc* d, const KvAttnArgs& a, AttnPla
   long long reach = (long long)d->max_pages * d->cache.page_size;   // tokens that a sequence's queries read at most
   if (d->max_len > 0) reach = std::min<long long>(reach, d->max_len);
   if (d->window > 0) reach = std::min<long long>(reach, (long long)d->window + d->sinks + d->max_q + 2 * kKvGroup);
+  if (rows > kChunkRows && d->seqs <= 65535) {
+    p->chunk = rows > 128 && D < 256 ? 2 : 1;
+    const int R = 128 * p->chunk;
+    p->blocks = (int)((rows + R - 1) / R);
+    const long long all = (long long)d->seqs * a.kv_heads * p->blocks, tiles = (reach + kChunkKeys - 1) / kChunkKeys;
+    p->splits = (int)std::max<long long>(1, std::min({sm_count() / std::max<long long>(all, 1), tiles / 2, 65535ll / std::max(d->seqs, 1)}));
+    p->ws = p->splits > 1 ? round_up((size_t)all * p->splits * R * (D * 4 + 8), 256) : 0;
+    return IFQ_OK;
+  }
+  p->chunk = 0;
   p->nt = rows > 8 && D < 256 ? 2 : 1;   // (two tiles of size 256 do not fit the registers)
   const int R = 8 * p->nt;
   const long long blocks = std::max<long long>(1, (rows + R - 1) / R);   // (the device checks max_q = 0 too)
@@ -140,21 +156,49 @@ int plan_attention(const ifq_kv4_attention_desc* d, const KvAttnArgs& a, AttnPla
   return IFQ_OK;
 }
 
+// Whether the instance's shared memory has been allowed on the current device; if not, do so.
+template <typename K>
+int allow_smem(K kern, int bytes, bool (&set)[kMaxDevices]) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return IFQ_ECUDA;
+  std::lock_guard<std::mutex> lk(g_lm_mu);
+  if (!set[dev]) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return IFQ_ECUDA;
+    set[dev] = true;
+  }
+  return IFQ_OK;
+}
+
+template <int D, bool BF, int RT>
+int run_chunk(const KvAttnArgs& a, const AttnPlan& p, void* ws, cudaStream_t st) {
+  using C = KvChunkShape<D, RT>;
+  static bool set[kMaxDevices];
+  const int rc = allow_smem(kv4_chunk_kernel<D, BF, RT>, C::bytes, set);
+  if (rc) return rc;
+  KvChunkArgs r = {};
+  r.a = a;
+  r.by_gpp = make_div(a.page_size / kKvGroup);
+  r.by_group = make_div(a.group);
+  r.blocks = p.blocks;
+  r.splits = p.splits;
+  if (p.splits > 1) {
+    r.part = (float*)ws;
+    r.part_ml = (float2*)(r.part + (size_t)a.seqs * a.kv_heads * p.blocks * p.splits * 128 * RT * D);
+  }
+  const cudaError_t e = launch_k(kv4_chunk_kernel<D, BF, RT>, dim3(p.blocks, a.kv_heads, a.seqs * p.splits), dim3(C::threads),
+                                 C::bytes, st, r);
+  if (e != cudaSuccess || p.splits == 1) return done(e);
+  const int rows = a.max_q * a.group;
+  return done(launch_k(kv4_chunk_join_kernel<D, BF>, dim3(ceil_div(rows, 8), a.kv_heads, a.seqs), dim3(256), 0, st, r, 128 * RT));
+}
+
 template <int D, bool BF, int NT>
 int run_rows(const KvAttnArgs& a, const AttnPlan& p, void* ws, cudaStream_t st) {
   constexpr int R = 8 * NT, smem = kv_rows_smem<D>(R);
   static_assert(smem <= 232448, "shared memory budget");
   static bool set[kMaxDevices];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return IFQ_ECUDA;
-  {
-    std::lock_guard<std::mutex> lk(g_lm_mu);
-    if (!set[dev]) {
-      if (cudaFuncSetAttribute(kv4_rows_kernel<D, BF, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
-        return IFQ_ECUDA;
-      set[dev] = true;
-    }
-  }
+  const int rc = allow_smem(kv4_rows_kernel<D, BF, NT>, smem, set);
+  if (rc) return rc;
   KvRowsArgs r = {};
   r.a = a;
   r.by_gpp = make_div(a.page_size / kKvGroup);
@@ -394,6 +438,9 @@ int ifq_kv4_attention(const ifq_kv4_attention_desc* d, const void* q, const void
   return by_head(d->cache.head_dim, d->dtype, [&](auto dim, auto bf) {
     constexpr int D = decltype(dim)::value;
     constexpr bool BF = decltype(bf)::value;
+    if constexpr (D < 256)
+      if (p.chunk == 2) return run_chunk<D, BF, 2>(a, p, ws, S(stream));
+    if (p.chunk) return run_chunk<D, BF, 1>(a, p, ws, S(stream));
     if constexpr (D < 256)
       if (p.nt == 2) return run_rows<D, BF, 2>(a, p, ws, S(stream));
     return run_rows<D, BF, 1>(a, p, ws, S(stream));

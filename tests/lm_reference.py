@@ -111,14 +111,14 @@ def fill(rng, cache, page_size, slots, D, spread=1.0):
             g[:, 16 * D + at + 4 * row:16 * D + at + 4 * row + 4] = par.view(np.uint8).reshape(heads, 4)
 
 
-def attention(q, cache, page_size, table, lens, starts, kv_heads, scale, window, sinks, u_out):
+def attention(q, cache, page_size, table, lens, starts, kv_heads, scale, window, sinks, u_out, half_values=False):
     """q float64 [T][Hq][D] -> out, lse, and how far a computation in single precision with half-precision weights
     may be off in each (per element of out, per row of lse).
 
     The bounds: the scores' sums of D products and the two affine terms err by at most (D + 8) 2^-23 of the sum T of
     their absolute values; a relative change of the weights by e^(2 delta) moves the output by 2 delta A, A the sum of
     p_j |V_j| with |V_j| <= s'_j c'_j + |m'_j|; rounding a weight to half moves it by 2^-11, or by 2^-24 of the largest
-    weight below the normal range; sums of n terms add n 2^-24 at most for each of the two sums; u_out is the result's
+    weight below the normal range; with half_values each V_j is rounded to half as well (2^-11 of it, or 2^-24); sums of n terms add n 2^-24 at most for each of the two sums; u_out is the result's
     own rounding."""
     T, Hq, D = q.shape
     out, lse = np.zeros((T, Hq, D)), np.full((T, Hq), -np.inf)
@@ -151,7 +151,8 @@ def attention(q, cache, page_size, table, lens, starts, kv_heads, scale, window,
                         delta = (D + 8) * 2.0 ** -23 * np.max(kabs[see] @ np.abs(x)) * abs(scale)
                         A = (w @ vabs[see]) / l
                         m = see.sum()
-                        tol[a + i, h * G + g] = (u_out * np.abs(o) + (2 * delta + 2.0 ** -11 + 2 * m * 2.0 ** -24) * A +
+                        vr = 2.0 ** -11 * A + 2.0 ** -24 if half_values else 0.0
+                        tol[a + i, h * G + g] = (vr + u_out * np.abs(o) + (2 * delta + 2.0 ** -11 + 2 * m * 2.0 ** -24) * A +
                                                  m * 2.0 ** -24 * vabs[see].max() / l + 1e-30)
                         out[a + i, h * G + g] = o
                         lse[a + i, h * G + g] = top + np.log(l)

@@ -232,12 +232,13 @@ def _run(lens, starts, table, cache, q, hq, hk, D, page, dtype, window=0, sinks=
         assert torch.equal(first[1].view(torch.int32), ls.view(torch.int32))
     assert (out[:, hq * D:] == 5).all()
     q64 = qd[:, :hq * D].double().cpu().numpy().reshape(T, hq, D)
-    return (out[:, :hq * D].double().cpu().numpy().reshape(T, hq, D), ls.double().cpu().numpy(), q64, scale, u)
+    many = d.max_q * (hq // hk) > 32     # the library then rounds values to half
+    return (out[:, :hq * D].double().cpu().numpy().reshape(T, hq, D), ls.double().cpu().numpy(), q64, scale, u, many)
 
 
 def _check(got, lens, starts, table, cache, hk, page, window=0, sinks=0, rows=None, lse=True):
-    out, ls, q64, scale, u = got
-    want, wl, tol, ltol = R.attention(q64, cache, page, table, lens, starts, hk, scale, window, sinks, u)
+    out, ls, q64, scale, u, many = got
+    want, wl, tol, ltol = R.attention(q64, cache, page, table, lens, starts, hk, scale, window, sinks, u, many)
     rows = slice(None) if rows is None else rows
     with np.errstate(all="ignore"):
         far = np.abs(out[rows] - want[rows]) - tol[rows]
