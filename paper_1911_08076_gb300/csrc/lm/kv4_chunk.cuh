@@ -14,7 +14,9 @@
 // row raised only when a score passes it by 8, in whole powers of two; their sum is that of the unrounded p.
 // A value that is not a number must reach only the rows that see it: its operand is 0 and its key's minimum NaN.
 //
-// Warps: one or two groups of four run the softmax, a thread a row, so that no value crosses threads; four expand codes
+// Warps: one or two groups of four run the softmax, in matrix fragments: a thread has four rows and two of every eight
+// keys (with a thread a row, as many broadcast loads of the keys' parameters as scores took 2000 of 4500 cycles a tile);
+// four expand codes
 // (global memory to registers a tile ahead, then to swizzled shared memory); one issues MMAs.  Two S buffers: with
 // RT = 2 one a row tile; else the key tiles alternate, and with two groups each has an O of its own, joined at the end.
 // A block's keys may be split over `splits` blocks, joined by kv4_chunk_join_kernel.
@@ -66,6 +68,32 @@ __device__ __forceinline__ void tmem_st16(uint32_t t, const uint32_t (&v)[16]) {
       "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
       "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
+}
+// 32 lanes x 32 columns as matrix fragments: with q = t / 4, thread t has v[h][4 k + 2 e + i] = column 8 k + 2 (t % 4) + i
+// of lane 16 h + q + 8 e.  In two steps: the values are there after the second.
+__device__ __forceinline__ void tmem_ld_begin(uint32_t t, uint32_t (&v)[2][16]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(v[h][0]), "=r"(v[h][1]), "=r"(v[h][2]), "=r"(v[h][3]), "=r"(v[h][4]), "=r"(v[h][5]), "=r"(v[h][6]),
+          "=r"(v[h][7]), "=r"(v[h][8]), "=r"(v[h][9]), "=r"(v[h][10]), "=r"(v[h][11]), "=r"(v[h][12]), "=r"(v[h][13]),
+          "=r"(v[h][14]), "=r"(v[h][15])
+        : "r"(t + ((uint32_t)(16 * h) << 16)));
+}
+__device__ __forceinline__ void tmem_ld_end(uint32_t (&v)[2][16]) {   // (names the registers, so that no use moves before it)
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[h][0]), "+r"(v[h][1]), "+r"(v[h][2]), "+r"(v[h][3]), "+r"(v[h][4]), "+r"(v[h][5]), "+r"(v[h][6]),
+                   "+r"(v[h][7]), "+r"(v[h][8]), "+r"(v[h][9]), "+r"(v[h][10]), "+r"(v[h][11]), "+r"(v[h][12]),
+                   "+r"(v[h][13]), "+r"(v[h][14]), "+r"(v[h][15]));
+}
+// 16 lanes x 16 columns from fragments: v[2 k + e] to column 4 k + t % 4 of lane t / 4 + 8 e.
+__device__ __forceinline__ void tmem_st_frag(uint32_t t, const uint32_t (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(t), "r"(v[0]), "r"(v[1]),
+               "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -168,7 +196,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
   auto first_key = [&](int i) { return (t0 + i < tiles.sg ? t0 + i : t0 + i + tiles.skip) * kChunkKeys; };
 
   if (warp < 4 * NG) {
-    // ------------------------------------------------------------ softmax: a thread a row
+    // ------------------------------------------------------------ softmax
     const int grp = warp >> 2, row = threadIdx.x & 127, rt = RT == 2 ? grp : 0, r = r0 + rt * 128 + row;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, tO = tmem + lanes + 256 + grp * D;
     const bool have = work && r < rows;
@@ -210,9 +238,35 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
         if (lane == 0) mbar_arrive(qready);
       }
     }
-    float m = 0.0f;
-    uint64_t l2 = 0;
-    bool fresh = have, ok = true;
+    // From here a thread has four rows, q + 8 y of its warp's 32 (q = lane / 4), and of every 8 keys two: a key's
+    // parameters then serve four rows a load.
+    const int quad = lane >> 2, pos = lane & 3;
+    uint64_t fa2[4], fb2[4], l2[4];
+    float m[4];
+    int py[4], pf[4];
+    uint32_t fresh = 0;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const float u = __shfl_sync(0xffffffffu, fa, quad + 8 * y), v = __shfl_sync(0xffffffffu, fb, quad + 8 * y);
+      fa2[y] = pair2(u, u);
+      fb2[y] = pair2(v, v);
+      l2[y] = 0;
+      m[y] = 0.0f;
+      py[y] = __shfl_sync(0xffffffffu, p, quad + 8 * y);
+      pf[y] = __shfl_sync(0xffffffffu, p_first, quad + 8 * y);
+      fresh |= (uint32_t)__shfl_sync(0xffffffffu, (int)have, quad + 8 * y) << y;
+    }
+    // of a value per own row, the one of row `lane` of the warp
+    auto by_lane = [&](const float (&x)[4]) {
+      float r = 0.0f;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const float t = __shfl_sync(0xffffffffu, x[y], 4 * (lane & 7));
+        r = lane >> 3 == y ? t : r;
+      }
+      return r;
+    };
+    bool ok = true;
     int mine = 0;   // steps of this group so far
     for (int x = grp; x < steps && ok; x += NG, ++mine) {
       const int i = x / RT, b = x & 1, pb = i % kChunkPar, j0 = first_key(i);
@@ -220,76 +274,101 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       ok = __all_sync(0xffffffffu, mbar_wait(pfull(pb), (i / kChunkPar) & 1) && mbar_wait(sfull(b), (x >> 1) & 1));
       if (!ok) break;
       tc_fence_after();
-      const float4* par = sPar + pb * (kChunkKeys / 2);
+      const float4* par = sPar + pb * (kChunkKeys / 2) + pos;
       const bool full = j0 + kChunkKeys - 1 <= p_lo && (a.window == 0 || j0 > p_hi - a.window || j0 + kChunkKeys <= a.sinks);
-      const uint64_t fa2 = pair2(fa, fa), fb2 = pair2(fb, fb);
+      uint32_t v[2][16];
+      tmem_ld_begin(tS, v);
+      tmem_ld_end(v);
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
-        uint32_t v[32];
-        tmem_ld<32>(tS + 32 * c, v);
-        float t[32];
-        const uint64_t m2 = pair2(-m, -m);
-        float top = -INFINITY;
+        float t[4][8];   // [row][2 k + i]: key 8 k + 2 pos + i of the 32
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const float4 kp = par[16 * c + k];
-          const float2 z = halves2(fma2v(pair2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])),
-                                         mul2(pair2(kp.x, kp.y), fa2), fma2v(pair2(kp.z, kp.w), fb2, m2)));
-          t[2 * k] = z.x;
-          t[2 * k + 1] = z.y;
+        for (int k = 0; k < 4; ++k) {
+          const float4 kp = par[16 * c + 4 * k];
+          const uint64_t s2 = pair2(kp.x, kp.y), n2 = pair2(kp.z, kp.w);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const uint32_t* w = &v[y >> 1][4 * k + 2 * (y & 1)];
+            const float2 z = halves2(fma2v(pair2(__uint_as_float(w[0]), __uint_as_float(w[1])), mul2(s2, fa2[y]),
+                                           fma2v(n2, fb2[y], pair2(-m[y], -m[y]))));
+            t[y][2 * k] = z.x;
+            t[y][2 * k + 1] = z.y;
+          }
         }
+        if (c < 3) tmem_ld_begin(tS + 32 * (c + 1), v);   // the next columns, behind these ones' exponentials
         if (!full) {
 #pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            const int j = j0 + 32 * c + k;
-            if (j > p || (j < p_first && j >= a.sinks)) t[k] = -INFINITY;
+          for (int k = 0; k < 8; ++k) {
+            const int j = j0 + 32 * c + 8 * (k >> 1) + 2 * pos + (k & 1);
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              if (j > py[y] || (j < pf[y] && j >= a.sinks)) t[y][k] = -INFINITY;
           }
         }
+        float top[4];
 #pragma unroll
-        for (int k = 0; k < 32; k += 2) top = fmaxf(top, fmaxf(t[k], t[k + 1]));
-        if (__any_sync(0xffffffffu, top > 8.0f || (fresh && top > -INFINITY))) {
-          const bool begin = fresh && top > -INFINITY;
-          const float rise = begin || top > 8.0f ? ceilf(top) : 0.0f, f = begin ? 1.0f : exp2_fast(-rise);
-          if (begin) fresh = false;
-          m += rise;
-          l2 = mul2(l2, pair2(f, f));
+        for (int y = 0; y < 4; ++y)
+          top[y] = fmaxf(fmaxf(fmaxf(t[y][0], t[y][1]), fmaxf(t[y][2], t[y][3])), fmaxf(fmaxf(t[y][4], t[y][5]), fmaxf(t[y][6], t[y][7])));
+        if (__any_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) > 8.0f || fresh)) {
+          float f[4];
 #pragma unroll
-          for (int k = 0; k < 32; ++k) t[k] -= rise;
-          // what this tile's columns and the sum already hold
-          const uint32_t fh = pack16<false>(f, f);
-          tmem_wait_st();
-          for (int d = 0; d < c; ++d) {
-            uint32_t w[16];
-            tmem_ld<16>(tS + 16 * d, w);
+          for (int y = 0; y < 4; ++y) {
+            top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], 1));
+            top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], 2));
+            const bool begin = (fresh >> y & 1u) && top[y] > -INFINITY;
+            const float rise = begin || top[y] > 8.0f ? ceilf(top[y]) : 0.0f;
+            f[y] = begin ? 1.0f : exp2_fast(-rise);
+            if (begin) fresh &= ~(1u << y);
+            m[y] += rise;
+            l2[y] = mul2(l2[y], pair2(f[y], f[y]));
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const __half2 y = __hmul2(*(const __half2*)&w[k], *(const __half2*)&fh);
-              w[k] = *(const uint32_t*)&y;
-            }
-            tmem_st16(tS + 16 * d, w);
+            for (int k = 0; k < 8; ++k) t[y][k] -= rise;
           }
-          if (mine > 0) {
-            ok = __all_sync(0xffffffffu, mbar_wait(odone(grp), (mine - 1) & 1));
-            if (!ok) break;
-            tc_fence_after();
-#pragma unroll 1
-            for (int d = 0; d < D; d += 16) {
+          const float fl = by_lane(f);
+          if (__any_sync(0xffffffffu, fl != 1.0f)) {
+            // what this tile's columns and the sum already hold
+            const uint32_t fh = pack16<false>(fl, fl);
+            tmem_wait_st();
+            for (int d = 0; d < c; ++d) {
               uint32_t w[16];
-              tmem_ld<16>(tO + d, w);
+              tmem_ld<16>(tS + 16 * d, w);
 #pragma unroll
-              for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * f);
-              tmem_st16(tO + d, w);
+              for (int k = 0; k < 16; ++k) {
+                const __half2 y = __hmul2(*(const __half2*)&w[k], *(const __half2*)&fh);
+                w[k] = *(const uint32_t*)&y;
+              }
+              tmem_st16(tS + 16 * d, w);
+            }
+            if (mine > 0) {
+              ok = __all_sync(0xffffffffu, mbar_wait(odone(grp), (mine - 1) & 1));
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int d = 0; d < D; d += 16) {
+                uint32_t w[16];
+                tmem_ld<16>(tO + d, w);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * fl);
+                tmem_st16(tO + d, w);
+              }
             }
           }
         }
-        uint32_t w[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const float u0 = exp2_fast(t[2 * k]), u1 = exp2_fast(t[2 * k + 1]);
-          l2 = add2(l2, pair2(u0, u1));
-          w[k] = pack16<false>(u0, u1);
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int y = 2 * h + e;
+              const float u0 = exp2_fast(t[y][2 * k]), u1 = exp2_fast(t[y][2 * k + 1]);
+              l2[y] = add2(l2[y], pair2(u0, u1));
+              w[2 * k + e] = pack16<false>(u0, u1);
+            }
+          tmem_st_frag(tS + ((uint32_t)(16 * h) << 16) + 16 * c, w);
         }
-        tmem_st16(tS + 16 * c, w);
+        if (c < 3) tmem_ld_end(v);
       }
       if (!ok) break;
       tmem_wait_st();
@@ -302,8 +381,17 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
     }
     if (mine > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(odone(grp), (mine - 1) & 1));
     tc_fence_after();
-    const float2 lh = halves2(l2);
-    float sum = lh.x + lh.y, top = fresh || !have ? kNoMax : m;
+    float sums[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const float2 u = halves2(l2[y]);
+      sums[y] = u.x + u.y;
+      sums[y] += __shfl_xor_sync(0xffffffffu, sums[y], 1);
+      sums[y] += __shfl_xor_sync(0xffffffffu, sums[y], 2);
+      if (fresh >> y & 1u) m[y] = kNoMax;
+    }
+    float sum = by_lane(sums), top = by_lane(m);   // a thread a row again
+    if (!have) top = kNoMax;
     float other_top = kNoMax, other_f = 0.0f, my_f = 1.0f;
     float* xo = (float*)sK;   // [128][D + 4], and the second group's references and sums
     float2* xml = (float2*)(xo + 128 * (D + 4));
