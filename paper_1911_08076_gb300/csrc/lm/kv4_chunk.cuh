@@ -8,10 +8,13 @@
 // Keys: codes are expanded to halves as the subnormals c 2^-24 and 16 c 2^-24 (masks alone, as in kv4_rows.cuh; q's
 // elements stand in the order that leaves the codes of a word in, with the factors 1/16 in them).  Products with them
 // are exact, sums fp32; the scale and the minimum of a key are applied to the sum,
-//   t = s (q . c) + m sum(q),   two packed fma a pair of keys, with the softmax's reference in the second.
+//   t = s (q . c) + (m sum(q) - reference),   two packed fma a pair of keys (scale, log2 e and powers of two in s).
+// q itself is multiplied by 16 to keep small elements out of the half's subnormals; a row with an element over 2^11 is
+// brought down by a power of two of its own, which its scores are then multiplied with (a branch no usual row takes).
 // Values: v = half((s' c' + m') / 2), one fma of halves: as fine as the minimum that the cache holds (a half), and
 // within the half's range where s' c' + m' would leave it.  Weights p are halves of 2^(t - m) with the reference m of a
-// row raised only when a score passes it by 8, in whole powers of two; their sum is that of the unrounded p.
+// row raised only when a sum of 8 of them passes 2^15 (no half overflows before), in whole powers of two; the
+// denominator is the sum of the unrounded p.
 // A value that is not a number must reach only the rows that see it: its operand is 0 and its key's minimum NaN.
 //
 // Warps: one or two groups of four run the softmax, in matrix fragments: a thread has four rows and two of every eight
@@ -70,24 +73,19 @@ __device__ __forceinline__ void tmem_st16(uint32_t t, const uint32_t (&v)[16]) {
       : "memory");
 }
 // 32 lanes x 32 columns as matrix fragments: with q = t / 4, thread t has v[h][4 k + 2 e + i] = column 8 k + 2 (t % 4) + i
-// of lane 16 h + q + 8 e.  In two steps: the values are there after the second.
-__device__ __forceinline__ void tmem_ld_begin(uint32_t t, uint32_t (&v)[2][16]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(v[h][0]), "=r"(v[h][1]), "=r"(v[h][2]), "=r"(v[h][3]), "=r"(v[h][4]), "=r"(v[h][5]), "=r"(v[h][6]),
-          "=r"(v[h][7]), "=r"(v[h][8]), "=r"(v[h][9]), "=r"(v[h][10]), "=r"(v[h][11]), "=r"(v[h][12]), "=r"(v[h][13]),
-          "=r"(v[h][14]), "=r"(v[h][15])
-        : "r"(t + ((uint32_t)(16 * h) << 16)));
-}
-__device__ __forceinline__ void tmem_ld_end(uint32_t (&v)[2][16]) {   // (names the registers, so that no use moves before it)
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(v[h][0]), "+r"(v[h][1]), "+r"(v[h][2]), "+r"(v[h][3]), "+r"(v[h][4]), "+r"(v[h][5]), "+r"(v[h][6]),
-                   "+r"(v[h][7]), "+r"(v[h][8]), "+r"(v[h][9]), "+r"(v[h][10]), "+r"(v[h][11]), "+r"(v[h][12]),
-                   "+r"(v[h][13]), "+r"(v[h][14]), "+r"(v[h][15]));
+// of lane 16 h + q + 8 e.
+__device__ __forceinline__ void tmem_ld_frag(uint32_t t, uint32_t (&v)[2][16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%32];\n\t"
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%33];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0][0]), "=r"(v[0][1]), "=r"(v[0][2]), "=r"(v[0][3]), "=r"(v[0][4]), "=r"(v[0][5]), "=r"(v[0][6]),
+        "=r"(v[0][7]), "=r"(v[0][8]), "=r"(v[0][9]), "=r"(v[0][10]), "=r"(v[0][11]), "=r"(v[0][12]), "=r"(v[0][13]),
+        "=r"(v[0][14]), "=r"(v[0][15]), "=r"(v[1][0]), "=r"(v[1][1]), "=r"(v[1][2]), "=r"(v[1][3]), "=r"(v[1][4]),
+        "=r"(v[1][5]), "=r"(v[1][6]), "=r"(v[1][7]), "=r"(v[1][8]), "=r"(v[1][9]), "=r"(v[1][10]), "=r"(v[1][11]),
+        "=r"(v[1][12]), "=r"(v[1][13]), "=r"(v[1][14]), "=r"(v[1][15])
+      : "r"(t), "r"(t + (16u << 16))
+      : "memory");
 }
 // 16 lanes x 16 columns from fragments: v[2 k + e] to column 4 k + t % 4 of lane t / 4 + 8 e.
 __device__ __forceinline__ void tmem_st_frag(uint32_t t, const uint32_t (&v)[8]) {
@@ -152,7 +150,8 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
   auto pfull = [&](int b) { return bars + 112 + 8 * b; };    // parameters
   auto pempty = [&](int b) { return bars + 112 + 8 * kChunkPar + 8 * b; };
   const uint32_t qready = bars + 112 + 16 * kChunkPar;
-  uint32_t* tptr = (uint32_t*)((uint8_t*)sPar + C::par_bytes + 112 + 16 * kChunkPar + 8);
+  auto olast = [&](int g) { return qready + 8 + 8 * g; };    // group g's last product
+  uint32_t* tptr = (uint32_t*)((uint8_t*)sPar + C::par_bytes + 112 + 16 * kChunkPar + 24);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int b = 0; b < 2; ++b) {
@@ -163,6 +162,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       mbar_init(sfull(b), 1);
       mbar_init(pready(b), 4);
       mbar_init(odone(b), 1);
+      mbar_init(olast(b), 1);
     }
     for (int b = 0; b < kChunkPar; ++b) {
       mbar_init(pfull(b), 4);
@@ -202,9 +202,9 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
     const bool have = work && r < rows;
     const int qi = have ? (int)kv_div(r, A.by_group) : 0, hq = head * a.group + (have ? r - qi * a.group : 0);
     const int p = q.len - q.n + qi, p_first = a.window > 0 ? p - a.window + 1 : 0;
-    float fa = 0.0f, fb = 0.0f;
+    float fa = 1.0f, fb = 0.0f;
     if (work) {
-      // the row of q, brought to half by a power of two; with one row tile the second group only needs the factors
+      // the row of q as halves; with one row tile the second group only needs the factors
       const uint16_t* src = a.q + (long long)(q.first + qi) * a.q_stride + (long long)hq * D;
       float top = 0.0f, sum = 0.0f;
 #pragma unroll 4
@@ -218,11 +218,10 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
           sum += f.x + f.y;
         }
       }
-      int e = (int)(__float_as_uint(top) >> 23) - 127 - 14;
-      e = max(-100, min(113, e));
-      const float down = __uint_as_float((uint32_t)(127 - e) << 23), low = down * 0.0625f, sc = a.scale * 1.44269504f;
-      fa = sc * __uint_as_float((uint32_t)(127 + e) << 23);
-      fb = sc * sum;
+      const int e = max(0, min(117, (int)(__float_as_uint(top) >> 23) - 127 - 10));   // (largest below 2^15 once it is 16 q 2^-e)
+      const float down = __uint_as_float((uint32_t)(131 - e) << 23), low = down * 0.0625f;
+      fa = __uint_as_float((uint32_t)(127 + e) << 23);
+      fb = a.scale * 1.44269504f * sum;
       if (RT == 2 || grp == 0) {
 #pragma unroll 4
         for (int i = 0; i < D / 8; ++i) {
@@ -241,14 +240,14 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
     // From here a thread has four rows, q + 8 y of its warp's 32 (q = lane / 4), and of every 8 keys two: a key's
     // parameters then serve four rows a load.
     const int quad = lane >> 2, pos = lane & 3;
-    uint64_t fa2[4], fb2[4], l2[4];
-    float m[4];
+    uint64_t fb2[4], l2[4];
+    float m[4], up[4];
     int py[4], pf[4];
     uint32_t fresh = 0;
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
-      const float u = __shfl_sync(0xffffffffu, fa, quad + 8 * y), v = __shfl_sync(0xffffffffu, fb, quad + 8 * y);
-      fa2[y] = pair2(u, u);
+      const float v = __shfl_sync(0xffffffffu, fb, quad + 8 * y);
+      up[y] = __shfl_sync(0xffffffffu, fa, quad + 8 * y);
       fb2[y] = pair2(v, v);
       l2[y] = 0;
       m[y] = 0.0f;
@@ -256,6 +255,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       pf[y] = __shfl_sync(0xffffffffu, p_first, quad + 8 * y);
       fresh |= (uint32_t)__shfl_sync(0xffffffffu, (int)have, quad + 8 * y) << y;
     }
+    const bool large = __any_sync(0xffffffffu, fa != 1.0f);   // some row's q is out of the usual range
     // of a value per own row, the one of row `lane` of the warp
     auto by_lane = [&](const float (&x)[4]) {
       float r = 0.0f;
@@ -276,12 +276,18 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       tc_fence_after();
       const float4* par = sPar + pb * (kChunkKeys / 2) + pos;
       const bool full = j0 + kChunkKeys - 1 <= p_lo && (a.window == 0 || j0 > p_hi - a.window || j0 + kChunkKeys <= a.sinks);
-      uint32_t v[2][16];
-      tmem_ld_begin(tS, v);
-      tmem_ld_end(v);
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
+        uint32_t v[2][16];
+        tmem_ld_frag(tS + 32 * c, v);
         float t[4][8];   // [row][2 k + i]: key 8 k + 2 pos + i of the 32
+        if (large) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) v[h][k] = __float_as_uint(__uint_as_float(v[h][k]) * up[2 * h + (k >> 1 & 1)]);
+          }
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const float4 kp = par[16 * c + 4 * k];
@@ -289,13 +295,12 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             const uint32_t* w = &v[y >> 1][4 * k + 2 * (y & 1)];
-            const float2 z = halves2(fma2v(pair2(__uint_as_float(w[0]), __uint_as_float(w[1])), mul2(s2, fa2[y]),
+            const float2 z = halves2(fma2v(pair2(__uint_as_float(w[0]), __uint_as_float(w[1])), s2,
                                            fma2v(n2, fb2[y], pair2(-m[y], -m[y]))));
             t[y][2 * k] = z.x;
             t[y][2 * k + 1] = z.y;
           }
         }
-        if (c < 3) tmem_ld_begin(tS + 32 * (c + 1), v);   // the next columns, behind these ones' exponentials
         if (!full) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
@@ -305,18 +310,36 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
               if (j > py[y] || (j < pf[y] && j >= a.sinks)) t[y][k] = -INFINITY;
           }
         }
-        float top[4];
+        uint32_t w[2][8];
+        uint64_t part[4];
+        float most = 0.0f;
+        auto weights = [&]() {
+          most = 0.0f;
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-          top[y] = fmaxf(fmaxf(fmaxf(t[y][0], t[y][1]), fmaxf(t[y][2], t[y][3])), fmaxf(fmaxf(t[y][4], t[y][5]), fmaxf(t[y][6], t[y][7])));
-        if (__any_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) > 8.0f || fresh)) {
+          for (int y = 0; y < 4; ++y) {
+            part[y] = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float u0 = exp2_fast(t[y][2 * k]), u1 = exp2_fast(t[y][2 * k + 1]);
+              part[y] = k ? add2(part[y], pair2(u0, u1)) : pair2(u0, u1);
+              w[y >> 1][2 * k + (y & 1)] = pack16<false>(u0, u1);
+            }
+            const float2 u = halves2(part[y]);
+            most = fmaxf(most, u.x + u.y);
+          }
+        };
+        weights();
+        if (__any_sync(0xffffffffu, most > 32768.0f || fresh)) {
           float f[4];
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], 1));
-            top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], 2));
-            const bool begin = (fresh >> y & 1u) && top[y] > -INFINITY;
-            const float rise = begin || top[y] > 8.0f ? ceilf(top[y]) : 0.0f;
+            float top = t[y][0];
+#pragma unroll
+            for (int k = 1; k < 8; ++k) top = fmaxf(top, t[y][k]);
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const bool begin = (fresh >> y & 1u) && top > -INFINITY;
+            const float rise = begin || top > 8.0f ? ceilf(top) : 0.0f;
             f[y] = begin ? 1.0f : exp2_fast(-rise);
             if (begin) fresh &= ~(1u << y);
             m[y] += rise;
@@ -324,51 +347,43 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
 #pragma unroll
             for (int k = 0; k < 8; ++k) t[y][k] -= rise;
           }
+          weights();
           const float fl = by_lane(f);
           if (__any_sync(0xffffffffu, fl != 1.0f)) {
             // what this tile's columns and the sum already hold
             const uint32_t fh = pack16<false>(fl, fl);
             tmem_wait_st();
             for (int d = 0; d < c; ++d) {
-              uint32_t w[16];
-              tmem_ld<16>(tS + 16 * d, w);
+              uint32_t x[16];
+              tmem_ld<16>(tS + 16 * d, x);
 #pragma unroll
               for (int k = 0; k < 16; ++k) {
-                const __half2 y = __hmul2(*(const __half2*)&w[k], *(const __half2*)&fh);
-                w[k] = *(const uint32_t*)&y;
+                const __half2 y = __hmul2(*(const __half2*)&x[k], *(const __half2*)&fh);
+                x[k] = *(const uint32_t*)&y;
               }
-              tmem_st16(tS + 16 * d, w);
+              tmem_st16(tS + 16 * d, x);
             }
             if (mine > 0) {
+              // (these scores were asked for after the product before the last, so the barrier is in the phase of the
+              // last one or past it)
               ok = __all_sync(0xffffffffu, mbar_wait(odone(grp), (mine - 1) & 1));
               if (!ok) break;
               tc_fence_after();
 #pragma unroll 1
               for (int d = 0; d < D; d += 16) {
-                uint32_t w[16];
-                tmem_ld<16>(tO + d, w);
+                uint32_t x[16];
+                tmem_ld<16>(tO + d, x);
 #pragma unroll
-                for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * fl);
-                tmem_st16(tO + d, w);
+                for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * fl);
+                tmem_st16(tO + d, x);
               }
             }
           }
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[8];
+        for (int y = 0; y < 4; ++y) l2[y] = add2(l2[y], part[y]);
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int y = 2 * h + e;
-              const float u0 = exp2_fast(t[y][2 * k]), u1 = exp2_fast(t[y][2 * k + 1]);
-              l2[y] = add2(l2[y], pair2(u0, u1));
-              w[2 * k + e] = pack16<false>(u0, u1);
-            }
-          tmem_st_frag(tS + ((uint32_t)(16 * h) << 16) + 16 * c, w);
-        }
-        if (c < 3) tmem_ld_end(v);
+        for (int h = 0; h < 2; ++h) tmem_st_frag(tS + ((uint32_t)(16 * h) << 16) + 16 * c, w[h]);
       }
       if (!ok) break;
       tmem_wait_st();
@@ -379,7 +394,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
         mbar_arrive(pempty(pb));
       }
     }
-    if (mine > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(odone(grp), (mine - 1) & 1));
+    if (mine > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(olast(grp), 0));
     tc_fence_after();
     float sums[4];
 #pragma unroll
@@ -528,7 +543,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
         float2 f = unpack16<false>(there ? kpar : 0u);
         if (there && !finite(vpar)) f.y = __uint_as_float(0x7fc00000u);   // NaN to the rows that see it
         float* dst = (float*)(sPar + pb * (kChunkKeys / 2) + tid / 2) + (tid & 1);
-        dst[0] = f.x * 16777216.0f;
+        dst[0] = f.x * (a.scale * 1.44269504f * 1048576.0f);   // codes are in units of 2^-24, q of 2^-4
         dst[2] = f.y;
         __syncwarp();
         if (lane == 0) mbar_arrive(pfull(pb));
@@ -617,10 +632,15 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
           mma_f16_ts(tmem + 256 + (x % NG) * D, tmem + (x & 1) * 128 + 8 * k, sdesc_sw128(v0 + (k >> 2) * (D * 128) + (k & 3) * 32),
                      io, x >= NG || k > 0);
         mma_commit(odone(x % NG));
+        if (x + NG >= steps) mma_commit(olast(x % NG));
         if (x % RT == RT - 1) mma_commit(vempty(b));
       }
       __syncwarp();
-      if (x + 2 < steps) ok = scores(x + 2);
+      if (x + 2 < steps) {
+        // The next S overwrites the weights that this product reads, and MMAs of different shapes need not run in the
+        // order they were issued in.
+        ok = __all_sync(0xffffffffu, mbar_wait(odone(x % NG), x / NG & 1)) && scores(x + 2);
+      }
     }
   }
   tc_fence_before();
