@@ -34,16 +34,26 @@ __device__ __forceinline__ int kv4_v_byte(int D, int row, int d) {
          (row % 2) * 2 + (dd % 4) / 2;
 }
 
+struct KvDiv {   // n / d for 0 <= n < 2^31
+  uint32_t d, mul, shift;
+};
+__device__ __forceinline__ uint32_t kv_div(uint32_t n, const KvDiv& f) {
+  return (uint32_t)(((uint64_t)__umulhi(n, f.mul) + n) >> f.shift);
+}
+
 struct KvCacheArgs {
   uint8_t* p;
   long long slots;     // pages * page_size
-  int page_size;
+  KvDiv by_page;       // tokens a page
   int kv_heads;
 };
-__device__ __forceinline__ uint8_t* kv4_group(const KvCacheArgs& c, int D, long long slot, int head) {
-  const long long page = slot / c.page_size;
-  const int row = (int)(slot - page * c.page_size);
-  return c.p + ((page * c.kv_heads + head) * (c.page_size / kKvGroup) + row / kKvGroup) * (long long)kv4_group_bytes(D);
+// Page of a slot and row in it (a 64-bit division only past 2^31 slots).
+__device__ __forceinline__ void kv4_place(const KvCacheArgs& c, long long slot, long long& page, int& row) {
+  page = c.slots <= 0x7fffffffll ? (long long)kv_div((uint32_t)slot, c.by_page) : slot / (long long)c.by_page.d;
+  row = (int)(slot - page * c.by_page.d);
+}
+__device__ __forceinline__ uint8_t* kv4_group(const KvCacheArgs& c, int D, long long page, int row, int head) {
+  return c.p + ((page * c.kv_heads + head) * (long long)(c.by_page.d / kKvGroup) + row / kKvGroup) * kv4_group_bytes(D);
 }
 
 __device__ __forceinline__ float min_nan(float a, float b) {
@@ -97,126 +107,142 @@ struct KvAppendArgs {
   const int64_t* slots;
   long long q_stride, k_stride, v_stride, q_out_stride;
   int tokens, q_heads;   // q_heads = 0: no q
-  int rope, rot, positions;
+  int rope, rot, positions, vec;   // vec: the tables are 16-byte aligned
 };
 
-constexpr int kAppendWarps = 8;
+// Both kernels: eight dimensions (16 bytes) a lane, so D / 8 lanes a head and 256 / D heads a warp at once, kKvPass
+// times; a warp's heads are of one token and one kind (q, k or v).  blockIdx.y: the kind and its heads, blockIdx.x:
+// eight tokens.  The heads' loads are all under way before the first is used, and cos and sin are read once for them
+// (a head a warp, 8-byte loads: 104 us for 8191 tokens of 32 + 2 x 8 heads of 128, and 31 us reading them back).
+constexpr int kAppendWarps = 8, kKvPass = 4;
+__host__ __device__ constexpr int kv4_warp_heads(int D) { return kKvPass * 256 / D; }
 
-// One warp a row (a head of q, k or v of a token), head size D = 32 E: lane l holds dimensions E l .. E l + E - 1.
-// In the pairs (i, i + rot/2) the partner of a lane's dimensions is a whole lane's (rot/2 is a multiple of 8 >= E).
+// Head size D; in the pairs (i, i + rot/2) the partner of a lane's dimensions is a whole lane's (rot/2 is a multiple of 8).
 template <int D, bool BF>
-__global__ void __launch_bounds__(32 * kAppendWarps) kv4_append_kernel(const KvAppendArgs a) {
-  constexpr int E = D / 32;
+__global__ void __launch_bounds__(32 * kAppendWarps) kv4_append_kernel(const __grid_constant__ KvAppendArgs a) {
+  constexpr int L = D / 8, HP = 32 / L, HB = kv4_warp_heads(D);   // lanes a head, heads a pass, heads a warp
   grid_dep_wait();
-  const int rows = a.q_heads + 2 * a.cache.kv_heads;
-  const long long item = (long long)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
-  if (item >= (long long)a.tokens * rows) return;
-  const int lane = threadIdx.x & 31, d0 = lane * E;
-  const int t = (int)(item / rows), r = (int)(item - (long long)t * rows);
-  const bool is_q = r < a.q_heads, is_v = r >= a.q_heads + a.cache.kv_heads;
-  const int head = is_q ? r : (r - a.q_heads) % a.cache.kv_heads;
-  const long long slot = a.slots[t];
-  int pos = 0;
-  if (a.rope != IFQ_ROPE_NONE) {
-    pos = a.pos[t];
-    if (pos < 0 || pos >= a.positions) {
-      if (lane == 0) set_status(IFQ_ERANGE);
-      return;
-    }
+  grid_dep_launch();
+  const int t = blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
+  if (t >= a.tokens) return;
+  const int lane = threadIdx.x & 31, dl = lane % L, d0 = 8 * dl;
+  const int qb = (a.q_heads + HB - 1) / HB, kb = (a.cache.kv_heads + HB - 1) / HB;
+  const int y = blockIdx.y;
+  const bool is_q = y < qb, is_v = y >= qb + kb;
+  const int heads = is_q ? a.q_heads : a.cache.kv_heads, h0 = (is_q ? y : is_v ? y - qb - kb : y - qb) * HB + lane / L;
+  const uint16_t* src = (is_q ? a.q + t * a.q_stride : is_v ? a.v + t * a.v_stride : a.k + t * a.k_stride) + d0;
+  uint32_t w[kKvPass][4];
+#pragma unroll
+  for (int u = 0; u < kKvPass; ++u) {
+    const int h = h0 + u * HP;
+    w[u][0] = w[u][1] = w[u][2] = w[u][3] = 0;
+    if (h < heads) load_words(w[u], src + (long long)h * D);
   }
-  if (slot >= a.cache.slots) {
+  const long long slot = a.slots[t];
+  const bool turn = a.rope != IFQ_ROPE_NONE;
+  const int pos = turn ? a.pos[t] : 0;
+  if ((turn && (pos < 0 || pos >= a.positions)) || slot >= a.cache.slots) {
     if (lane == 0) set_status(IFQ_ERANGE);
     return;
   }
   if (!is_q && slot < 0) return;
 
-  const uint16_t* src = is_q   ? a.q + t * a.q_stride + head * D
-                        : is_v ? a.v + t * a.v_stride + head * D
-                               : a.k + t * a.k_stride + head * D;
-  uint32_t w[E / 2];
-  load_words(w, src + d0);
-  float x[E];
+  const int half = a.rot / 2;
+  const bool turned = turn && !is_v && d0 < a.rot, halves = a.rope == IFQ_ROPE_HALVES;
+  const bool first = d0 < half;
+  float cs[8], sn[8];
+  if (turned) {   // halves: a lane's eight pairs; pairs: its four
+    const int at = halves ? (first ? d0 : d0 - half) : d0 / 2;
+    const float *c = a.cos + (long long)pos * half + at, *s = a.sin + (long long)pos * half + at;
 #pragma unroll
-  for (int i = 0; i < E / 2; ++i) {
-    const float2 f = unpack16<BF>(w[i]);
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
+    for (int i = 0; i < 8; i += 4)
+      if (halves || i < 4) {
+        const float4 u = a.vec ? *(const float4*)(c + i) : make_float4(c[i], c[i + 1], c[i + 2], c[i + 3]);
+        const float4 v = a.vec ? *(const float4*)(s + i) : make_float4(s[i], s[i + 1], s[i + 2], s[i + 3]);
+        cs[i] = u.x, cs[i + 1] = u.y, cs[i + 2] = u.z, cs[i + 3] = u.w;
+        sn[i] = v.x, sn[i + 1] = v.y, sn[i + 2] = v.z, sn[i + 3] = v.w;
+      }
   }
-  if (!is_v && a.rope == IFQ_ROPE_HALVES) {
-    const int half = a.rot / 2, hl = half / E;
-    const bool first = d0 < half, turned = d0 < a.rot;
-    uint32_t pw[E / 2];
+  long long page = 0;
+  int row = 0;
+  if (!is_q) kv4_place(a.cache, slot, page, row);
+
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) pw[i] = __shfl_sync(0xffffffffu, w[i], (turned ? (first ? lane + hl : lane - hl) : lane));
-    if (turned) {
-      const float* c = a.cos + (long long)pos * half + (first ? d0 : d0 - half);
-      const float* s = a.sin + (long long)pos * half + (first ? d0 : d0 - half);
+  for (int u = 0; u < kKvPass; ++u) {
+    const int h = h0 + u * HP;
+    float x[8];
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const float2 f = unpack16<BF>(pw[i / 2]);
-        const float p = i % 2 ? f.y : f.x;
-        const float m = __fmul_rn(x[i], c[i]), n = __fmul_rn(p, s[i]);
-        x[i] = first ? __fsub_rn(m, n) : __fadd_rn(m, n);   // a cos - b sin, b cos + a sin
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = unpack16<BF>(w[u][i]);
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
+    if (!is_v && turn) {
+      if (halves) {
+        const int from = turned ? (first ? lane + half / 8 : lane - half / 8) : lane;
+        uint32_t pw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pw[i] = __shfl_sync(0xffffffffu, w[u][i], from);
+        if (turned) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float2 f = unpack16<BF>(pw[i / 2]);
+            const float m = __fmul_rn(x[i], cs[i]), n = __fmul_rn(i % 2 ? f.y : f.x, sn[i]);
+            x[i] = first ? __fsub_rn(m, n) : __fadd_rn(m, n);   // a cos - b sin, b cos + a sin
+          }
+        }
+      } else if (turned) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          const float p = x[i], q = x[i + 1], c = cs[i / 2], s = sn[i / 2];
+          x[i] = __fsub_rn(__fmul_rn(p, c), __fmul_rn(q, s));
+          x[i + 1] = __fadd_rn(__fmul_rn(q, c), __fmul_rn(p, s));
+        }
       }
     }
-  } else if (!is_v && a.rope == IFQ_ROPE_PAIRS && d0 < a.rot) {
-    const float* c = a.cos + (long long)pos * (a.rot / 2) + d0 / 2;
-    const float* s = a.sin + (long long)pos * (a.rot / 2) + d0 / 2;
+    if (is_q) {
+      if (h < heads) {
+        uint32_t o[4];
 #pragma unroll
-    for (int i = 0; i < E; i += 2) {
-      const float u = x[i], v = x[i + 1], cc = c[i / 2], ss = s[i / 2];
-      x[i] = __fsub_rn(__fmul_rn(u, cc), __fmul_rn(v, ss));
-      x[i + 1] = __fadd_rn(__fmul_rn(v, cc), __fmul_rn(u, ss));
+        for (int i = 0; i < 4; ++i) o[i] = pack16<BF>(x[2 * i], x[2 * i + 1]);
+        store_words(a.q_out + t * a.q_out_stride + (long long)h * D + d0, o);
+      }
+      continue;
     }
-  }
-  if (is_q) {
+    float lo = 65504.0f, hi = -65504.0f;
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) w[i] = pack16<BF>(x[2 * i], x[2 * i + 1]);
-    store_words(a.q_out + t * a.q_out_stride + head * D + d0, w);
-    return;
-  }
-
-  float lo = 65504.0f, hi = -65504.0f;
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    x[i] = min_nan(max_nan(x[i], -65504.0f), 65504.0f);
-    lo = min_nan(lo, x[i]);
-    hi = max_nan(hi, x[i]);
-  }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-  }
-  const __half hs = __float2half_rn(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)), hm = __float2half_rn(lo);
-  const float sc = __half2float(hs), mn = __half2float(hm);
-  uint32_t code[E];
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const float c = rintf(__fdiv_rn(__fsub_rn(x[i], mn), sc));
-    code[i] = sc > 0.0f ? (uint32_t)fminf(fmaxf(c, 0.0f), 15.0f) : 0u;   // (also 0 where the scale is NaN)
-  }
-  uint8_t* g = kv4_group(a.cache, D, slot, head);
-  const int row = (int)(slot % a.cache.page_size) % kKvGroup;
-  uint8_t b[E / 2];
-#pragma unroll
-  for (int i = 0; i < E / 2; ++i) b[i] = (uint8_t)(code[2 * i] | code[2 * i + 1] << 4);
-  if (is_v) {
-#pragma unroll
-    for (int i = 0; i < E / 2; i += 2) {
-      uint8_t* p = g + kv4_v_byte(D, row, d0 + 2 * i);
-      if constexpr (E >= 4) *(uint16_t*)p = (uint16_t)(b[i] | b[i + 1] << 8);
-      else *p = b[i];
+    for (int i = 0; i < 8; ++i) {
+      x[i] = min_nan(max_nan(x[i], -65504.0f), 65504.0f);
+      lo = min_nan(lo, x[i]);
+      hi = max_nan(hi, x[i]);
     }
-  } else {
-    uint8_t* p = g + kv4_k_byte(D, row, d0);
-    if constexpr (E == 2) *p = b[0];
-    else if constexpr (E == 4) *(uint16_t*)p = (uint16_t)(b[0] | b[1] << 8);
-    else *(uint32_t*)p = (uint32_t)b[0] | (uint32_t)b[1] << 8 | (uint32_t)b[2] << 16 | (uint32_t)b[3] << 24;
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) {
+      lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    }
+    const __half hs = __float2half_rn(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)), hm = __float2half_rn(lo);
+    const float sc = __half2float(hs), mn = __half2float(hm);
+    uint32_t code = 0;
+    if (sc > 0.0f) {   // (0 where the scale is NaN)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        code |= (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], mn), sc)), 0.0f), 15.0f) << (4 * i);
+    }
+    if (h < heads) {
+      uint8_t* g = kv4_group(a.cache, D, page, row, h);
+      const int r = row % kKvGroup;
+      if (is_v) {
+        *(uint16_t*)(g + kv4_v_byte(D, r, d0)) = (uint16_t)code;
+        *(uint16_t*)(g + kv4_v_byte(D, r, d0 + 4)) = (uint16_t)(code >> 16);
+      } else {
+        *(uint32_t*)(g + kv4_k_byte(D, r, d0)) = code;
+      }
+      if (dl == 0)
+        *(uint32_t*)(g + 16 * D + (is_v ? 64 : 0) + 4 * r) = (uint32_t)__half_as_ushort(hs) | (uint32_t)__half_as_ushort(hm) << 16;
+    }
+    __syncwarp();
   }
-  if (lane == 0)
-    *(uint32_t*)(g + 16 * D + (is_v ? 64 : 0) + 4 * row) =
-        (uint32_t)__half_as_ushort(hs) | (uint32_t)__half_as_ushort(hm) << 16;
 }
 
 struct KvReadArgs {
@@ -226,37 +252,51 @@ struct KvReadArgs {
   int tokens;
 };
 
-// One warp a head of a token's K or V.
 template <int D, bool BF>
-__global__ void __launch_bounds__(32 * kAppendWarps) kv4_read_kernel(const KvReadArgs a) {
-  constexpr int E = D / 32;
+__global__ void __launch_bounds__(32 * kAppendWarps) kv4_read_kernel(const __grid_constant__ KvReadArgs a) {
+  constexpr int L = D / 8, HP = 32 / L, HB = kv4_warp_heads(D);
   grid_dep_wait();
-  const int hk = a.cache.kv_heads;
-  const long long item = (long long)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
-  if (item >= (long long)a.tokens * 2 * hk) return;
-  const int lane = threadIdx.x & 31, d0 = lane * E;
-  const int t = (int)(item / (2 * hk)), r = (int)(item - (long long)t * 2 * hk), head = r % hk;
-  const bool is_v = r >= hk;
+  grid_dep_launch();
+  const int t = blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
+  if (t >= a.tokens) return;
+  const int lane = threadIdx.x & 31, dl = lane % L, d0 = 8 * dl, hk = a.cache.kv_heads, kb = (hk + HB - 1) / HB;
+  const bool is_v = (int)blockIdx.y >= kb;
   uint16_t* out = is_v ? a.v_out : a.k_out;
   if (!out) return;
+  const int h0 = (is_v ? blockIdx.y - kb : blockIdx.y) * HB + lane / L;
   const long long slot = a.slots[t];
+  const bool there = slot >= 0 && slot < a.cache.slots;
   if (slot >= a.cache.slots && lane == 0) set_status(IFQ_ERANGE);
-  uint32_t w[E / 2];
-  if (slot < 0 || slot >= a.cache.slots) {
+  uint32_t code[kKvPass], par[kKvPass];
+  long long page = 0;
+  int row = 0;
+  if (there) kv4_place(a.cache, slot, page, row);
+  const int r = row % kKvGroup;
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) w[i] = 0;
-  } else {
-    const uint8_t* g = kv4_group(a.cache, D, slot, head);
-    const int row = (int)(slot % a.cache.page_size) % kKvGroup;
-    const float2 par = __half22float2(*(const __half2*)(g + 16 * D + (is_v ? 64 : 0) + 4 * row));
-#pragma unroll
-    for (int i = 0; i < E / 2; ++i) {
-      const uint32_t b = g[is_v ? kv4_v_byte(D, row, d0 + 2 * i) : kv4_k_byte(D, row, d0 + 2 * i)];
-      w[i] = pack16<BF>(__fadd_rn(__fmul_rn((float)(b & 15u), par.x), par.y),
-                        __fadd_rn(__fmul_rn((float)(b >> 4), par.x), par.y));
+  for (int u = 0; u < kKvPass; ++u) {
+    const int h = h0 + u * HP;
+    code[u] = par[u] = 0;
+    if (there && h < hk) {
+      const uint8_t* g = kv4_group(a.cache, D, page, row, h);
+      par[u] = *(const uint32_t*)(g + 16 * D + (is_v ? 64 : 0) + 4 * r);
+      if (is_v)
+        code[u] = (uint32_t) * (const uint16_t*)(g + kv4_v_byte(D, r, d0)) | (uint32_t) * (const uint16_t*)(g + kv4_v_byte(D, r, d0 + 4)) << 16;
+      else
+        code[u] = *(const uint32_t*)(g + kv4_k_byte(D, r, d0));
     }
   }
-  store_words(out + ((long long)t * hk + head) * D + d0, w);
+#pragma unroll
+  for (int u = 0; u < kKvPass; ++u) {
+    const int h = h0 + u * HP;
+    const float2 p = unpack16<false>(par[u]);
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t c = code[u] >> (8 * i);
+      w[i] = pack16<BF>(__fadd_rn(__fmul_rn((float)(c & 15u), p.x), p.y), __fadd_rn(__fmul_rn((float)(c >> 4 & 15u), p.x), p.y));
+    }
+    if (h < hk) store_words(out + ((long long)t * hk + h) * D + d0, w);
+  }
 }
 
 }  // namespace ifq

@@ -27,13 +27,6 @@ namespace ifq {
 
 constexpr float kNoMax = -3.0e38f;   // stands for the maximum of nothing
 
-struct KvDiv {   // n / d for 0 <= n < 2^31
-  uint32_t d, mul, shift;
-};
-__device__ __forceinline__ uint32_t kv_div(uint32_t n, const KvDiv& f) {
-  return (uint32_t)(((uint64_t)__umulhi(n, f.mul) + n) >> f.shift);
-}
-
 struct KvRowsArgs {
   KvAttnArgs a;
   KvDiv by_gpp, by_group;   // groups a page, query heads a key head

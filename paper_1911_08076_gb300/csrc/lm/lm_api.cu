@@ -59,17 +59,6 @@ int stride_of(int64_t given, long long width, long long* out) {
   return IFQ_OK;
 }
 
-KvCacheArgs cache_args(const ifq_kv4_cache& c, const void* p) {
-  KvCacheArgs a;
-  a.p = (uint8_t*)p;
-  a.slots = (long long)c.pages * c.page_size;
-  a.page_size = c.page_size;
-  a.kv_heads = c.kv_heads;
-  return a;
-}
-
-// ---------------------------------------------------------------- attention
-
 KvDiv make_div(uint32_t d) {
   KvDiv f;
   f.d = d;
@@ -78,6 +67,17 @@ KvDiv make_div(uint32_t d) {
   f.mul = (uint32_t)(((1ull << 32) * ((1ull << f.shift) - d)) / d + 1ull);
   return f;
 }
+
+KvCacheArgs cache_args(const ifq_kv4_cache& c, const void* p) {
+  KvCacheArgs a;
+  a.p = (uint8_t*)p;
+  a.slots = (long long)c.pages * c.page_size;
+  a.by_page = make_div(c.page_size);
+  a.kv_heads = c.kv_heads;
+  return a;
+}
+
+// ---------------------------------------------------------------- attention
 
 int check_attention(const ifq_kv4_attention_desc* d, KvAttnArgs* a) {
   if (!d) return IFQ_EINVAL;
@@ -370,13 +370,14 @@ int ifq_kv4_append(const ifq_kv4_append_desc* d, const void* q, const void* k, c
   a.rope = d->rope;
   a.rot = d->rot_dim;
   a.positions = d->positions;
-  const long long items = (long long)d->tokens * (a.q_heads + 2 * d->cache.kv_heads);
-  const long long blocks = (items + kAppendWarps - 1) / kAppendWarps;
-  if (blocks > INT_MAX) return IFQ_ERANGE;
-  if (!blocks) return IFQ_OK;
+  a.vec = aligned16(cos) && aligned16(sin);
+  if (!d->tokens) return IFQ_OK;
+  const int HB = kv4_warp_heads(D);
+  const dim3 grid(ceil_div(d->tokens, kAppendWarps), ceil_div(a.q_heads, HB) + 2 * ceil_div(d->cache.kv_heads, HB));
+  if (grid.y > 65535) return IFQ_ERANGE;
   return by_head(D, d->dtype, [&](auto dim, auto bf) {
-    return done(launch_k(kv4_append_kernel<decltype(dim)::value, decltype(bf)::value>, dim3((unsigned)blocks),
-                         dim3(32 * kAppendWarps), 0, S(stream), a));
+    return done(launch_k(kv4_append_kernel<decltype(dim)::value, decltype(bf)::value>, grid, dim3(32 * kAppendWarps), 0,
+                         S(stream), a));
   });
 }
 
@@ -388,9 +389,9 @@ int ifq_kv4_read(const ifq_kv4_append_desc* d, const void* cache, const int64_t*
   if (rc) return rc;
   if (d->tokens < 0 || !is16(d->dtype) || !cache || !slots) return IFQ_EINVAL;
   if (!aligned16(cache) || !aligned16(k_out) || !aligned16(v_out) || !aligned(slots, 8)) return IFQ_EALIGN;
-  const long long blocks = ((long long)d->tokens * 2 * d->cache.kv_heads + kAppendWarps - 1) / kAppendWarps;
-  if (blocks > INT_MAX) return IFQ_ERANGE;
-  if (!blocks || (!k_out && !v_out)) return IFQ_OK;
+  if (!d->tokens || (!k_out && !v_out)) return IFQ_OK;
+  const dim3 grid(ceil_div(d->tokens, kAppendWarps), 2 * ceil_div(d->cache.kv_heads, kv4_warp_heads(d->cache.head_dim)));
+  if (grid.y > 65535) return IFQ_ERANGE;
   KvReadArgs a;
   a.cache = cache_args(d->cache, cache);
   a.slots = slots;
@@ -398,8 +399,8 @@ int ifq_kv4_read(const ifq_kv4_append_desc* d, const void* cache, const int64_t*
   a.v_out = (uint16_t*)v_out;
   a.tokens = d->tokens;
   return by_head(d->cache.head_dim, d->dtype, [&](auto dim, auto bf) {
-    return done(launch_k(kv4_read_kernel<decltype(dim)::value, decltype(bf)::value>, dim3((unsigned)blocks),
-                         dim3(32 * kAppendWarps), 0, S(stream), a));
+    return done(launch_k(kv4_read_kernel<decltype(dim)::value, decltype(bf)::value>, grid, dim3(32 * kAppendWarps), 0,
+                         S(stream), a));
   });
 }
 
@@ -468,11 +469,11 @@ int ifq_fp8_quantize(const ifq_fp8_desc* d, const void* x, void* codes, float* s
   a.m = d->m;
   a.k = d->k;
   a.kb = ceil_div(d->k, kFp8Block);
-  const long long blocks = ((long long)a.m * a.kb + kFp8QuantWarps - 1) / kFp8QuantWarps;
-  if (blocks > INT_MAX) return IFQ_ERANGE;
-  if (!blocks) return IFQ_OK;
-  return done(d->dtype == IFQ_BF16 ? launch_k(fp8_quantize_kernel<true>, dim3((unsigned)blocks), dim3(32 * kFp8QuantWarps), 0, S(stream), a)
-                                   : launch_k(fp8_quantize_kernel<false>, dim3((unsigned)blocks), dim3(32 * kFp8QuantWarps), 0, S(stream), a));
+  if (!a.m) return IFQ_OK;
+  const dim3 grid(ceil_div(a.m, kFp8QuantWarps), ceil_div(a.kb, 2 * kFp8Pass));
+  if (grid.y > 65535) return IFQ_ERANGE;
+  return done(d->dtype == IFQ_BF16 ? launch_k(fp8_quantize_kernel<true>, grid, dim3(32 * kFp8QuantWarps), 0, S(stream), a)
+                                   : launch_k(fp8_quantize_kernel<false>, grid, dim3(32 * kFp8QuantWarps), 0, S(stream), a));
 }
 
 int ifq_fp8_workspace_bytes(const ifq_fp8_desc* d, size_t* bytes) {
