@@ -131,6 +131,14 @@ __device__ __forceinline__ KvTiles kv_tiles(const KvAttnArgs& a, int len, int p_
   return t;
 }
 
+// Keeps the use of loaded registers after this point: work on them that is moved up to the loads waits for them there
+// (900 of 3200 cycles a tile).
+template <int N>
+__device__ __forceinline__ void hold(uint32_t (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(v[i]));
+}
+
 template <int D, bool BF, int RT>
 __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_kernel(const __grid_constant__ KvChunkArgs A) {
   using C = KvChunkShape<D, RT>;
@@ -148,10 +156,9 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
   auto pready = [&](int b) { return bars + 80 + 8 * b; };
   auto odone = [&](int r) { return bars + 96 + 8 * r; };
   auto pfull = [&](int b) { return bars + 112 + 8 * b; };    // parameters
-  auto pempty = [&](int b) { return bars + 112 + 8 * kChunkPar + 8 * b; };
-  const uint32_t qready = bars + 112 + 16 * kChunkPar;
+  const uint32_t qready = bars + 112 + 8 * kChunkPar;
   auto olast = [&](int g) { return qready + 8 + 8 * g; };    // group g's last product
-  uint32_t* tptr = (uint32_t*)((uint8_t*)sPar + C::par_bytes + 112 + 16 * kChunkPar + 24);
+  uint32_t* tptr = (uint32_t*)((uint8_t*)sPar + C::par_bytes + 112 + 8 * kChunkPar + 24);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int b = 0; b < 2; ++b) {
@@ -164,10 +171,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       mbar_init(odone(b), 1);
       mbar_init(olast(b), 1);
     }
-    for (int b = 0; b < kChunkPar; ++b) {
-      mbar_init(pfull(b), 4);
-      mbar_init(pempty(b), 4 * RT);
-    }
+    for (int b = 0; b < kChunkPar; ++b) mbar_init(pfull(b), 4);
     mbar_init(qready, 4 * RT);
     fence_mbar_init();
   }
@@ -389,10 +393,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(pready(b));
-        mbar_arrive(pempty(pb));
-      }
+      if (lane == 0) mbar_arrive(pready(b));
     }
     if (mine > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(olast(grp), 0));
     tc_fence_after();
@@ -483,63 +484,100 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
     const int kg = tid >> 4, krow = tid & 15;                                  // the key's group of the tile, row of it
     const int c8 = lane & 7, vg = (w >> 1) * 4 + (c8 >> 1), vh = c8 & 1, slice = (lane >> 3) | (w & 1) << 2;
     uint32_t kw[NBLK * WPB * 4], vw[NBLK * WPB * 4], kpar = 0, vpar = 0, vp[8];
-    auto group = [&](int i, int g) -> const uint8_t* {   // group g of tile i, if it holds tokens
-      const int gi = first_key(i) / kKvGroup + g;
-      if (gi * kKvGroup >= q.len) return nullptr;
-      const int pi = kv_div(gi, A.by_gpp), page = a.table[(long long)s * a.max_pages + pi];
-      if (page < 0 || page >= a.pages) {
-        set_status(IFQ_ERANGE);
-        return nullptr;
+    // The thread's two groups of each tile, a cursor each: place in the page table, group of the page.  A page's number
+    // is read two tiles ahead, so that nothing waits for it; nor is any load made on a condition, which would be waited
+    // for at once: a group past the tokens is looked up in the last page's place, and where there is no page any
+    // group's bytes will do (codes are numbers, and the parameters are then left out).
+    const int32_t* table = a.table + (long long)s * a.max_pages;
+    const int gpp = A.by_gpp.d, last_group = (q.len - 1) / kKvGroup, last_page = (int)kv_div(max(last_group, 0), A.by_gpp);
+    const int step_pages = 8 / gpp, step_groups = 8 - step_pages * gpp;   // (8 groups a tile)
+    const long long page_bytes = (long long)a.kv_heads * gpp * GB;
+    const uint8_t* heads = a.cache + (long long)head * gpp * GB;
+    struct Cursor {
+      int group, page, in;   // group of the sequence; its place in the table and in its page
+    };
+    auto at_tile = [&](int i, int g) {
+      Cursor c;
+      c.group = first_key(i) / kKvGroup + g;
+      c.page = kv_div(c.group, A.by_gpp);
+      c.in = c.group - c.page * gpp;
+      return c;
+    };
+    auto forward = [&](Cursor& c, int i, int g) {   // from tile i - 1 to i
+      if (t0 + i == tiles.sg && tiles.skip) {
+        c = at_tile(i, g);
+        return;
       }
-      return a.cache + (((long long)page * a.kv_heads + head) * A.by_gpp.d + (gi - pi * A.by_gpp.d)) * GB;
+      c.group += 8;
+      c.page += step_pages;
+      c.in += step_groups;
+      if (c.in >= gpp) c.in -= gpp, ++c.page;
+    };
+    auto look = [&](const Cursor& c) { return table[min(c.page, last_page)]; };
+    auto place = [&](const Cursor& c, int page, bool& there) -> const uint8_t* {
+      const bool tokens = c.group <= last_group, known = page >= 0 && page < a.pages;
+      if (tokens && !known) set_status(IFQ_ERANGE);
+      there = tokens && known;
+      return heads + (known ? page : 0) * page_bytes + c.in * GB;
     };
     auto load_k = [&](const uint8_t* g) {
 #pragma unroll
       for (int b = 0; b < NBLK; ++b)
 #pragma unroll
         for (int k = 0; k < WPB; ++k) {
-          uint4 y = make_uint4(0, 0, 0, 0);
-          if (g) y = *(const uint4*)(g + b * 8 * DB + krow * (DB / 2) + 16 * k);
+          const uint4 y = *(const uint4*)(g + b * 8 * DB + krow * (DB / 2) + 16 * k);
           const int o = (b * WPB + k) * 4;
           kw[o] = y.x, kw[o + 1] = y.y, kw[o + 2] = y.z, kw[o + 3] = y.w;
         }
-      kpar = g ? *(const uint32_t*)(g + 16 * D + 4 * krow) : 0u;
-      vpar = g ? *(const uint32_t*)(g + 16 * D + 64 + 4 * krow) : 0u;
+      kpar = *(const uint32_t*)(g + 16 * D + 4 * krow);
+      vpar = *(const uint32_t*)(g + 16 * D + 64 + 4 * krow);
     };
     auto load_v = [&](const uint8_t* g) {
 #pragma unroll
       for (int b = 0; b < NBLK; ++b)
 #pragma unroll
         for (int k = 0; k < WPB; ++k) {
-          uint4 y = make_uint4(0, 0, 0, 0);
-          if (g) y = *(const uint4*)(g + 8 * D + b * 8 * DB + vh * 4 * DB + slice * 4 * (DB / 8) + 16 * k);
+          const uint4 y = *(const uint4*)(g + 8 * D + b * 8 * DB + vh * 4 * DB + slice * 4 * (DB / 8) + 16 * k);
           const int o = (b * WPB + k) * 4;
           vw[o] = y.x, vw[o + 1] = y.y, vw[o + 2] = y.z, vw[o + 3] = y.w;
         }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        uint4 y = make_uint4(0, 0, 0, 0);
-        if (g) y = *(const uint4*)(g + 16 * D + 64 + 32 * vh + 16 * k);
+        const uint4 y = *(const uint4*)(g + 16 * D + 64 + 32 * vh + 16 * k);
         vp[4 * k] = y.x, vp[4 * k + 1] = y.y, vp[4 * k + 2] = y.z, vp[4 * k + 3] = y.w;
       }
     };
     // a key's parameters that are numbers (neither an infinity nor a NaN in either half)
     auto finite = [](uint32_t par) { return (par & 0x7c00u) != 0x7c00u && (par & 0x7c000000u) != 0x7c000000u; };
     bool ok = true;
+    int page_k = 0, page_v = 0;             // of the tile after the one at hand
+    bool have_k = false, have_v = false;    // whether the tile at hand has the thread's groups
+    Cursor ck = {}, cv = {}, nk = {}, nv = {};   // of the tile after the one at hand, and of the one after that
     if (nt > 0) {
-      load_k(group(0, kg));
-      load_v(group(0, vg));
+      ck = at_tile(0, kg);
+      cv = at_tile(0, vg);
+      load_k(place(ck, look(ck), have_k));
+      load_v(place(cv, look(cv), have_v));
+      forward(ck, 1, kg);
+      forward(cv, 1, vg);
+      page_k = look(ck);
+      page_v = look(cv);
+      nk = ck;
+      nv = cv;
     }
     for (int i = 0; i < nt && ok; ++i) {
       const int b = i % NB, pb = i % kChunkPar, j0 = first_key(i);
-      const uint8_t *gk = nullptr, *gv = nullptr;
-      if (i + 1 < nt) gk = group(i + 1, kg), gv = group(i + 1, vg);
-      ok = (i < kChunkPar || mbar_wait(pempty(pb), (i / kChunkPar - 1) & 1)) &&
-           (i < NB || mbar_wait(kempty(b), (i / NB - 1) & 1));
-      ok = __all_sync(0xffffffffu, ok);
+      forward(nk, i + 2, kg);
+      forward(nv, i + 2, vg);
+      const int next_k = look(nk), next_v = look(nv);
+      // (The buffer's last S is done.  It was asked for after the weights of the tile two before it, so the parameters
+      // of tile i - 4 have been used too.)
+      ok = __all_sync(0xffffffffu, i < NB || mbar_wait(kempty(b), (i / NB - 1) & 1));
       if (!ok) break;
+      hold(kw);
+      asm volatile("" : "+r"(kpar), "+r"(vpar));
       {
-        const bool there = j0 + tid < q.len;
+        const bool there = have_k && j0 + tid < q.len;
         float2 f = unpack16<false>(there ? kpar : 0u);
         if (there && !finite(vpar)) f.y = __uint_as_float(0x7fc00000u);   // NaN to the rows that see it
         float* dst = (float*)(sPar + pb * (kChunkKeys / 2) + tid / 2) + (tid & 1);
@@ -558,16 +596,18 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(kfull(b));
-      if (i + 1 < nt) load_k(gk);
+      if (i + 1 < nt) load_k(place(ck, page_k, have_k));
       ok = __all_sync(0xffffffffu, i < NB || mbar_wait(vempty(b), (i / NB - 1) & 1));
       if (!ok) break;
+      hold(vw);
+      hold(vp);
       uint8_t* dv = sV + b * C::kv_bytes + (w >> 1) * (D * 128);
       __half2 vs[4], vm[4];   // pairs of tokens: scales and minima, halved
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int j = j0 + vg * kKvGroup + 8 * vh + 2 * t;
-        const uint32_t y0 = j < q.len && finite(vp[2 * t]) ? vp[2 * t] : 0u;
-        const uint32_t y1 = j + 1 < q.len && finite(vp[2 * t + 1]) ? vp[2 * t + 1] : 0u;
+        const uint32_t y0 = have_v && j < q.len && finite(vp[2 * t]) ? vp[2 * t] : 0u;
+        const uint32_t y1 = have_v && j + 1 < q.len && finite(vp[2 * t + 1]) ? vp[2 * t + 1] : 0u;
         const uint32_t sc = __byte_perm(y0, y1, 0x5410), mn = __byte_perm(y0, y1, 0x7632);
         vs[t] = __hmul2(*(const __half2*)&sc, __float2half2_rn(0.5f));
         vm[t] = __hmul2(*(const __half2*)&mn, __float2half2_rn(0.5f));
@@ -596,7 +636,11 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(vfull(b));
-      if (i + 1 < nt) load_v(gv);
+      if (i + 1 < nt) load_v(place(cv, page_v, have_v));
+      page_k = next_k;
+      page_v = next_v;
+      ck = nk;
+      cv = nv;
     }
   } else {
     // ------------------------------------------------------------ MMA

@@ -161,18 +161,27 @@ def lib(build_if_missing: bool = True):
 def _ptr(t) -> Optional[int]:
     if t is None:
         return None
-    if isinstance(t, int):
-        return t
-    if isinstance(t, np.ndarray):
-        return t.ctypes.data
-    return t.data_ptr()
+    try:   # a tensor, most often
+        return t.data_ptr()
+    except AttributeError:
+        return t if isinstance(t, int) else t.ctypes.data
+
+
+_current_stream = None   # torch's handle of the current stream, looked up once (it initialises CUDA where need be)
+
+
+def _first_stream() -> int:
+    global _current_stream
+    import torch
+    device = torch.cuda.current_device()
+    get_device, get_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    _current_stream = lambda: get_stream(get_device())   # noqa: E731 (the handle without a Stream object around it)
+    return get_stream(device)
 
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        # (the handle without a Stream object around it)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return _current_stream() if _current_stream is not None else _first_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
