@@ -41,7 +41,7 @@ template <int D>
 struct KvRowsShape {
   static constexpr int W = 7;                       // computing warps; with the fetching one, two a scheduler
   static constexpr int U = D == 64 ? 4 : 2;         // groups a unit
-  static constexpr int stages = 2;                  // units in flight a warp
+  static constexpr int stages = 3;                  // units in flight a warp
   static constexpr int threads = 32 * (W + 1);
   static_assert(W * U <= 32, "a fetching lane a group");
 };
@@ -50,7 +50,7 @@ __host__ __device__ constexpr int kv_rows_per_sm(int D, int NT) { return D < 256
 template <int D>
 __host__ __device__ constexpr int kv_rows_smem(int R) {
   using C = KvRowsShape<D>;
-  return C::W * C::stages * (C::U * kv4_group_bytes(D) + 16) + C::W * 8 * (D + 4) * 4 + 3 * C::W * R * 4 + 16 * 8;
+  return C::W * C::stages * (C::U * kv4_group_bytes(D) + 16) + C::W * 4 * (D + 4) * 4 + 3 * C::W * R * 4 + 16 * 8;
 }
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -121,12 +121,12 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
   extern __shared__ __align__(128) uint8_t smem[];
   const KvAttnArgs& a = A.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
-  float* jO = (float*)(smem + W * ST * U * GB);             // [W][8][D + 4]
-  float* jm = jO + W * 8 * (D + 4);                         // [W][R] each
+  float* jO = (float*)(smem + W * ST * U * GB);             // [W][4][D + 4]
+  float* jm = jO + W * 4 * (D + 4);                         // [W][R] each
   float *jl = jm + W * R, *jz = jl + W * R;
   uint64_t* bars = (uint64_t*)(jz + W * R);                 // full [W][ST], empty [W][ST]
   long long* scan = (long long*)(bars + 2 * W * ST);        // [W + 1]
-  __shared__ int first[3];
+  __shared__ KvCursor first;
   const uint32_t bar_full = smem_u32(bars), bar_empty = smem_u32(bars + W * ST);
   if (threadIdx.x == 0) {
     for (int i = 0; i < W * ST; ++i) {
@@ -174,7 +174,9 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
       if (w < warp) before += scan[w];
       total += scan[w];
     }
-    long long share = (total + gridDim.x - 1) / gridDim.x;
+    // (64-bit divisions only where they are needed: they take as long as the loads above)
+    const bool small = total < 0x7fff0000ll;
+    long long share = small ? ((uint32_t)total + gridDim.x - 1) / gridDim.x : (total + gridDim.x - 1) / gridDim.x;
     if (share < W) share = W;
     const long long start = share * blockIdx.x;
     if (start >= total) {
@@ -193,42 +195,59 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
         at += c;
       }
       const long long in = start - at;
-      first[0] = t.s;
-      first[1] = (int)(in / t.nu);
-      first[2] = (int)(in % t.nu);
+      t.it = small ? (int)((uint32_t)in / (uint32_t)t.nu) : (int)(in / t.nu);
+      t.base = -(int)(in - (long long)t.it * t.nu);
+      first = t;
     }
     __syncthreads();
-    cur.s = first[0];
-    kv_shape<R, U>(A, cur);
-    cur.it = first[1];
-    cur.base = -first[2];
+    cur = first;
   }
 
   if (warp == W) {
-    // fetch: lane (w, u) the u-th group of warp w's units
+    // fetch: lane (w, u) the u-th group of warp w's units.  No lane waits for another warp's buffers.
     const int w = lane / U, u = lane % U;
     if (w < W) {
       const uint32_t ring = smem_u32(smem + w * ST * U * GB + u * GB);
-      int k = 0;
-      for (int o = w; o < n; o += W, ++k) {
+      int o = w, k = 0, st = 0, page = 0, gi = 0;
+      bool there = false;
+      auto look_up = [&]() {   // the next unit's page
+        if (o >= n) return;
         kv_advance<R, U>(A, cur, o);
-        const int g = (o - cur.base) * U + u, gi = g < cur.sg ? g : g + cur.skip;
-        const bool there = g < cur.ng && gi * kKvGroup < cur.q.len;
-        const int pi = kv_div(gi, A.by_gpp);
-        int page = 0;
-        if (there) {
-          page = a.table[(long long)cur.s * a.max_pages + pi];
-          if (page < 0 || page >= a.pages) set_status(IFQ_ERANGE);
-        }
-        const int st = k % ST, head = cur.it % a.kv_heads;
-        if (k >= ST && !mbar_wait(bar_empty + 8 * (w * ST + st), (k / ST - 1) & 1)) break;
-        const uint32_t bar = bar_full + 8 * (w * ST + st);
-        if (there && page >= 0 && page < a.pages) {
-          const uint8_t* src = a.cache + (((long long)page * a.kv_heads + head) * A.by_gpp.d + (gi - pi * A.by_gpp.d)) * GB;
-          mbar_arrive_expect_tx(bar, GB);
-          bulk_copy_g2s(ring + st * U * GB, src, GB, bar);
+        const int g = (o - cur.base) * U + u;
+        gi = g < cur.sg ? g : g + cur.skip;
+        there = g < cur.ng && gi * kKvGroup < cur.q.len;
+        if (there) page = a.table[(long long)cur.s * a.max_pages + kv_div(gi, A.by_gpp)];
+      };
+      look_up();
+      unsigned long long t0 = 0;
+      uint32_t idle = 0;
+      while (o < n) {
+        if (k < ST || mbar_test(bar_empty + 8 * (w * ST + st), (k / ST - 1) & 1)) {
+          const uint32_t bar = bar_full + 8 * (w * ST + st);
+          if (there && page >= 0 && page < a.pages) {
+            const int head = cur.it % a.kv_heads, in = gi - (int)kv_div(gi, A.by_gpp) * (int)A.by_gpp.d;
+            const uint8_t* src = a.cache + (((long long)page * a.kv_heads + head) * A.by_gpp.d + in) * GB;
+            mbar_arrive_expect_tx(bar, GB);
+            bulk_copy_g2s(ring + st * U * GB, src, GB, bar);
+          } else {
+            if (there) set_status(IFQ_ERANGE);
+            mbar_arrive(bar);
+          }
+          o += W;
+          ++k;
+          st = st + 1 < ST ? st + 1 : 0;
+          idle = 0;
+          look_up();
         } else {
-          mbar_arrive(bar);
+          __nanosleep(40);   // (the computing warps' issue slots)
+          if ((++idle & 255u) == 0) {
+            const unsigned long long now = global_ns();
+            if (idle == 256) t0 = now;
+            else if (now - t0 > 2 * kWaitNs) {   // a computing warp gave up
+              set_status(IFQ_ETIMEOUT);
+              break;
+            }
+          }
         }
       }
     }
@@ -511,29 +530,32 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
     const bool whole = o0 == cur.base && o1 - cur.base == cur.nu;
     const float back = 16777216.0f / vmul;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+    for (int pass = 0; pass < 2 * NT; ++pass) {   // four rows: those of half the lanes
+      const int nt = pass >> 1, four = pass & 1;
+      if (tig >> 1 == four) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int row = 2 * tig + c;
-        float top = kNoMax;
+        for (int c = 0; c < 2; ++c) {
+          const int row = nt * 8 + 2 * tig + c;
+          float top = kNoMax;
 #pragma unroll
-        for (int w = 0; w < W; ++w) top = fmaxf(top, jm[w * R + nt * 8 + row]);
-        const float f = exp2_fast(m[nt][c] - top) * back;
-        float* dst = jO + (warp * 8 + row) * (D + 4);
+          for (int w = 0; w < W; ++w) top = fmaxf(top, jm[w * R + row]);
+          const float f = exp2_fast(m[nt][c] - top) * back;
+          float* dst = jO + (warp * 4 + (row & 3)) * (D + 4);
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+          for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int i = 0; i < WPL; ++i)
+            for (int i = 0; i < WPL; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float* v = o[(b * WPL + i) * 2 + h][nt];
-              *(float2*)(dst + b * DB + gid * (DB / 8) + 4 * i + 2 * h) =
-                  make_float2((v[c] - ow[nt][c]) * f, (v[2 + c] * 0.0625f - ow[nt][c]) * f);
-            }
+              for (int h = 0; h < 2; ++h) {
+                const float* v = o[(b * WPL + i) * 2 + h][nt];
+                *(float2*)(dst + b * DB + gid * (DB / 8) + 4 * i + 2 * h) =
+                    make_float2((v[c] - ow[nt][c]) * f, (v[2 + c] * 0.0625f - ow[nt][c]) * f);
+              }
+        }
       }
       named_bar(1, 32 * W);
-      for (int i = threadIdx.x; i < 8 * D / 4; i += 32 * W) {   // four dimensions of a row each
-        const int row = i / (D / 4), d0 = i % (D / 4) * 4, r = rb * R + nt * 8 + row;
+      for (int i = threadIdx.x; i < 4 * D / 4; i += 32 * W) {   // four dimensions of a row each
+        const int r4 = i / (D / 4), d0 = i % (D / 4) * 4, row = 4 * four + r4, r = rb * R + nt * 8 + row;
         if (r >= nrows) break;
         float top = kNoMax, sum = 0.0f, zs = 0.0f;
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -544,7 +566,7 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
           const float f = exp2_fast(jm[w * R + nt * 8 + row] - top);
           sum += jl[w * R + nt * 8 + row] * f;
           zs += jz[w * R + nt * 8 + row] * f;
-          const float4 x = *(const float4*)(jO + (w * 8 + row) * (D + 4) + d0);
+          const float4 x = *(const float4*)(jO + (w * 4 + r4) * (D + 4) + d0);
           v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
         }
         if (whole) {
@@ -603,7 +625,7 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const __grid_constant__ K
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float sum = 0.0f;
   if (p0 < P)
-#pragma unroll 4
+#pragma unroll 8
     for (int i = p0; i < parts; i += P) {
       const float2 ml = A.part_ml[at(i)];
       const float f = exp2_fast(ml.x - top);
