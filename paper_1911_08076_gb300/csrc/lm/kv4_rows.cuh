@@ -15,11 +15,12 @@
 // the sum with the minima stays fp32.
 //
 // Work: an item's groups are taken in units of U; the units of all items in a row are cut into as many equal ranges as
-// there are blocks, whatever the lengths (an item cut by a range's end leaves partial sums in the workspace, joined by
-// kv4_join_kernel); or, where no sequence is long, one block an item.  Each warp takes every W-th unit of its block's
-// range.  One more warp fetches for all of them, a lane a group (page lookup and one bulk copy of the group's
-// contiguous bytes), two units ahead and across the ends of items.  At an item's end the warps' sums are joined in
-// shared memory.
+// there are blocks, whatever the lengths; or, where no sequence is long, a block takes an item.  In a block whose range
+// lies within one item the warps take the units in turn and their sums are joined in shared memory; else the range is
+// cut again, a contiguous part a warp, so that no warp waits for another at an item's end (joining at each of them took
+// 8000 cycles beside 2700 a unit).  An item that several parts share leaves sums in the workspace, which
+// kv4_join_kernel adds (the block itself, where its warps have all of it).  One more warp fetches for all, a lane a group (page lookup and one bulk copy of the group's
+// contiguous bytes), three units ahead and across the ends of items.
 #pragma once
 #include "kv4_attention.cuh"
 
@@ -31,15 +32,18 @@ struct KvRowsArgs {
   KvAttnArgs a;
   KvDiv by_gpp, by_group;   // groups a page, query heads a key head
   int direct;               // one block an item: blockIdx = (key head, block of rows, sequence)
-  // workspace of the ranges: parts [blocks][2][R][D], their (max, sum) [blocks][2][R], and who is cut [blocks]
+  // workspace of the ranges, a part a block and warp: sums [parts][2][R][D], their (max, sum) [parts][2][R], of an item
+  // begun before the part (0) and of one it leaves open (1), and which item that is [parts]
   float* part;
   float2* part_ml;
-  int4* cut;                // (sequence, block of rows * key heads + head, parts, 0) of the item a range leaves open
+  int4* cut;                // (sequence, block of rows * key heads + head, blocks it reaches into (0: none), last warp)
 };
+
+constexpr int kKvRowsWarps = 7;   // computing warps of a block; with the fetching one, two a scheduler
 
 template <int D>
 struct KvRowsShape {
-  static constexpr int W = 7;                       // computing warps; with the fetching one, two a scheduler
+  static constexpr int W = kKvRowsWarps;
   static constexpr int U = D == 64 ? 4 : 2;         // groups a unit
   static constexpr int stages = 3;                  // units in flight a warp
   static constexpr int threads = 32 * (W + 1);
@@ -111,6 +115,84 @@ __device__ __forceinline__ void kv_advance(const KvRowsArgs& A, KvCursor& c, int
   }
 }
 
+// A warp's sum of parts of a row: reference, sum of the weights, and values (four dimensions a lane).
+template <int D>
+struct KvSum {
+  static constexpr int N = D > 128 ? 2 : 1;
+  float top = kNoMax, sum = 0.0f;
+  float4 v[N] = {};
+
+  __device__ __forceinline__ void raise(float now) {
+    const float old = exp2_fast(top - now);
+    top = now;
+    sum *= old;
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n].x *= old, v[n].y *= old, v[n].z *= old, v[n].w *= old;
+  }
+  // Parts i0, i0 + step, .. (a lane each, below `parts`); at(i): where part i stands.
+  template <typename F>
+  __device__ __forceinline__ void add(const KvRowsArgs& A, int lane, int i0, int step, int parts, F&& at) {
+    const int mine = i0 + step * lane;
+    const float2 ml = mine < parts ? A.part_ml[at(mine)] : make_float2(kNoMax, 0.0f);
+    float now = fmaxf(top, ml.x);
+#pragma unroll
+    for (int k = 16; k; k >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, k));
+    raise(now);
+    // (nothing seen: no sums were written; a sum that is not a number is taken along)
+    uint32_t some = __ballot_sync(0xffffffffu, !(ml.x == kNoMax && ml.y == 0.0f));
+    while (some) {   // eight at a time, so that their loads are under way together
+      float4 x[8][N];
+      float f[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int j = some ? __ffs(some) - 1 : 0;
+        const float jm = __shfl_sync(0xffffffffu, ml.x, j), jl = __shfl_sync(0xffffffffu, ml.y, j);
+        f[k] = some ? exp2_fast(jm - top) : 0.0f;
+        if (some) sum += jl * f[k];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          x[k][n] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (some && lane * 4 + 128 * n < D) x[k][n] = *(const float4*)(A.part + at(i0 + step * j) * D + lane * 4 + 128 * n);
+        }
+        some &= some - 1;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          v[n].x += x[k][n].x * f[k], v[n].y += x[k][n].y * f[k];
+          v[n].z += x[k][n].z * f[k], v[n].w += x[k][n].w * f[k];
+        }
+    }
+  }
+  // Another warp's.
+  __device__ __forceinline__ void add(float2 ml, const float* x, int lane) {
+    raise(fmaxf(top, ml.x));
+    const float f = exp2_fast(ml.x - top);
+    sum += ml.y * f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (lane * 4 + 128 * n < D) {
+        const float4 y = *(const float4*)(x + lane * 4 + 128 * n);
+        v[n].x += y.x * f, v[n].y += y.y * f, v[n].z += y.z * f, v[n].w += y.w * f;
+      }
+  }
+  template <bool BF>
+  __device__ __forceinline__ void write(const KvRowsArgs& A, const KvSeq& q, int head, int r, int lane) const {
+    const KvAttnArgs& a = A.a;
+    const int qi = kv_div(r, A.by_group), hq = head * a.group + r - qi * a.group;
+    const long long t = q.first + qi;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (lane * 4 + 128 * n < D) {
+        const uint32_t w[2] = {pack16<BF>(v[n].x * inv, v[n].y * inv), pack16<BF>(v[n].z * inv, v[n].w * inv)};
+        store_words(a.out + t * a.out_stride + (long long)hq * D + lane * 4 + 128 * n, w);
+      }
+    if (a.lse && lane == 0) a.lse[t * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
+  }
+};
+
 template <int D, bool BF, int NT>
 __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)) kv4_rows_kernel(const __grid_constant__ KvRowsArgs A) {
   using C = KvRowsShape<D>;
@@ -127,6 +209,7 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
   uint64_t* bars = (uint64_t*)(jz + W * R);                 // full [W][ST], empty [W][ST]
   long long* scan = (long long*)(bars + 2 * W * ST);        // [W + 1]
   __shared__ KvCursor first;
+  __shared__ int4 cuts[W];
   const uint32_t bar_full = smem_u32(bars), bar_empty = smem_u32(bars + W * ST);
   if (threadIdx.x == 0) {
     for (int i = 0; i < W * ST; ++i) {
@@ -141,6 +224,8 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
 
   KvCursor cur;
   int n;        // units of this block
+  int full_share = 0;     // of a block whose range is not the last
+  long long ends = 0;     // units from this block's start to the end of all
   if (A.direct) {
     cur.s = blockIdx.z;
     kv_shape<R, U>(A, cur);
@@ -177,12 +262,14 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
     // (64-bit divisions only where they are needed: they take as long as the loads above)
     const bool small = total < 0x7fff0000ll;
     long long share = small ? ((uint32_t)total + gridDim.x - 1) / gridDim.x : (total + gridDim.x - 1) / gridDim.x;
-    if (share < W) share = W;
+    if (share < 2 * W) share = 2 * W;
     const long long start = share * blockIdx.x;
     if (start >= total) {
-      if (threadIdx.x == 0) A.cut[blockIdx.x] = make_int4(0, 0, 0, 0);
+      if (threadIdx.x < W) A.cut[blockIdx.x * W + threadIdx.x] = make_int4(0, 0, 0, 0);
       return;
     }
+    full_share = (int)min(share, (long long)0x7fffffff);
+    ends = total - start;
     n = (int)min(share, total - start);
     if (start >= before && start < before + mine) {   // one thread: its sequences hold the start
       long long at = before;
@@ -203,15 +290,19 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
     cur = first;
   }
 
+  const bool one = cur.base + cur.nu >= n;   // the range lies within one item
+  auto part_begin = [&](int w) { return one ? w : (int)((long long)n * w / W); };
+  auto part_end = [&](int w) { return one ? n : (int)((long long)n * (w + 1) / W); };
+  const int step = one ? W : 1;
   if (warp == W) {
     // fetch: lane (w, u) the u-th group of warp w's units.  No lane waits for another warp's buffers.
-    const int w = lane / U, u = lane % U;
+    const int w = lane / U, u = lane % U, last = part_end(w);
     if (w < W) {
       const uint32_t ring = smem_u32(smem + w * ST * U * GB + u * GB);
-      int o = w, k = 0, st = 0, page = 0, gi = 0;
+      int o = part_begin(w), k = 0, st = 0, page = 0, gi = 0;
       bool there = false;
       auto look_up = [&]() {   // the next unit's page
-        if (o >= n) return;
+        if (o >= last) return;
         kv_advance<R, U>(A, cur, o);
         const int g = (o - cur.base) * U + u;
         gi = g < cur.sg ? g : g + cur.skip;
@@ -221,7 +312,7 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
       look_up();
       unsigned long long t0 = 0;
       uint32_t idle = 0;
-      while (o < n) {
+      while (o < last) {
         if (k < ST || mbar_test(bar_empty + 8 * (w * ST + st), (k / ST - 1) & 1)) {
           const uint32_t bar = bar_full + 8 * (w * ST + st);
           if (there && page >= 0 && page < a.pages) {
@@ -233,7 +324,7 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
             if (there) set_status(IFQ_ERANGE);
             mbar_arrive(bar);
           }
-          o += W;
+          o += step;
           ++k;
           st = st + 1 < ST ? st + 1 : 0;
           idle = 0;
@@ -255,11 +346,12 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
   }
 
   const uint8_t* ring = smem + warp * ST * U * GB;
-  int used = 0, co = warp;
-  bool alive = true;
-  for (int o0 = 0; o0 < n;) {
+  const int last = part_end(warp);
+  int used = 0, co = part_begin(warp);
+  bool alive = true, open = false;
+  for (int o0 = one ? 0 : co; o0 < last;) {
     kv_advance<R, U>(A, cur, o0);
-    const int o1 = min(n, cur.base + cur.nu);
+    const int o1 = min(last, cur.base + cur.nu);
     const int rb = cur.it / a.kv_heads, head = cur.it - rb * a.kv_heads, nrows = cur.q.n * a.group;
     const int p_lo = cur.q.len - cur.q.n + (int)kv_div(rb * R, A.by_group);
     const int p_hi = cur.q.len - cur.q.n + (int)kv_div(min(nrows, rb * R + R) - 1, A.by_group);
@@ -338,7 +430,7 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
       for (int c = 0; c < 2; ++c) fresh |= (rb * R + nt * 8 + 2 * tig + c < nrows ? 1u : 0u) << (2 * nt + c);
     float vmul = 1.0f, vtop = 0.0f;   // factor of the value scales, and the scale that raises it
 
-    for (; co < o1; co += W) {
+    for (; co < o1; co += step) {
       const int st = used % ST;
       if (alive) alive = mbar_wait(bar_full + 8 * (warp * ST + st), (used / ST) & 1);
       ++used;
@@ -508,7 +600,9 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
       if (lane == 0) mbar_arrive(bar_empty + 8 * (warp * ST + st));
     }
 
-    // join the warps' sums: of each row the maximum, then everything relative to it
+    const bool whole = o0 == cur.base && o1 - cur.base == cur.nu;
+    open = o0 == cur.base && !whole;
+    const float back = 16777216.0f / vmul;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -519,28 +613,93 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
           z[nt][c] += __shfl_xor_sync(0xffffffffu, z[nt][c], k);
         }
         if (fresh >> (2 * nt + c) & 1u) m[nt][c] = kNoMax;
-        if (gid == 0) {
-          const int r = warp * R + nt * 8 + 2 * tig + c;
-          jm[r] = m[nt][c];
-          jl[r] = l[nt][c];
-          jz[r] = z[nt][c];
-        }
       }
-    named_bar(1, 32 * W);
-    const bool whole = o0 == cur.base && o1 - cur.base == cur.nu;
-    const float back = 16777216.0f / vmul;
+    if (one) {
+      // join the warps' sums: of each row the maximum, then everything relative to it
+      if (gid == 0) {
 #pragma unroll
-    for (int pass = 0; pass < 2 * NT; ++pass) {   // four rows: those of half the lanes
-      const int nt = pass >> 1, four = pass & 1;
-      if (tig >> 1 == four) {
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const int r = warp * R + nt * 8 + 2 * tig + c;
+            jm[r] = m[nt][c];
+            jl[r] = l[nt][c];
+            jz[r] = z[nt][c];
+          }
+      }
+      named_bar(1, 32 * W);
+#pragma unroll
+      for (int pass = 0; pass < 2 * NT; ++pass) {   // four rows: those of half the lanes
+        const int nt = pass >> 1, four = pass & 1;
+        if (tig >> 1 == four) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const int row = nt * 8 + 2 * tig + c;
+            float top = kNoMax;
+#pragma unroll
+            for (int w = 0; w < W; ++w) top = fmaxf(top, jm[w * R + row]);
+            const float f = exp2_fast(m[nt][c] - top) * back;
+            float* dst = jO + (warp * 4 + (row & 3)) * (D + 4);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+              for (int i = 0; i < WPL; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  const float* v = o[(b * WPL + i) * 2 + h][nt];
+                  *(float2*)(dst + b * DB + gid * (DB / 8) + 4 * i + 2 * h) =
+                      make_float2((v[c] - ow[nt][c]) * f, (v[2 + c] * 0.0625f - ow[nt][c]) * f);
+                }
+          }
+        }
+        named_bar(1, 32 * W);
+        for (int i = threadIdx.x; i < 4 * D / 4; i += 32 * W) {   // four dimensions of a row each
+          const int r4 = i / (D / 4), d0 = i % (D / 4) * 4, row = 4 * four + r4, r = rb * R + nt * 8 + row;
+          if (r >= nrows) break;
+          float top = kNoMax, sum = 0.0f, zs = 0.0f;
+          float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+          for (int w = 0; w < W; ++w) top = fmaxf(top, jm[w * R + nt * 8 + row]);
+#pragma unroll
+          for (int w = 0; w < W; ++w) {
+            const float f = exp2_fast(jm[w * R + nt * 8 + row] - top);
+            sum += jl[w * R + nt * 8 + row] * f;
+            zs += jz[w * R + nt * 8 + row] * f;
+            const float4 x = *(const float4*)(jO + (w * 4 + r4) * (D + 4) + d0);
+            v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+          }
+          if (whole) {
+            const int qi = kv_div(r, A.by_group), hq = head * a.group + r - qi * a.group;
+            const long long t = cur.q.first + qi;
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const uint32_t w[2] = {pack16<BF>((v.x + zs) * inv, (v.y + zs) * inv), pack16<BF>((v.z + zs) * inv, (v.w + zs) * inv)};
+            store_words(a.out + t * a.out_stride + (long long)hq * D + d0, w);
+            if (a.lse && d0 == 0)
+              a.lse[t * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
+          } else {
+            const long long at = ((long long)blockIdx.x * W * 2 + (o0 == cur.base ? 1 : 0)) * R + nt * 8 + row;
+            *(float4*)(A.part + at * D + d0) = make_float4(v.x + zs, v.y + zs, v.z + zs, v.w + zs);
+            if (d0 == 0) A.part_ml[at] = make_float2(top, sum);
+          }
+        }
+        named_bar(1, 32 * W);
+      }
+      if (!whole && warp > 0)   // the block's part is the first warp's
+        for (int r = lane; r < R; r += 32) A.part_ml[((long long)(blockIdx.x * W + warp) * 2) * R + r] = make_float2(kNoMax, 0.0f);
+    } else {
+      // this warp's own
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const int row = nt * 8 + 2 * tig + c;
-          float top = kNoMax;
-#pragma unroll
-          for (int w = 0; w < W; ++w) top = fmaxf(top, jm[w * R + row]);
-          const float f = exp2_fast(m[nt][c] - top) * back;
-          float* dst = jO + (warp * 4 + (row & 3)) * (D + 4);
+          const int row = nt * 8 + 2 * tig + c, r = rb * R + row;
+          if (r >= nrows) continue;
+          const int qi = kv_div(r, A.by_group), hq = head * a.group + r - qi * a.group;
+          const long long t = cur.q.first + qi;
+          const float inv = l[nt][c] == 0.0f ? 0.0f : 1.0f / l[nt][c], f = whole ? back * inv : back, zf = whole ? z[nt][c] * inv : z[nt][c];
+          const long long at = ((long long)(blockIdx.x * W + warp) * 2 + (o0 == cur.base ? 1 : 0)) * R + row;
+          uint16_t* out = a.out + t * a.out_stride + (long long)hq * D;
+          float* part = A.part + at * D;
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -548,112 +707,86 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
                 const float* v = o[(b * WPL + i) * 2 + h][nt];
-                *(float2*)(dst + b * DB + gid * (DB / 8) + 4 * i + 2 * h) =
-                    make_float2((v[c] - ow[nt][c]) * f, (v[2 + c] * 0.0625f - ow[nt][c]) * f);
+                const int d = b * DB + gid * (DB / 8) + 4 * i + 2 * h;
+                const float x = (v[c] - ow[nt][c]) * f + zf, y = (v[2 + c] * 0.0625f - ow[nt][c]) * f + zf;
+                if (whole) *(uint32_t*)(out + d) = pack16<BF>(x, y);
+                else *(float2*)(part + d) = make_float2(x, y);
               }
+          if (gid == 0) {
+            if (!whole) A.part_ml[at] = make_float2(m[nt][c], l[nt][c]);
+            else if (a.lse)
+              a.lse[t * a.q_heads + hq] = l[nt][c] == 0.0f ? -INFINITY : (m[nt][c] + log2f(l[nt][c])) * 0.69314718f;
+          }
         }
-      }
-      named_bar(1, 32 * W);
-      for (int i = threadIdx.x; i < 4 * D / 4; i += 32 * W) {   // four dimensions of a row each
-        const int r4 = i / (D / 4), d0 = i % (D / 4) * 4, row = 4 * four + r4, r = rb * R + nt * 8 + row;
-        if (r >= nrows) break;
-        float top = kNoMax, sum = 0.0f, zs = 0.0f;
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-        for (int w = 0; w < W; ++w) top = fmaxf(top, jm[w * R + nt * 8 + row]);
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-          const float f = exp2_fast(jm[w * R + nt * 8 + row] - top);
-          sum += jl[w * R + nt * 8 + row] * f;
-          zs += jz[w * R + nt * 8 + row] * f;
-          const float4 x = *(const float4*)(jO + (w * 4 + r4) * (D + 4) + d0);
-          v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
-        }
-        if (whole) {
-          const int qi = kv_div(r, A.by_group), hq = head * a.group + r - qi * a.group;
-          const long long t = cur.q.first + qi;
-          const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-          const uint32_t w[2] = {pack16<BF>((v.x + zs) * inv, (v.y + zs) * inv), pack16<BF>((v.z + zs) * inv, (v.w + zs) * inv)};
-          store_words(a.out + t * a.out_stride + (long long)hq * D + d0, w);
-          if (a.lse && d0 == 0)
-            a.lse[t * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
-        } else {
-          const int slot = o0 == cur.base ? 1 : 0;   // an item left open by the range's end, or one begun before it
-          const long long at = ((long long)blockIdx.x * 2 + slot) * R + nt * 8 + row;
-          *(float4*)(A.part + at * D + d0) = make_float4(v.x + zs, v.y + zs, v.z + zs, v.w + zs);
-          if (d0 == 0) A.part_ml[at] = make_float2(top, sum);
-        }
-      }
-      named_bar(1, 32 * W);
-    }
-    if (!A.direct && o1 == n && threadIdx.x == 0) {
-      const bool open = o0 == cur.base && !whole;
-      // the ranges that the item's units reach into: each has n of them, the last one or fewer
-      const int rest = cur.nu - (o1 - o0);
-      A.cut[blockIdx.x] = make_int4(cur.s, cur.it, open ? 1 + (rest + n - 1) / n : 0, 0);
     }
     o0 = o1;
   }
+  if (!A.direct && lane == 0) {
+    // the parts that the item which this one leaves open reaches into: to the block and warp of its last unit
+    int blocks = 0, w = 0;
+    if (open && (!one || warp == 0)) {
+      const long long to = (long long)cur.base + cur.nu - 1;
+      const int blk = (int)(to / full_share), in = (int)(to - (long long)blk * full_share);
+      const int units = (int)min((long long)full_share, ends - (long long)blk * full_share);
+      blocks = blk + 1;
+      w = (int)(((long long)(in + 1) * W - 1) / units);
+    }
+    A.cut[blockIdx.x * W + warp] = cuts[warp] = make_int4(cur.s, cur.it, blocks, w);
+  }
+  if (!A.direct && !one && part_begin(warp) == last)   // nothing: an item that others share has no sums here
+    for (int r = lane; r < R; r += 32) A.part_ml[((long long)(blockIdx.x * W + warp) * 2) * R + r] = make_float2(kNoMax, 0.0f);
+  if (A.direct || one) return;
+  // the items that several warps of this block share and no other block: a warp an item and row
+  named_bar(1, 32 * W);
+  for (int i = warp; i < W * R; i += W) {
+    const int w0 = i / R, row = i - w0 * R;
+    const int4 cut = cuts[w0];
+    if (cut.z != 1) continue;
+    const KvSeq q = kv_seq(a, cut.x);
+    const int rb = cut.y / a.kv_heads, head = cut.y - rb * a.kv_heads, r = rb * R + row;
+    if (r >= q.n * a.group) continue;
+    KvSum<D> t;
+    t.add(A, lane, 0, 1, cut.w - w0 + 1, [&](int k) { return ((long long)(blockIdx.x * W + w0 + k) * 2 + (k == 0 ? 1 : 0)) * R + row; });
+    t.template write<BF>(A, q, head, r, lane);
+  }
 }
 
-// The parts of an item that several ranges share: one block a range and a row; the range that begins the item does it.
+// The parts of the item that a range leaves to the next ones: a block a range and row, its four warps a quarter of the
+// parts each.  Of the ranges between the item's first and last it has all, in one part each.
 template <int D, bool BF, int NT>
 __global__ void __launch_bounds__(128) kv4_join_kernel(const __grid_constant__ KvRowsArgs A) {
-  constexpr int R = 8 * NT, T = D / 4, P = 128 / T > 0 ? 128 / T : 1;   // threads a row's dimensions, parts at once
-  __shared__ float4 sv[P][T];
-  __shared__ float ss[P], st[4];
+  constexpr int R = 8 * NT, W = kKvRowsWarps;
+  __shared__ float sv[4][D];
+  __shared__ float2 ss[4];
   grid_dep_wait();
   grid_dep_launch();
   const KvAttnArgs& a = A.a;
-  const int4 cut = A.cut[blockIdx.x];
-  const int parts = cut.z;
-  if (parts == 0) return;
-  KvCursor c;
-  c.s = cut.x;
-  kv_shape<R, KvRowsShape<D>::U>(A, c);
-  const int rb = cut.y / a.kv_heads, head = cut.y - rb * a.kv_heads, r = rb * R + blockIdx.y;
-  if (r >= c.q.n * a.group) return;
-  auto at = [&](int i) { return ((long long)(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * R + blockIdx.y; };
-  float top = kNoMax;
-  for (int i = threadIdx.x; i < parts; i += 128) top = fmaxf(top, A.part_ml[at(i)].x);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, blk = blockIdx.x, row = blockIdx.y;
+  const int4 mine = lane < W ? A.cut[blk * W + lane] : make_int4(0, 0, 0, 0);
+  const uint32_t some = __ballot_sync(0xffffffffu, mine.z > 1);
+  if (!some) return;
+  const int w0 = __ffs(some) - 1;
+  const int4 cut = make_int4(__shfl_sync(0xffffffffu, mine.x, w0), __shfl_sync(0xffffffffu, mine.y, w0),
+                             __shfl_sync(0xffffffffu, mine.z, w0), __shfl_sync(0xffffffffu, mine.w, w0));
+  const KvSeq q = kv_seq(a, cut.x);
+  const int rb = cut.y / a.kv_heads, head = cut.y - rb * a.kv_heads, r = rb * R + row;
+  if (r >= q.n * a.group) return;
+  const int own = W - w0, mid = cut.z - 2, parts = own + mid + cut.w + 1;
+  auto at = [&](int i) {
+    const int p = i < own ? blk * W + w0 + i : i < own + mid ? (blk + 1 + i - own) * W : (blk + cut.z - 1) * W + i - own - mid;
+    return ((long long)p * 2 + (i == 0 ? 1 : 0)) * R + row;
+  };
+  KvSum<D> t;
+  for (int i0 = warp; i0 < parts; i0 += 128) t.add(A, lane, i0, 4, parts, at);
 #pragma unroll
-  for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-  if (threadIdx.x % 32 == 0) st[threadIdx.x / 32] = top;
+  for (int n = 0; n < t.N; ++n)
+    if (lane * 4 + 128 * n < D) *(float4*)(sv[warp] + lane * 4 + 128 * n) = t.v[n];
+  if (lane == 0) ss[warp] = make_float2(t.top, t.sum);
   __syncthreads();
-  top = fmaxf(fmaxf(st[0], st[1]), fmaxf(st[2], st[3]));
-  const int d = threadIdx.x % T, p0 = threadIdx.x / T;
-  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  float sum = 0.0f;
-  if (p0 < P)
-#pragma unroll 8
-    for (int i = p0; i < parts; i += P) {
-      const float2 ml = A.part_ml[at(i)];
-      const float f = exp2_fast(ml.x - top);
-      const float4 x = *(const float4*)(A.part + at(i) * D + 4 * d);
-      v.x += x.x * f, v.y += x.y * f, v.z += x.z * f, v.w += x.w * f;
-      sum += ml.y * f;
-    }
-  if (p0 < P) {
-    sv[p0][d] = v;
-    if (d == 0) ss[p0] = sum;
-  }
-  __syncthreads();
-  if (threadIdx.x < T) {
-    v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    sum = 0.0f;
+  if (warp > 0) return;
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const float4 x = sv[p][d];
-      v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
-      sum += ss[p];
-    }
-    const int qi = kv_div(r, A.by_group), hq = head * a.group + r - qi * a.group;
-    const long long t = c.q.first + qi;
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    uint32_t w[2] = {pack16<BF>(v.x * inv, v.y * inv), pack16<BF>(v.z * inv, v.w * inv)};
-    store_words(a.out + t * a.out_stride + (long long)hq * D + 4 * d, w);
-    if (a.lse && d == 0) a.lse[t * a.q_heads + hq] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
-  }
+  for (int k = 1; k < 4; ++k) t.add(ss[k], sv[k], lane);
+  t.template write<BF>(A, q, head, r, lane);
 }
 
 }  // namespace ifq

@@ -150,9 +150,12 @@ int plan_attention(const ifq_kv4_attention_desc* d, const KvAttnArgs& a, AttnPla
   p->nt = rows > 8 && D < 256 ? 2 : 1;   // (two tiles of size 256 do not fit the registers)
   const int R = 8 * p->nt;
   const long long blocks = std::max<long long>(1, (rows + R - 1) / R);   // (the device checks max_q = 0 too)
-  p->direct = reach <= 64 * kKvGroup && blocks <= 65535 && d->seqs <= 65535;
+  const long long items = blocks * a.kv_heads * d->seqs;
+  // A block an item where no sequence is long: always up to 1024 tokens, and up to 2048 where the items occupy half the
+  // SMs (64 windows of 1028 tokens, two heads: 7.8 us, in ranges 16 to 18).
+  p->direct = (reach <= 1024 || (reach <= 2048 && items >= sm_count() / 2)) && blocks <= 65535 && d->seqs <= 65535;
   p->blocks = p->direct ? (int)blocks : sm_count() * kv_rows_per_sm(D, p->nt);
-  p->ws = p->direct ? 0 : round_up((size_t)p->blocks * (2 * R * (D * 4 + 8) + 16), 256);
+  p->ws = p->direct ? 0 : round_up((size_t)p->blocks * kKvRowsWarps * (2 * R * (D * 4 + 8) + 16), 256);
   return IFQ_OK;
 }
 
@@ -206,8 +209,8 @@ int run_rows(const KvAttnArgs& a, const AttnPlan& p, void* ws, cudaStream_t st) 
   r.direct = p.direct;
   if (!p.direct) {
     r.cut = (int4*)ws;
-    r.part_ml = (float2*)(r.cut + p.blocks);
-    r.part = (float*)(r.part_ml + (size_t)p.blocks * 2 * R);
+    r.part_ml = (float2*)(r.cut + p.blocks * kKvRowsWarps);
+    r.part = (float*)(r.part_ml + (size_t)p.blocks * kKvRowsWarps * 2 * R);
   }
   const dim3 grid = p.direct ? dim3(a.kv_heads, p.blocks, a.seqs) : dim3(p.blocks);
   const cudaError_t e = launch_k(kv4_rows_kernel<D, BF, NT>, grid, dim3(KvRowsShape<D>::threads), smem, st, r);
