@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(32 * kFp8QuantWarps) fp8_quantize_kernel(const
 // Where there are many rows of x, A is x and B is w; with few (SWAP) A is w, so that the weights, which
 // are then what is read, fill the lanes, and the rows of x are as few columns as 16.
 //
-// A block of 128 along k is one pipeline stage and one tensor-memory accumulator (two take turns): its
+// A block of 128 along k is one pipeline stage and one tensor-memory accumulator (two or four take turns): its
 // sum has scales of its own, so it leaves tensor memory for registers, where the tile's sum is kept:
 //   acc += (x_scale w_scale) * block      (one fma an element; the factor is a lane's own, or with SWAP
 //                                          a column's).
@@ -105,10 +105,12 @@ struct Fp8Shape {
   static constexpr bool split = BN < 256;
   // a receive slot a rank: the owner's columns, 129 floats each
   static constexpr int recv = split ? (BN + 8) * 129 * 4 : 0;
-  static constexpr int fit = (232448 - 1024 - 1024 - recv) / stage;
+  static constexpr int fac = SWAP ? kFp8Promote * 2 * (BN / 2) * 4 : 0;   // the columns' factors, two a warp
+  static constexpr int fit = (232448 - 1024 - 1024 - recv - fac) / stage;
   static constexpr int stages = fit < 8 ? fit : 8;
-  static constexpr int bytes = 1024 + stages * stage + recv + 256;
-  static constexpr int cols = 2 * BN < 32 ? 32 : 2 * BN;   // tensor memory
+  static constexpr int bytes = 1024 + stages * stage + recv + fac + 256;
+  static constexpr int acc = BN <= 64 ? 4 : 2;              // accumulators
+  static constexpr int cols = acc * BN;                     // tensor memory
   static_assert(bytes <= 232448 && stages >= 3, "shared memory budget");
 };
 
@@ -164,18 +166,19 @@ template <int BN, bool SWAP>
 __global__ void __launch_bounds__(kFp8Threads, 1)
     fp8_matmul_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const __grid_constant__ Fp8Args a) {
   using C = Fp8Shape<BN, SWAP>;
-  constexpr int ST = C::stages, HC = BN / 2;   // columns a thread
+  constexpr int ST = C::stages, NA = C::acc, HC = BN / 2;   // columns a thread
   constexpr int LD = HC < 32 ? HC : HC > 64 ? 16 : 32;       // columns a load (few registers are left beside 128 sums)
   extern __shared__ uint8_t raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   const uint32_t base = smem_u32(smem);
   float* recv = (float*)(smem + ST * C::stage);
-  const uint32_t bars = base + ST * C::stage + C::recv;
+  float* fac = (float*)(smem + ST * C::stage + C::recv);
+  const uint32_t bars = base + ST * C::stage + C::recv + C::fac;
   auto full = [&](int s) { return bars + 8 * s; };
   auto empty = [&](int s) { return bars + 8 * (ST + s); };
   auto dfull = [&](int b) { return bars + 8 * (2 * ST + b); };
-  auto dempty = [&](int b) { return bars + 8 * (2 * ST + 2 + b); };
-  uint32_t* tptr = (uint32_t*)(smem + ST * C::stage + C::recv + 8 * (2 * ST + 4));
+  auto dempty = [&](int b) { return bars + 8 * (2 * ST + NA + b); };
+  uint32_t* tptr = (uint32_t*)(smem + ST * C::stage + C::recv + C::fac + 8 * (2 * ST + 2 * NA));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int ks = a.ks, rank = ks > 1 ? (int)cluster_ctarank() : 0;
   if (threadIdx.x == 0) {
@@ -183,7 +186,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
       mbar_init(full(i), 1);
       mbar_init(empty(i), 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < NA; ++b) {
       mbar_init(dfull(b), 1);
       mbar_init(dempty(b), kFp8Promote);
     }
@@ -237,9 +240,9 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
     bool ok = true;
     for (int t = first; t < a.tiles && ok; t += step)
       for (int k = k0; k < k1; ++k, ++it) {
-        const int s = it % ST, b = it & 1;
+        const int s = it % ST, b = it % NA;
         if (!__all_sync(0xffffffffu, mbar_wait(full(s), (it / ST) & 1)) ||
-            (it >= 2 && !__all_sync(0xffffffffu, mbar_wait(dempty(b), (it / 2 - 1) & 1)))) { ok = false; break; }
+            (it >= NA && !__all_sync(0xffffffffu, mbar_wait(dempty(b), (it / NA - 1) & 1)))) { ok = false; break; }
         tc_fence_after();
         if (elect_one()) {
           const uint64_t da = sdesc_sw128(base + s * C::stage), db = sdesc_sw128(base + s * C::stage + 16384);
@@ -264,18 +267,28 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
       for (int i = 0; i < HC / 2; ++i) acc[i] = 0;
       // the factors of block k: a thread's own row of x and its columns' 128 rows of w; with SWAP its row of w, and
       // lane c of a warp has column c0 + c's (and c0 + 32 + c's) of x
-      const int wb = SWAP ? ia : (ib * BN + c0) / 128;
-      const int xr = SWAP ? ib * BN + c0 + lane : ia * 128 + row;
-      const bool have = xr < a.m && (!SWAP || lane < HC) && (SWAP || wb * 128 < a.n);
+      // (past the operands' ends the last row's, for results that are not stored: no load waits for a condition)
+      const int wb = min(SWAP ? ia : (ib * BN + c0) / 128, (a.n - 1) / 128);
+      const int xr = min(SWAP ? ib * BN + c0 + lane : ia * 128 + row, a.m - 1);
       const float* xp = a.xs + xr;
       const float* wp = a.ws + (long long)wb * a.kb;
-      float fn = have ? xp[(long long)k0 * a.m] * wp[k0] : 0.0f;
+      // (the next block's, loaded a block ahead and multiplied only when that block is there: a product that moves up to
+      // the loads waits for them)
+      float xn = xp[(long long)k0 * a.m], wn = wp[k0];
       for (int k = k0; k < k1; ++k, ++it) {
-        const float f = fn;
-        if (k + 1 < k1 && have) fn = xp[(long long)(k + 1) * a.m] * wp[k + 1];
-        const int b = it & 1;
-        if (!__all_sync(0xffffffffu, mbar_wait(dfull(b), (it / 2) & 1))) { ok = false; break; }
+        const int b = it % NA;
+        if (!__all_sync(0xffffffffu, mbar_wait(dfull(b), (it / NA) & 1))) { ok = false; break; }
         tc_fence_after();
+        asm volatile("" : "+f"(xn), "+f"(wn));
+        const float f = xn * wn;
+        const int kn = min(k + 1, k1 - 1);
+        xn = xp[(long long)kn * a.m];
+        wn = wp[kn];
+        float* fw = fac + (warp * 2 + (it & 1)) * HC;
+        if constexpr (SWAP) {
+          if (lane < HC) fw[lane] = f;
+          __syncwarp();
+        }
 #pragma unroll
         for (int c = 0; c < HC; c += LD) {
           uint32_t v[LD];
@@ -286,11 +299,10 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
             if (lane == 0) mbar_arrive(dempty(b));
           }
 #pragma unroll
-          for (int i = 0; i < LD; i += 2) {
-            if constexpr (SWAP)
-              fma2(acc[(c + i) / 2], v[i], v[i + 1], __shfl_sync(0xffffffffu, f, i), __shfl_sync(0xffffffffu, f, i + 1));
-            else
-              fma2(acc[(c + i) / 2], v[i], v[i + 1], f, f);
+          for (int i = 0; i < LD; i += 4) {
+            const float4 g = SWAP ? *(const float4*)(fw + c + i) : make_float4(f, f, f, f);
+            fma2(acc[(c + i) / 2], v[i], v[i + 1], g.x, g.y);
+            fma2(acc[(c + i) / 2 + 1], v[i + 2], v[i + 3], g.z, g.w);
           }
         }
       }
