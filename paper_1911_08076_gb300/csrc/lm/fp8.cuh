@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(32 * kFp8QuantWarps) fp8_quantize_kernel(const
 //   acc += (x_scale w_scale) * block      (one fma an element; the factor is a lane's own, or with SWAP
 //                                          a column's).
 // Warps: eight that promote and store (32 lanes x half the columns each), one that loads (TMA, 128-byte
-// swizzle), one that issues MMAs.
+// swizzle), two that issue MMAs, every other block each (one alone took 650 cycles a block, whatever BN).
 //
 // A tile's k may be split over a cluster of ks blocks: each sends its partial columns to the block that
 // owns them through distributed shared memory, which adds them in the order of the ranks.
@@ -97,7 +97,7 @@ struct Fp8Args {
 };
 
 constexpr int kFp8Promote = 8;
-constexpr int kFp8Threads = 32 * (kFp8Promote + 2);
+constexpr int kFp8Threads = 32 * (kFp8Promote + 3);
 
 template <int BN, bool SWAP>
 struct Fp8Shape {
@@ -234,12 +234,14 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
     }
     if (!ok)   // what was loaded has landed before the block may exit
       for (int i = it - ST < 0 ? 0 : it - ST; i < it; ++i) mbar_wait(full(i % ST), (i / ST) & 1);
-  } else if (warp == kFp8Promote + 1) {
+  } else if (warp > kFp8Promote) {
+    const int parity = warp - kFp8Promote - 1;
     constexpr uint32_t idesc = idesc_e4m3_f32(128, BN);
     int it = 0;
     bool ok = true;
     for (int t = first; t < a.tiles && ok; t += step)
       for (int k = k0; k < k1; ++k, ++it) {
+        if ((it & 1) != parity) continue;
         const int s = it % ST, b = it % NA;
         if (!__all_sync(0xffffffffu, mbar_wait(full(s), (it / ST) & 1)) ||
             (it >= NA && !__all_sync(0xffffffffu, mbar_wait(dempty(b), (it / NA - 1) & 1)))) { ok = false; break; }
@@ -249,7 +251,6 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
 #pragma unroll
           for (int j = 0; j < kFp8Block / 32; ++j)   // 32 bytes along k: two 16-byte units of the descriptors' address
             mma_e4m3(tmem + b * BN, da + 2 * j, db + 2 * j, idesc, j > 0);
-          mma_commit(empty(s));
           mma_commit(dfull(b));
         }
         __syncwarp();
@@ -279,6 +280,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
         const int b = it % NA;
         if (!__all_sync(0xffffffffu, mbar_wait(dfull(b), (it / NA) & 1))) { ok = false; break; }
         tc_fence_after();
+        if (threadIdx.x == 0) mbar_arrive(empty(it % ST));   // (the block's operands have been read)
         asm volatile("" : "+f"(xn), "+f"(wn));
         const float f = xn * wn;
         const int kn = min(k + 1, k1 - 1);
