@@ -93,7 +93,7 @@ struct Fp8Args {
   void* out;
   long long out_stride;
   int m, n, kb, out_type, vec;   // vec: 16-byte stores are aligned
-  int tiles, tiles_a, ks;        // tiles of A
+  int tiles, tiles_a, tiles_b, ks;   // tiles in all, of A and of B; blocks a tile's k is split over
 };
 
 constexpr int kFp8Promote = 8;
@@ -206,11 +206,13 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
   grid_dep_wait();
   grid_dep_launch();
 
-  const int k0 = (int)((long long)rank * a.kb / ks), k1 = (int)((long long)(rank + 1) * a.kb / ks);
-  const int first = blockIdx.x / ks, step = gridDim.x / ks;
+  // (32-bit divisions: 64-bit ones took 1400 cycles before the first load)
+  const uint32_t uks = ks;
+  const int k0 = (uint32_t)(rank * a.kb) / uks, k1 = (uint32_t)((rank + 1) * a.kb) / uks;
+  const int first = blockIdx.x / uks, step = gridDim.x / uks;
   // tiles in groups of 16 tiles of A, within a group along A first
-  auto tile = [&](int t, int& ia, int& ib) {
-    const int tb_n = a.tiles / a.tiles_a, g = t / (16 * tb_n), in = t - g * 16 * tb_n, wide = min(16, a.tiles_a - 16 * g);
+  auto tile = [&](uint32_t t, int& ia, int& ib) {
+    const uint32_t g = t / (16u * a.tiles_b), in = t - g * 16u * a.tiles_b, wide = min(16u, a.tiles_a - 16u * g);
     ib = in / wide;
     ia = 16 * g + in - ib * wide;
   };
@@ -310,15 +312,19 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
       }
       if (!ok) break;
       if (C::split && ks > 1) {
+        const int per = (BN + ks - 1) / uks;
+        int own = ((c0 + 1) * uks - 1) / BN, end = (own + 1) * BN / uks;   // owner of column c: own BN / ks <= c < end
+        auto slot = [&](int lo) { return mapa_shared(smem_u32(recv + (rank * per - lo) * 129 + row), own); };
+        uint32_t to = slot(own * BN / uks);
 #pragma unroll
-        for (int i = 0; i < HC / 2; ++i) {
-          const float2 v = halves2(acc[i]);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int c = c0 + 2 * i + e, own = ((c + 1) * ks - 1) / BN, lo = own * BN / ks, per = (BN + ks - 1) / ks;
-            const uint32_t at = mapa_shared(smem_u32(recv + (rank * per + c - lo) * 129 + row), own);
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(e ? v.y : v.x) : "memory");
+        for (int i = 0; i < HC; ++i) {
+          const int c = c0 + i;
+          if (c == end) {
+            to = (++own, slot(end));
+            end = (own + 1) * BN / uks;
           }
+          const float2 v = halves2(acc[i / 2]);
+          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + c * 129 * 4), "f"(i & 1 ? v.y : v.x) : "memory");
         }
         break;
       }
@@ -369,14 +375,28 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
     if (warp < kFp8Promote) {
       int ia, ib;
       tile(first, ia, ib);
-      const int lo = rank * BN / ks, hi = (rank + 1) * BN / ks, wide = hi - lo, per = (BN + ks - 1) / ks;
-      for (int i = threadIdx.x; i < 128 * wide; i += 32 * kFp8Promote) {
-        // out rows are contiguous along w's rows: those are the lanes (SWAP) or the columns
-        const int r = SWAP ? i % 128 : i / wide, c = SWAP ? i / 128 : i - r * wide;
-        float v = 0.0f;
-        for (int p = 0; p < ks; ++p) v += recv[(p * per + c) * 129 + r];
-        const int m = SWAP ? ib * BN + lo + c : ia * 128 + r, n = SWAP ? ia * 128 + r : ib * BN + lo + c;
-        if (m < a.m && n < a.n) fp8_store(a, (long long)m * a.out_stride + n, v);
+      const int lo = rank * BN / uks, hi = (rank + 1) * BN / uks, wide = hi - lo, per = (BN + ks - 1) / uks;
+      // Out rows are contiguous along w's rows: those are the lanes (SWAP) or the columns.  Eight outputs a thread at a
+      // time, so that their loads are under way together.
+      const int total = 128 * wide;
+      for (int i0 = threadIdx.x; i0 < total; i0 += 8 * 32 * kFp8Promote) {
+        float v[8];
+        int r[8], c[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int i = min(i0 + j * 32 * kFp8Promote, total - 1);
+          r[j] = SWAP ? i % 128 : i / (uint32_t)wide;
+          c[j] = SWAP ? i / 128 : i - r[j] * wide;
+          v[j] = 0.0f;
+        }
+        for (int p = 0; p < ks; ++p)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] += recv[(p * per + c[j]) * 129 + r[j]];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int m = SWAP ? ib * BN + lo + c[j] : ia * 128 + r[j], n = SWAP ? ia * 128 + r[j] : ib * BN + lo + c[j];
+          if (i0 + j * 32 * kFp8Promote < total && m < a.m && n < a.n) fp8_store(a, (long long)m * a.out_stride + n, v[j]);
+        }
       }
     }
   }

@@ -294,7 +294,8 @@ int run_fp8(const ifq_fp8_desc* d, const Fp8Operands& o) {
   a.out_type = d->out_dtype;
   a.vec = a.out_stride * (d->out_dtype == IFQ_F32 ? 4 : 2) % 16 == 0;
   a.tiles_a = ceil_div(SWAP ? d->n : d->m, 128);
-  const long long tiles = (long long)a.tiles_a * ceil_div(SWAP ? d->m : d->n, BN);
+  a.tiles_b = ceil_div(SWAP ? d->m : d->n, BN);
+  const long long tiles = (long long)a.tiles_a * a.tiles_b;
   if (tiles > INT_MAX / kFp8MaxSplit) return IFQ_ERANGE;
   a.tiles = (int)tiles;
   // the split of k with the fewest blocks of k in a row, each launch or cluster also costing as much as a few blocks
