@@ -651,7 +651,8 @@ int ifq_kv4_attention_workspace_bytes(const ifq_kv4_attention_desc* d, size_t* b
  * with K and V the values the cache holds.  Codes enter the products as exact
  * numbers; scales, minima, sums and the softmax are in IEEE single, the weights
  * of V in half.  Where a key head has more than 32 rows
- * (max_q * q_heads / kv_heads), the values of V are rounded to half as well.
+ * (max_q * q_heads / kv_heads) and dtype is bfloat16, the values of V are
+ * rounded to half as well.
  * out (device): [q_tokens] rows of [q_heads][head_dim], dtype.  lse (device,
  * may be NULL): float [q_tokens][q_heads], the log of the softmax's sum.  A
  * query that sees nothing gives zeros and -infinity.

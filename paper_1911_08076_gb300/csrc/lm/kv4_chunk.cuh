@@ -11,9 +11,12 @@
 //   t = s (q . c) + (m sum(q) - reference),   two packed fma a pair of keys (scale, log2 e and powers of two in s).
 // q itself is multiplied by 16 to keep small elements out of the half's subnormals; a row with an element over 2^11 is
 // brought down by a power of two of its own, which its scores are then multiplied with (a branch no usual row takes).
-// Values: v = half((s' c' + m') / 2), one fma of halves: as fine as the minimum that the cache holds (a half), and
-// within the half's range where s' c' + m' would leave it.  Weights p are halves of 2^(t - m) with the reference m of a
-// row raised only when a sum of 8 of them passes 2^15 (no half overflows before), in whole powers of two; the
+// Values: where rows are bfloat16, v = half((s' c' + m') / 2), one fma of halves: eight times finer than the result, as
+// fine as the minimum that the cache holds (a half), and within the half's range where s' c' + m' would leave it.  Where
+// rows are half the product takes c' - 8, exact, and the scale goes into the weight's exponent, w = 2^(t - m + log2 s');
+// then sum p = sum w / s', and the values of code 8, m'' = m' + 8 s', are added in fp32, sum w m'' / s'.  (The rounding of
+// v would be as large as that of the result.)  Weights are halves of 2^(t - m) with the reference m of a row raised only
+// when a sum of 8 of them, or for exact values one, passes 2^15 (no half overflows before), in whole powers of two; the
 // denominator is the sum of the unrounded p.
 // A value that is not a number must reach only the rows that see it: its operand is 0 and its key's minimum NaN.
 //
@@ -44,7 +47,7 @@ struct KvChunkShape {
   static constexpr int NB = D == 256 ? 1 : 2;               // key and value buffers
   static constexpr int threads = 32 * (4 * NG + 5);
   static constexpr int q_bytes = RT * 128 * D * 2, kv_bytes = 128 * D * 2;
-  static constexpr int par_bytes = kChunkPar * kChunkKeys * 8;
+  static constexpr int par_bytes = kChunkPar * kChunkKeys * 20;
   static constexpr int bytes = 1024 + q_bytes + 2 * NB * kv_bytes + par_bytes + 512;
   static_assert(RT == 1 || NG == 2, "a group a row tile");
   static_assert(bytes <= 232448, "shared memory budget");
@@ -142,11 +145,14 @@ __device__ __forceinline__ void hold(uint32_t (&v)[N]) {
 template <int D, bool BF, int RT>
 __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_kernel(const __grid_constant__ KvChunkArgs A) {
   using C = KvChunkShape<D, RT>;
+  constexpr bool EX = !BF;   // exact values
   constexpr int NG = C::NG, NB = C::NB, DB = kv4_block(D), NBLK = D / DB, WPB = DB / 32, GB = kv4_group_bytes(D);
   extern __shared__ uint8_t raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   uint8_t *sQ = smem, *sK = sQ + C::q_bytes, *sV = sK + NB * C::kv_bytes;
-  float4* sPar = (float4*)(sV + NB * C::kv_bytes);          // [kChunkPar][64 pairs of keys]: s, s, m, m
+  float4* sPar = (float4*)(sV + NB * C::kv_bytes);          // [kChunkPar][64 pairs of keys]: s, s, m, m of the keys
+  float4* sVal = sPar + kChunkPar * (kChunkKeys / 2);       // of values in half: 1/s', 1/s', m''/s', m''/s'
+  float2* sLog = (float2*)(sVal + kChunkPar * (kChunkKeys / 2));   // and log2 s', twice
   const uint32_t bars = smem_u32(sPar) + C::par_bytes;
   auto kfull = [&](int b) { return bars + 8 * b; };          // expanded keys
   auto kempty = [&](int b) { return bars + 16 + 8 * b; };
@@ -244,7 +250,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
     // From here a thread has four rows, q + 8 y of its warp's 32 (q = lane / 4), and of every 8 keys two: a key's
     // parameters then serve four rows a load.
     const int quad = lane >> 2, pos = lane & 3;
-    uint64_t fb2[4], l2[4];
+    uint64_t fb2[4], l2[4], z2[4];
     float m[4], up[4];
     int py[4], pf[4];
     uint32_t fresh = 0;
@@ -254,6 +260,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       up[y] = __shfl_sync(0xffffffffu, fa, quad + 8 * y);
       fb2[y] = pair2(v, v);
       l2[y] = 0;
+      z2[y] = 0;
       m[y] = 0.0f;
       py[y] = __shfl_sync(0xffffffffu, p, quad + 8 * y);
       pf[y] = __shfl_sync(0xffffffffu, p_first, quad + 8 * y);
@@ -278,7 +285,8 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       ok = __all_sync(0xffffffffu, mbar_wait(pfull(pb), (i / kChunkPar) & 1) && mbar_wait(sfull(b), (x >> 1) & 1));
       if (!ok) break;
       tc_fence_after();
-      const float4* par = sPar + pb * (kChunkKeys / 2) + pos;
+      const float4 *par = sPar + pb * (kChunkKeys / 2) + pos, *val = sVal + pb * (kChunkKeys / 2) + pos;
+      const float2* slog = sLog + pb * (kChunkKeys / 2) + pos;
       const bool full = j0 + kChunkKeys - 1 <= p_lo && (a.window == 0 || j0 > p_hi - a.window || j0 + kChunkKeys <= a.sinks);
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
@@ -296,11 +304,12 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
         for (int k = 0; k < 4; ++k) {
           const float4 kp = par[16 * c + 4 * k];
           const uint64_t s2 = pair2(kp.x, kp.y), n2 = pair2(kp.z, kp.w);
+          const float2 lg = EX ? slog[16 * c + 4 * k] : make_float2(0.0f, 0.0f);
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             const uint32_t* w = &v[y >> 1][4 * k + 2 * (y & 1)];
-            const float2 z = halves2(fma2v(pair2(__uint_as_float(w[0]), __uint_as_float(w[1])), s2,
-                                           fma2v(n2, fb2[y], pair2(-m[y], -m[y]))));
+            const uint64_t ref = pair2(EX ? lg.x - m[y] : -m[y], EX ? lg.y - m[y] : -m[y]);
+            const float2 z = halves2(fma2v(pair2(__uint_as_float(w[0]), __uint_as_float(w[1])), s2, fma2v(n2, fb2[y], ref)));
             t[y][2 * k] = z.x;
             t[y][2 * k + 1] = z.y;
           }
@@ -332,8 +341,15 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
             most = fmaxf(most, u.x + u.y);
           }
         };
-        weights();
-        if (__any_sync(0xffffffffu, most > 32768.0f || fresh)) {
+        if constexpr (EX) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) most = fmaxf(most, fmaxf(t[y][k], t[y][k + 1]));
+        } else {
+          weights();
+        }
+        if (__any_sync(0xffffffffu, most > (EX ? 15.0f : 32768.0f) || fresh)) {
           float f[4];
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
@@ -348,10 +364,11 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
             if (begin) fresh &= ~(1u << y);
             m[y] += rise;
             l2[y] = mul2(l2[y], pair2(f[y], f[y]));
+            if constexpr (EX) z2[y] = mul2(z2[y], pair2(f[y], f[y]));
 #pragma unroll
             for (int k = 0; k < 8; ++k) t[y][k] -= rise;
           }
-          weights();
+          if constexpr (!EX) weights();
           const float fl = by_lane(f);
           if (__any_sync(0xffffffffu, fl != 1.0f)) {
             // what this tile's columns and the sum already hold
@@ -384,8 +401,24 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
             }
           }
         }
+        if constexpr (EX) {
 #pragma unroll
-        for (int y = 0; y < 4; ++y) l2[y] = add2(l2[y], part[y]);
+          for (int k = 0; k < 4; ++k) {
+            const float4 q4 = val[16 * c + 4 * k];
+            const uint64_t i2 = pair2(q4.x, q4.y), v2 = pair2(q4.z, q4.w);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const float u0 = exp2_fast(t[y][2 * k]), u1 = exp2_fast(t[y][2 * k + 1]);
+              const uint32_t h2 = w[y >> 1][2 * k + (y & 1)] = pack16<false>(u0, u1);
+              const float2 r = unpack16<false>(h2);   // as the product has them: what is lost goes with v, not with c' - 8
+              l2[y] = fma2v(pair2(u0, u1), i2, l2[y]);
+              z2[y] = fma2v(pair2(r.x, r.y), v2, z2[y]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int y = 0; y < 4; ++y) l2[y] = add2(l2[y], part[y]);
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) tmem_st_frag(tS + ((uint32_t)(16 * h) << 16) + 16 * c, w[h]);
       }
@@ -406,7 +439,17 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       sums[y] += __shfl_xor_sync(0xffffffffu, sums[y], 2);
       if (fresh >> y & 1u) m[y] = kNoMax;
     }
-    float sum = by_lane(sums), top = by_lane(m);   // a thread a row again
+    float sum = by_lane(sums), top = by_lane(m), zl = 0.0f;   // a thread a row again
+    if constexpr (EX) {
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const float2 u = halves2(z2[y]);
+        sums[y] = u.x + u.y;
+        sums[y] += __shfl_xor_sync(0xffffffffu, sums[y], 1);
+        sums[y] += __shfl_xor_sync(0xffffffffu, sums[y], 2);
+      }
+      zl = by_lane(sums);
+    }
     if (!have) top = kNoMax;
     float other_top = kNoMax, other_f = 0.0f, my_f = 1.0f;
     float* xo = (float*)sK;   // [128][D + 4], and the second group's references and sums
@@ -423,7 +466,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
 #pragma unroll
           for (int k = 0; k < 16; k += 4)
             *(float4*)(xo + row * (D + 4) + d + k) =
-                mine > 0 ? make_float4(__uint_as_float(w[k]), __uint_as_float(w[k + 1]), __uint_as_float(w[k + 2]), __uint_as_float(w[k + 3]))
+                mine > 0 ? make_float4(__uint_as_float(w[k]) + zl, __uint_as_float(w[k + 1]) + zl, __uint_as_float(w[k + 2]) + zl, __uint_as_float(w[k + 3]) + zl)
                          : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
       }
@@ -441,14 +484,15 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
     if (work && (RT == 2 || grp == 0)) {
       const bool parts = A.splits > 1;
       const long long at = ((((long long)s * a.kv_heads + head) * A.blocks + r0 / (128 * RT)) * A.splits + sp) * (128 * RT) + rt * 128 + row;
-      const float inv = parts ? 2.0f : sum == 0.0f ? 0.0f : 2.0f / sum;
+      constexpr float kUnit = EX ? 1.0f : 2.0f;
+      const float inv = parts ? kUnit : sum == 0.0f ? 0.0f : kUnit / sum;
 #pragma unroll 1
       for (int d = 0; d < D; d += 16) {
         uint32_t w[16];
         if (mine > 0) tmem_ld<16>(tO + d, w);
         float o[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) o[k] = mine > 0 ? __uint_as_float(w[k]) : 0.0f;
+        for (int k = 0; k < 16; ++k) o[k] = mine > 0 ? __uint_as_float(w[k]) + zl : 0.0f;
         if (NG == 2 && RT == 1) {
 #pragma unroll
           for (int k = 0; k < 16; k += 4) {
@@ -583,6 +627,16 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
         float* dst = (float*)(sPar + pb * (kChunkKeys / 2) + tid / 2) + (tid & 1);
         dst[0] = f.x * (a.scale * 1.44269504f * 1048576.0f);   // codes are in units of 2^-24, q of 2^-4
         dst[2] = f.y;
+        if constexpr (EX) {
+          // (a scale of 0 counts as the smallest half: its codes are 0, and the value of code 8 makes up for it)
+          const bool some = there && finite(vpar);
+          const float2 y = unpack16<false>(some ? vpar : 0u);
+          const float sc = fmaxf(y.x, 5.9604645e-8f), r = 1.0f / sc;
+          float* dv4 = (float*)(sVal + pb * (kChunkKeys / 2) + tid / 2) + (tid & 1);
+          dv4[0] = some ? r : 0.0f;
+          dv4[2] = some ? (y.y + 8.0f * sc) * r : 0.0f;
+          ((float*)(sLog + pb * (kChunkKeys / 2)))[tid] = some ? log2f(sc) : 0.0f;
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(pfull(pb));
       }
@@ -624,9 +678,10 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
             for (int t = 0; t < 4; ++t) {
               const uint32_t u = vw[blk * WPB * 4 + t * WPB + k] >> (n & 2 ? 8 : 0);
               const uint32_t g = (u & (n & 1 ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;   // 1024 + c, 1024 + 16 c
-              const __half2 code = n & 1 ? __hfma2(*(const __half2*)&g, __float2half2_rn(0.0625f), __float2half2_rn(-64.0f))
-                                         : __hadd2(*(const __half2*)&g, __float2half2_rn(-1024.0f));
-              const __half2 v = __hfma2(code, vs[t], vm[t]);
+              const float off = EX ? 8.0f : 0.0f;
+              const __half2 code = n & 1 ? __hfma2(*(const __half2*)&g, __float2half2_rn(0.0625f), __float2half2_rn(-64.0f - off))
+                                         : __hadd2(*(const __half2*)&g, __float2half2_rn(-1024.0f - off));
+              const __half2 v = EX ? code : __hfma2(code, vs[t], vm[t]);
               y[t] = *(const uint32_t*)&v;
             }
             const int d = d0 + n;

@@ -55,7 +55,7 @@ def test_prompt_and_steps(hq, hk, d, dtype, window, sinks):
         assert np.array_equal(num(block.q), q)
         out, _, tol, _ = R.attention(q.astype(np.float64).reshape(len(pos), hq, d), want, page, step.table.cpu().numpy(),
                                      step.lens.cpu().numpy(), step.starts.cpu().numpy(), hk, d ** -0.5, window, sinks, u,
-                                     max(counts) * (hq // hk) > 32)
+                                     dtype == torch.bfloat16 and max(counts) * (hq // hk) > 32)
         assert (np.abs(num(block.context).reshape(out.shape) - out) <= tol).all()
         product(block.context, block.w_out, block.s_out, y)
 

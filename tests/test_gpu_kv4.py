@@ -232,7 +232,7 @@ def _run(lens, starts, table, cache, q, hq, hk, D, page, dtype, window=0, sinks=
         assert torch.equal(first[1].view(torch.int32), ls.view(torch.int32))
     assert (out[:, hq * D:] == 5).all()
     q64 = qd[:, :hq * D].double().cpu().numpy().reshape(T, hq, D)
-    many = d.max_q * (hq // hk) > 32     # the library then rounds values to half
+    many = dtype == "bf16" and d.max_q * (hq // hk) > 32     # the library then rounds values to half
     return (out[:, :hq * D].double().cpu().numpy().reshape(T, hq, D), ls.double().cpu().numpy(), q64, scale, u, many)
 
 
