@@ -109,8 +109,19 @@ int check_attention(const ifq_kv4_attention_desc* d, KvAttnArgs* a) {
   return IFQ_OK;
 }
 
-// More rows of a key head than this take the kernel for many.
+// Rows of a key head from which the kernel for many may be taken.
 constexpr int kChunkRows = 32;
+
+// Whether it is.  The kernel for few reads the cache once for every 8 or 16 rows, the one for many once for 128 or 256,
+// but expands it to halves first and takes longer to begin.  In picoseconds a token and key head, measured with 5 to 40
+// queries on up to 4096 tokens (16 x 5 queries of 8 heads a key head, 40 rows: 53 against 66 us; 2 x 40 of 4, 160 rows:
+// 12.6 against 24; 16 x 12 of 8 with heads of 64, 96 rows: 30 against 18).
+bool take_chunk(int D, long long rows, int nt, long long tokens) {
+  const double pass = D == 64 ? 80 : 64, block = D == 64 ? 94 : D == 128 ? 160 : 460;
+  const double few = pass * ((rows + 8 * nt - 1) / (8 * nt));
+  const double many = rows <= 128 ? block : D < 256 ? 1.25 * block * ((rows + 255) / 256) : block * ((rows + 127) / 128);
+  return rows > kChunkRows && few * tokens > many * tokens + 24e6;
+}
 
 struct AttnPlan {
   int chunk;       // the kernel for many rows (kv4_chunk.cuh): row tiles of 128 a block; 0: that for few
@@ -137,7 +148,8 @@ int plan_attention(const ifq_kv4_attention_desc* d, const KvAttnArgs& a, AttnPla
   long long reach = (long long)d->max_pages * d->cache.page_size;   // tokens that a sequence's queries read at most
   if (d->max_len > 0) reach = std::min<long long>(reach, d->max_len);
   if (d->window > 0) reach = std::min<long long>(reach, (long long)d->window + d->sinks + d->max_q + 2 * kKvGroup);
-  if (rows > kChunkRows && d->seqs <= 65535) {
+  p->nt = rows > 8 && D < 256 ? 2 : 1;   // (two tiles of size 256 do not fit the registers)
+  if (d->seqs <= 65535 && take_chunk(D, rows, p->nt, reach * d->seqs * a.kv_heads)) {
     p->chunk = rows > 128 && D < 256 ? 2 : 1;
     const int R = 128 * p->chunk;
     p->blocks = (int)((rows + R - 1) / R);
@@ -147,7 +159,6 @@ int plan_attention(const ifq_kv4_attention_desc* d, const KvAttnArgs& a, AttnPla
     return IFQ_OK;
   }
   p->chunk = 0;
-  p->nt = rows > 8 && D < 256 ? 2 : 1;   // (two tiles of size 256 do not fit the registers)
   const int R = 8 * p->nt;
   const long long blocks = std::max<long long>(1, (rows + R - 1) / R);   // (the device checks max_q = 0 too)
   const long long items = blocks * a.kv_heads * d->seqs;

@@ -205,10 +205,14 @@ def _setup(rng, lens, nq, hq, hk, D, page, garbage=0xFF, spread=1.0, spare=2, fi
 
 
 def _run(lens, starts, table, cache, q, hq, hk, D, page, dtype, window=0, sinks=0, scale=None, max_q=None, max_len=0,
-         pad=0, use_starts=True, lse=True, cache_dev=None, pages=None, stream=None):
+         pad=0, use_starts=True, lse=True, cache_dev=None, pages=None, stream=None, wide=False):
+    """wide: bounds as for long sequences with many queries, which choose other kernels and launch shapes."""
     code, dt, u = TYPES[dtype]
     scale = D ** -0.5 if scale is None else scale
     T = q.shape[0]
+    if wide:
+        table = np.concatenate([table, np.full((len(table), 200000 // page), -3, np.int32)], 1)
+        max_q = max(300, int(np.diff(starts).max())) if max_q is None else max_q
     qd = torch.zeros(T, hq * D + pad, dtype=dt, device=DEV)
     qd[:, :hq * D] = _dev(q.reshape(T, -1), dt)
     out = torch.full((T, hq * D + pad), 5.0, dtype=dt, device=DEV)
@@ -276,28 +280,31 @@ CASES = [
 ]
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("case", CASES)
-def test_attention_equals_its_definition(case):
+def test_attention_equals_its_definition(case, wide):
     lens, nq, hq, hk, D, page, dtype, window, sinks = case
     rng = np.random.default_rng(sum(lens) + hq)
     lens, starts, table, cache, q = _setup(rng, lens, nq, hq, hk, D, page)
-    got = _run(lens, starts, table, cache, q, hq, hk, D, page, dtype, window, sinks, pad=8 if hq % 2 else 0)
+    got = _run(lens, starts, table, cache, q, hq, hk, D, page, dtype, window, sinks, pad=8 if hq % 2 else 0, wide=wide)
     assert _status() == ifq.IFQ_OK
     _check(got, lens, starts, table, cache, hk, page, window, sinks)
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("D,hq,hk,n", [(128, 8, 2, 1), (64, 4, 1, 3), (128, 4, 1, 80), (256, 2, 1, 40)])
-def test_attention_of_peaked_and_of_flat_scores(D, hq, hk, n):
+def test_attention_of_peaked_and_of_flat_scores(D, hq, hk, n, wide):
     """Scores that differ by hundreds (one token takes everything), and scores that are all the same."""
     rng = np.random.default_rng(5)
     lens, starts, table, cache, q = _setup(rng, [450], [n], hq, hk, D, 16, spread=3.0)
     for scale in (8.0, 0.0, -0.3):
-        got = _run(lens, starts, table, cache, q, hq, hk, D, 16, "bf16", scale=scale)
+        got = _run(lens, starts, table, cache, q, hq, hk, D, 16, "bf16", scale=scale, wide=wide)
         _check(got, lens, starts, table, cache, hk, 16)
 
 
-@pytest.mark.parametrize("n", [1, 90])
-def test_attention_of_values_of_very_different_sizes(n):
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("n,dtype", [(1, "f16"), (90, "f16"), (90, "bf16")])
+def test_attention_of_values_of_very_different_sizes(n, dtype, wide):
     """Value scales over 20 binary orders, ascending and descending along the sequence: nothing that matters is lost
     in the weights' half precision."""
     rng = np.random.default_rng(6)
@@ -309,12 +316,13 @@ def test_attention_of_values_of_very_different_sizes(n):
             sc = np.float16(2.0 ** (-14 + 20 * ((L - 1 - j) if down else j) / (L - 1)))
             g = cache[pg, 0, off // 16]
             g[16 * D + 64 + 4 * (off % 16):16 * D + 68 + 4 * (off % 16)] = np.array([sc, -3 * sc], np.float16).view(np.uint8)
-        got = _run(lens, starts, table, cache, q, hq, hk, D, page, "f16")
+        got = _run(lens, starts, table, cache, q, hq, hk, D, page, dtype, wide=wide)
         _check(got, lens, starts, table, cache, hk, page)
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("n", [1, 70])
-def test_attention_of_tiny_and_huge_queries(n):
+def test_attention_of_tiny_and_huge_queries(n, wide):
     rng = np.random.default_rng(7)
     D, page, hk, hq = 128, 16, 2, 4
     lens, starts, table, cache, q = _setup(rng, [200], [n], hq, hk, D, page)
@@ -322,19 +330,20 @@ def test_attention_of_tiny_and_huge_queries(n):
     q[:, 1] *= 3e4
     q[:, 2] = 0
     q[:, 3, ::2] *= 1e-6
-    got = _run(lens, starts, table, cache, q, hq, hk, D, page, "bf16")
+    got = _run(lens, starts, table, cache, q, hq, hk, D, page, "bf16", wide=wide)
     _check(got, lens, starts, table, cache, hk, page)
 
 
+@pytest.mark.parametrize("dtype,wide", [("bf16", False), ("bf16", True), ("f16", True)])
 @pytest.mark.parametrize("n", [1, 4, 100])
-def test_what_is_not_finite_stays_where_it_is_seen(n):
+def test_what_is_not_finite_stays_where_it_is_seen(n, dtype, wide):
     """A NaN query row makes its own output NaN alone; a NaN token those of the rows that see it."""
     rng = np.random.default_rng(8)
     D, page, hk, hq = 128, 16, 2, 4
     lens, starts, table, cache, q = _setup(rng, [210, 180], [n, n], hq, hk, D, page)
     q2 = q.copy()
     q2[0, 1, 3] = np.nan
-    got = _run(lens, starts, table, cache, q2, hq, hk, D, page, "bf16")
+    got = _run(lens, starts, table, cache, q2, hq, hk, D, page, dtype, wide=wide)
     assert np.isnan(got[0][0, 1]).all()
     keep = np.ones(got[0].shape[:2], bool)
     keep[0, 1] = False
@@ -344,7 +353,7 @@ def test_what_is_not_finite_stays_where_it_is_seen(n):
     pg, off = table[0, 209 // page], 209 % page
     c2[pg, 0, off // 16][16 * D + 4 * (off % 16):16 * D + 4 * (off % 16) + 4] = 0xFF
     c2[pg, 0, off // 16][16 * D + 64 + 4 * (off % 16):16 * D + 68 + 4 * (off % 16)] = 0xFF
-    got = _run(lens, starts, table, c2, q, hq, hk, D, page, "bf16")
+    got = _run(lens, starts, table, c2, q, hq, hk, D, page, dtype, wide=wide)
     assert np.isnan(got[0][n - 1, :2]).all()
     keep = np.ones(got[0].shape[:2], bool)
     keep[n - 1, :2] = False
@@ -367,21 +376,21 @@ def test_one_query_a_sequence_without_starts_and_without_lse():
     _check(got, lens, starts, table, cache, 4, 16, lse=False)
 
 
-@pytest.mark.parametrize("n", [1, 5, 65])
-def test_many_sequences(n):
+@pytest.mark.parametrize("n,wide", [(1, False), (5, False), (65, False), (5, True), (65, True)])
+def test_many_sequences(n, wide):
     """More sequences than a block has threads, lengths from none to a few pages."""
     rng = np.random.default_rng(11)
     lens = rng.integers(0, 40, 1030)
     nq = np.minimum(rng.integers(0, 2, 1030), 1) * n
     nq[:2] = n
     lens, starts, table, cache, q = _setup(rng, lens, nq, 2, 1, 64, 16)
-    got = _run(lens, starts, table, cache, q, 2, 1, 64, 16, "f16")
+    got = _run(lens, starts, table, cache, q, 2, 1, 64, 16, "f16", wide=wide)
     assert _status() == ifq.IFQ_OK
     _check(got, lens, starts, table, cache, 1, 16)
 
 
-@pytest.mark.parametrize("n", [1, 3, 72])
-def test_pages_past_four_gigabytes(n):
+@pytest.mark.parametrize("n,wide", [(1, False), (3, False), (72, False), (1, True), (72, True)])
+def test_pages_past_four_gigabytes(n, wide):
     rng = np.random.default_rng(12)
     D, page, hk, hq = 128, 64, 2, 4
     lens, starts, table, cache, q = _setup(rng, [300], [n], hq, hk, D, page, spare=0)
@@ -390,12 +399,12 @@ def test_pages_past_four_gigabytes(n):
     big = torch.empty((first + cache.shape[0], hk, page // 16, R.group_bytes(D)), dtype=torch.uint8, device=DEV)
     big[first:] = _dev(cache)
     got = _run(lens, starts, np.where(table >= 0, table + first, table).astype(np.int32), cache, q, hq, hk, D, page, "bf16",
-               cache_dev=big, pages=big.shape[0])
+               cache_dev=big, pages=big.shape[0], wide=wide)
     _check(got, lens, starts, table, cache, hk, page)
 
 
-@pytest.mark.parametrize("n", [1, 80])
-def test_bad_lengths_starts_and_pages_are_reported(n):
+@pytest.mark.parametrize("n,wide", [(1, False), (80, False), (1, True), (80, True)])
+def test_bad_lengths_starts_and_pages_are_reported(n, wide):
     rng = np.random.default_rng(13)
     D, page, hk, hq = 64, 16, 1, 2
     lens, starts, table, cache, q = _setup(rng, [120, 130, 90], [n] * 3, hq, hk, D, page)
@@ -404,20 +413,20 @@ def test_bad_lengths_starts_and_pages_are_reported(n):
     for what in ("long", "negative", "page", "low page"):
         l2, t2 = lens.copy(), table.copy()
         if what == "long":
-            l2[1] = table.shape[1] * page + 1
+            l2[1] = (table.shape[1] + 200000) * page + 1
         elif what == "negative":
             l2[1] = -1
         else:
             t2[1, 2] = cache.shape[0] if what == "page" else -1
-        got = _run(l2, starts, t2, cache, q, hq, hk, D, page, "f16")
+        got = _run(l2, starts, t2, cache, q, hq, hk, D, page, "f16", wide=wide)
         assert _status() == ifq.IFQ_ERANGE, what
         _check(got, lens, starts, table, cache, hk, page, rows=others)
         if what in ("long", "negative"):
             assert (got[0][n:2 * n] == 5).all()
     for st in ([0, n, n - 1, 3 * n], [0, n, 2 * n, 3 * n + 1]):
-        _run(lens, np.array(st, np.int32), table, cache, q, hq, hk, D, page, "f16", max_q=n)
+        _run(lens, np.array(st, np.int32), table, cache, q, hq, hk, D, page, "f16", max_q=n, wide=wide)
         assert _status() == ifq.IFQ_ERANGE
-    _run(lens, starts, table, cache, q, hq, hk, D, page, "f16", max_q=n - 1)
+    _run(lens, starts, table, cache, q, hq, hk, D, page, "f16", max_q=n - 1, wide=wide)
     assert _status() == ifq.IFQ_ERANGE
 
 
