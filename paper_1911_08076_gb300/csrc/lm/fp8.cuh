@@ -103,8 +103,8 @@ template <int BN, bool SWAP>
 struct Fp8Shape {
   static constexpr int stage = 16384 + BN * 128;
   static constexpr bool split = BN < 256;
-  // a receive slot a rank: the owner's columns, 129 floats each
-  static constexpr int recv = split ? (BN + 8) * 129 * 4 : 0;
+  // a receive slot a rank: the owner's columns, 129 floats each; or 32 x 32 results a warp on their way out
+  static constexpr int recv = split ? (BN + 8) * 129 * 4 : kFp8Promote * 32 * 33 * 4;
   static constexpr int fac = SWAP ? kFp8Promote * 2 * (BN / 2) * 4 : 0;   // the columns' factors, two a warp
   static constexpr int fit = (232448 - 1024 - 1024 - recv - fac) / stage;
   static constexpr int stages = fit < 8 ? fit : 8;
@@ -339,6 +339,26 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
             if (m + 1 < a.m) fp8_store(a, (long long)(m + 1) * a.out_stride + n, v.y);
           }
         }
+      } else if (!a.vec) {
+        // rows that start anywhere: 32 columns at a time through shared memory, so that a warp's stores are a row's
+        float* turn = recv + warp * 32 * 33;
+        const int m0 = ia * 128 + quad * 32;
+#pragma unroll
+        for (int i = 0; i < HC; i += 32) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            const float2 v = halves2(acc[(i + j) / 2]);
+            turn[lane * 33 + j] = v.x;
+            turn[lane * 33 + j + 1] = v.y;
+          }
+          __syncwarp();
+          const int n = ib * BN + c0 + i + lane;
+          const int rows = min(32, a.m - m0);
+          if (n < a.n)
+#pragma unroll 8
+            for (int r = 0; r < rows; ++r) fp8_store(a, (long long)(m0 + r) * a.out_stride + n, turn[r * 33 + lane]);
+          __syncwarp();
+        }
       } else {
         const int m = ia * 128 + row, n = ib * BN + c0;
         if (m < a.m) {
@@ -348,7 +368,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
             float2 v[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = halves2(acc[i / 2 + j]);
-            if (a.vec && n + i + 8 <= a.n) {
+            if (n + i + 8 <= a.n) {
               if (a.out_type == IFQ_F32) {
                 *(float4*)((float*)a.out + at) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
                 *(float4*)((float*)a.out + at + 4) = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);

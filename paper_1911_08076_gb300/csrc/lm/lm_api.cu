@@ -161,11 +161,17 @@ int plan_attention(const ifq_kv4_attention_desc* d, const KvAttnArgs& a, AttnPla
   p->chunk = 0;
   const int R = 8 * p->nt;
   const long long blocks = std::max<long long>(1, (rows + R - 1) / R);   // (the device checks max_q = 0 too)
-  const long long items = blocks * a.kv_heads * d->seqs;
-  // A block an item where no sequence is long: always up to 1024 tokens, and up to 2048 where the items occupy half the
-  // SMs (64 windows of 1028 tokens, two heads: 7.8 us, in ranges 16 to 18).
-  p->direct = (reach <= 1024 || (reach <= 2048 && items >= sm_count() / 2)) && blocks <= 65535 && d->seqs <= 65535;
-  p->blocks = p->direct ? (int)blocks : sm_count() * kv_rows_per_sm(D, p->nt);
+  // A block an item, or ranges: the longer of an item's units in seven warps and of what all items leave to an SM,
+  // against three quarters of all units evenly spread and a longer start and a second kernel.  (Microseconds as measured:
+  // 64 windows of 1028 tokens, two heads of 64: 7.8 against 16 to 18; 6 sequences of up to 1233, four heads of 64: in
+  // ranges 11.3.)
+  const int per_sm = kv_rows_per_sm(D, p->nt), unit = kKvGroup * (D == 64 ? 4 : 2), sms = sm_count();
+  const double items = (double)blocks * a.kv_heads * d->seqs, units = (double)((reach + unit - 1) / unit);
+  const double us = D == 64 ? 1.6 : D == 128 ? 1.45 : 2.2, lanes = (double)kKvRowsWarps * per_sm * sms;
+  const double alone = 4.5 + us * std::ceil(units / kKvRowsWarps) * std::max(1.0, items / (per_sm * sms));
+  const double spread = 9.5 + us * std::ceil(0.75 * items * units / lanes);
+  p->direct = alone < spread && blocks <= 65535 && d->seqs <= 65535;
+  p->blocks = p->direct ? (int)blocks : sms * per_sm;
   p->ws = p->direct ? 0 : round_up((size_t)p->blocks * kKvRowsWarps * (2 * R * (D * 4 + 8) + 16), 256);
   return IFQ_OK;
 }
