@@ -26,7 +26,8 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
 
 // Eight values (16 bytes) a lane, 16 lanes a block, kFp8Pass times two blocks in a row a warp, their loads all under way
 // before the first is used (k is a multiple of 16, so a lane's eight are all there or none).  blockIdx.x: eight rows,
-// blockIdx.y: blocks along k.  Bound by memory and by the eight divisions.  (A block a warp: 50 us for 4096 x 9216.)
+// blockIdx.y: blocks along k.  Bound by memory and by the eight divisions: 29 us, 3.9 TB/s, for
+// 4096 x 9216.  (A block a warp: 50.)
 constexpr int kFp8Pass = 4;
 
 template <bool BF>
@@ -88,6 +89,10 @@ __global__ void __launch_bounds__(32 * kFp8QuantWarps) fp8_quantize_kernel(const
 //
 // A tile's k may be split over a cluster of ks blocks: each sends its partial columns to the block that
 // owns them through distributed shared memory, which adds them in the order of the ranks.
+//
+// Bound, with many rows, by the operands' way from L2 to shared memory (48 KB a block of 128 with BN = 256, 62 bytes a
+// cycle and SM) beside the promotion: 4096 x 4096 x 9216 in 138 us, 2.2 PFLOP/s.  With few rows by the launch, the
+// cluster's join and a block's way through the pipeline (425 cycles): 1 x 4096 x 9216 in 10 us, 3.8 TB/s of weights.
 struct Fp8Args {
   const float *xs, *ws;
   void* out;

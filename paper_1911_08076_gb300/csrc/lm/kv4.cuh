@@ -113,7 +113,8 @@ struct KvAppendArgs {
 // Both kernels: eight dimensions (16 bytes) a lane, so D / 8 lanes a head and 256 / D heads a warp at once, kKvPass
 // times; a warp's heads are of one token and one kind (q, k or v).  blockIdx.y: the kind and its heads, blockIdx.x:
 // eight tokens.  The heads' loads are all under way before the first is used, and cos and sin are read once for them
-// (a head a warp, 8-byte loads: 104 us for 8191 tokens of 32 + 2 x 8 heads of 128, and 31 us reading them back).
+// (8191 tokens of 32 + 2 x 8 heads of 128: 57 us, 2.6 TB/s, with 60 % of the issue slots at work on the exact steps, and
+// 14 us reading them back; with a head a warp and 8-byte loads 104 and 31).
 constexpr int kAppendWarps = 8, kKvPass = 4;
 __host__ __device__ constexpr int kv4_warp_heads(int D) { return kKvPass * 256 / D; }
 

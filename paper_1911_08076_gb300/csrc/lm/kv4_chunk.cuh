@@ -3,7 +3,8 @@
 // A block takes 128 RT rows of a key head (query tokens x the heads that share it) and their keys in tiles of 128:
 //   S[row][key] = sum_d q[row][d] c[key][d]    (half x half, both operands in shared memory),
 //   O[row][d]  += sum_key p[row][key] v[key][d] (p from tensor memory, over S's columns; v in shared memory).
-// Bound by the tensor cores' half rate in the limit, by the softmax's instructions beside them as measured.
+// Bound by the tensor cores' half rate in the limit, by the softmax's instructions beside them as measured: 2 x 2048
+// queries of 32 heads of 128 on up to 8192 tokens in 278 us, 0.9 to 1.0 PFLOP/s, with 30 % of the tensor pipe.
 //
 // Keys: codes are expanded to halves as the subnormals c 2^-24 and 16 c 2^-24 (masks alone, as in kv4_rows.cuh; q's
 // elements stand in the order that leaves the codes of a word in, with the factors 1/16 in them).  Products with them
@@ -22,9 +23,9 @@
 //
 // Warps: one or two groups of four run the softmax, in matrix fragments: a thread has four rows and two of every eight
 // keys (with a thread a row, as many broadcast loads of the keys' parameters as scores took 2000 of 4500 cycles a tile);
-// four expand codes
-// (global memory to registers a tile ahead, then to swizzled shared memory); one issues MMAs.  Two S buffers: with
-// RT = 2 one a row tile; else the key tiles alternate, and with two groups each has an O of its own, joined at the end.
+// four expand codes (global memory to registers a tile ahead, then to swizzled shared memory); one issues MMAs.  Two S
+// buffers: with RT = 2 one a row tile; else the key tiles alternate, and with two groups each has an O of its own, joined
+// at the end.
 // A block's keys may be split over `splits` blocks, joined by kv4_chunk_join_kernel.
 #pragma once
 #include "kv4_rows.cuh"

@@ -19,8 +19,13 @@
 // lies within one item the warps take the units in turn and their sums are joined in shared memory; else the range is
 // cut again, a contiguous part a warp, so that no warp waits for another at an item's end (joining at each of them took
 // 8000 cycles beside 2700 a unit).  An item that several parts share leaves sums in the workspace, which
-// kv4_join_kernel adds (the block itself, where its warps have all of it).  One more warp fetches for all, a lane a group (page lookup and one bulk copy of the group's
-// contiguous bytes), three units ahead and across the ends of items.
+// kv4_join_kernel adds (the block itself, where its warps have all of it).  One more warp fetches for all, a lane a group
+// (page lookup and one bulk copy of the group's contiguous bytes), three units ahead and across the ends of items.
+//
+// Measured, the join with it: one sequence of 131072 tokens, 8 key heads of 128 and 4 rows each, 36.6 us (3.9 TB/s); 48
+// sequences of up to 8192 57.7 us (3.7 TB/s); 64 windows of 1028 tokens 7.8 us; 40 rows on 16 sequences of up to 4096,
+// three passes, 54.5 us.  Issue slots are 52 % busy, with 268 instructions a group: bound by the latency of 3.5
+// computing warps a scheduler.
 #pragma once
 #include "kv4_attention.cuh"
 
