@@ -90,24 +90,33 @@ __global__ void __launch_bounds__(32 * kFp8QuantWarps) fp8_quantize_kernel(const
 // A tile's k may be split over a cluster of ks blocks: each sends its partial columns to the block that
 // owns them through distributed shared memory, which adds them in the order of the ranks.
 //
-// Bound, with many rows, by the operands' way from L2 to shared memory (48 KB a block of 128 with BN = 256, 62 bytes a
-// cycle and SM) beside the promotion: 4096 x 4096 x 9216 in 138 us, 2.2 PFLOP/s.  With few rows by the launch, the
-// cluster's join and a block's way through the pipeline (425 cycles): 1 x 4096 x 9216 in 10 us, 3.8 TB/s of weights.
+// Where BN = 256 a block's 128 sums a thread and two loads from tensor memory under way take more registers than three
+// warps a scheduler may have, so the warpgroups divide them anew; and where the tiles of the last turn fill half of the
+// SMs or less, they are cut in two (1300 x 4096 x 4096 with both: 36.4 -> 31.5 us, 4096 x 4096 x 1024 32.2 -> 28.8).
+//
+// Measured with many rows: 4096 x 4096 x 9216 in 138 us, 2.2 PFLOP/s.  Without the promotion it takes 117, with a quarter of
+// the MMAs as long; tiles of 256 x 256 on two SMs, with two thirds of the bytes from L2, took 141.  With few rows the
+// launch, the cluster's join and a block's way through the pipeline (425 cycles) count: 1 x 4096 x 9216 in 10.8 us, 3.5 TB/s.
 struct Fp8Args {
   const float *xs, *ws;
   void* out;
   long long out_stride;
   int m, n, kb, out_type, vec;   // vec: 16-byte stores are aligned
-  int tiles, tiles_a, tiles_b, ks;   // tiles in all, of A and of B; blocks a tile's k is split over
+  int tiles, tiles_a, tiles_b, ks;   // items in all, tiles of A and of B; blocks a tile's k is split over
+  int whole;                         // items that are whole tiles; the rest are halves (BN = 256)
 };
 
 constexpr int kFp8Promote = 8;
-constexpr int kFp8Threads = 32 * (kFp8Promote + 3);
+// Registers a thread of the promoting warpgroups and of the other one where BN = 256: 2 x 128 x 216 + 128 x 72 =
+// 384 x 168, what the block is launched with.
+constexpr int kFp8MoreRegs = 216, kFp8FewRegs = 72;
 
 template <int BN, bool SWAP>
 struct Fp8Shape {
+  static constexpr bool wide = BN == 256;
   static constexpr int stage = 16384 + BN * 128;
   static constexpr bool split = BN < 256;
+  static constexpr int threads = 32 * (kFp8Promote + (wide ? 4 : 3));   // (the last warp makes a whole warpgroup)
   // a receive slot a rank: the owner's columns, 129 floats each; or 32 x 32 results a warp on their way out
   static constexpr int recv = split ? (BN + 8) * 129 * 4 : kFp8Promote * 32 * 33 * 4;
   static constexpr int fac = SWAP ? kFp8Promote * 2 * (BN / 2) * 4 : 0;   // the columns' factors, two a warp
@@ -147,6 +156,21 @@ __device__ __forceinline__ void tmem_ld(uint32_t t, uint32_t (&v)[X]) {
         : "r"(t)
         : "memory");
 }
+// Two steps, for work beside the load; between them nothing may read v, and what does after them is volatile.
+__device__ __forceinline__ void tmem_ld_begin(uint32_t t, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(t)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_end() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fma2_after(uint64_t& c, uint32_t a0, uint32_t a1, float f) {
+  asm volatile("{.reg .b64 a, f; mov.b64 a, {%1, %2}; mov.b64 f, {%3, %3}; fma.rn.f32x2 %0, a, f, %0;}"
+               : "+l"(c)
+               : "r"(a0), "r"(a1), "f"(f));
+}
 __device__ __forceinline__ void fma2(uint64_t& c, uint32_t a0, uint32_t a1, float f0, float f1) {
   uint64_t a, f;
   asm("mov.b64 %0, {%1, %2};" : "=l"(a) : "r"(a0), "r"(a1));
@@ -168,11 +192,12 @@ __device__ __forceinline__ uint32_t fp8_pack(int type, float a, float b) {
 }
 
 template <int BN, bool SWAP>
-__global__ void __launch_bounds__(kFp8Threads, 1)
+__global__ void __launch_bounds__((Fp8Shape<BN, SWAP>::threads), 1)
     fp8_matmul_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const __grid_constant__ Fp8Args a) {
   using C = Fp8Shape<BN, SWAP>;
   constexpr int ST = C::stages, NA = C::acc, HC = BN / 2;   // columns a thread
-  constexpr int LD = HC < 32 ? HC : HC > 64 ? 16 : 32;       // columns a load (few registers are left beside 128 sums)
+  constexpr bool WIDE = C::wide;
+  constexpr int LD = HC < 32 ? HC : 32;                      // columns a load with SWAP
   extern __shared__ uint8_t raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   const uint32_t base = smem_u32(smem);
@@ -215,38 +240,49 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
   const uint32_t uks = ks;
   const int k0 = (uint32_t)(rank * a.kb) / uks, k1 = (uint32_t)((rank + 1) * a.kb) / uks;
   const int first = blockIdx.x / uks, step = gridDim.x / uks;
-  // tiles in groups of 16 tiles of A, within a group along A first
-  auto tile = [&](uint32_t t, int& ia, int& ib) {
-    const uint32_t g = t / (16u * a.tiles_b), in = t - g * 16u * a.tiles_b, wide = min(16u, a.tiles_a - 16u * g);
-    ib = in / wide;
+  // Item t: columns n0 to n0 + wd of the tile's rows of A, 128 ia.  Tiles in groups of 16 tiles of A, within a group along A
+  // first; from tile a.whole on, halves of tiles.
+  auto tile = [&](uint32_t t, int& ia, int& n0, int& wd) {
+    wd = BN;
+    uint32_t odd = 0;
+    if (WIDE && t >= (uint32_t)a.whole) {
+      odd = (t - a.whole) & 1;
+      t = a.whole + (t - a.whole) / 2;
+      wd = BN / 2;
+    }
+    const uint32_t g = t / (16u * a.tiles_b), in = t - g * 16u * a.tiles_b, wide = min(16u, a.tiles_a - 16u * g), ib = in / wide;
     ia = 16 * g + in - ib * wide;
+    n0 = ib * BN + odd * (BN / 2);
   };
 
+  if (warp >= kFp8Promote) {
+    if constexpr (WIDE) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFp8FewRegs));
   if (warp == kFp8Promote) {
     int it = 0;
     bool ok = true;
     for (int t = first; t < a.tiles && ok; t += step) {
-      int ia, ib;
-      tile(t, ia, ib);
+      int ia, n0, wd;
+      tile(t, ia, n0, wd);
       for (int k = k0; k < k1; ++k, ++it) {
         const int s = it % ST;
         if (it >= ST && !__all_sync(0xffffffffu, mbar_wait(empty(s), (it / ST - 1) & 1))) { ok = false; break; }
         if (elect_one()) {
-          mbar_arrive_expect_tx(full(s), C::stage);
+          mbar_arrive_expect_tx(full(s), 16384 + 128 * wd);
           tma_load_2d(base + s * C::stage, &ta, full(s), k * kFp8Block, ia * 128);
-          tma_load_2d(base + s * C::stage + 16384, &tb, full(s), k * kFp8Block, ib * BN);
+          tma_load_2d(base + s * C::stage + 16384, &tb, full(s), k * kFp8Block, n0);
+          if (WIDE && wd == BN) tma_load_2d(base + s * C::stage + 32768, &tb, full(s), k * kFp8Block, n0 + 128);
         }
         __syncwarp();
       }
     }
-    if (!ok)   // what was loaded has landed before the block may exit
-      for (int i = it - ST < 0 ? 0 : it - ST; i < it; ++i) mbar_wait(full(i % ST), (i / ST) & 1);
-  } else if (warp > kFp8Promote) {
+    // what was loaded has landed, and in the end been read, before the block may exit
+    for (int i = it - ST < 0 ? 0 : it - ST; i < it; ++i) mbar_wait(ok ? empty(i % ST) : full(i % ST), (i / ST) & 1);
+  } else if (warp <= kFp8Promote + 2) {
     const int parity = warp - kFp8Promote - 1;
-    constexpr uint32_t idesc = idesc_e4m3_f32(128, BN);
     int it = 0;
     bool ok = true;
-    for (int t = first; t < a.tiles && ok; t += step)
+    for (int t = first; t < a.tiles && ok; t += step) {
+      const uint32_t idesc = WIDE && t >= a.whole ? idesc_e4m3_f32(128, BN / 2) : idesc_e4m3_f32(128, BN);
       for (int k = k0; k < k1; ++k, ++it) {
         if ((it & 1) != parity) continue;
         const int s = it % ST, b = it % NA;
@@ -258,26 +294,31 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
 #pragma unroll
           for (int j = 0; j < kFp8Block / 32; ++j)   // 32 bytes along k: two 16-byte units of the descriptors' address
             mma_e4m3(tmem + b * BN, da + 2 * j, db + 2 * j, idesc, j > 0);
+          mma_commit(empty(s));
           mma_commit(dfull(b));
         }
         __syncwarp();
       }
+    }
+  }
   } else {
-    const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane, c0 = half * HC;
-    const uint32_t tl = tmem + ((uint32_t)(quad * 32) << 16) + c0;
+    if constexpr (WIDE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kFp8MoreRegs));
+    const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane;
+    const uint32_t tl = tmem + ((uint32_t)(quad * 32) << 16);
     int it = 0;
     bool ok = true;
     for (int t = first; t < a.tiles && ok; t += step) {
-      int ia, ib;
-      tile(t, ia, ib);
+      int ia, n0, wd;
+      tile(t, ia, n0, wd);
+      const int hc = WIDE ? wd / 2 : HC, c0 = half * hc;   // this thread's columns
       uint64_t acc[HC / 2];
 #pragma unroll
       for (int i = 0; i < HC / 2; ++i) acc[i] = 0;
       // the factors of block k: a thread's own row of x and its columns' 128 rows of w; with SWAP its row of w, and
       // lane c of a warp has column c0 + c's (and c0 + 32 + c's) of x
       // (past the operands' ends the last row's, for results that are not stored: no load waits for a condition)
-      const int wb = min(SWAP ? ia : (ib * BN + c0) / 128, (a.n - 1) / 128);
-      const int xr = min(SWAP ? ib * BN + c0 + lane : ia * 128 + row, a.m - 1);
+      const int wb = min(SWAP ? ia : (n0 + c0) / 128, (a.n - 1) / 128);
+      const int xr = min(SWAP ? n0 + c0 + lane : ia * 128 + row, a.m - 1);
       const float* xp = a.xs + xr;
       const float* wp = a.ws + (long long)wb * a.kb;
       // (the next block's, loaded a block ahead and multiplied only when that block is there: a product that moves up to
@@ -287,7 +328,6 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
         const int b = it % NA;
         if (!__all_sync(0xffffffffu, mbar_wait(dfull(b), (it / NA) & 1))) { ok = false; break; }
         tc_fence_after();
-        if (threadIdx.x == 0) mbar_arrive(empty(it % ST));   // (the block's operands have been read)
         asm volatile("" : "+f"(xn), "+f"(wn));
         const float f = xn * wn;
         const int kn = min(k + 1, k1 - 1);
@@ -298,20 +338,37 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
           if (lane < HC) fw[lane] = f;
           __syncwarp();
         }
+        auto release = [&] {   // the accumulator has been read
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(dempty(b));
+        };
+        if constexpr (!SWAP) {   // the next columns are on their way while these are added
+          constexpr int NC = HC / 16;
+          uint32_t v[2][16];
+          tmem_ld_begin(tl + b * BN + c0, v[0]);
 #pragma unroll
-        for (int c = 0; c < HC; c += LD) {
-          uint32_t v[LD];
-          tmem_ld<LD>(tl + b * BN + c, v);
-          if (c + LD == HC) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(dempty(b));
+          for (int c = 0; c < NC; ++c) {
+            tmem_ld_end();
+            const bool last = c + 1 == NC || (WIDE && 16 * (c + 1) == hc);
+            if (last) release();
+            else tmem_ld_begin(tl + b * BN + c0 + 16 * (c + 1), v[(c + 1) & 1]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) fma2_after(acc[8 * c + i], v[c & 1][2 * i], v[c & 1][2 * i + 1], f);
+            if (last) break;
           }
+        } else {
 #pragma unroll
-          for (int i = 0; i < LD; i += 4) {
-            const float4 g = SWAP ? *(const float4*)(fw + c + i) : make_float4(f, f, f, f);
-            fma2(acc[(c + i) / 2], v[i], v[i + 1], g.x, g.y);
-            fma2(acc[(c + i) / 2 + 1], v[i + 2], v[i + 3], g.z, g.w);
+          for (int c = 0; c < HC; c += LD) {
+            uint32_t v[LD];
+            tmem_ld<LD>(tl + b * BN + c0 + c, v);
+            if (c + LD == HC) release();
+#pragma unroll
+            for (int i = 0; i < LD; i += 4) {
+              const float4 g = *(const float4*)(fw + c + i);
+              fma2(acc[(c + i) / 2], v[i], v[i + 1], g.x, g.y);
+              fma2(acc[(c + i) / 2 + 1], v[i + 2], v[i + 3], g.z, g.w);
+            }
           }
         }
       }
@@ -339,7 +396,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
 #pragma unroll
           for (int i = 0; i < HC / 2; ++i) {
             const float2 v = halves2(acc[i]);
-            const int m = ib * BN + c0 + 2 * i;
+            const int m = n0 + c0 + 2 * i;
             if (m < a.m) fp8_store(a, (long long)m * a.out_stride + n, v.x);
             if (m + 1 < a.m) fp8_store(a, (long long)(m + 1) * a.out_stride + n, v.y);
           }
@@ -350,6 +407,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
         const int m0 = ia * 128 + quad * 32;
 #pragma unroll
         for (int i = 0; i < HC; i += 32) {
+          if (WIDE && i == hc) break;
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
             const float2 v = halves2(acc[(i + j) / 2]);
@@ -357,7 +415,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
             turn[lane * 33 + j + 1] = v.y;
           }
           __syncwarp();
-          const int n = ib * BN + c0 + i + lane;
+          const int n = n0 + c0 + i + lane;
           const int rows = min(32, a.m - m0);
           if (n < a.n)
 #pragma unroll 8
@@ -365,10 +423,11 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
           __syncwarp();
         }
       } else {
-        const int m = ia * 128 + row, n = ib * BN + c0;
+        const int m = ia * 128 + row, n = n0 + c0;
         if (m < a.m) {
 #pragma unroll
           for (int i = 0; i < HC; i += 8) {
+            if (WIDE && i == hc) break;
             const long long at = (long long)m * a.out_stride + n + i;
             float2 v[4];
 #pragma unroll
@@ -398,8 +457,8 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
     __syncwarp();
     cluster_sync_all();   // every partial sum has arrived
     if (warp < kFp8Promote) {
-      int ia, ib;
-      tile(first, ia, ib);
+      int ia, n0, wd;
+      tile(first, ia, n0, wd);
       const int lo = rank * BN / uks, hi = (rank + 1) * BN / uks, wide = hi - lo, per = (BN + ks - 1) / uks;
       // Out rows are contiguous along w's rows: those are the lanes (SWAP) or the columns.  Eight outputs a thread at a
       // time, so that their loads are under way together.
@@ -419,7 +478,7 @@ __global__ void __launch_bounds__(kFp8Threads, 1)
           for (int j = 0; j < 8; ++j) v[j] += recv[(p * per + c[j]) * 129 + r[j]];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int m = SWAP ? ib * BN + lo + c[j] : ia * 128 + r[j], n = SWAP ? ia * 128 + r[j] : ib * BN + lo + c[j];
+          const int m = SWAP ? n0 + lo + c[j] : ia * 128 + r[j], n = SWAP ? ia * 128 + r[j] : n0 + lo + c[j];
           if (i0 + j * 32 * kFp8Promote < total && m < a.m && n < a.n) fp8_store(a, (long long)m * a.out_stride + n, v[j]);
         }
       }

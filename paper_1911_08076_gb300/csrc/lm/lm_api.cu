@@ -275,7 +275,7 @@ int fp8_setup(const int** slots) {
     for (int ks = 2; C::split && ks <= kFp8MaxSplit; ++ks) {
       cudaLaunchConfig_t cfg = {};
       cfg.gridDim = dim3((unsigned)(sms / ks * ks));
-      cfg.blockDim = dim3(kFp8Threads);
+      cfg.blockDim = dim3(C::threads);
       cfg.dynamicSmemBytes = C::bytes;
       cudaLaunchAttribute at[1];
       at[0].id = cudaLaunchAttributeClusterDimension;
@@ -315,6 +315,13 @@ int run_fp8(const ifq_fp8_desc* d, const Fp8Operands& o) {
   const long long tiles = (long long)a.tiles_a * a.tiles_b;
   if (tiles > INT_MAX / kFp8MaxSplit) return IFQ_ERANGE;
   a.tiles = (int)tiles;
+  // The tiles of a last turn that fills half of the SMs or less are cut in two.
+  a.whole = a.tiles;
+  const int rest = a.tiles % slots[1];
+  if (C::wide && 2 * rest <= slots[1]) {
+    a.whole -= rest;
+    a.tiles += rest;
+  }
   // the split of k with the fewest blocks of k in a row, each launch or cluster also costing as much as a few blocks
   a.ks = 1;
   double best = (double)ceil_div(a.tiles, slots[1]) * (a.kb + 6);
@@ -324,12 +331,13 @@ int run_fp8(const ifq_fp8_desc* d, const Fp8Operands& o) {
     if (c < best) best = c, a.ks = ks;
   }
   CUtensorMap tx, tw;
-  if (!encode_e4m3(o.x, d->m, d->k, SWAP ? BN : 128, &tx) || !encode_e4m3(o.w, d->n, d->k, SWAP ? 128 : BN, &tw)) return IFQ_ECUDA;
+  const int box = std::min(BN, 128);
+  if (!encode_e4m3(o.x, d->m, d->k, SWAP ? box : 128, &tx) || !encode_e4m3(o.w, d->n, d->k, SWAP ? 128 : box, &tw)) return IFQ_ECUDA;
   const CUtensorMap &ta = SWAP ? tw : tx, &tb = SWAP ? tx : tw;
   if (a.ks > 1)
-    return done(launch_k_cluster(fp8_matmul_kernel<BN, SWAP>, a.ks, dim3((unsigned)(a.tiles * a.ks)), dim3(kFp8Threads), C::bytes,
+    return done(launch_k_cluster(fp8_matmul_kernel<BN, SWAP>, a.ks, dim3((unsigned)(a.tiles * a.ks)), dim3(C::threads), C::bytes,
                                  o.st, ta, tb, a));
-  return done(launch_k(fp8_matmul_kernel<BN, SWAP>, dim3((unsigned)std::min(a.tiles, slots[1])), dim3(kFp8Threads), C::bytes, o.st,
+  return done(launch_k(fp8_matmul_kernel<BN, SWAP>, dim3((unsigned)std::min(a.tiles, slots[1])), dim3(C::threads), C::bytes, o.st,
                        ta, tb, a));
 }
 

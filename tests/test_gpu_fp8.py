@@ -100,6 +100,12 @@ def test_product_equals_its_definition(m, n, k, out, pad):
     assert (far <= 0).all(), (far.max(), np.argwhere(far > 0)[:4])
 
 
+@pytest.mark.parametrize("m,n,k,out,pad", [(2500, 2041, 272, "f32", 3), (2305, 2177, 528, "bf16", 7), (130, 19600, 400, "f16", 0),
+                                           (5000, 4000, 144, "bf16", 0)])
+def test_large_product_equals_its_definition(m, n, k, out, pad):
+    test_product_equals_its_definition(m, n, k, out, pad)
+
+
 @pytest.mark.parametrize("m,n,k", [(3, 200, 400), (70, 130, 256), (260, 256, 384)])
 def test_a_row_that_is_not_finite_stays_by_itself(m, n, k):
     rng = np.random.default_rng(m)
