@@ -36,6 +36,28 @@ def test_quantised_activations_are_exact(m, k, dtype, pad):
     assert np.array_equal(tab[q.cpu().numpy()], tab[qw])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_quantised_activations_are_exact_near_middles_of_codes(dtype):
+    # every half or bfloat16 of a few binades against largest values around 448 2^e, where quotients meet the middles
+    code, dt, _ = TYPES[dtype]
+    bits = {"bf16": 7, "f16": 10}[dtype]
+    mant = np.concatenate([2.0 ** e * (1 + np.arange(2 ** bits) / 2 ** bits) for e in range(-8, 9)]).astype(np.float32)
+    rows = []
+    for top in (448, 449, 450, 452, 455, 440, 512, 511, 480, 300, 257, 256):
+        t = np.concatenate([mant[mant <= top], np.zeros(-len(mant[mant <= top]) % 112, np.float32)]).reshape(-1, 112)
+        t = np.concatenate([t * np.where(np.arange(112) % 3 == 0, -1, 1), np.full((len(t), 16), top)], 1)
+        rows += [t * 2.0 ** e for e in (0, -7, 5)]
+    x = np.concatenate(rows).astype(np.float32)
+    m = len(x)
+    xd = torch.from_numpy(x).to(DEV).to(dt)
+    q, s = torch.empty(m, 128, dtype=torch.uint8, device=DEV), torch.empty(1, m, device=DEV)
+    ifq.ifq_fp8_quantize(ifq.fp8_desc(m, 8, 128, code), xd, q, s)
+    qw, sw = R.fp8_quantise(xd.float().cpu().numpy())
+    tab = R.e4m3_table()
+    assert np.array_equal(s.cpu().numpy(), sw)
+    assert np.array_equal(tab[q.cpu().numpy()], tab[qw])
+
+
 def test_quantiser_says_what_is_not_finite():
     x = torch.ones(3, 256, device=DEV).bfloat16()
     x[0, 3], x[1, 200], x[2, 255] = float("nan"), float("inf"), -float("inf")
