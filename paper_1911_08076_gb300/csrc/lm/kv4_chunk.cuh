@@ -16,9 +16,11 @@
 // fine as the minimum that the cache holds (a half), and within the half's range where s' c' + m' would leave it.  Where
 // rows are half the product takes c' - 8, exact, and the scale goes into the weight's exponent, w = 2^(t - m + log2 s');
 // then sum p = sum w / s', and the values of code 8, m'' = m' + 8 s', are added in fp32, sum w m'' / s'.  (The rounding of
-// v would be as large as that of the result.)  Weights are halves of 2^(t - m) with the reference m of a row raised only
-// when a sum of 8 of them, or for exact values one, passes 2^15 (no half overflows before), in whole powers of two; the
-// denominator is the sum of the unrounded p.
+// v would be as large as that of the result.)  Both sums take w as the product has it, rounded, so that what it loses is
+// 2^-11 of v.  A value far from 0 beside its scale (a constant one: s' = 0) would have a weight that vanishes as a half while
+// m'' / s' is large: it takes the scale S = 2^k s' in place of s', with |m''| <= 16 S, and (c' - 8) 2^-k, still exact.
+// Weights are halves of 2^(t - m) with the reference m of a row raised only when a sum of 8 of them, or for exact values
+// one, passes 2^15 (no half overflows before), in whole powers of two; the denominator is the sum of the unrounded p.
 // A value that is not a number must reach only the rows that see it: its operand is 0 and its key's minimum NaN.
 //
 // Warps: one or two groups of four run the softmax, in matrix fragments: a thread has four rows and two of every eight
@@ -135,6 +137,19 @@ __device__ __forceinline__ KvTiles kv_tiles(const KvAttnArgs& a, int len, int p_
   return t;
 }
 
+// Parameters of an exact value: its scale (0 counts as the smallest half: its codes are 0, and the value of code 8 makes up
+// for it), the value of code 8, and the k that brings that within 16 2^k scales of 0 (by their exponents).
+struct KvExact {
+  float sc, eight;
+  int k;
+  __device__ __forceinline__ explicit KvExact(uint32_t par) {
+    const float2 y = unpack16<false>(par);
+    sc = fmaxf(y.x, 5.9604645e-8f);
+    eight = y.y + 8.0f * sc;
+    k = max(0, (int)(__float_as_uint(eight) >> 23 & 255u) - (int)(__float_as_uint(sc) >> 23) - 3);
+  }
+};
+
 // Keeps the use of loaded registers after this point: work on them that is moved up to the loads waits for them there
 // (900 of 3200 cycles a tile).
 template <int N>
@@ -152,8 +167,8 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
   uint8_t* smem = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   uint8_t *sQ = smem, *sK = sQ + C::q_bytes, *sV = sK + NB * C::kv_bytes;
   float4* sPar = (float4*)(sV + NB * C::kv_bytes);          // [kChunkPar][64 pairs of keys]: s, s, m, m of the keys
-  float4* sVal = sPar + kChunkPar * (kChunkKeys / 2);       // of values in half: 1/s', 1/s', m''/s', m''/s'
-  float2* sLog = (float2*)(sVal + kChunkPar * (kChunkKeys / 2));   // and log2 s', twice
+  float4* sVal = sPar + kChunkPar * (kChunkKeys / 2);       // of values in half: 1/S, 1/S, m''/S, m''/S
+  float2* sLog = (float2*)(sVal + kChunkPar * (kChunkKeys / 2));   // and log2 S, twice
   const uint32_t bars = smem_u32(sPar) + C::par_bytes;
   auto kfull = [&](int b) { return bars + 8 * b; };          // expanded keys
   auto kempty = [&](int b) { return bars + 16 + 8 * b; };
@@ -528,7 +543,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
     const int tid = threadIdx.x - 128 * NG, w = warp - 4 * NG;
     const int kg = tid >> 4, krow = tid & 15;                                  // the key's group of the tile, row of it
     const int c8 = lane & 7, vg = (w >> 1) * 4 + (c8 >> 1), vh = c8 & 1, slice = (lane >> 3) | (w & 1) << 2;
-    uint32_t kw[NBLK * WPB * 4], vw[NBLK * WPB * 4], kpar = 0, vpar = 0, vp[8];
+    uint32_t kw[NBLK * WPB * 4], vw[NBLK * WPB * 4], kpar = 0, vpar = 0, vp[EX ? 2 : 8];
     // The thread's two groups of each tile, a cursor each: place in the page table, group of the page.  A page's number
     // is read two tiles ahead, so that nothing waits for it; nor is any load made on a condition, which would be waited
     // for at once: a group past the tokens is looked up in the last page's place, and where there is no page any
@@ -586,10 +601,14 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
           const int o = (b * WPB + k) * 4;
           vw[o] = y.x, vw[o + 1] = y.y, vw[o + 2] = y.z, vw[o + 3] = y.w;
         }
+      if constexpr (EX) {   // two of the eight tokens, the others' from the three lanes that share them
+        load_words(vp, g + 16 * D + 64 + 32 * vh + 8 * (lane >> 3));
+      } else {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint4 y = *(const uint4*)(g + 16 * D + 64 + 32 * vh + 16 * k);
-        vp[4 * k] = y.x, vp[4 * k + 1] = y.y, vp[4 * k + 2] = y.z, vp[4 * k + 3] = y.w;
+        for (int k = 0; k < 2; ++k) {
+          const uint4 y = *(const uint4*)(g + 16 * D + 64 + 32 * vh + 16 * k);
+          vp[4 * k] = y.x, vp[4 * k + 1] = y.y, vp[4 * k + 2] = y.z, vp[4 * k + 3] = y.w;
+        }
       }
     };
     // a key's parameters that are numbers (neither an infinity nor a NaN in either half)
@@ -629,14 +648,13 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
         dst[0] = f.x * (a.scale * 1.44269504f * 1048576.0f);   // codes are in units of 2^-24, q of 2^-4
         dst[2] = f.y;
         if constexpr (EX) {
-          // (a scale of 0 counts as the smallest half: its codes are 0, and the value of code 8 makes up for it)
           const bool some = there && finite(vpar);
-          const float2 y = unpack16<false>(some ? vpar : 0u);
-          const float sc = fmaxf(y.x, 5.9604645e-8f), r = 1.0f / sc;
+          const KvExact y(some ? vpar : 0u);
+          const float r = __uint_as_float((uint32_t)(127 - y.k) << 23) / y.sc;
           float* dv4 = (float*)(sVal + pb * (kChunkKeys / 2) + tid / 2) + (tid & 1);
           dv4[0] = some ? r : 0.0f;
-          dv4[2] = some ? (y.y + 8.0f * sc) * r : 0.0f;
-          ((float*)(sLog + pb * (kChunkKeys / 2)))[tid] = some ? log2f(sc) : 0.0f;
+          dv4[2] = some ? y.eight * r : 0.0f;
+          ((float*)(sLog + pb * (kChunkKeys / 2)))[tid] = some ? log2f(y.sc) + (float)y.k : 0.0f;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(pfull(pb));
@@ -652,21 +670,35 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       __syncwarp();
       if (lane == 0) mbar_arrive(kfull(b));
       if (i + 1 < nt) load_k(place(ck, page_k, have_k));
+      hold(vp);
+      __half2 vs[4], vm[4];   // pairs of tokens: scales and minima, halved; of exact values 2^-k
+      auto param = [&](int i, int j) { return have_v && j0 + vg * kKvGroup + 8 * vh + j < q.len && finite(vp[i]) ? vp[i] : 0u; };
+      bool down = false;      // some k is not 0
+      if constexpr (EX) {
+        const int k0 = KvExact(param(0, 2 * (lane >> 3))).k, k1 = KvExact(param(1, 2 * (lane >> 3) + 1)).k;
+        down = __any_sync(0xffffffffu, k0 | k1);
+        if (down) {   // (past 2^20 a step is nothing beside the value)
+          const uint32_t f = pack16<false>(__uint_as_float(k0 > 20 ? 0u : (uint32_t)(127 - k0) << 23),
+                                           __uint_as_float(k1 > 20 ? 0u : (uint32_t)(127 - k1) << 23));
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const uint32_t y = __shfl_sync(0xffffffffu, f, t << 3 | c8);
+            vs[t] = *(const __half2*)&y;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t y0 = param(2 * t, 2 * t), y1 = param(2 * t + 1, 2 * t + 1);
+          const uint32_t sc = __byte_perm(y0, y1, 0x5410), mn = __byte_perm(y0, y1, 0x7632);
+          vs[t] = __hmul2(*(const __half2*)&sc, __float2half2_rn(0.5f));
+          vm[t] = __hmul2(*(const __half2*)&mn, __float2half2_rn(0.5f));
+        }
+      }
       ok = __all_sync(0xffffffffu, i < NB || mbar_wait(vempty(b), (i / NB - 1) & 1));
       if (!ok) break;
       hold(vw);
-      hold(vp);
       uint8_t* dv = sV + b * C::kv_bytes + (w >> 1) * (D * 128);
-      __half2 vs[4], vm[4];   // pairs of tokens: scales and minima, halved
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int j = j0 + vg * kKvGroup + 8 * vh + 2 * t;
-        const uint32_t y0 = have_v && j < q.len && finite(vp[2 * t]) ? vp[2 * t] : 0u;
-        const uint32_t y1 = have_v && j + 1 < q.len && finite(vp[2 * t + 1]) ? vp[2 * t + 1] : 0u;
-        const uint32_t sc = __byte_perm(y0, y1, 0x5410), mn = __byte_perm(y0, y1, 0x7632);
-        vs[t] = __hmul2(*(const __half2*)&sc, __float2half2_rn(0.5f));
-        vm[t] = __hmul2(*(const __half2*)&mn, __float2half2_rn(0.5f));
-      }
 #pragma unroll
       for (int blk = 0; blk < NBLK; ++blk)
 #pragma unroll
@@ -684,6 +716,13 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
                                          : __hadd2(*(const __half2*)&g, __float2half2_rn(-1024.0f - off));
               const __half2 v = EX ? code : __hfma2(code, vs[t], vm[t]);
               y[t] = *(const uint32_t*)&v;
+            }
+            if (EX && down) {
+#pragma unroll
+              for (int t = 0; t < 4; ++t) {
+                const __half2 v = __hmul2(*(const __half2*)&y[t], vs[t]);
+                y[t] = *(const uint32_t*)&v;
+              }
             }
             const int d = d0 + n;
             *(uint4*)(dv + d * 128 + ((c8 ^ (d & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);

@@ -1,0 +1,80 @@
+"""Attention over values of mixed sizes, constant value rows, dominant tokens and parameters that are no numbers.
+
+Tolerances are those of lm_reference.attention, whose term for rounded weights goes with s' c' + |m'|; the kernels round the
+weights of c' - 8 (|c' - 8| <= 8) and add the minima unrounded, which the term of _near adds: 2^-11 of sum p 8 s' / sum p, and
+for weights below half's normal range `small` of the largest 8 s' or |V| a token."""
+import numpy as np
+import pytest
+import torch
+
+import lm_reference as R
+import test_gpu_kv4 as base
+from paper_1911_08076_gb300 import ifq
+
+pytestmark = pytest.mark.gpu
+
+
+def _value(cache, table, page, D, seq, j, scale, mn, code=None):
+    """Value parameters of token j (all heads), and one code for all dimensions if given."""
+    pg, off = table[seq, j // page], j % page
+    g, row = cache[pg, :, off // 16], off % 16
+    g[:, 16 * D + 64 + 4 * row:16 * D + 68 + 4 * row] = np.array([scale, mn], np.float16).view(np.uint8)
+    if code is not None:
+        byte, shift = R.v_place(D)
+        low, high = byte[row][shift[row] == 0], byte[row][shift[row] == 4]
+        assert np.array_equal(low, high)
+        g[:, low] = code | code << 4
+
+
+def _near(got, lens, starts, table, cache, hk, page, small=0.0, rows=None, lse=True, window=0, sinks=0):
+    out, ls, q64, scale, u, many = got
+    want, wl, tol, ltol = R.attention(q64, cache, page, table, lens, starts, hk, scale, window, sinks, u, many)
+    # the same attention over 8 s' in place of the values: its mean, and the largest
+    eight = cache.copy()
+    D = q64.shape[2]
+    par = eight[..., 16 * D + 64:].reshape(-1, 16, 4).view(np.float16)
+    with np.errstate(all="ignore"):
+        par[..., 1] = np.where(np.isfinite(par[..., 0]), 8 * par[..., 0], 0)
+    par[..., 0] = 0
+    eight[..., 16 * D + 64:] = par.view(np.uint8).reshape(*eight.shape[:-1], 64)
+    mean, _, _, _ = R.attention(q64, eight, page, table, lens, starts, hk, scale, window, sinks, 0.0)
+    with np.errstate(all="ignore"):
+        tol = tol + 2.0 ** -11 * mean
+    if small:
+        top = 0.0
+        for s, n in enumerate(lens):
+            j = np.arange(n)
+            _, (v, _, vp) = R.read(cache, page, table[s, j // page].astype(np.int64) * page + j % page, D)
+            top = max(top, np.abs(v).max(), 8 * float(vp[..., 0].max()))
+        tol = tol + small * top * int(max(lens))
+    keep = np.ones(out.shape[:2], bool) if rows is None else rows
+    far = np.abs(out[keep] - want[keep]) - tol[keep]
+    assert (far <= 0).all(), (np.nanmax(far), np.isnan(far).sum(), np.argwhere(~(far <= 0))[:5])
+    if lse:
+        far = np.abs(ls[keep] - wl[keep]) - ltol[keep]
+        assert (far <= 0).all(), (np.nanmax(far), np.isnan(far).sum())
+
+
+MANY = [dict(), dict(wide=True), dict(wide=True, max_q=30)]     # by estimate; wide row blocks; 128 rows a block, split keys
+
+
+@pytest.mark.parametrize("bounds", MANY, ids=["as is", "wide", "wide 30"])
+@pytest.mark.parametrize("n,dtype", [(1, "f16"), (30, "f16"), (30, "bf16")])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("kind", ["constant rows", "scales to 1", "scales to 64"])
+def test_values_with_minima_that_do_not_go_with_their_scales(kind, D, n, dtype, bounds):
+    """Every other value row constant (scale 0, codes 0, as the append writes them) beside usual ones, or scales from 0 and
+    2^-24 up: what a token adds does not depend on how small its scale is."""
+    rng = np.random.default_rng(21)
+    page, hk, hq, L = 16, 1, 4, 300
+    lens, starts, table, cache, q = base._setup(rng, [L], [n], hq, hk, D, page)
+    top = {"constant rows": 0, "scales to 1": 0, "scales to 64": 6}[kind]
+    for j in range(L):
+        if j % 2:
+            _value(cache, table, page, D, 0, j, 0, rng.uniform(1, 5), 0)
+        elif kind == "constant rows":
+            _value(cache, table, page, D, 0, j, 0.5, -3.75)
+        else:
+            _value(cache, table, page, D, 0, j, 2.0 ** rng.uniform(-24, top), 5.0)
+    got = base._run(lens, starts, table, cache, q, hq, hk, D, page, dtype, **bounds)
+    _near(got, lens, starts, table, cache, hk, page)
