@@ -387,16 +387,15 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
           if constexpr (!EX) weights();
           const float fl = by_lane(f);
           if (__any_sync(0xffffffffu, fl != 1.0f)) {
-            // what this tile's columns and the sum already hold
-            const uint32_t fh = pack16<false>(fl, fl);
+            // what this tile's columns and the sum already hold (the factor may be below what a half can be)
             tmem_wait_st();
             for (int d = 0; d < c; ++d) {
               uint32_t x[16];
               tmem_ld<16>(tS + 16 * d, x);
 #pragma unroll
               for (int k = 0; k < 16; ++k) {
-                const __half2 y = __hmul2(*(const __half2*)&x[k], *(const __half2*)&fh);
-                x[k] = *(const uint32_t*)&y;
+                const float2 y = unpack16<false>(x[k]);
+                x[k] = pack16<false>(y.x * fl, y.y * fl);
               }
               tmem_st16(tS + 16 * d, x);
             }

@@ -26,6 +26,13 @@ def _value(cache, table, page, D, seq, j, scale, mn, code=None):
         g[:, low] = code | code << 4
 
 
+def _key(cache, table, page, D, seq, j, value):
+    """A key with every element `value` (scale 0)."""
+    pg, off = table[seq, j // page], j % page
+    g, row = cache[pg, :, off // 16], off % 16
+    g[:, 16 * D + 4 * row:16 * D + 4 * row + 4] = np.array([0, value], np.float16).view(np.uint8)
+
+
 def _near(got, lens, starts, table, cache, hk, page, small=0.0, rows=None, lse=True, window=0, sinks=0):
     out, ls, q64, scale, u, many = got
     want, wl, tol, ltol = R.attention(q64, cache, page, table, lens, starts, hk, scale, window, sinks, u, many)
@@ -77,4 +84,27 @@ def test_values_with_minima_that_do_not_go_with_their_scales(kind, D, n, dtype, 
         else:
             _value(cache, table, page, D, 0, j, 2.0 ** rng.uniform(-24, top), 5.0)
     got = base._run(lens, starts, table, cache, q, hq, hk, D, page, dtype, **bounds)
+    _near(got, lens, starts, table, cache, hk, page)
+
+
+@pytest.mark.parametrize("bounds", MANY[1:], ids=["wide", "wide 30"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("last", [24.6, 26.5, 29.5])
+def test_a_maximum_that_rises_by_many_binades_within_a_tile(last, D, dtype, bounds):
+    """Tokens 0 to 31 of the first tile at score 2^0, the next 64 at 2^11.5 (2^14 for f16), token 96 at 2^last, whose value
+    is 0: what the 64 add is all there is to see."""
+    rng = np.random.default_rng(22)
+    page, hk, hq, L, n = 16, 1, 4, 200, 30
+    lens, starts, table, cache, q = base._setup(rng, [L], [n], hq, hk, D, page)
+    q[:] = 0
+    q[:, :, 0] = 1
+    for j in range(L):
+        _key(cache, table, page, D, 0, j, 0.0 if not 32 <= j <= 96 else last if j == 96 else 14.0 if dtype == "f16" else 11.5)
+        _value(cache, table, page, D, 0, j, 0.25, 1.0)
+    if dtype == "f16":
+        _value(cache, table, page, D, 0, 96, 0.25, -2.0, 8)
+    else:
+        _value(cache, table, page, D, 0, 96, 0.0, 0.0, 0)
+    got = base._run(lens, starts, table, cache, q, hq, hk, D, page, dtype, scale=float(np.float32(np.log(2))), **bounds)
     _near(got, lens, starts, table, cache, hk, page)
