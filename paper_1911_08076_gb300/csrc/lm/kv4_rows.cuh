@@ -326,7 +326,12 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
             mbar_arrive_expect_tx(bar, GB);
             bulk_copy_g2s(ring + st * U * GB, src, GB, bar);
           } else {
-            if (there) set_status(IFQ_ERANGE);
+            if (there) {   // no such page: parameters of 0, so that the result does not depend on what was here before
+              set_status(IFQ_ERANGE);
+              uint4* par = (uint4*)(smem + w * ST * U * GB + st * U * GB + u * GB + 16 * D);
+              for (int i = 0; i < 8; ++i) par[i] = make_uint4(0, 0, 0, 0);
+              fence_proxy_async_smem();   // (the next copy to this place comes after)
+            }
             mbar_arrive(bar);
           }
           o += step;

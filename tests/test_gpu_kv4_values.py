@@ -108,3 +108,24 @@ def test_a_maximum_that_rises_by_many_binades_within_a_tile(last, D, dtype, boun
         _value(cache, table, page, D, 0, 96, 0.0, 0.0, 0)
     got = base._run(lens, starts, table, cache, q, hq, hk, D, page, dtype, scale=float(np.float32(np.log(2))), **bounds)
     _near(got, lens, starts, table, cache, hk, page)
+
+
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("n,dtype", [(1, "bf16"), (5, "f16"), (60, "bf16"), (60, "f16")])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_a_page_past_the_cache_does_not_bring_in_what_another_call_left(D, n, dtype, wide):
+    """The values of such a page are undefined, but the same each time: nothing of the calls before shows in them."""
+    rng = np.random.default_rng(27)
+    page, hk, hq, L = 16, 1, 2, 700
+    a = base._setup(rng, [L], [n], hq, hk, D, page)
+    bad = a[2].copy()
+    bad[0, 2::5] = a[3].shape[0] + 3
+    outs = []
+    for spread in (0.5, 2.0, 7.0):
+        other = base._setup(rng, [L, L], [n, n], hq, hk, D, page, spread=spread)
+        base._run(*other, hq, hk, D, page, dtype, wide=wide)
+        got = base._run(a[0], a[1], bad, a[3], a[4], hq, hk, D, page, dtype, wide=wide)
+        assert base._status() == ifq.IFQ_ERANGE
+        outs.append(got)
+    for o in outs[1:]:
+        assert np.array_equal(o[0], outs[0][0], equal_nan=True) and np.array_equal(o[1], outs[0][1], equal_nan=True)
