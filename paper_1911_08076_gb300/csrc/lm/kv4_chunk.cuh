@@ -21,7 +21,8 @@
 // m'' / s' is large: it takes the scale S = 2^k s' in place of s', with |m''| <= 16 S, and (c' - 8) 2^-k, still exact.
 // Weights are halves of 2^(t - m) with the reference m of a row raised only when a sum of 8 of them, or for exact values
 // one, passes 2^15 (no half overflows before), in whole powers of two; the denominator is the sum of the unrounded p.
-// A value that is not a number must reach only the rows that see it: its operand is 0 and its key's minimum NaN.
+// A value whose parameters are not finite must reach only the rows that see it, and not their log-sum-exp: its operand is a
+// number, and a block that met one looks its keys' parameters through again at the end, for the rows that see them.
 //
 // Warps: one or two groups of four run the softmax, in matrix fragments: a thread has four rows and two of every eight
 // keys (with a thread a row, as many broadcast loads of the keys' parameters as scores took 2000 of 4500 cycles a tile);
@@ -150,6 +151,11 @@ struct KvExact {
   }
 };
 
+// Whether a value's parameters are numbers: neither an infinity nor a NaN in either half.
+__device__ __forceinline__ bool kv_finite(uint32_t par) {
+  return (par & 0x7c00u) != 0x7c00u && (par & 0x7c000000u) != 0x7c000000u;
+}
+
 // Keeps the use of loaded registers after this point: work on them that is moved up to the loads waits for them there
 // (900 of 3200 cycles a tile).
 template <int N>
@@ -181,8 +187,10 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
   const uint32_t qready = bars + 112 + 8 * kChunkPar;
   auto olast = [&](int g) { return qready + 8 + 8 * g; };    // group g's last product
   uint32_t* tptr = (uint32_t*)((uint8_t*)sPar + C::par_bytes + 112 + 8 * kChunkPar + 24);
+  uint32_t* sOdd = tptr + 1;   // some value's parameters are not finite
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
+    *sOdd = 0;
     for (int b = 0; b < 2; ++b) {
       mbar_init(kfull(b), 4);
       mbar_init(kempty(b), 1);
@@ -219,6 +227,10 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
   const KvTiles tiles = kv_tiles(a, q.len, p_lo, p_hi);
   const int t0 = work ? (int)((long long)tiles.n * sp / A.splits) : 0, t1 = work ? (int)((long long)tiles.n * (sp + 1) / A.splits) : 0;
   const int nt = t1 - t0, steps = nt * RT;   // step x: tile x / RT, S buffer x % 2, softmax group x % NG
+  const int gpp = A.by_gpp.d;   // groups a page
+  const long long page_bytes = (long long)a.kv_heads * gpp * GB;
+  const uint8_t* heads = a.cache + (long long)head * gpp * GB;
+  const int32_t* table = a.table + (long long)s * a.max_pages;
   auto first_key = [&](int i) { return (t0 + i < tiles.sg ? t0 + i : t0 + i + tiles.skip) * kChunkKeys; };
 
   if (warp < 4 * NG) {
@@ -496,6 +508,18 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
         top = all;
       }
     }
+    if (work && (RT == 2 || grp == 0) && *sOdd && have && nt > 0) {
+      const int last_seen = min(p, q.len - 1);
+      for (int i = 0; i < nt; ++i)
+        for (int j = first_key(i), end = min(j + kChunkKeys, last_seen + 1); j < end; j += kKvGroup) {
+          const int group = j / kKvGroup, in_table = kv_div(group, A.by_gpp), page = table[in_table];
+          if (page < 0 || page >= a.pages) continue;
+          const uint32_t* par = (const uint32_t*)(heads + page * page_bytes + (group - in_table * gpp) * GB + 16 * D + 64);
+          for (int k = 0; k < kKvGroup; ++k)
+            if (j + k < end && (j + k >= p_first || j + k < a.sinks) && !kv_finite(par[k])) zl = __uint_as_float(0x7fc00000u);
+        }
+    }
+    __syncwarp();
     if (work && (RT == 2 || grp == 0)) {
       const bool parts = A.splits > 1;
       const long long at = ((((long long)s * a.kv_heads + head) * A.blocks + r0 / (128 * RT)) * A.splits + sp) * (128 * RT) + rt * 128 + row;
@@ -547,11 +571,8 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
     // is read two tiles ahead, so that nothing waits for it; nor is any load made on a condition, which would be waited
     // for at once: a group past the tokens is looked up in the last page's place, and where there is no page any
     // group's bytes will do (codes are numbers, and the parameters are then left out).
-    const int32_t* table = a.table + (long long)s * a.max_pages;
-    const int gpp = A.by_gpp.d, last_group = (q.len - 1) / kKvGroup, last_page = (int)kv_div(max(last_group, 0), A.by_gpp);
+    const int last_group = (q.len - 1) / kKvGroup, last_page = (int)kv_div(max(last_group, 0), A.by_gpp);
     const int step_pages = 8 / gpp, step_groups = 8 - step_pages * gpp;   // (8 groups a tile)
-    const long long page_bytes = (long long)a.kv_heads * gpp * GB;
-    const uint8_t* heads = a.cache + (long long)head * gpp * GB;
     struct Cursor {
       int group, page, in;   // group of the sequence; its place in the table and in its page
     };
@@ -610,8 +631,6 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
         }
       }
     };
-    // a key's parameters that are numbers (neither an infinity nor a NaN in either half)
-    auto finite = [](uint32_t par) { return (par & 0x7c00u) != 0x7c00u && (par & 0x7c000000u) != 0x7c000000u; };
     bool ok = true;
     int page_k = 0, page_v = 0;             // of the tile after the one at hand
     bool have_k = false, have_v = false;    // whether the tile at hand has the thread's groups
@@ -641,19 +660,18 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       asm volatile("" : "+r"(kpar), "+r"(vpar));
       {
         const bool there = have_k && j0 + tid < q.len;
-        float2 f = unpack16<false>(there ? kpar : 0u);
-        if (there && !finite(vpar)) f.y = __uint_as_float(0x7fc00000u);   // NaN to the rows that see it
+        const float2 f = unpack16<false>(there ? kpar : 0u);
+        if (there && !kv_finite(vpar)) *sOdd = 1;
         float* dst = (float*)(sPar + pb * (kChunkKeys / 2) + tid / 2) + (tid & 1);
         dst[0] = f.x * (a.scale * 1.44269504f * 1048576.0f);   // codes are in units of 2^-24, q of 2^-4
         dst[2] = f.y;
         if constexpr (EX) {
-          const bool some = there && finite(vpar);
-          const KvExact y(some ? vpar : 0u);
+          const KvExact y(there && kv_finite(vpar) ? vpar : 0x3c00u);   // (scale 1, minimum 0)
           const float r = __uint_as_float((uint32_t)(127 - y.k) << 23) / y.sc;
           float* dv4 = (float*)(sVal + pb * (kChunkKeys / 2) + tid / 2) + (tid & 1);
-          dv4[0] = some ? r : 0.0f;
-          dv4[2] = some ? y.eight * r : 0.0f;
-          ((float*)(sLog + pb * (kChunkKeys / 2)))[tid] = some ? log2f(y.sc) + (float)y.k : 0.0f;
+          dv4[0] = there ? r : 0.0f;
+          dv4[2] = there ? y.eight * r : 0.0f;
+          ((float*)(sLog + pb * (kChunkKeys / 2)))[tid] = there ? log2f(y.sc) + (float)y.k : 0.0f;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(pfull(pb));
@@ -671,7 +689,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       if (i + 1 < nt) load_k(place(ck, page_k, have_k));
       hold(vp);
       __half2 vs[4], vm[4];   // pairs of tokens: scales and minima, halved; of exact values 2^-k
-      auto param = [&](int i, int j) { return have_v && j0 + vg * kKvGroup + 8 * vh + j < q.len && finite(vp[i]) ? vp[i] : 0u; };
+      auto param = [&](int i, int j) { return have_v && j0 + vg * kKvGroup + 8 * vh + j < q.len && kv_finite(vp[i]) ? vp[i] : 0u; };
       bool down = false;      // some k is not 0
       if constexpr (EX) {
         const int k0 = KvExact(param(0, 2 * (lane >> 3))).k, k1 = KvExact(param(1, 2 * (lane >> 3) + 1)).k;

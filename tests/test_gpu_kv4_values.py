@@ -129,3 +129,21 @@ def test_a_page_past_the_cache_does_not_bring_in_what_another_call_left(D, n, dt
         outs.append(got)
     for o in outs[1:]:
         assert np.array_equal(o[0], outs[0][0], equal_nan=True) and np.array_equal(o[1], outs[0][1], equal_nan=True)
+
+
+@pytest.mark.parametrize("bounds", MANY, ids=["as is", "wide", "wide 30"])
+@pytest.mark.parametrize("n,dtype", [(1, "bf16"), (4, "f16"), (4, "bf16"), (30, "f16"), (30, "bf16")])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_a_value_that_is_not_a_number_leaves_the_log_sum_exp(D, n, dtype, bounds):
+    rng = np.random.default_rng(24)
+    page, hk, hq, L = 16, 1, 4, 150
+    lens, starts, table, cache, q = base._setup(rng, [L], [n], hq, hk, D, page)
+    c2 = cache.copy()
+    _value(c2, table, page, D, 0, L - 2, np.nan, np.nan)        # seen by the last two queries
+    got = base._run(lens, starts, table, c2, q, hq, hk, D, page, dtype, **bounds)
+    sees = np.arange(n) >= n - 2
+    assert np.isnan(got[0][sees]).all()
+    rows = np.broadcast_to(~sees[:, None], got[0].shape[:2])
+    _near(got, lens, starts, table, cache, hk, page, rows=rows)
+    _, wl, _, ltol = R.attention(got[2], cache, page, table, lens, starts, hk, got[3], 0, 0, got[4], got[5])
+    assert (np.abs(got[1] - wl) <= ltol).all()
