@@ -19,8 +19,11 @@
 // v would be as large as that of the result.)  Both sums take w as the product has it, rounded, so that what it loses is
 // 2^-11 of v.  A value far from 0 beside its scale (a constant one: s' = 0) would have a weight that vanishes as a half while
 // m'' / s' is large: it takes the scale S = 2^k s' in place of s', with |m''| <= 16 S, and (c' - 8) 2^-k, still exact.
-// Weights are halves of 2^(t - m) with the reference m of a row raised only when a sum of 8 of them, or for exact values
-// one, passes 2^15 (no half overflows before), in whole powers of two; the denominator is the sum of the unrounded p.
+// Weights are halves of 2^(t - m), the denominator is the sum of the unrounded p.  The reference m of a row is set 10 below
+// its first maximum, and again below a later one when a sum of 8 weights passes 61440, or for exact values one 2^15.5 (no
+// half overflows before), in whole powers of two: weights keep their 11 bits down to 2^-23 of that maximum and vanish at
+// 2^-34.  (With the reference at the maximum a first token that takes almost all left the others 10 bits fewer.  A limit of
+// 2^15 for the sum, which is passed more often, took 675 us where this takes 655.)
 // A value whose parameters are not finite must reach only the rows that see it, and not their log-sum-exp: its operand is a
 // number, and a block that met one looks its keys' parameters through again at the end, for the rows that see them.
 //
@@ -44,6 +47,7 @@ struct KvChunkArgs {
 };
 
 constexpr int kChunkKeys = 128, kChunkPar = 4;   // keys a tile; tiles whose parameters are held
+constexpr float kChunkAbove = 10.0f;             // a row's reference is this far below its maximum when it is set
 
 template <int D, int RT>
 struct KvChunkShape {
@@ -377,7 +381,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
         } else {
           weights();
         }
-        if (__any_sync(0xffffffffu, most > (EX ? 15.0f : 32768.0f) || fresh)) {
+        if (__any_sync(0xffffffffu, most > (EX ? 15.5f : 61440.0f) || fresh)) {
           float f[4];
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
@@ -387,7 +391,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const bool begin = (fresh >> y & 1u) && top > -INFINITY;
-            const float rise = begin || top > 8.0f ? ceilf(top) : 0.0f;
+            const float rise = begin || top > kChunkAbove ? ceilf(top) - kChunkAbove : 0.0f;
             f[y] = begin ? 1.0f : exp2_fast(-rise);
             if (begin) fresh &= ~(1u << y);
             m[y] += rise;

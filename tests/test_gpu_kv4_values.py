@@ -147,3 +147,40 @@ def test_a_value_that_is_not_a_number_leaves_the_log_sum_exp(D, n, dtype, bounds
     _near(got, lens, starts, table, cache, hk, page, rows=rows)
     _, wl, _, ltol = R.attention(got[2], cache, page, table, lens, starts, hk, got[3], 0, 0, got[4], got[5])
     assert (np.abs(got[1] - wl) <= ltol).all()
+
+
+@pytest.mark.parametrize("bounds", MANY[1:], ids=["wide", "wide 30"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("binades", [20.0, 24.5, 26.0, 28.0])
+def test_a_first_token_that_dominates_and_holds_nothing(binades, D, dtype, bounds):
+    """A first token with almost all of the weight and a value of 0.  The others' weights lie `binades` below: a reference
+    ten binades below the first maximum leaves them 2^-25 / 2^9 of it as the step of half's subnormals."""
+    rng = np.random.default_rng(23)
+    page, hk, hq, L, n = 16, 1, 4, 260, 30
+    lens, starts, table, cache, q = base._setup(rng, [L], [n], hq, hk, D, page)
+    q[:] = 0
+    q[:, :, 0] = 1
+    for j in range(L):
+        _key(cache, table, page, D, 0, j, binades if j == 0 else 0.0)
+    if dtype == "f16":
+        _value(cache, table, page, D, 0, 0, 0.25, -2.0, 8)
+    else:
+        _value(cache, table, page, D, 0, 0, 0.0, 0.0, 0)
+    got = base._run(lens, starts, table, cache, q, hq, hk, D, page, dtype, scale=float(np.float32(np.log(2))), **bounds)
+    out, ls, q64, scale, u, many = got
+    # by hand: the terms of lm_reference.attention for all but the first token, whose weight is exact and whose value is 0
+    (_, (v, vc, vp)) = R.read(cache, page, table[0, np.arange(L) // page].astype(np.int64) * page + np.arange(L) % page, D)
+    v, s8 = v[:, 0], 8 * vp[:, 0, 0].astype(np.float64)
+    mag = np.abs(v).max(1) + s8
+    p = np.exp(np.where(np.arange(L) == 0, binades, 0.0) * scale - binades * scale)
+    delta = (D + 8) * 2.0 ** -23 * binades * scale
+    for i in range(n):
+        m = L - n + 1 + i
+        w = p[:m] / p[:m].sum()
+        want = w @ v[:m]
+        others = (w[1:] * mag[1:m]).sum()
+        tol = u * np.abs(want) + (2 * delta + 2.0 ** -10 + 2 * m * 2.0 ** -24) * others + m * 2.0 ** -34 * mag[:m].max() + 2.0 ** -24 * w[1:].sum()
+        tol = tol + (2.0 ** -25 if dtype == "f16" else 0)       # results below half's normal range
+        far = np.abs(out[i] - want) - tol
+        assert (far <= 0).all(), (i, far.max(), tol.max(), np.abs(want).max())
