@@ -521,6 +521,13 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
         wide = fmaxf(wide, fmaxf(v[u][0].x, v[u][1].x));
       }
       if (__any_sync(0xffffffffu, most > 8.0f || wide > vtop || fresh)) {
+        if (wide > 65504.0f) {   // an infinite scale: the factor is every row's, also theirs that do not see it
+          wide = 0.0f;
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) wide = fmaxf(wide, v[u][h].x <= 65504.0f ? v[u][h].x : 0.0f);
+        }
 #pragma unroll
         for (int k = 4; k <= 16; k <<= 1) wide = fmaxf(wide, __shfl_xor_sync(0xffffffffu, wide, k));
         float vf = 1.0f;

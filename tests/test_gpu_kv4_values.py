@@ -184,3 +184,19 @@ def test_a_first_token_that_dominates_and_holds_nothing(binades, D, dtype, bound
         tol = tol + (2.0 ** -25 if dtype == "f16" else 0)       # results below half's normal range
         far = np.abs(out[i] - want) - tol
         assert (far <= 0).all(), (i, far.max(), tol.max(), np.abs(want).max())
+
+
+@pytest.mark.parametrize("bounds", MANY, ids=["as is", "wide", "wide 30"])
+@pytest.mark.parametrize("n,dtype", [(2, "f16"), (4, "bf16"), (30, "f16"), (30, "bf16")])
+@pytest.mark.parametrize("what", ["scale", "min", "both"])
+def test_an_infinite_value_reaches_only_the_rows_that_see_it(what, n, dtype, bounds):
+    rng = np.random.default_rng(25)
+    page, hk, hq, L, D = 16, 2, 4, 210, 128
+    lens, starts, table, cache, q = base._setup(rng, [L], [n], hq, hk, D, page)
+    c2 = cache.copy()
+    _value(c2, table, page, D, 0, L - 1, np.inf if what != "min" else 0.2, np.inf if what != "scale" else -1.5)
+    got = base._run(lens, starts, table, c2, q, hq, hk, D, page, dtype, **bounds)
+    assert not np.isfinite(got[0][n - 1]).any()
+    rows = np.ones(got[0].shape[:2], bool)
+    rows[n - 1] = False
+    _near(got, lens, starts, table, cache, hk, page, rows=rows)
