@@ -12,7 +12,7 @@
 //   t = s (q . c) + (m sum(q) - reference),   two packed fma a pair of keys (scale, log2 e and powers of two in s).
 // q itself is multiplied by 16 to keep small elements out of the half's subnormals; a row with an element over 2^11 is
 // brought down by a power of two of its own, which its scores are then multiplied with (a branch no usual row takes).
-// Values: where rows are bfloat16, v = half((s' c' + m') / 2), one fma of halves: eight times finer than the result, as
+// Values: where rows are bfloat16, v = half(s' (c' / 2) + m' / 2), one fma of halves: eight times finer than the result, as
 // fine as the minimum that the cache holds (a half), and within the half's range where s' c' + m' would leave it.  Where
 // rows are half the product takes c' - 8, exact, and the scale goes into the weight's exponent, w = 2^(t - m + log2 s');
 // then sum p = sum w / s', and the values of code 8, m'' = m' + 8 s', are added in fp32, sum w m'' / s'.  (The rounding of
@@ -692,7 +692,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
       if (lane == 0) mbar_arrive(kfull(b));
       if (i + 1 < nt) load_k(place(ck, page_k, have_k));
       hold(vp);
-      __half2 vs[4], vm[4];   // pairs of tokens: scales and minima, halved; of exact values 2^-k
+      __half2 vs[4], vm[4];   // pairs of tokens: scales, and minima halved; of exact values 2^-k
       auto param = [&](int i, int j) { return have_v && j0 + vg * kKvGroup + 8 * vh + j < q.len && kv_finite(vp[i]) ? vp[i] : 0u; };
       bool down = false;      // some k is not 0
       if constexpr (EX) {
@@ -712,7 +712,7 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
         for (int t = 0; t < 4; ++t) {
           const uint32_t y0 = param(2 * t, 2 * t), y1 = param(2 * t + 1, 2 * t + 1);
           const uint32_t sc = __byte_perm(y0, y1, 0x5410), mn = __byte_perm(y0, y1, 0x7632);
-          vs[t] = __hmul2(*(const __half2*)&sc, __float2half2_rn(0.5f));
+          vs[t] = *(const __half2*)&sc;   // (the codes are halved: a scale may be one of the smallest halves)
           vm[t] = __hmul2(*(const __half2*)&mn, __float2half2_rn(0.5f));
         }
       }
@@ -732,9 +732,10 @@ __global__ void __launch_bounds__(KvChunkShape<D, RT>::threads, 1) kv4_chunk_ker
             for (int t = 0; t < 4; ++t) {
               const uint32_t u = vw[blk * WPB * 4 + t * WPB + k] >> (n & 2 ? 8 : 0);
               const uint32_t g = (u & (n & 1 ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;   // 1024 + c, 1024 + 16 c
-              const float off = EX ? 8.0f : 0.0f;
-              const __half2 code = n & 1 ? __hfma2(*(const __half2*)&g, __float2half2_rn(0.0625f), __float2half2_rn(-64.0f - off))
-                                         : __hadd2(*(const __half2*)&g, __float2half2_rn(-1024.0f - off));
+              // c' - 8, or c' / 2
+              const __half2 code = n & 1 ? __hfma2(*(const __half2*)&g, __float2half2_rn(EX ? 0.0625f : 0.03125f), __float2half2_rn(EX ? -72.0f : -32.0f))
+                                   : EX  ? __hadd2(*(const __half2*)&g, __float2half2_rn(-1032.0f))
+                                         : __hfma2(*(const __half2*)&g, __float2half2_rn(0.5f), __float2half2_rn(-512.0f));
               const __half2 v = EX ? code : __hfma2(code, vs[t], vm[t]);
               y[t] = *(const uint32_t*)&v;
             }

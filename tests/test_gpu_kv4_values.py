@@ -200,3 +200,22 @@ def test_an_infinite_value_reaches_only_the_rows_that_see_it(what, n, dtype, bou
     rows = np.ones(got[0].shape[:2], bool)
     rows[n - 1] = False
     _near(got, lens, starts, table, cache, hk, page, rows=rows)
+
+
+@pytest.mark.parametrize("bounds", MANY, ids=["as is", "wide", "wide 30"])
+@pytest.mark.parametrize("n", [1, 30])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_values_below_the_normal_range_of_half(D, n, bounds):
+    """Scales of a few dozen times 2^-24, in bfloat16: rounding a value to half takes 2^-24 of it at most, and half of its
+    minimum as much again."""
+    rng = np.random.default_rng(26)
+    page, hk, hq, L = 16, 1, 4, 200
+    lens, starts, table, cache, q = base._setup(rng, [L], [n], hq, hk, D, page)
+    for j in range(L):
+        k = 4 * int(rng.integers(1, 15)) + 1
+        _value(cache, table, page, D, 0, j, k * 2.0 ** -24, -7 * k * 2.0 ** -24)
+    got = base._run(lens, starts, table, cache, q, hq, hk, D, page, "bf16", **bounds)
+    out, ls, q64, scale, u, many = got
+    want, wl, tol, ltol = R.attention(q64, cache, page, table, lens, starts, hk, scale, 0, 0, u, many)
+    far = np.abs(out - want) - tol - 2.0 ** -24
+    assert (far <= 0).all(), (far.max(), tol.max())
