@@ -25,7 +25,7 @@ def quantise_weights(w: torch.Tensor):
     """Weights [n][k] (k a multiple of 16) to e4m3 with a scale per 128 x 128 block, once: (codes, scales)."""
     n, k = w.shape
     nb, kb = -(-n // 128), -(-k // 128)
-    padded = torch.zeros(nb * 128, kb * 128, device=w.device)
+    padded = torch.zeros(nb * 128, kb * 128, dtype=torch.float32, device=w.device)
     padded[:n, :k] = w.float()
     blocks = padded.view(nb, 128, kb, 128)
     scales = (blocks.abs().amax((1, 3)) / 448.0).clamp_min(1e-30).contiguous()
@@ -131,7 +131,7 @@ class DecoderAttention:
         rows, k = x.shape
         d = ifq.fp8_desc(rows, w.shape[0], k, self.code, self.code)
         codes = self._buffer(name + "_codes", rows, k, torch.float8_e4m3fn)
-        xs = torch.empty(-(-k // 128), rows, device=x.device)
+        xs = torch.empty(-(-k // 128), rows, dtype=torch.float32, device=x.device)
         size = ifq.ifq_fp8_workspace_bytes(d)
         ifq.ifq_fp8_quantize(d, x, codes, xs)
         ifq.ifq_fp8_matmul(d, codes, xs, w, scales, out, self._room(size), size)

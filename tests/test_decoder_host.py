@@ -1,0 +1,47 @@
+"""The decoder block's host side (no GPU): what its calls are given.  The calls that launch kernels are replaced by ones
+that note their arguments."""
+import pytest
+import torch
+
+from paper_1911_08076_gb300 import decoder, ifq
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The arguments of every launching call, in order: (name, arguments)."""
+    seen = []
+    for name in ("ifq_fp8_quantize", "ifq_fp8_matmul", "ifq_kv4_append", "ifq_kv4_attention"):
+        monkeypatch.setattr(ifq, name, lambda *a, _name=name, **k: seen.append((_name, a)))
+    return seen
+
+
+def _block(hidden=64, hq=2, hk=1, d=64, pages=8, page=16, positions=64, **kw):
+    torch.manual_seed(1)
+    return decoder.DecoderAttention(torch.randn((hq + 2 * hk) * d, hidden), torch.randn(hidden, hq * d), hq, hk, d, pages,
+                                    page, positions, **kw)
+
+
+@pytest.fixture
+def default_dtype():
+    was = torch.get_default_dtype()
+    yield torch.set_default_dtype
+    torch.set_default_dtype(was)
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float16, torch.float64])
+def test_scales_are_float_whatever_the_default_type(calls, default_dtype, default):
+    """The library reads and writes scales as floats: a buffer of a 16-bit default type would be half as large."""
+    w = torch.randn(130, 272)
+    codes, scales = decoder.quantise_weights(w)
+    default_dtype(default)
+    codes2, scales2 = decoder.quantise_weights(w)
+    assert scales2.dtype == torch.float32 and torch.equal(scales, scales2)
+    assert torch.equal(codes.view(torch.uint8), codes2.view(torch.uint8))
+    block, seqs = _block(), decoder.PagedSequences(8, 16, device="cpu")
+    block.forward(torch.zeros(5, 64, dtype=torch.bfloat16), seqs.extend([seqs.add()], [5]))
+    assert block.s_qkv.dtype == block.s_out.dtype == block.cos.dtype == block.sin.dtype == torch.float32
+    for name, a in calls:
+        if name == "ifq_fp8_quantize":
+            assert a[3].dtype == torch.float32 and a[3].numel() == -(-a[0].k // 128) * 5
+        if name == "ifq_fp8_matmul":
+            assert a[2].dtype == a[4].dtype == torch.float32
