@@ -1,8 +1,8 @@
 """The attention block of a quantised decoder layer: e4m3 projections around attention over a 4-bit paged cache.
 
 PagedSequences keeps, on the host, which pages belong to which sequence and gives a step's index tensors;
-DecoderAttention holds the quantised weights, the cache and the buffers, and runs a step (a batch of
-sequences with one or several new tokens each) as six calls on the current stream:
+DecoderAttention holds the quantised weights and the cache, and runs a step (a batch of sequences with
+one or several new tokens each) as six calls on the current stream:
 
     quantise x, x Wqkv^T, rotate + quantise + append, attend, quantise the context, context Wo^T
 
@@ -113,24 +113,15 @@ class DecoderAttention:
         self.cos, self.sin = rotation_tables(max_positions, self.rot_dim, rope_base, dev)
         self.pool = ifq.kv4_cache(pages, page_size, kv_heads, head_dim)
         self.cache = torch.zeros(ifq.ifq_kv4_cache_bytes(self.pool), dtype=torch.uint8, device=dev)
-        self._buffers = {}
-        self._workspace = torch.empty(16, dtype=torch.uint8, device=dev)
-
-    def _buffer(self, name, rows, width, dtype):
-        b = self._buffers.get(name)
-        if b is None or b.shape[0] < rows:
-            b = self._buffers[name] = torch.empty(rows, width, dtype=dtype, device=self.cache.device)
-        return b[:rows]
 
     def _room(self, size):
-        if self._workspace.numel() < size:
-            self._workspace = torch.empty(size, dtype=torch.uint8, device=self.cache.device)
-        return self._workspace
+        return torch.empty(max(size, 1), dtype=torch.uint8, device=self.cache.device)
 
-    def _product(self, name, x, w, scales, out):
+    def _product(self, x, w, scales):
         rows, k = x.shape
         d = ifq.fp8_desc(rows, w.shape[0], k, self.code, self.code)
-        codes = self._buffer(name + "_codes", rows, k, torch.float8_e4m3fn)
+        out = torch.empty(rows, w.shape[0], dtype=self.dtype, device=x.device)
+        codes = torch.empty(rows, k, dtype=torch.float8_e4m3fn, device=x.device)
         xs = torch.empty(-(-k // 128), rows, dtype=torch.float32, device=x.device)
         size = ifq.ifq_fp8_workspace_bytes(d)
         ifq.ifq_fp8_quantize(d, x, codes, xs)
@@ -143,17 +134,18 @@ class DecoderAttention:
             raise ValueError("x is a dense [tokens][hidden] tensor of the block's dtype, a row a token of the step")
         rows, hq, hk, d = x.shape[0], self.q_heads, self.kv_heads, self.head_dim
         wide = (hq + 2 * hk) * d
-        self.qkv = self._product("x", x, self.w_qkv, self.s_qkv, self._buffer("qkv", rows, wide, self.dtype))
-        self.q = self._buffer("q", rows, hq * d, self.dtype)
+        # Every step's buffers are its own, from torch's allocator for the current stream (or the graph being captured), so
+        # steps on several streams and replays of captured ones do not meet.  self.qkv, self.q and self.context are the last
+        # step's.
+        qkv = self.qkv = self._product(x, self.w_qkv, self.s_qkv)
+        q = self.q = torch.empty(rows, hq * d, dtype=self.dtype, device=x.device)
         a = ifq.kv4_append_desc(self.pool, rows, hq, self.code, self.rope, self.rot_dim, self.cos.shape[0],
                                 q_stride=wide, k_stride=wide, v_stride=wide)
-        ifq.ifq_kv4_append(a, self.qkv, self.qkv[:, hq * d:], self.qkv[:, (hq + hk) * d:], self.cos, self.sin,
-                           step.positions, step.slots, self.q, self.cache)
-        self.context = self._buffer("context", rows, hq * d, self.dtype)
+        ifq.ifq_kv4_append(a, qkv, qkv[:, hq * d:], qkv[:, (hq + hk) * d:], self.cos, self.sin, step.positions, step.slots,
+                           q, self.cache)
+        context = self.context = torch.empty(rows, hq * d, dtype=self.dtype, device=x.device)
         t = ifq.kv4_attention_desc(self.pool, step.lens.numel(), rows, step.max_q, step.table.shape[1], hq, self.code,
                                    1.0 / math.sqrt(d), self.window, self.sinks, max_len=step.max_len)
         size = ifq.ifq_kv4_attention_workspace_bytes(t)
-        ifq.ifq_kv4_attention(t, self.q, self.cache, step.table, step.lens, step.starts, self.context, None,
-                              self._room(size), size)
-        return self._product("context", self.context, self.w_out, self.s_out,
-                             torch.empty(rows, self.hidden, dtype=self.dtype, device=x.device))
+        ifq.ifq_kv4_attention(t, q, self.cache, step.table, step.lens, step.starts, context, None, self._room(size), size)
+        return self._product(context, self.w_out, self.s_out)

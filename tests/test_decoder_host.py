@@ -45,3 +45,23 @@ def test_scales_are_float_whatever_the_default_type(calls, default_dtype, defaul
             assert a[3].dtype == torch.float32 and a[3].numel() == -(-a[0].k // 128) * 5
         if name == "ifq_fp8_matmul":
             assert a[2].dtype == a[4].dtype == torch.float32
+
+
+def test_steps_share_no_buffers(calls):
+    """Two steps may be under way on two streams, and a captured one is replayed after a larger one: what a step writes
+    belongs to it alone (but for the cache)."""
+    block, seqs = _block(window=8), decoder.PagedSequences(8, 16, device="cpu")
+    ids = [seqs.add(), seqs.add()]
+    held = []
+    for n in (3, 3, 40, 3):
+        step = seqs.extend(ids[:1] if n == 3 else ids[1:], [n])
+        x = torch.zeros(n, 64, dtype=torch.bfloat16)
+        first = len(calls)
+        y = block.forward(x, step)
+        own = [y] + [t for _, a in calls[first:] for t in a[1:] if isinstance(t, torch.Tensor)]
+        shared = {t.untyped_storage().data_ptr() for t in (block.w_qkv, block.s_qkv, block.w_out, block.s_out, block.cos,
+                                                           block.sin, block.cache)}
+        held.append((own, {t.untyped_storage().data_ptr() for t in own if t.numel()} - shared))
+    for i, (_, a) in enumerate(held):
+        for _, b in held[:i]:
+            assert not a & b
