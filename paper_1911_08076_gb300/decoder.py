@@ -41,18 +41,19 @@ def rotation_tables(positions: int, rot_dim: int, base: float = 10000.0, device=
 
 
 class Step:
-    """Index tensors of one step (device), and the sizes that choose the kernels (host)."""
+    """Index tensors of one step (device), the sizes that choose the kernels, and the pool that its pages are of (host)."""
 
-    def __init__(self, positions, slots, lens, starts, table, max_q, max_len):
+    def __init__(self, positions, slots, lens, starts, table, max_q, max_len, pages=None, page_size=None):
         self.positions, self.slots, self.lens, self.starts, self.table = positions, slots, lens, starts, table
         self.max_q, self.max_len = max_q, max_len
+        self.pages, self.page_size = pages, page_size
 
 
 class PagedSequences:
     """Page bookkeeping of a batch of sequences over `pages` pages of `page_size` tokens."""
 
     def __init__(self, pages: int, page_size: int, device="cuda"):
-        self.page_size, self.device = page_size, torch.device(device)
+        self.count, self.page_size, self.device = pages, page_size, torch.device(device)
         self.free: List[int] = list(range(pages - 1, -1, -1))
         self.pages: List[List[int]] = []
         self.length: List[int] = []
@@ -91,7 +92,7 @@ class PagedSequences:
         cat = lambda a, t: dev(np.concatenate(a) if a else np.zeros(0), t)               # noqa: E731
         return Step(cat(positions, np.int32), cat(slots, np.int64), dev(lens, np.int32),
                     dev(np.concatenate([[0], np.cumsum(counts)]), np.int32), dev(table, np.int32),
-                    max([0] + list(counts)), int(lens.max(initial=0)))
+                    max([0] + list(counts)), int(lens.max(initial=0)), self.count, self.page_size)
 
 
 class DecoderAttention:
@@ -129,9 +130,16 @@ class DecoderAttention:
         return out
 
     def forward(self, x: torch.Tensor, step: Step) -> torch.Tensor:
-        """x [tokens][hidden], the tokens of `step` in order -> [tokens][hidden]."""
+        """x [tokens][hidden], the tokens of `step` in order -> [tokens][hidden].  ValueError where a sequence runs past
+        max_positions, or the step's pages are not those of the cache."""
         if x.dtype != self.dtype or not x.is_contiguous() or x.shape != (step.positions.numel(), self.hidden):
             raise ValueError("x is a dense [tokens][hidden] tensor of the block's dtype, a row a token of the step")
+        # (the calls would skip such tokens, and say so in the device's status alone)
+        if self.rope != ifq.IFQ_ROPE_NONE and step.max_len > self.cos.shape[0]:
+            raise ValueError(f"a sequence of {step.max_len} tokens runs past the {self.cos.shape[0]} positions of the tables")
+        if step.page_size not in (None, self.pool.page_size) or (step.pages or 0) > self.pool.pages:
+            raise ValueError(f"the step's pages ({step.pages} of {step.page_size} tokens) are not the cache's "
+                             f"({self.pool.pages} of {self.pool.page_size})")
         rows, hq, hk, d = x.shape[0], self.q_heads, self.kv_heads, self.head_dim
         wide = (hq + 2 * hk) * d
         # Every step's buffers are its own, from torch's allocator for the current stream (or the graph being captured), so

@@ -65,3 +65,26 @@ def test_steps_share_no_buffers(calls):
     for i, (_, a) in enumerate(held):
         for _, b in held[:i]:
             assert not a & b
+
+
+def test_a_step_that_the_block_has_no_positions_or_pages_for_is_refused(calls):
+    block = _block(pages=8, page=16, positions=48)
+    run = lambda seqs, s, n: block.forward(torch.zeros(n, 64, dtype=torch.bfloat16), seqs.extend([s], [n]))   # noqa: E731
+    seqs = decoder.PagedSequences(8, 16, device="cpu")
+    a, b = seqs.add(), seqs.add()
+    run(seqs, a, 47)
+    run(seqs, a, 1)              # position 47, the last
+    before = len(calls)
+    for s, n in ((a, 1), (b, 49)):
+        with pytest.raises(ValueError, match="position"):
+            run(seqs, s, n)
+    for other in (decoder.PagedSequences(9, 16, device="cpu"), decoder.PagedSequences(8, 32, device="cpu")):
+        with pytest.raises(ValueError, match="page"):
+            run(other, other.add(), 1)
+    assert len(calls) == before
+    fewer = decoder.PagedSequences(7, 16, device="cpu")
+    run(fewer, fewer.add(), 1)
+    # without a rotation there are no tables to run past
+    block = _block(pages=8, page=16, positions=48, rope=ifq.IFQ_ROPE_NONE)
+    seqs = decoder.PagedSequences(8, 16, device="cpu")
+    run(seqs, seqs.add(), 60)
