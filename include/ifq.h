@@ -567,8 +567,8 @@ enum { IFQ_ROPE_NONE = 0, IFQ_ROPE_HALVES = 1, IFQ_ROPE_PAIRS = 2 };
  * v may be parts of one projection's rows.  dtype is IFQ_F16 or IFQ_BF16.
  * rot_dim: the rotated dimensions of a head, the first ones, a multiple of 16
  * (<= head_dim; ignored for IFQ_ROPE_NONE); positions: rows of the cos and sin
- * tables.  tokens may be 0.  Strides are multiples of 8 elements and at least
- * a row's width (IFQ_EINVAL otherwise).
+ * tables.  tokens may be 0 (pointers are not looked at then).  Strides are
+ * multiples of 8 elements and at least a row's width (IFQ_EINVAL otherwise).
  */
 typedef struct {
   ifq_kv4_cache cache;
@@ -626,7 +626,8 @@ int ifq_kv4_read(const ifq_kv4_append_desc* d, const void* cache, const int64_t*
  * q_tokens: rows of q; max_q: no sequence has more queries than this;
  * max_pages: entries of a row of page_table; max_len: no sequence is longer
  * (0: max_pages * page_size).  max_q and max_len choose the kernel and its
- * launch shape.  Strides of q and out as in ifq_kv4_append_desc.
+ * launch shape.  Strides of q and out as in ifq_kv4_append_desc.  seqs and
+ * q_tokens may be 0 (pointers other than q_starts are not looked at then).
  */
 typedef struct {
   ifq_kv4_cache cache;
@@ -677,7 +678,8 @@ int ifq_kv4_attention(const ifq_kv4_attention_desc* d, const void* q, const void
  *               sum over k in block b of x[i][k] * w[j][k]
  * x: [m][k] e4m3, w: [n][k] e4m3 (dense rows), x_scale: float [ceil(k/128)][m],
  * w_scale: float [ceil(n/128)][ceil(k/128)].  The last block may hold fewer
- * than 128.  k is a multiple of 16 (IFQ_ESHAPE otherwise); m may be 0.
+ * than 128.  k is a multiple of 16 (IFQ_ESHAPE otherwise); m may be 0 (pointers
+ * are not looked at then).
  * dtype: type of the activations that ifq_fp8_quantize reads (IFQ_F16 or
  * IFQ_BF16), with x_stride elements from row to row (0: dense; a multiple of
  * 8).  out_dtype: IFQ_F16, IFQ_BF16 or IFQ_F32, with out_stride elements from

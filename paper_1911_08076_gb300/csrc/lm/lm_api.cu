@@ -380,6 +380,7 @@ int ifq_kv4_append(const ifq_kv4_append_desc* d, const void* q, const void* k, c
   if ((rc = stride_of(d->q_out_stride, (long long)d->q_heads * D, &a.q_out_stride))) return rc;
   if ((rc = stride_of(d->k_stride, (long long)d->cache.kv_heads * D, &a.k_stride))) return rc;
   if ((rc = stride_of(d->v_stride, (long long)d->cache.kv_heads * D, &a.v_stride))) return rc;
+  if (!d->tokens) return IFQ_OK;   // (before the pointers: those of empty tensors may be NULL)
   if (!k || !v || !slots || !cache || (q && (!q_out || d->q_heads < 1))) return IFQ_EINVAL;
   if (d->rope != IFQ_ROPE_NONE && (!cos || !sin || !positions)) return IFQ_EINVAL;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q ? q_out : nullptr) || !aligned16(cache) ||
@@ -400,7 +401,6 @@ int ifq_kv4_append(const ifq_kv4_append_desc* d, const void* q, const void* k, c
   a.rot = d->rot_dim;
   a.positions = d->positions;
   a.vec = aligned16(cos) && aligned16(sin);
-  if (!d->tokens) return IFQ_OK;
   const int HB = kv4_warp_heads(D);
   const dim3 grid(ceil_div(d->tokens, kAppendWarps), ceil_div(a.q_heads, HB) + 2 * ceil_div(d->cache.kv_heads, HB));
   if (grid.y > 65535) return IFQ_ERANGE;
@@ -416,9 +416,11 @@ int ifq_kv4_read(const ifq_kv4_append_desc* d, const void* cache, const int64_t*
   size_t bytes;
   int rc = check_cache(&d->cache, &bytes);
   if (rc) return rc;
-  if (d->tokens < 0 || !is16(d->dtype) || !cache || !slots) return IFQ_EINVAL;
+  if (d->tokens < 0 || !is16(d->dtype)) return IFQ_EINVAL;
+  if (!d->tokens) return IFQ_OK;
+  if (!cache || !slots) return IFQ_EINVAL;
   if (!aligned16(cache) || !aligned16(k_out) || !aligned16(v_out) || !aligned(slots, 8)) return IFQ_EALIGN;
-  if (!d->tokens || (!k_out && !v_out)) return IFQ_OK;
+  if (!k_out && !v_out) return IFQ_OK;
   const dim3 grid(ceil_div(d->tokens, kAppendWarps), 2 * ceil_div(d->cache.kv_heads, kv4_warp_heads(d->cache.head_dim)));
   if (grid.y > 65535) return IFQ_ERANGE;
   KvReadArgs a;
@@ -450,14 +452,15 @@ int ifq_kv4_attention(const ifq_kv4_attention_desc* d, const void* q, const void
   AttnPlan p;
   int rc = check_attention(d, &a);
   if (rc) return rc;
-  if (!q || !cache || !lens || !out || (!page_table && d->max_pages > 0)) return IFQ_EINVAL;
+  const bool some = d->q_tokens && d->seqs;
+  if (some && (!q || !cache || !lens || !out || (!page_table && d->max_pages > 0))) return IFQ_EINVAL;
   if (!q_starts && (d->q_tokens != d->seqs)) return IFQ_ESHAPE;
+  if (!some) return IFQ_OK;
   if (!aligned16(q) || !aligned16(cache) || !aligned16(out) || !aligned(page_table, 4) || !aligned(lens, 4) ||
       !aligned(q_starts, 4) || !aligned(lse, 4) || !aligned16(ws))
     return IFQ_EALIGN;
   if ((rc = plan_attention(d, a, &p))) return rc;
   if (p.ws && (!ws || ws_bytes < p.ws)) return IFQ_EWORKSPACE;
-  if (!d->q_tokens || !d->seqs) return IFQ_OK;
   a.q = (const uint16_t*)q;
   a.cache = (const uint8_t*)cache;
   a.table = page_table;
@@ -490,6 +493,7 @@ int ifq_fp8_quantize(const ifq_fp8_desc* d, const void* x, void* codes, float* s
   Fp8QuantArgs a;
   if (!is16(d->dtype)) return IFQ_EINVAL;
   if ((rc = stride_of(d->x_stride, d->k, &a.x_stride))) return rc;
+  if (!d->m) return IFQ_OK;
   if (!x || !codes || !scales) return IFQ_EINVAL;
   if (!aligned16(x) || !aligned16(codes) || !aligned(scales, 4)) return IFQ_EALIGN;
   a.x = (const uint16_t*)x;
@@ -498,7 +502,6 @@ int ifq_fp8_quantize(const ifq_fp8_desc* d, const void* x, void* codes, float* s
   a.m = d->m;
   a.k = d->k;
   a.kb = ceil_div(d->k, kFp8Block);
-  if (!a.m) return IFQ_OK;
   const dim3 grid(ceil_div(a.m, kFp8QuantWarps), ceil_div(a.kb, 2 * kFp8Pass));
   if (grid.y > 65535) return IFQ_ERANGE;
   return done(d->dtype == IFQ_BF16 ? launch_k(fp8_quantize_kernel<true>, grid, dim3(32 * kFp8QuantWarps), 0, S(stream), a)
@@ -519,11 +522,11 @@ int ifq_fp8_matmul(const ifq_fp8_desc* d, const void* x, const float* x_scale, c
   if (rc) return rc;
   if (!is16(d->out_dtype) && d->out_dtype != IFQ_F32) return IFQ_EINVAL;
   if (d->out_stride < 0 || (d->out_stride != 0 && d->out_stride < d->n)) return IFQ_EINVAL;
+  if (!d->m) return IFQ_OK;
   if (!x || !x_scale || !w || !w_scale || !out) return IFQ_EINVAL;
   if (!aligned16(x) || !aligned16(w) || !aligned16(out) || !aligned16(ws) || !aligned(x_scale, 4) || !aligned(w_scale, 4))
     return IFQ_EALIGN;
   (void)ws_bytes;
-  if (!d->m) return IFQ_OK;
   if (!get_encode()) return IFQ_ECUDA;
   const Fp8Operands o = {x, x_scale, w, w_scale, out, S(stream)};
   if (d->m <= 16) return run_fp8<16, true>(d, o);
