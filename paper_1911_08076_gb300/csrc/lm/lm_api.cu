@@ -376,8 +376,8 @@ int ifq_kv4_append(const ifq_kv4_append_desc* d, const void* q, const void* k, c
   if (d->rope != IFQ_ROPE_NONE && (d->rot_dim < 16 || d->rot_dim > D || d->rot_dim % 16 != 0)) return IFQ_ESHAPE;
   if (d->rope != IFQ_ROPE_NONE && d->positions < 1) return IFQ_EINVAL;
   KvAppendArgs a = {};
-  if ((rc = stride_of(d->q_stride, (long long)d->q_heads * D, &a.q_stride))) return rc;
-  if ((rc = stride_of(d->q_out_stride, (long long)d->q_heads * D, &a.q_out_stride))) return rc;
+  if (q && (rc = stride_of(d->q_stride, (long long)d->q_heads * D, &a.q_stride))) return rc;
+  if (q && (rc = stride_of(d->q_out_stride, (long long)d->q_heads * D, &a.q_out_stride))) return rc;
   if ((rc = stride_of(d->k_stride, (long long)d->cache.kv_heads * D, &a.k_stride))) return rc;
   if ((rc = stride_of(d->v_stride, (long long)d->cache.kv_heads * D, &a.v_stride))) return rc;
   if (!d->tokens) return IFQ_OK;   // (before the pointers: those of empty tensors may be NULL)

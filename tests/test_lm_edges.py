@@ -46,3 +46,14 @@ def test_a_step_without_tokens(monkeypatch, seqs):
     pages = decoder.PagedSequences(8, 16, device="cpu")
     step = pages.extend([pages.add() for _ in range(seqs)], [0] * seqs)
     assert block.forward(torch.zeros(0, 64, dtype=torch.bfloat16), step).shape == (0, 64)
+
+
+def test_a_stride_of_q_does_not_count_without_q():
+    pool = ifq.kv4_cache(2, 16, 2, 128)
+    for stride in (0, 8, 1000, 1024, 12):
+        for q_out in (0, 8):
+            d = ifq.kv4_append_desc(pool, 0, 8, ifq.IFQ_BF16, ifq.IFQ_ROPE_NONE, q_stride=stride, q_out_stride=q_out)
+            ifq.ifq_kv4_append(d, None, FAKE, FAKE, None, None, None, FAKE, None, FAKE, stream=0)
+    d = ifq.kv4_append_desc(pool, 0, 8, ifq.IFQ_BF16, ifq.IFQ_ROPE_NONE, q_stride=8)
+    with pytest.raises(ifq.IfqError):
+        ifq.ifq_kv4_append(d, FAKE, FAKE, FAKE, None, None, None, FAKE, FAKE, FAKE, stream=0)
