@@ -526,7 +526,9 @@ int ifq_device_status(void* stream, int* status);
  * The attention block of a quantised decoder.
  *
  * The same conventions hold for these calls (status, ownership, streams, no
- * allocation).  Types of 16- and 32-bit tensors:
+ * allocation).  Rows, columns, tokens, and the tokens of a row of the page
+ * table are at most 2^31 - 1024 (IFQ_ERANGE otherwise).  Types of 16- and
+ * 32-bit tensors:
  */
 enum { IFQ_F16 = 1, IFQ_BF16 = 2, IFQ_F32 = 3 };
 

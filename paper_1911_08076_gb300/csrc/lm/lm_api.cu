@@ -24,6 +24,9 @@ inline bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) =
 inline int done(cudaError_t e) { return e == cudaSuccess ? IFQ_OK : IFQ_ECUDA; }
 inline bool is16(int dtype) { return dtype == IFQ_F16 || dtype == IFQ_BF16; }
 
+// Rows, tokens and columns are ints, and so are the ends of the blocks that they are rounded up to.
+constexpr int kMaxSize = INT_MAX - 1023;
+
 std::mutex g_lm_mu;   // guards the per-device state below
 
 // The kernel instance of a head size and type: f(head size, bfloat16) with both as types.
@@ -88,8 +91,8 @@ int check_attention(const ifq_kv4_attention_desc* d, KvAttnArgs* a) {
       d->window < 0 || d->sinks < 0 || !is16(d->dtype) || !std::isfinite(d->scale))
     return IFQ_EINVAL;
   if (d->q_heads % d->cache.kv_heads != 0) return IFQ_ESHAPE;
-  if (d->q_heads > 65536 || (long long)d->max_pages * d->cache.page_size > INT_MAX ||
-      (long long)d->max_q * d->q_heads > INT_MAX)
+  if (d->q_heads > 65536 || (long long)d->max_pages * d->cache.page_size > kMaxSize ||
+      (long long)d->max_q * d->q_heads > kMaxSize || d->seqs > kMaxSize || d->q_tokens > kMaxSize)
     return IFQ_ERANGE;
   const long long width = (long long)d->q_heads * d->cache.head_dim;
   if ((rc = stride_of(d->q_stride, width, &a->q_stride))) return rc;
@@ -371,7 +374,7 @@ int ifq_kv4_append(const ifq_kv4_append_desc* d, const void* q, const void* k, c
   if (rc) return rc;
   const int D = d->cache.head_dim;
   if (d->tokens < 0 || d->q_heads < 0 || !is16(d->dtype)) return IFQ_EINVAL;
-  if (d->q_heads > 65536) return IFQ_ERANGE;
+  if (d->q_heads > 65536 || d->tokens > kMaxSize) return IFQ_ERANGE;
   if (d->rope != IFQ_ROPE_NONE && d->rope != IFQ_ROPE_HALVES && d->rope != IFQ_ROPE_PAIRS) return IFQ_EINVAL;
   if (d->rope != IFQ_ROPE_NONE && (d->rot_dim < 16 || d->rot_dim > D || d->rot_dim % 16 != 0)) return IFQ_ESHAPE;
   if (d->rope != IFQ_ROPE_NONE && d->positions < 1) return IFQ_EINVAL;
@@ -417,6 +420,7 @@ int ifq_kv4_read(const ifq_kv4_append_desc* d, const void* cache, const int64_t*
   int rc = check_cache(&d->cache, &bytes);
   if (rc) return rc;
   if (d->tokens < 0 || !is16(d->dtype)) return IFQ_EINVAL;
+  if (d->tokens > kMaxSize) return IFQ_ERANGE;
   if (!d->tokens) return IFQ_OK;
   if (!cache || !slots) return IFQ_EINVAL;
   if (!aligned16(cache) || !aligned16(k_out) || !aligned16(v_out) || !aligned(slots, 8)) return IFQ_EALIGN;
@@ -484,6 +488,7 @@ static int check_fp8(const ifq_fp8_desc* d) {
   if (!d) return IFQ_EINVAL;
   if (d->m < 0 || d->n < 1 || d->k < 1) return IFQ_EINVAL;
   if (d->k % 16 != 0) return IFQ_ESHAPE;
+  if (d->m > kMaxSize || d->n > kMaxSize || d->k > kMaxSize) return IFQ_ERANGE;
   return IFQ_OK;
 }
 

@@ -57,3 +57,33 @@ def test_a_stride_of_q_does_not_count_without_q():
     d = ifq.kv4_append_desc(pool, 0, 8, ifq.IFQ_BF16, ifq.IFQ_ROPE_NONE, q_stride=8)
     with pytest.raises(ifq.IfqError):
         ifq.ifq_kv4_append(d, FAKE, FAKE, FAKE, None, None, None, FAKE, FAKE, FAKE, stream=0)
+
+
+def _status(f, *a, **k):
+    with pytest.raises(ifq.IfqError) as e:
+        f(*a, **k)
+    return e.value.status
+
+
+def test_sizes_that_end_past_31_bits():
+    """Sizes so near 2^31 that the end of a last block would lie past it are refused, not wrapped."""
+    top = 2 ** 31 - 1
+    for m, n, k in ((top, 8, 16), (8, top, 16), (8, 8, 2 ** 31 - 16), (top - 1022, 8, 16)):
+        d = ifq.fp8_desc(m, n, k)
+        assert _status(ifq.ifq_fp8_matmul, d, FAKE, FAKE, FAKE, FAKE, FAKE, stream=0) == ifq.IFQ_ERANGE
+        assert _status(ifq.ifq_fp8_quantize, d, FAKE, FAKE, FAKE, stream=0) == ifq.IFQ_ERANGE
+        assert _status(ifq.ifq_fp8_workspace_bytes, d) == ifq.IFQ_ERANGE
+    assert ifq.ifq_fp8_workspace_bytes(ifq.fp8_desc(top - 1023, top - 1023, 2 ** 31 - 1024)) == 0
+    pool = ifq.kv4_cache(2, 16, 2, 128)
+    d = ifq.kv4_append_desc(pool, top, 2, ifq.IFQ_BF16, ifq.IFQ_ROPE_NONE)
+    assert _status(ifq.ifq_kv4_append, d, None, FAKE, FAKE, None, None, None, FAKE, None, FAKE, stream=0) == ifq.IFQ_ERANGE
+    assert _status(ifq.ifq_kv4_read, d, FAKE, FAKE, FAKE, FAKE, stream=0) == ifq.IFQ_ERANGE
+    ok = dict(seqs=2, q_tokens=2, max_q=1, max_pages=4, q_heads=8, dtype=ifq.IFQ_BF16, scale=0.1)
+    for name, value in (("seqs", top), ("q_tokens", top), ("max_pages", 2 ** 27 - 1), ("max_q", top // 8), ("max_len", top)):
+        d = ifq.kv4_attention_desc(pool, **{**ok, name: value})
+        want = ifq.IFQ_OK if name == "max_len" else ifq.IFQ_ERANGE     # (a bound of any size says nothing)
+        if want:
+            assert _status(ifq.ifq_kv4_attention_workspace_bytes, d) == want
+        else:
+            ifq.ifq_kv4_attention_workspace_bytes(d)
+    ifq.ifq_kv4_attention_workspace_bytes(ifq.kv4_attention_desc(pool, **{**ok, "max_pages": 2 ** 27 - 64}))
