@@ -152,7 +152,7 @@ int plan_attention(const ifq_kv4_attention_desc* d, const KvAttnArgs& a, AttnPla
   if (d->max_len > 0) reach = std::min<long long>(reach, d->max_len);
   if (d->window > 0) reach = std::min<long long>(reach, (long long)d->window + d->sinks + d->max_q + 2 * kKvGroup);
   p->nt = rows > 8 && D < 256 ? 2 : 1;   // (two tiles of size 256 do not fit the registers)
-  if (d->seqs <= 65535 && take_chunk(D, rows, p->nt, reach * d->seqs * a.kv_heads)) {
+  if (d->seqs <= 65535 && a.kv_heads <= 65535 && take_chunk(D, rows, p->nt, reach * d->seqs * a.kv_heads)) {
     p->chunk = rows > 128 && D < 256 ? 2 : 1;
     const int R = 128 * p->chunk;
     p->blocks = (int)((rows + R - 1) / R);
