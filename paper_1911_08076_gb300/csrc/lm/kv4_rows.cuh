@@ -351,6 +351,8 @@ __global__ void __launch_bounds__(KvRowsShape<D>::threads, kv_rows_per_sm(D, NT)
           }
         }
       }
+      // the block's memory is there until its last copies have landed, also where a computing warp gave up
+      for (int i = max(k - ST, 0); i < k; ++i) mbar_wait_backoff(bar_full + 8 * (w * ST + i % ST), (i / ST) & 1, 100);
     }
     return;
   }
