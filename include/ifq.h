@@ -653,9 +653,12 @@ int ifq_kv4_attention_workspace_bytes(const ifq_kv4_attention_desc* d, size_t* b
  * ifq_kv4_attention -- out = softmax(scale * q K^T) V over the visible tokens,
  * with K and V the values the cache holds.  Codes enter the products as exact
  * numbers; scales, minima, sums and the softmax are in IEEE single, the weights
- * of V in half.  Where a key head has more than 32 rows
+ * of V in half: eleven bits down to 2^-20 of the largest product of a weight and
+ * a value's scale.  Where a key head has more than 32 rows
  * (max_q * q_heads / kv_heads) and dtype is bfloat16, the values of V are
- * rounded to half as well.
+ * rounded to half as well.  A token whose value parameters are not finite makes
+ * the results of the queries that see it not finite and leaves their lse; one
+ * whose key parameters are NaN makes both NaN.
  * out (device): [q_tokens] rows of [q_heads][head_dim], dtype.  lse (device,
  * may be NULL): float [q_tokens][q_heads], the log of the softmax's sum.  A
  * query that sees nothing gives zeros and -infinity.
@@ -665,7 +668,7 @@ int ifq_kv4_attention_workspace_bytes(const ifq_kv4_attention_desc* d, size_t* b
  * Device-side checks: a length that is negative or past the table's row,
  * q_starts out of order or past q_tokens, or more queries than max_q set
  * IFQ_ERANGE and leave that sequence's rows unwritten; a page past the cache
- * sets IFQ_ERANGE and its values are undefined.
+ * sets IFQ_ERANGE and its values are undefined (but the same in every call).
  * ws (device): ifq_kv4_attention_workspace_bytes bytes, 16-byte aligned; calls
  * in flight at the same time must not share it.  Results do not depend on
  * what it holds, nor on timing.
@@ -708,11 +711,11 @@ int ifq_fp8_quantize(const ifq_fp8_desc* d, const void* x, void* codes, float* s
 int ifq_fp8_workspace_bytes(const ifq_fp8_desc* d, size_t* bytes);
 
 /*
- * ifq_fp8_matmul -- the product above.  Products and their sums within a block
- * are the tensor cores' in IEEE single, the scaled blocks are added in IEEE
- * single, and the sum is rounded once to out_dtype.  All pointers are device
- * pointers, 16-byte aligned (scales 4; out 16, and out rows start on a multiple
- * of their element).
+ * ifq_fp8_matmul -- the product above.  Products are exact, their sums within a
+ * block the tensor cores' in single precision (which may truncate), the scaled
+ * blocks are added in IEEE single, and the sum is rounded once to out_dtype.
+ * All pointers are device pointers, 16-byte aligned (scales 4; out 16, and out
+ * rows start on a multiple of their element).
  */
 int ifq_fp8_matmul(const ifq_fp8_desc* d, const void* x, const float* x_scale, const void* w, const float* w_scale,
                    void* out, void* ws, size_t ws_bytes, void* stream);

@@ -6,8 +6,7 @@
 // In both the attention kernels take a word apart with masks alone into pairs of codes that are
 // operand registers of the tensor cores (see kv4_attention.cuh).
 //
-// Both kernels move each value once and do little with it: they are bound by memory (and by their
-// launch where a call has few tokens).
+// Both kernels move each value once: memory is their floor (and their launch where a call has few tokens).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -113,7 +112,7 @@ struct KvAppendArgs {
 // Both kernels: eight dimensions (16 bytes) a lane, so D / 8 lanes a head and 256 / D heads a warp at once, kKvPass
 // times; a warp's heads are of one token and one kind (q, k or v).  blockIdx.y: the kind and its heads, blockIdx.x:
 // eight tokens.  The heads' loads are all under way before the first is used, and cos and sin are read once for them
-// (8191 tokens of 32 + 2 x 8 heads of 128: 57 us, 2.6 TB/s, with 60 % of the issue slots at work on the exact steps, and
+// (8191 tokens of 32 + 2 x 8 heads of 128: 57 us, 2.6 TB/s of DRAM traffic, with 60 % of the issue slots at work on the exact steps, and
 // 14 us reading them back; with a head a warp and 8-byte loads 104 and 31).
 constexpr int kAppendWarps = 8, kKvPass = 4;
 __host__ __device__ constexpr int kv4_warp_heads(int D) { return kKvPass * 256 / D; }

@@ -3,8 +3,9 @@
 // A block takes 128 RT rows of a key head (query tokens x the heads that share it) and their keys in tiles of 128:
 //   S[row][key] = sum_d q[row][d] c[key][d]    (half x half, both operands in shared memory),
 //   O[row][d]  += sum_key p[row][key] v[key][d] (p from tensor memory, over S's columns; v in shared memory).
-// Bound by the tensor cores' half rate in the limit, by the softmax's instructions beside them as measured: 2 x 2048
-// queries of 32 heads of 128 on up to 8192 tokens in 278 us, 0.9 to 1.0 PFLOP/s, with 30 % of the tensor pipe.
+// Bound by the tensor cores' half rate in the limit, by the chain of product, softmax and product of a tile as measured:
+// 2 x 2048 queries of 32 heads of 128 on 8192 tokens each in 656 us (bfloat16; half 840), 0.73 PFLOP/s, with 36 % of the
+// tensor pipe and 40 % of the issue slots.
 //
 // Keys: codes are expanded to halves as the subnormals c 2^-24 and 16 c 2^-24 (masks alone, as in kv4_rows.cuh; q's
 // elements stand in the order that leaves the codes of a word in, with the factors 1/16 in them).  Products with them
@@ -23,7 +24,7 @@
 // its first maximum, and again below a later one when a sum of 8 weights passes 61440, or for exact values one 2^15.5 (no
 // half overflows before), in whole powers of two: weights keep their 11 bits down to 2^-23 of that maximum and vanish at
 // 2^-34.  (With the reference at the maximum a first token that takes almost all left the others 10 bits fewer.  A limit of
-// 2^15 for the sum, which is passed more often, took 675 us where this takes 655.)
+// 2^15 for the sum, which is passed more often, took 675 us where this takes 655, on 2 x 8192 tokens.)
 // A value whose parameters are not finite must reach only the rows that see it, and not their log-sum-exp: its operand is a
 // number, and a block that met one looks its keys' parameters through again at the end, for the rows that see them.
 //

@@ -22,10 +22,10 @@
 // kv4_join_kernel adds (the block itself, where its warps have all of it).  One more warp fetches for all, a lane a group
 // (page lookup and one bulk copy of the group's contiguous bytes), three units ahead and across the ends of items.
 //
-// Measured, the join with it: one sequence of 131072 tokens, 8 key heads of 128 and 4 rows each, 36.6 us (3.9 TB/s); 48
-// sequences of up to 8192 57.7 us (3.7 TB/s); 64 windows of 1028 tokens 7.8 us; 40 rows on 16 sequences of up to 4096,
-// three passes, 54.5 us.  Issue slots are 52 % busy, with 268 instructions a group: bound by the latency of 3.5
-// computing warps a scheduler.
+// Measured, the join with it: one sequence of 131072 tokens, 8 key heads of 128 and 4 rows each, 36.7 us (3.9 TB/s); 48
+// sequences of up to 8192, 195780 tokens in all, 54 us (4.0 TB/s); 64 windows of 1028 tokens 7.9 us from L2, 15 from
+// memory; 40 rows on 16 sequences of 4096, three passes, 61 us.  Issue slots are 50 % busy, with 268 instructions a group:
+// bound by the latency of 3.5 computing warps a scheduler.
 #pragma once
 #include "kv4_attention.cuh"
 
