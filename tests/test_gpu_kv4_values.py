@@ -219,3 +219,21 @@ def test_values_below_the_normal_range_of_half(D, n, bounds):
     want, wl, tol, ltol = R.attention(q64, cache, page, table, lens, starts, hk, scale, 0, 0, u, many)
     far = np.abs(out - want) - tol - 2.0 ** -24
     assert (far <= 0).all(), (far.max(), tol.max())
+
+
+@pytest.mark.parametrize("bounds", MANY, ids=["as is", "wide", "wide 30"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("at,seen", [(60, 0), (100, 20), (1, 30), (3, 0)])
+def test_a_value_that_is_not_a_number_beside_a_window(at, seen, dtype, bounds):
+    """Queries at 120 to 149 see their last 40 tokens and the first three: token 60 is seen by none, 100 by those below 140."""
+    rng = np.random.default_rng(28)
+    page, hk, hq, L, n, D = 32, 2, 8, 150, 30, 128
+    lens, starts, table, cache, q = base._setup(rng, [L], [n], hq, hk, D, page)
+    c2 = cache.copy()
+    _value(c2, table, page, D, 0, at, np.nan, 0.5)
+    got = base._run(lens, starts, table, c2, q, hq, hk, D, page, dtype, 40, 3, **bounds)
+    assert np.isnan(got[0][:seen]).all()
+    rows = np.broadcast_to((np.arange(n) >= seen)[:, None], got[0].shape[:2])
+    _near(got, lens, starts, table, cache, hk, page, rows=rows, window=40, sinks=3)
+    _, wl, _, ltol = R.attention(got[2], cache, page, table, lens, starts, hk, got[3], 40, 3, got[4], got[5])
+    assert (np.abs(got[1] - wl) <= ltol).all()
