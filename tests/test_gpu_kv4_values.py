@@ -1,8 +1,7 @@
 """Attention over values of mixed sizes, constant value rows, dominant tokens and parameters that are no numbers.
 
 Tolerances are those of lm_reference.attention, whose term for rounded weights goes with s' c' + |m'|; the kernels round the
-weights of c' - 8 (|c' - 8| <= 8) and add the minima unrounded, which the term of _near adds: 2^-11 of sum p 8 s' / sum p, and
-for weights below half's normal range `small` of the largest 8 s' or |V| a token."""
+weights of c' - 8 (|c' - 8| <= 8) and add the minima unrounded, which the term of _near adds: 2^-11 of sum p 8 s' / sum p."""
 import numpy as np
 import pytest
 import torch
@@ -33,7 +32,7 @@ def _key(cache, table, page, D, seq, j, value):
     g[:, 16 * D + 4 * row:16 * D + 4 * row + 4] = np.array([0, value], np.float16).view(np.uint8)
 
 
-def _near(got, lens, starts, table, cache, hk, page, small=0.0, rows=None, lse=True, window=0, sinks=0):
+def _near(got, lens, starts, table, cache, hk, page, rows=None, lse=True, window=0, sinks=0):
     out, ls, q64, scale, u, many = got
     want, wl, tol, ltol = R.attention(q64, cache, page, table, lens, starts, hk, scale, window, sinks, u, many)
     # the same attention over 8 s' in place of the values: its mean, and the largest
@@ -47,13 +46,6 @@ def _near(got, lens, starts, table, cache, hk, page, small=0.0, rows=None, lse=T
     mean, _, _, _ = R.attention(q64, eight, page, table, lens, starts, hk, scale, window, sinks, 0.0)
     with np.errstate(all="ignore"):
         tol = tol + 2.0 ** -11 * mean
-    if small:
-        top = 0.0
-        for s, n in enumerate(lens):
-            j = np.arange(n)
-            _, (v, _, vp) = R.read(cache, page, table[s, j // page].astype(np.int64) * page + j % page, D)
-            top = max(top, np.abs(v).max(), 8 * float(vp[..., 0].max()))
-        tol = tol + small * top * int(max(lens))
     keep = np.ones(out.shape[:2], bool) if rows is None else rows
     far = np.abs(out[keep] - want[keep]) - tol[keep]
     assert (far <= 0).all(), (np.nanmax(far), np.isnan(far).sum(), np.argwhere(~(far <= 0))[:5])
