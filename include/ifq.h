@@ -720,6 +720,138 @@ int ifq_fp8_workspace_bytes(const ifq_fp8_desc* d, size_t* bytes);
 int ifq_fp8_matmul(const ifq_fp8_desc* d, const void* x, const float* x_scale, const void* w, const float* w_scale,
                    void* out, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * The rest of a quantised decoder layer, and its answers: products with weights
+ * in 4 bits, the norm between the blocks, and scores of tokens.  Sizes as for
+ * the attention block: at most 2^31 - 1024 (IFQ_ERANGE otherwise).
+ */
+
+/*
+ * Weights held in 4 bits: w[j][c] = code * scale + min, rounded once to dtype
+ * (IFQ_F16 or IFQ_BF16), with a scale and a minimum of that type for each row j
+ * and group of 32, 64 or 128 along k (IFQ_EUNSUPPORTED otherwise; the last group
+ * may hold fewer).  k is a multiple of 8 (IFQ_ESHAPE otherwise).  gated = 0: n
+ * rows.  gated = 1: a pair of matrices of n rows each, 2n rows in all, the
+ * gate's first.
+ */
+typedef struct {
+  int n, k, group;
+  int dtype;
+  int gated;
+} ifq_w4_weights;
+
+/* Bytes of the packed weights (host, pure). */
+int ifq_w4_bytes(const ifq_w4_weights* w, size_t* bytes);
+
+/*
+ * ifq_w4_pack -- the layout that the products read, made once per matrix.
+ * codes (device): bytes [rows][k / 2], the even column in the low half of a
+ * byte; scales, mins (device): dtype [rows][ceil(k / group)].  packed (device):
+ * ifq_w4_bytes bytes, all of them written.  codes are 4-byte aligned, scales and
+ * mins 2, packed 16.  The layout is the library's own; packed weights may be
+ * copied as bytes.
+ */
+int ifq_w4_pack(const ifq_w4_weights* w, const void* codes, const void* scales, const void* mins, void* packed,
+                void* stream);
+
+/* What the gate's products go through before they meet the others'. */
+enum { IFQ_ACT_SILU = 1, IFQ_ACT_GELU = 2, IFQ_ACT_GELU_TANH = 3 };
+
+/*
+ * A product of m rows.  Strides count elements from row to row (0: dense); x's
+ * is a multiple of 8.  out_dtype: IFQ_F16, IFQ_BF16 or IFQ_F32, the type of out
+ * and residual.  act: of ifq_w4_gated (ignored by ifq_w4_matmul).  m may be 0
+ * (pointers are not looked at then).  All device pointers are 16-byte aligned.
+ */
+typedef struct {
+  ifq_w4_weights weights;
+  int m;
+  int out_dtype;
+  int act;
+  int64_t x_stride, out_stride, residual_stride;
+} ifq_w4_desc;
+
+/*
+ * ifq_w4_matmul -- out[i][j] = sum over c of x[i][c] * w[j][c] (+ residual[i][j]).
+ * x (device): [m][k] of the weights' dtype; residual (device): [m][n], may be
+ * NULL, and may be out where the strides agree.  Products are exact, sums in
+ * single precision (which the tensor cores may truncate), rounded once to
+ * out_dtype.  Results do not depend on timing; they may on m, which chooses the
+ * kernel and so the order of the sums.  What is not finite in a row of x or of
+ * the weights stays in that row of out, or column.  weights.gated is 0.
+ */
+int ifq_w4_matmul(const ifq_w4_desc* d, const void* x, const void* packed, void* out, const void* residual,
+                  void* stream);
+
+/*
+ * ifq_w4_gated -- out[i][j] = act(sum x[i][c] * w[j][c]) * sum x[i][c] * w[n+j][c]:
+ * both projections of a gated feed-forward block, the activation and the product
+ * in one launch, with sums as above, act in single precision, and one rounding.
+ *   IFQ_ACT_SILU: a / (1 + e^-a);  IFQ_ACT_GELU: a * (1 + erf(a / sqrt 2)) / 2;
+ *   IFQ_ACT_GELU_TANH: a * (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2.
+ * weights.gated is 1, out_dtype the weights' dtype.  residual_stride is not read.
+ */
+int ifq_w4_gated(const ifq_w4_desc* d, const void* x, const void* packed, void* out, void* stream);
+
+/*
+ * Rows of dim values of dtype (IFQ_F16 or IFQ_BF16).  dim is a multiple of 8
+ * (IFQ_ESHAPE) and at most 65536 (IFQ_EUNSUPPORTED); eps is finite and >= 0.
+ * Strides count elements from row to row (0: dense), multiples of 8.
+ */
+typedef struct {
+  int rows, dim;
+  int dtype;
+  float eps;
+  int64_t x_stride, residual_stride, sum_stride, out_stride;
+} ifq_norm_desc;
+
+/*
+ * ifq_rms_norm -- out = h * weight / sqrt(mean(h * h) + eps), with h = x, or with
+ * a residual h = x + residual rounded to dtype, which is written to sum (may be
+ * NULL).  Squares and their sum in single precision (in double where they leave
+ * its range), out rounded once.  weight (device): dtype [dim].  sum and out may
+ * each be x or residual, where the strides agree, but not the same buffer.
+ * Without a residual sum is NULL.
+ * rows may be 0.  Pointers are 16-byte aligned.
+ */
+int ifq_rms_norm(const ifq_norm_desc* d, const void* x, const void* residual, const void* weight, void* sum, void* out,
+                 void* stream);
+
+/*
+ * Rows of vocab logits of dtype (IFQ_F16, IFQ_BF16 or IFQ_F32), stride elements
+ * from row to row (0: dense; any number of them).  top: how many of the
+ * likeliest tokens are wanted, 0 to 32 (IFQ_EUNSUPPORTED) and at most vocab
+ * (IFQ_ESHAPE).  scale: finite, > 0 (one over a temperature).
+ */
+typedef struct {
+  int rows, vocab;
+  int dtype;
+  int top;
+  float scale;
+  int64_t stride;
+} ifq_scores_desc;
+
+/*
+ * ifq_token_scores -- with z = scale * logits of a row and p = softmax(z):
+ *   lse = log sum exp z, logprobs = z[token] - lse, entropy = -sum p log p,
+ *   top_ids: the tokens of the top largest logits, in descending order, of equals
+ *   the lowest first; top_logprobs: z - lse of those.
+ * tokens (device): int64 [rows]; a negative one (padding) gives 0; one past the
+ * vocabulary sets IFQ_ERANGE (ifq_device_status) and gives NaN.  logprobs, lse,
+ * entropy (device): float [rows]; top_ids: int64 [rows][top]; top_logprobs:
+ * float [rows][top].  Each output may be NULL (tokens too, with logprobs).
+ * A token of -infinity has no share in lse and entropy; where all are, lse and
+ * all log probabilities are -infinity and the entropy is 0.  A logit of
+ * +infinity makes lse +infinity and the entropy NaN, a NaN all of the row's
+ * numbers; NaN comes before every number among top_ids.  Computed in single
+ * precision; results do not depend on timing.  logits are aligned to their
+ * type, tokens and top_ids to 8 bytes.
+ * rows may be 0 (pointers are not looked at then).
+ */
+int ifq_token_scores(const ifq_scores_desc* d, const void* logits, const int64_t* tokens, float* logprobs, float* lse,
+                     float* entropy, int64_t* top_ids, float* top_logprobs, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

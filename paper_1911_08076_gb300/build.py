@@ -71,12 +71,14 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tag = f"{os.getpid()}"
     o_cu = os.path.join(OUT, f"ifq_api.{tag}.o")
     o_lm = os.path.join(OUT, f"lm_api.{tag}.o")
+    o_layer = os.path.join(OUT, f"layer_api.{tag}.o")
     o_cpp = os.path.join(OUT, f"ifq_host.{tag}.o")
     cu = [nvcc, *ARCH, "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC,
           "-Xptxas", "-v", "-c"]
     cmds = [
         [*cu, os.path.join(CSRC, "ifq_api.cu"), "-o", o_cu],
         [*cu, os.path.join(CSRC, "lm", "lm_api.cu"), "-o", o_lm],
+        [*cu, os.path.join(CSRC, "lm", "layer_api.cu"), "-o", o_layer],
         ["g++", "-O2", "-std=c++17", "-fPIC", "-ffp-contract=off", "-fno-fast-math", "-I", INCLUDE, "-c",
          os.path.join(CSRC, "ifq_host.cpp"), "-o", o_cpp],
     ]
@@ -94,9 +96,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
         raise RuntimeError("tensor-core kernels spill registers to local memory: " + ", ".join(spilled))
     tmp = LIB + f".{tag}.tmp"
     cudalib = os.path.join(os.path.dirname(os.path.dirname(nvcc)), "lib64")
-    run([nvcc, *ARCH, "-shared", "-cudart", "shared", o_cu, o_lm, o_cpp, "-Xlinker", f"-rpath={cudalib}", "-o", tmp])
+    run([nvcc, *ARCH, "-shared", "-cudart", "shared", o_cu, o_lm, o_layer, o_cpp, "-Xlinker", f"-rpath={cudalib}", "-o", tmp])
     os.replace(tmp, LIB)
-    for o in (o_cu, o_lm, o_cpp):
+    for o in (o_cu, o_lm, o_layer, o_cpp):
         os.remove(o)
     if verbose:
         sys.stdout.write("".join(logs))

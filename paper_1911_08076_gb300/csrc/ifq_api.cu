@@ -2081,11 +2081,11 @@ int ifq_wait_selftest(int limit_us, void* stream) {
 int ifq_device_status(void* stream, int* status) {
   if (!status) return IFQ_EINVAL;
   if (cudaStreamSynchronize(S(stream)) != cudaSuccess) return IFQ_ECUDA;
-  int v = 0, lm = 0, zero = 0;
+  int v = 0, lm = 0, layer = 0, zero = 0;
   if (cudaMemcpyFromSymbol(&v, ifq::g_status, sizeof(int)) != cudaSuccess) return IFQ_ECUDA;
   if (v != 0 && cudaMemcpyToSymbol(ifq::g_status, &zero, sizeof(int)) != cudaSuccess) return IFQ_ECUDA;
-  if (lm_take_status(&lm) != IFQ_OK) return IFQ_ECUDA;
-  if (v == 0) v = lm;
+  if (lm_take_status(&lm) != IFQ_OK || layer_take_status(&layer) != IFQ_OK) return IFQ_ECUDA;
+  if (v == 0) v = lm ? lm : layer;
   *status = v;
   return IFQ_OK;
 }

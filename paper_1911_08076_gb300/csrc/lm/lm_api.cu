@@ -4,30 +4,19 @@
 
 #include <cmath>
 #include <algorithm>
-#include <climits>
-#include <mutex>
 #include <type_traits>
 
-#include "../launch.cuh"
 #include "fp8.cuh"
 #include "ifq.h"
 #include "kv4.cuh"
 #include "kv4_attention.cuh"
 #include "kv4_chunk.cuh"
 #include "kv4_rows.cuh"
+#include "lm_host.h"
 
 namespace {
 
 using namespace ifq;
-
-inline bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-inline int done(cudaError_t e) { return e == cudaSuccess ? IFQ_OK : IFQ_ECUDA; }
-inline bool is16(int dtype) { return dtype == IFQ_F16 || dtype == IFQ_BF16; }
-
-// Rows, tokens and columns are ints, and so are the ends of the blocks that they are rounded up to.
-constexpr int kMaxSize = INT_MAX - 1023;
-
-std::mutex g_lm_mu;   // guards the per-device state below
 
 // The kernel instance of a head size and type: f(head size, bfloat16) with both as types.
 template <int D, typename F>
@@ -52,13 +41,6 @@ int check_cache(const ifq_kv4_cache* c, size_t* bytes) {
   const double b = (double)c->pages * c->page_size * c->kv_heads * (c->head_dim + 8);
   if (b > 4e18 || (double)c->pages * c->page_size > 4e18 || c->kv_heads > 65536) return IFQ_ERANGE;
   *bytes = (size_t)c->pages * c->kv_heads * (c->page_size / kKvGroup) * kv4_group_bytes(c->head_dim);
-  return IFQ_OK;
-}
-
-// A row stride in elements (0: dense): at least a row, in units of 16 bytes of a 16-bit type.
-int stride_of(int64_t given, long long width, long long* out) {
-  if (given < 0 || (given != 0 && (given < width || given % 8 != 0))) return IFQ_EINVAL;
-  *out = given ? given : width;
   return IFQ_OK;
 }
 
@@ -135,16 +117,6 @@ struct AttnPlan {
   size_t ws;
 };
 
-// SM count of the current device, or a full GB300's where there is none.
-int sm_count() {
-  static int known[kMaxDevices];
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 152;
-  std::lock_guard<std::mutex> lk(g_lm_mu);
-  if (!known[dev] && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) known[dev] = n;
-  return known[dev] ? known[dev] : 152;
-}
-
 int plan_attention(const ifq_kv4_attention_desc* d, const KvAttnArgs& a, AttnPlan* p) {
   const int D = d->cache.head_dim;
   const long long rows = (long long)d->max_q * a.group;
@@ -176,19 +148,6 @@ int plan_attention(const ifq_kv4_attention_desc* d, const KvAttnArgs& a, AttnPla
   p->direct = alone < spread && blocks <= 65535 && d->seqs <= 65535;
   p->blocks = p->direct ? (int)blocks : sms * per_sm;
   p->ws = p->direct ? 0 : round_up((size_t)p->blocks * kKvRowsWarps * (2 * R * (D * 4 + 8) + 16), 256);
-  return IFQ_OK;
-}
-
-// Whether the instance's shared memory has been allowed on the current device; if not, do so.
-template <typename K>
-int allow_smem(K kern, int bytes, bool (&set)[kMaxDevices]) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return IFQ_ECUDA;
-  std::lock_guard<std::mutex> lk(g_lm_mu);
-  if (!set[dev]) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return IFQ_ECUDA;
-    set[dev] = true;
-  }
   return IFQ_OK;
 }
 

@@ -1,0 +1,126 @@
+// Products with weights in 4 bits: the packed layout, and the kernel that makes it.
+//
+// w = round(code * scale + min): one fma in the weights' type, so every kernel multiplies the same values.
+//
+// A row block is 16 packed rows: 16 rows of w, or of a gated pair the gate's rows 8 b .. 8 b + 7 and the other's after
+// them, so that a lane that holds rows g and g + 8 of a block has both factors of an output.  A block of 128 columns
+// of a row block is contiguous, 1024 bytes of codes and 64 of parameters a group, and a row block's blocks follow each
+// other:
+//   codes       [2 units of 64 columns][32 lanes][4 words]; the word of step j (16 columns) in lane 4 g + t holds four
+//               pairs of neighbouring columns, pair i in bits 4 i .. 4 i + 3 and 16 + 4 i .. 16 + 4 i + 3:
+//               i = 0, 1: rows g, g + 8, columns 16 j + 2 t and the next; i = 2, 3: the same rows, 8 columns further
+//   parameters  [128 / group][8][2] pairs (scale, min): of row g, of row g + 8
+// A pair of codes masked out of a word and made floats is thus one register of an mma.sync operand (A, 16 x 16), and a
+// register of a tcgen05.st in 16-lane fragments.  Rows and columns past the matrix hold zeros up to whole tiles of 128.
+#pragma once
+#include "kv4.cuh"
+
+namespace ifq {
+
+constexpr int kW4Rows = 16, kW4Cols = 128;
+
+__host__ __device__ constexpr int w4_block_bytes(int group) { return 1024 + 64 * (kW4Cols / group); }
+
+struct W4Args {
+  const uint8_t* w;
+  const uint16_t* x;
+  const void* res;     // NULL: none
+  void* out;
+  long long x_stride, res_stride, out_stride;
+  int m, n, k, kb;     // kb: blocks of 128 columns
+  int out_type, act;
+};
+
+// code * scale + min in the weights' type.
+template <bool BF>
+__device__ __forceinline__ float w4_value(int code, uint16_t scale, uint16_t min) {
+  if constexpr (BF) return __bfloat162float(__hfma(__int2bfloat16_rn(code), __ushort_as_bfloat16(scale), __ushort_as_bfloat16(min)));
+  else return __half2float(__hfma(__int2half_rn(code), __ushort_as_half(scale), __ushort_as_half(min)));
+}
+
+// act(a) of a gated pair.  The exponentials are of -|.|, so that none overflows.
+__device__ __forceinline__ float w4_sigmoid(float a) {
+  const float e = __expf(-fabsf(a)), s = __fdividef(1.0f, 1.0f + e);
+  return a < 0.0f ? e * s : s;
+}
+__device__ __forceinline__ float w4_act(int act, float a) {
+  if (act == IFQ_ACT_SILU) return a * w4_sigmoid(a);
+  if (act == IFQ_ACT_GELU) return 0.5f * a * erfcf(-0.70710678118654752f * a);
+  return a * w4_sigmoid(1.5957691216057308f * (a + 0.044715f * a * a * a));
+}
+
+__device__ __forceinline__ float w4_load(int type, const void* p, long long at) {
+  if (type == IFQ_F32) return ((const float*)p)[at];
+  if (type == IFQ_F16) return __half2float(((const __half*)p)[at]);
+  return __bfloat162float(((const __nv_bfloat16*)p)[at]);
+}
+__device__ __forceinline__ void w4_store(int type, void* p, long long at, float v) {
+  if (type == IFQ_F32) ((float*)p)[at] = v;
+  else if (type == IFQ_F16) ((__half*)p)[at] = __float2half_rn(v);
+  else ((__nv_bfloat16*)p)[at] = __float2bfloat16_rn(v);
+}
+
+// ---------------------------------------------------------------- packing
+
+struct W4PackArgs {
+  const uint8_t* codes;
+  const uint16_t *scales, *mins;
+  uint8_t* out;
+  int n, k, kb, groups, gated;
+  int row_blocks;   // all of them, those past the matrix too
+};
+
+constexpr int kW4PackWarps = 8;
+
+// A warp makes one block (16 rows x 128 columns): its codes go through shared memory, where a row has 17 words, so that
+// the bytes that a lane gathers (rows g and g + 8) lie in different banks.
+template <int G>
+__global__ void __launch_bounds__(32 * kW4PackWarps) w4_pack_kernel(const __grid_constant__ W4PackArgs a) {
+  grid_dep_wait();
+  grid_dep_launch();
+  __shared__ uint32_t turn[kW4PackWarps][16 * 17];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane / 4, t = lane % 4;
+  uint32_t* in = turn[warp];
+  const long long blocks = (long long)a.row_blocks * a.kb, words = a.k / 8;
+  const auto source = [&](long long rb, int r) -> long long {   // the row of the matrix, or -1
+    const long long j = a.gated ? rb * 8 + r % 8 : rb * 16 + r;
+    return j >= a.n ? -1 : a.gated && r >= 8 ? j + a.n : j;
+  };
+  for (long long b = (long long)blockIdx.x * kW4PackWarps + warp; b < blocks; b += (long long)gridDim.x * kW4PackWarps) {
+    const long long rb = b / a.kb;
+    const int kb = (int)(b - rb * a.kb);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 2 * i + lane / 16, c = lane % 16;
+      const long long j = source(rb, r), at = kb * 16ll + c;
+      in[r * 17 + c] = j >= 0 && at < words ? ((const uint32_t*)a.codes)[j * words + at] : 0u;
+    }
+    __syncwarp();
+    uint8_t* out = a.out + b * w4_block_bytes(G);
+    const uint8_t* bytes = (const uint8_t*)in;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        w[j] = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t v = bytes[(g + 8 * (i & 1)) * 68 + (64 * u + 16 * j + 2 * t + 8 * (i >> 1)) / 2];
+          w[j] |= (v & 15u) << (4 * i) | (v >> 4) << (16 + 4 * i);
+        }
+      }
+      *(uint4*)(out + 512 * u + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    for (int i = lane; i < 16 * (kW4Cols / G); i += 32) {
+      const int q = i / 16, r = i % 16;
+      const long long j = source(rb, r), at = (long long)kb * (kW4Cols / G) + q;
+      uint32_t v = 0;
+      if (j >= 0 && at < a.groups) v = a.scales[j * a.groups + at] | (uint32_t)a.mins[j * a.groups + at] << 16;
+      *(uint32_t*)(out + 1024 + 64 * q + 8 * (r % 8) + 4 * (r / 8)) = v;
+    }
+    __syncwarp();
+  }
+}
+
+}  // namespace ifq

@@ -26,6 +26,7 @@ IFQ_LAYER_CONV, IFQ_LAYER_POOL, IFQ_LAYER_FIXED = 1, 2, 3
 IFQ_FORWARD_LAYERS, IFQ_FORWARD_PERSISTENT = 1, 2
 IFQ_F16, IFQ_BF16, IFQ_F32 = 1, 2, 3
 IFQ_ROPE_NONE, IFQ_ROPE_HALVES, IFQ_ROPE_PAIRS = 0, 1, 2
+IFQ_ACT_SILU, IFQ_ACT_GELU, IFQ_ACT_GELU_TANH = 1, 2, 3
 
 
 class IfqError(RuntimeError):
@@ -77,6 +78,25 @@ class Fp8Desc(ctypes.Structure):
         [("x_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
 
 
+class W4Weights(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int) for f in ("n", "k", "group", "dtype", "gated")]
+
+
+class W4Desc(ctypes.Structure):
+    _fields_ = [("weights", W4Weights)] + [(f, ctypes.c_int) for f in ("m", "out_dtype", "act")] + \
+        [(f, ctypes.c_int64) for f in ("x_stride", "out_stride", "residual_stride")]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int) for f in ("rows", "dim", "dtype")] + [("eps", ctypes.c_float)] + \
+        [(f, ctypes.c_int64) for f in ("x_stride", "residual_stride", "sum_stride", "out_stride")]
+
+
+class ScoresDesc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int) for f in ("rows", "vocab", "dtype", "top")] + \
+        [("scale", ctypes.c_float), ("stride", ctypes.c_int64)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _SZ = ctypes.c_size_t
@@ -123,6 +143,12 @@ _SIGS = {
     "ifq_fp8_quantize": ([ctypes.POINTER(Fp8Desc), _P, _P, _P, _P], _I),
     "ifq_fp8_workspace_bytes": ([ctypes.POINTER(Fp8Desc), ctypes.POINTER(_SZ)], _I),
     "ifq_fp8_matmul": ([ctypes.POINTER(Fp8Desc), _P, _P, _P, _P, _P, _P, _SZ, _P], _I),
+    "ifq_w4_bytes": ([ctypes.POINTER(W4Weights), ctypes.POINTER(_SZ)], _I),
+    "ifq_w4_pack": ([ctypes.POINTER(W4Weights), _P, _P, _P, _P, _P], _I),
+    "ifq_w4_matmul": ([ctypes.POINTER(W4Desc), _P, _P, _P, _P, _P], _I),
+    "ifq_w4_gated": ([ctypes.POINTER(W4Desc), _P, _P, _P, _P], _I),
+    "ifq_rms_norm": ([ctypes.POINTER(NormDesc), _P, _P, _P, _P, _P, _P], _I),
+    "ifq_token_scores": ([ctypes.POINTER(ScoresDesc), _P, _P, _P, _P, _P, _P, _P, _P], _I),
     "ifq_wait_selftest": ([_I, _P], _I),
     "ifq_device_status": ([_P, ctypes.POINTER(_I)], _I),
 }
@@ -478,6 +504,61 @@ def ifq_fp8_matmul(d: Fp8Desc, x, x_scale, w, w_scale, out, ws=None, ws_bytes: i
     """out = x w^T with e4m3 operands and block scales."""
     _ok(lib().ifq_fp8_matmul(ctypes.byref(d), _ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(out), _ptr(ws),
                              ws_bytes, _stream(stream)), "ifq_fp8_matmul")
+
+
+def w4_weights(n: int, k: int, group: int = 128, dtype: int = IFQ_BF16, gated: bool = False) -> W4Weights:
+    """n rows of k weights in 4 bits; gated: a pair of matrices of n rows each."""
+    return W4Weights(n, k, group, dtype, int(gated))
+
+
+def ifq_w4_bytes(w: W4Weights) -> int:
+    out = _SZ()
+    _ok(lib().ifq_w4_bytes(ctypes.byref(w), ctypes.byref(out)), "ifq_w4_bytes")
+    return out.value
+
+
+def ifq_w4_pack(w: W4Weights, codes, scales, mins, packed, stream=None):
+    """Codes [rows][k / 2] with scales and minima [rows][groups] to the layout that the products read."""
+    _ok(lib().ifq_w4_pack(ctypes.byref(w), _ptr(codes), _ptr(scales), _ptr(mins), _ptr(packed), _stream(stream)),
+        "ifq_w4_pack")
+
+
+def w4_desc(weights: W4Weights, m: int, out_dtype: int = IFQ_BF16, act: int = 0, x_stride: int = 0, out_stride: int = 0,
+            residual_stride: int = 0) -> W4Desc:
+    return W4Desc(weights, m, out_dtype, act, x_stride, out_stride, residual_stride)
+
+
+def ifq_w4_matmul(d: W4Desc, x, packed, out, residual=None, stream=None):
+    """out = x w^T (+ residual) with weights in 4 bits."""
+    _ok(lib().ifq_w4_matmul(ctypes.byref(d), _ptr(x), _ptr(packed), _ptr(out), _ptr(residual), _stream(stream)),
+        "ifq_w4_matmul")
+
+
+def ifq_w4_gated(d: W4Desc, x, packed, out, stream=None):
+    """out = act(x wg^T) * (x wu^T) with a gated pair of weights in 4 bits."""
+    _ok(lib().ifq_w4_gated(ctypes.byref(d), _ptr(x), _ptr(packed), _ptr(out), _stream(stream)), "ifq_w4_gated")
+
+
+def norm_desc(rows: int, dim: int, dtype: int = IFQ_BF16, eps: float = 1e-5, x_stride: int = 0, residual_stride: int = 0,
+              sum_stride: int = 0, out_stride: int = 0) -> NormDesc:
+    return NormDesc(rows, dim, dtype, eps, x_stride, residual_stride, sum_stride, out_stride)
+
+
+def ifq_rms_norm(d: NormDesc, x, residual, weight, sum, out, stream=None):
+    """out = root-mean-square norm of x, or of sum = x + residual."""
+    _ok(lib().ifq_rms_norm(ctypes.byref(d), _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum), _ptr(out),
+                           _stream(stream)), "ifq_rms_norm")
+
+
+def scores_desc(rows: int, vocab: int, dtype: int = IFQ_F32, top: int = 0, scale: float = 1.0, stride: int = 0) -> ScoresDesc:
+    return ScoresDesc(rows, vocab, dtype, top, scale, stride)
+
+
+def ifq_token_scores(d: ScoresDesc, logits, tokens, logprobs=None, lse=None, entropy=None, top_ids=None,
+                     top_logprobs=None, stream=None):
+    """Log probabilities of tokens, log-sum-exp, entropy and the likeliest tokens of rows of logits."""
+    _ok(lib().ifq_token_scores(ctypes.byref(d), _ptr(logits), _ptr(tokens), _ptr(logprobs), _ptr(lse), _ptr(entropy),
+                               _ptr(top_ids), _ptr(top_logprobs), _stream(stream)), "ifq_token_scores")
 
 
 def ifq_wait_selftest(limit_us: int, stream=None):
