@@ -36,6 +36,7 @@
 // A block's keys may be split over `splits` blocks, joined by kv4_chunk_join_kernel.
 #pragma once
 #include "kv4_rows.cuh"
+#include "tmem.cuh"
 
 namespace ifq {
 
@@ -62,18 +63,9 @@ struct KvChunkShape {
   static_assert(bytes <= 232448, "shared memory budget");
 };
 
-// Instruction descriptor, kind::f16, half operands, fp32 accumulator, both K-major.
-__host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N) {
-  return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
 __device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(d),
                "l"(a), "l"(b), "r"(idesc), "r"(acc)
-               : "memory");
-}
-__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;}" ::"r"(d),
-               "r"(a), "l"(b), "r"(idesc), "r"(acc)
                : "memory");
 }
 // 16 / 32 registers of a lane to consecutive columns of its row.
@@ -99,14 +91,6 @@ __device__ __forceinline__ void tmem_ld_frag(uint32_t t, uint32_t (&v)[2][16]) {
       : "r"(t), "r"(t + (16u << 16))
       : "memory");
 }
-// 16 lanes x 16 columns from fragments: v[2 k + e] to column 4 k + t % 4 of lane t / 4 + 8 e.
-__device__ __forceinline__ void tmem_st_frag(uint32_t t, const uint32_t (&v)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(t), "r"(v[0]), "r"(v[1]),
-               "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
-}
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
 __device__ __forceinline__ uint64_t pair2(float a, float b) {
   uint64_t r;
   asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));

@@ -10,7 +10,7 @@
 #include "norm.cuh"
 #include "scores.cuh"
 #include "w4.cuh"
-#include "w4_plain.cuh"
+#include "w4_many.cuh"
 
 namespace {
 
@@ -70,6 +70,85 @@ int check_w4_desc(const ifq_w4_desc* d, int gated, W4Args* a) {
   return IFQ_OK;
 }
 
+// TMA descriptor of x: [m][k] 16-bit values, boxes of `box` rows x 64 in the 128-byte swizzle; what is past the ends reads
+// as zeros.
+bool encode_x(const W4Args& a, int box, CUtensorMap* tm) {
+  const cuuint64_t gdim[2] = {(cuuint64_t)a.k, (cuuint64_t)a.m}, gstride[1] = {(cuuint64_t)a.x_stride * 2};
+  const cuuint32_t bdim[2] = {64, (cuuint32_t)box}, estr[2] = {1, 1};
+  return g_encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<uint16_t*>(a.x), gdim, gstride, bdim, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int kW4MaxSplit = 8, kW4SplitCols = 128;
+
+// One-time setup of an instance on the current device: its shared memory, and how many clusters of each size run at once
+// (in `slots`; a plain launch is size 1).
+template <typename K>
+int w4_many_setup(K kern, int (&known)[kMaxDevices][kW4MaxSplit + 1], const int** slots) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return IFQ_ECUDA;
+  const int sms = sm_count();
+  std::lock_guard<std::mutex> lk(g_lm_mu);
+  int* s = known[dev];
+  if (!s[1]) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kW4ManySmem) != cudaSuccess) return IFQ_ECUDA;
+    for (int ks = 2; ks <= kW4MaxSplit; ++ks) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3((unsigned)(sms / ks * ks));
+      cfg.blockDim = dim3(kW4ManyThreads);
+      cfg.dynamicSmemBytes = kW4ManySmem;
+      cudaLaunchAttribute at[1];
+      at[0].id = cudaLaunchAttributeClusterDimension;
+      at[0].val.clusterDim.x = (unsigned)ks;
+      at[0].val.clusterDim.y = 1;
+      at[0].val.clusterDim.z = 1;
+      cfg.attrs = at;
+      cfg.numAttrs = 1;
+      int n = 0;
+      s[ks] = cudaOccupancyMaxActiveClusters(&n, kern, &cfg) == cudaSuccess ? n : 0;
+    }
+    cudaGetLastError();   // (a cluster size that does not fit is no error of this call)
+    s[1] = sms;
+  }
+  *slots = s;
+  return IFQ_OK;
+}
+
+template <bool BF, int G, bool GATED>
+int run_w4_many(const W4Args& a, cudaStream_t st) {
+  static int known[kMaxDevices][kW4MaxSplit + 1];
+  const auto kern = w4_many_kernel<BF, G, GATED>;
+  const int* slots;
+  const int rc = w4_many_setup(kern, known, &slots);
+  if (rc) return rc;
+  W4Many r;
+  r.a = a;
+  r.tiles_w = ceil_div(a.n, GATED ? 64 : 128);
+  // The columns of a tile and the split of k with the least time: blocks of k in a row, each 256 cycles of expansion or
+  // 4 a column of MMAs, and what a tile and a cluster's join cost besides.
+  double best = 1e300;
+  for (int tx = ceil_div(a.m, 256), n = 0; n < 3; ++n, ++tx) {
+    const int bn = (int)round_up(ceil_div(a.m, tx), 16);
+    const long long tiles = (long long)r.tiles_w * ceil_div(a.m, bn);
+    if (tiles > INT_MAX / kW4MaxSplit) return IFQ_ERANGE;
+    const double block = std::max(350.0, 4.0 * bn);
+    for (int ks = 1; ks <= kW4MaxSplit && ks <= a.kb; ++ks) {
+      if (slots[ks] < 1 || (ks > 1 && bn > kW4SplitCols)) continue;
+      const double turns = (double)((tiles + slots[ks] - 1) / slots[ks]);
+      const double c = turns * (ceil_div(a.kb, ks) * block + 1500 + 4 * bn) + (ks > 1 ? 2500 : 0);
+      if (c < best) best = c, r.bn = bn, r.ks = ks, r.tiles = (int)tiles;
+    }
+  }
+  r.tiles_x = ceil_div(a.m, r.bn);
+  r.stages = w4_many_stages(G, r.bn, r.ks);
+  CUtensorMap tx;
+  if (!encode_x(a, r.bn, &tx)) return IFQ_ECUDA;
+  if (r.ks > 1)
+    return done(launch_k_cluster(kern, r.ks, dim3((unsigned)(r.tiles * r.ks)), dim3(kW4ManyThreads), kW4ManySmem, st, tx, r));
+  return done(launch_k(kern, dim3((unsigned)std::min(r.tiles, slots[1])), dim3(kW4ManyThreads), kW4ManySmem, st, tx, r));
+}
+
 int run_w4(const ifq_w4_desc* d, W4Args& a, const void* x, const void* packed, void* out, const void* res, cudaStream_t st) {
   if (!d->m) return IFQ_OK;
   if (!x || !packed || !out) return IFQ_EINVAL;
@@ -78,10 +157,11 @@ int run_w4(const ifq_w4_desc* d, W4Args& a, const void* x, const void* packed, v
   a.w = (const uint8_t*)packed;
   a.out = out;
   a.res = res;
+  if (!get_encode()) return IFQ_ECUDA;
   return by_weights(d->weights, [&](auto bf, auto group) {
     constexpr bool BF = decltype(bf)::value;
     constexpr int G = decltype(group)::value;
-    return done(launch_k(w4_plain_kernel<BF, G>, dim3(ceil_div(a.n, 32), std::min(ceil_div(a.m, 8), 65535)), dim3(256), 0, st, a));
+    return d->weights.gated ? run_w4_many<BF, G, true>(a, st) : run_w4_many<BF, G, false>(a, st);
   });
 }
 
