@@ -128,7 +128,7 @@ int run_w4_many(const W4Args& a, cudaStream_t st) {
   // The columns of a tile and the split of k with the least time: blocks of k in a row, each 256 cycles of expansion or
   // 4 a column of MMAs, and what a tile and a cluster's join cost besides.
   double best = 1e300;
-  for (int tx = ceil_div(a.m, 256), n = 0; n < 3; ++n, ++tx) {
+  for (int tx = ceil_div(a.m, kW4MaxCols), n = 0; n < 3; ++n, ++tx) {
     const int bn = (int)round_up(ceil_div(a.m, tx), 16);
     const long long tiles = (long long)r.tiles_w * ceil_div(a.m, bn);
     if (tiles > INT_MAX / kW4MaxSplit) return IFQ_ERANGE;

@@ -5,8 +5,9 @@
 // fragments need no swizzle, no shared memory, and leave its bandwidth to x.  A block of 128 columns of 16 rows is
 // contiguous, so the codes of a tile's block are eight bulk copies; x comes by TMA in the 128-byte swizzle.
 //
-// Warps: eight that expand (a quadrant of 32 lanes and every other 64 columns of k each), two that load, one that
-// issues MMAs, four that take results out.  The results leave tensor memory while the next tile's weights are expanded.
+// Warps: sixteen that expand (a quadrant of 32 lanes, half of the columns of every other block of k each), two that load,
+// one that issues MMAs, four that take results out.  Two accumulators take turns, so that a tile's results leave tensor
+// memory beside the next tile's products.
 //
 // A tile's k may be split over a cluster of ks blocks: each sends its partial columns to the block that owns them through
 // distributed shared memory, which adds them in the order of the ranks.
@@ -20,13 +21,13 @@ namespace ifq {
 
 struct W4Many {
   W4Args a;
-  int bn, stages;              // columns a tile (a multiple of 16); shared-memory stages of 64 columns of k
+  int bn, stages;              // columns a tile (a multiple of 16, up to 192); shared-memory stages of 64 columns of k
   int tiles, tiles_w, tiles_x; // items; tiles of w's rows and of x's
   int ks;                      // blocks that a tile's k is split over
 };
 
-constexpr int kW4Expand = 8, kW4ManyThreads = 512;
-constexpr int kW4CodeSlots = 4, kW4AStages = 8, kW4AccCols = 256;
+constexpr int kW4Expand = 16, kW4Out = kW4Expand + 4, kW4ManyThreads = 32 * (kW4Out + 4);   // first warp that stores
+constexpr int kW4CodeSlots = 4, kW4AStages = 4, kW4MaxCols = 192, kW4ACol = 2 * kW4MaxCols;
 constexpr int kW4ManySmem = 232448;
 
 __host__ __device__ constexpr int w4_many_codes(int group) { return kW4CodeSlots * 8 * w4_block_bytes(group); }
@@ -81,8 +82,9 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
   auto cempty = [&](int s) { return fixed + 8 * (CS + s); };
   auto afull = [&](int s) { return fixed + 8 * (2 * CS + s); };
   auto aempty = [&](int s) { return fixed + 8 * (2 * CS + AS + s); };
-  const uint32_t dfull = fixed + 8 * (2 * CS + 2 * AS), dempty = dfull + 8;
-  uint32_t* tptr = (uint32_t*)(smem + (dempty + 8 - base));
+  auto dfull = [&](int b) { return fixed + 8 * (2 * CS + 2 * AS + b); };
+  auto dempty = [&](int b) { return fixed + 8 * (2 * CS + 2 * AS + 2 + b); };
+  uint32_t* tptr = (uint32_t*)(smem + (dempty(2) - base));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int ks = r.ks, rank = ks > 1 ? (int)cluster_ctarank() : 0;
   if (threadIdx.x == 0) {
@@ -92,14 +94,16 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
     }
     for (int i = 0; i < CS; ++i) {
       mbar_init(cfull(i), 1);
-      mbar_init(cempty(i), kW4Expand);
+      mbar_init(cempty(i), kW4Expand / 2);
     }
     for (int i = 0; i < AS; ++i) {
       mbar_init(afull(i), 4);
       mbar_init(aempty(i), 1);
     }
-    mbar_init(dfull, 1);
-    mbar_init(dempty, 4);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(dfull(i), 1);
+      mbar_init(dempty(i), 4);
+    }
     fence_mbar_init();
     prefetch_tmap(&tx);
   }
@@ -126,48 +130,54 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
   };
 
   if (warp < kW4Expand) {
-    const int q = warp & 3, h = warp >> 2;
-    const uint32_t tl = tmem + kW4AccCols + ((uint32_t)(q * 32) << 16);
-    uint32_t it = 0;
+    const int q = warp & 3, h = (warp >> 2) & 1, odd = warp >> 3;
+    constexpr int NP = G == 32 ? 2 : 1;   // groups in 64 columns
+    const uint32_t tl = tmem + kW4ACol + ((uint32_t)(q * 32) << 16);
+    // this warp's blocks are every other one of all that the CTA goes through
+    const uint32_t turns = first < r.tiles ? (r.tiles - first + step - 1) / step : 0, total = turns * (k1 - k0);
+    uint4 w[2];
+    uint2 p[2][NP];
     bool ok = true;
-    for (int t = first; t < r.tiles && ok; t += step)
-      for (int k = k0; k < k1; ++k, ++it) {
-        const uint32_t slot = it % CS, ph = (it / CS) & 1, as = (2 * it + h) % AS, aph = ((2 * it + h) / AS) & 1;
-        if (!__all_sync(0xffffffffu, mbar_wait(cfull(slot), ph))) { ok = false; break; }
-        uint4 w[2];
-        uint2 p[2][G == 32 ? 2 : 1];
+    auto fetch = [&](uint32_t it) {
+      const uint32_t slot = it % CS;
+      if (!__all_sync(0xffffffffu, mbar_wait(cfull(slot), (it / CS) & 1))) { ok = false; return; }
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const uint8_t* c = codes + (slot * 8 + 2 * q + b) * WB;
-          w[b] = *(const uint4*)(c + 512 * h + 16 * lane);
+      for (int b = 0; b < 2; ++b) {
+        const uint8_t* c = codes + (slot * 8 + 2 * q + b) * WB;
+        w[b] = *(const uint4*)(c + 512 * h + 16 * lane);
 #pragma unroll
-          for (int i = 0; i < (G == 32 ? 2 : 1); ++i)
-            p[b][i] = *(const uint2*)(c + 1024 + 64 * (h * 64 / G + i) + 8 * (lane / 4));
-        }
-        if (!__all_sync(0xffffffffu, mbar_wait(aempty(as), aph ^ 1))) { ok = false; break; }
-        tc_fence_after();
+        for (int i = 0; i < NP; ++i) p[b][i] = *(const uint2*)(c + 1024 + 64 * (h * 64 / G + i) + 8 * (lane / 4));
+      }
+    };
+    if (odd < total) fetch(odd);
+    for (uint32_t it = odd; it < total && ok; it += 2) {
+      const uint32_t as = (2 * it + h) % AS, aph = ((2 * it + h) / AS) & 1;
+      uint32_t v[2][2][8];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const uint32_t to = tl + 32 * as + ((uint32_t)(16 * b) << 16);
-          const uint32_t words[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
-          uint32_t s[2], m[2];
+      for (int b = 0; b < 2; ++b) {
+        const uint32_t words[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
+        uint32_t s[2], m[2];
 #pragma unroll
-          for (int j = 0; j < 4; j += 2) {
-            if (j == 0 || G == 32) w4_params(p[b][G == 32 ? j / 2 : 0], s, m);
-            uint32_t v[8];
-            w4_expand<BF>(words[j], s, m, v);
-            w4_expand<BF>(words[j + 1], s, m, v + 4);
-            tmem_st_frag(to + 8 * j, v);
-          }
-        }
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(cempty(slot));
-          mbar_arrive(afull(as));
+        for (int j = 0; j < 2; ++j) {
+          if (j < NP) w4_params(p[b][j], s, m);
+          w4_expand<BF>(words[2 * j], s, m, v[b][j]);
+          w4_expand<BF>(words[2 * j + 1], s, m, v[b][j] + 4);
         }
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(cempty(it % CS));
+      if (it + 2 < total) fetch(it + 2);   // the next codes are on their way while these go to tensor memory
+      if (!ok || !__all_sync(0xffffffffu, mbar_wait(aempty(as), aph ^ 1))) break;
+      tc_fence_after();
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) tmem_st_frag(tl + 32 * as + ((uint32_t)(16 * b) << 16) + 16 * j, v[b][j]);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(afull(as));
+    }
   } else if (warp == kW4Expand) {   // x
     int it = 0;
     bool ok = true;
@@ -208,7 +218,8 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
     uint32_t it = 0, nt = 0;
     bool ok = true;
     for (int t = first; t < r.tiles && ok; t += step, ++nt) {
-      if (nt && !__all_sync(0xffffffffu, mbar_wait(dempty, (nt - 1) & 1))) break;
+      const uint32_t acc = nt & 1, td = tmem + acc * kW4MaxCols;
+      if (nt > 1 && !__all_sync(0xffffffffu, mbar_wait(dempty(acc), (nt / 2 - 1) & 1))) break;
       for (int k = 2 * k0; k < 2 * k1; ++k, ++it) {
         const uint32_t s = it % ST, as = it % AS;
         if (!__all_sync(0xffffffffu, mbar_wait(xfull(s), (it / ST) & 1)) ||
@@ -216,25 +227,25 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
         tc_fence_after();
         if (elect_one()) {
           const uint64_t db = sdesc_sw128(base + s * xb);
-          const uint32_t ta = tmem + kW4AccCols + 32 * as;
+          const uint32_t ta = tmem + kW4ACol + 32 * as;
 #pragma unroll
           for (int j = 0; j < 4; ++j)   // 16 columns of k: 8 of tensor memory, two 16-byte units of the descriptor's address
-            mma_f16_ts(tmem, ta + 8 * j, db + 2 * j, idesc, (k > 2 * k0) | (j > 0));
+            mma_f16_ts(td, ta + 8 * j, db + 2 * j, idesc, (k > 2 * k0) | (j > 0));
           mma_commit(xempty(s));
           mma_commit(aempty(as));
-          if (k + 1 == 2 * k1) mma_commit(dfull);
+          if (k + 1 == 2 * k1) mma_commit(dfull(acc));
         }
         __syncwarp();
       }
     }
-  } else if (warp >= 12) {   // results
+  } else if (warp >= kW4Out) {   // results
     const int q = warp & 3, row = q * 32 + lane;
-    const uint32_t tl = tmem + ((uint32_t)(q * 32) << 16);
     uint32_t nt = 0;
     for (int t = first; t < r.tiles; t += step, ++nt) {
       int iw, ix;
       tile(t, iw, ix);
-      if (!__all_sync(0xffffffffu, mbar_wait(dfull, nt & 1))) break;
+      const uint32_t acc = nt & 1, tl = tmem + acc * kW4MaxCols + ((uint32_t)(q * 32) << 16);
+      if (!__all_sync(0xffffffffu, mbar_wait(dfull(acc), (nt / 2) & 1))) break;
       tc_fence_after();
       if (ks > 1) {
         const int per = (r.bn + ks - 1) / uks;
@@ -251,18 +262,31 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
         }
         break;
       }
+      const int e = (lane >> 3) & 1;
+      const int n = GATED ? iw * 64 + q * 16 + (lane >> 4) * 8 + (lane & 7) : iw * 128 + row;
+      float add[16], next[16];   // the residual, loaded 16 columns ahead
+      auto residual = [&](int c0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int m = ix * r.bn + c0 + i;
+          next[i] = c0 < r.bn && m < a.m && n < a.n ? w4_load(a.out_type, a.res, m * a.res_stride + n) : 0.0f;
+        }
+      };
+      if (!GATED && a.res) residual(0);
       for (int c0 = 0; c0 < r.bn; c0 += 16) {
         uint32_t v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) add[i] = next[i];
+        if (!GATED && a.res) residual(c0 + 16);
         tmem_ld<16>(tl + c0, v);
         if (c0 + 16 == r.bn) {   // the accumulator has been read
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(dempty);
+          if (lane == 0) mbar_arrive(dempty(acc));
         }
         const int m0 = ix * r.bn + c0;
         if constexpr (GATED) {
           // lanes with bit 3 clear hold the gate's rows: they do the even columns, the others the odd ones
-          const int e = (lane >> 3) & 1, n = iw * 64 + q * 16 + (lane >> 4) * 8 + (lane & 7);
 #pragma unroll
           for (int i = 0; i < 16; i += 2) {
             const float mine = __uint_as_float(e ? v[i + 1] : v[i]);
@@ -272,15 +296,11 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
             if (m < a.m && n < a.n) w4_store(BF ? IFQ_BF16 : IFQ_F16, a.out, m * a.out_stride + n, y);
           }
         } else {
-          const int n = iw * 128 + row;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int m = m0 + i;
-            if (m < a.m && n < a.n) {
-              float y = __uint_as_float(v[i]);
-              if (a.res) y += w4_load(a.out_type, a.res, m * a.res_stride + n);
-              w4_store(a.out_type, a.out, m * a.out_stride + n, y);
-            }
+            const float y = __uint_as_float(v[i]) + (a.res ? add[i] : 0.0f);
+            if (m < a.m && n < a.n) w4_store(a.out_type, a.out, m * a.out_stride + n, y);
           }
         }
       }
