@@ -21,21 +21,21 @@ namespace ifq {
 
 struct W4Many {
   W4Args a;
-  int bn, stages;              // columns a tile (a multiple of 16, up to 192); shared-memory stages of 64 columns of k
+  int bn, stages;              // columns a tile (a multiple of 16, up to 192); shared-memory stages of 128 columns of k
   int tiles, tiles_w, tiles_x; // items; tiles of w's rows and of x's
   int ks;                      // blocks that a tile's k is split over
 };
 
 constexpr int kW4Expand = 16, kW4Out = kW4Expand + 4, kW4ManyThreads = 32 * (kW4Out + 4);   // first warp that stores
-constexpr int kW4CodeSlots = 4, kW4AStages = 4, kW4MaxCols = 192, kW4ACol = 2 * kW4MaxCols;
+constexpr int kW4CodeSlots = 3, kW4AStages = 2, kW4MaxCols = 192, kW4ACol = 2 * kW4MaxCols;
 constexpr int kW4ManySmem = 232448;
 
 __host__ __device__ constexpr int w4_many_codes(int group) { return kW4CodeSlots * 8 * w4_block_bytes(group); }
 // a receive slot a rank: the owner's columns, 129 floats each
 __host__ __device__ constexpr int w4_many_recv(int bn, int ks) { return ks > 1 ? (bn + 8) * 129 * 4 : 0; }
 constexpr int w4_many_stages(int group, int bn, int ks) {
-  const int n = (kW4ManySmem - 1024 - 512 - w4_many_codes(group) - w4_many_recv(bn, ks)) / (bn * 128);
-  return n < 12 ? n : 12;
+  const int n = (kW4ManySmem - 1024 - 512 - w4_many_codes(group) - w4_many_recv(bn, ks)) / (bn * 256);
+  return n < 8 ? n : 8;
 }
 
 // A word's four pairs of codes to 16-bit values: rows g (s[0], m[0]) and g + 8 (s[1], m[1]).
@@ -70,35 +70,30 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
   extern __shared__ uint8_t raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   const uint32_t base = smem_u32(smem);
-  const int ST = r.stages, xb = r.bn * 128;
+  const int ST = r.stages, xb = r.bn * 256;
   uint8_t* codes = smem + ST * xb;
   float* recv = (float*)(codes + CS * 8 * WB);
   const uint32_t cbase = smem_u32(codes);
   const uint32_t bars = cbase + CS * 8 * WB + w4_many_recv(r.bn, r.ks);
-  auto xfull = [&](int s) { return bars + 8 * s; };
-  auto xempty = [&](int s) { return bars + 8 * (ST + s); };
+  // full: a block's x has landed and its weights stand in tensor memory; free: its products are done
+  auto full = [&](int s) { return bars + 8 * s; };
+  auto free = [&](int s) { return bars + 8 * (ST + s); };
   const uint32_t fixed = bars + 16 * ST;
   auto cfull = [&](int s) { return fixed + 8 * s; };
   auto cempty = [&](int s) { return fixed + 8 * (CS + s); };
-  auto afull = [&](int s) { return fixed + 8 * (2 * CS + s); };
-  auto aempty = [&](int s) { return fixed + 8 * (2 * CS + AS + s); };
-  auto dfull = [&](int b) { return fixed + 8 * (2 * CS + 2 * AS + b); };
-  auto dempty = [&](int b) { return fixed + 8 * (2 * CS + 2 * AS + 2 + b); };
+  auto dfull = [&](int b) { return fixed + 8 * (2 * CS + b); };
+  auto dempty = [&](int b) { return fixed + 8 * (2 * CS + 2 + b); };
   uint32_t* tptr = (uint32_t*)(smem + (dempty(2) - base));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int ks = r.ks, rank = ks > 1 ? (int)cluster_ctarank() : 0;
   if (threadIdx.x == 0) {
     for (int i = 0; i < ST; ++i) {
-      mbar_init(xfull(i), 1);
-      mbar_init(xempty(i), 1);
+      mbar_init(full(i), 1 + kW4Expand / 2);
+      mbar_init(free(i), 1);
     }
     for (int i = 0; i < CS; ++i) {
       mbar_init(cfull(i), 1);
       mbar_init(cempty(i), kW4Expand / 2);
-    }
-    for (int i = 0; i < AS; ++i) {
-      mbar_init(afull(i), 4);
-      mbar_init(aempty(i), 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(dfull(i), 1);
@@ -151,7 +146,6 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
     };
     if (odd < total) fetch(odd);
     for (uint32_t it = odd; it < total && ok; it += 2) {
-      const uint32_t as = (2 * it + h) % AS, aph = ((2 * it + h) / AS) & 1;
       uint32_t v[2][2][8];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
@@ -167,16 +161,17 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(cempty(it % CS));
       if (it + 2 < total) fetch(it + 2);   // the next codes are on their way while these go to tensor memory
-      if (!ok || !__all_sync(0xffffffffu, mbar_wait(aempty(as), aph ^ 1))) break;
+      // (two blocks stand in tensor memory: the products of the last but one are done)
+      if (!ok || (it >= AS && !__all_sync(0xffffffffu, mbar_wait(free((it - AS) % ST), ((it - AS) / ST) & 1)))) break;
       tc_fence_after();
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) tmem_st_frag(tl + 32 * as + ((uint32_t)(16 * b) << 16) + 16 * j, v[b][j]);
+        for (int j = 0; j < 2; ++j) tmem_st_frag(tl + 64 * odd + 32 * h + ((uint32_t)(16 * b) << 16) + 16 * j, v[b][j]);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(afull(as));
+      if (lane == 0) mbar_arrive(full(it % ST));
     }
   } else if (warp == kW4Expand) {   // x
     int it = 0;
@@ -184,18 +179,19 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
     for (int t = first; t < r.tiles && ok; t += step) {
       int iw, ix;
       tile(t, iw, ix);
-      for (int k = 2 * k0; k < 2 * k1; ++k, ++it) {
+      for (int k = k0; k < k1; ++k, ++it) {
         const int s = it % ST;
-        if (it >= ST && !__all_sync(0xffffffffu, mbar_wait(xempty(s), (it / ST - 1) & 1))) { ok = false; break; }
+        if (it >= ST && !__all_sync(0xffffffffu, mbar_wait(free(s), (it / ST - 1) & 1))) { ok = false; break; }
         if (elect_one()) {
-          mbar_arrive_expect_tx(xfull(s), xb);
-          tma_load_2d(base + s * xb, &tx, xfull(s), k * 64, ix * r.bn);
+          mbar_arrive_expect_tx(full(s), xb);
+          tma_load_2d(base + s * xb, &tx, full(s), k * 128, ix * r.bn);
+          tma_load_2d(base + s * xb + xb / 2, &tx, full(s), k * 128 + 64, ix * r.bn);
         }
         __syncwarp();
       }
     }
     // what was loaded has landed, and in the end been read, before the block may exit
-    for (int i = it - ST < 0 ? 0 : it - ST; i < it; ++i) mbar_wait(ok ? xempty(i % ST) : xfull(i % ST), (i / ST) & 1);
+    for (int i = it - ST < 0 ? 0 : it - ST; i < it; ++i) mbar_wait(ok ? free(i % ST) : full(i % ST), (i / ST) & 1);
   } else if (warp == kW4Expand + 1) {   // codes and parameters
     int it = 0;
     bool ok = true;
@@ -215,27 +211,27 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
     for (int i = it - CS < 0 ? 0 : it - CS; i < it; ++i) mbar_wait(ok ? cempty(i % CS) : cfull(i % CS), (i / CS) & 1);
   } else if (warp == kW4Expand + 2) {   // MMAs
     const uint32_t idesc = idesc_f16_f32(128, r.bn, BF);
-    uint32_t it = 0, nt = 0;
+    uint32_t it = 0, nt = 0, ph = 0;
+    int s = 0;
     bool ok = true;
     for (int t = first; t < r.tiles && ok; t += step, ++nt) {
       const uint32_t acc = nt & 1, td = tmem + acc * kW4MaxCols;
       if (nt > 1 && !__all_sync(0xffffffffu, mbar_wait(dempty(acc), (nt / 2 - 1) & 1))) break;
-      for (int k = 2 * k0; k < 2 * k1; ++k, ++it) {
-        const uint32_t s = it % ST, as = it % AS;
-        if (!__all_sync(0xffffffffu, mbar_wait(xfull(s), (it / ST) & 1)) ||
-            !__all_sync(0xffffffffu, mbar_wait(afull(as), (it / AS) & 1))) { ok = false; break; }
+      for (int k = k0; k < k1; ++k) {
+        if (!__all_sync(0xffffffffu, mbar_wait(full(s), ph))) { ok = false; break; }
         tc_fence_after();
         if (elect_one()) {
           const uint64_t db = sdesc_sw128(base + s * xb);
-          const uint32_t ta = tmem + kW4ACol + 32 * as;
+          const uint32_t ta = tmem + kW4ACol + 64 * (it & 1);
 #pragma unroll
-          for (int j = 0; j < 4; ++j)   // 16 columns of k: 8 of tensor memory, two 16-byte units of the descriptor's address
-            mma_f16_ts(td, ta + 8 * j, db + 2 * j, idesc, (k > 2 * k0) | (j > 0));
-          mma_commit(xempty(s));
-          mma_commit(aempty(as));
-          if (k + 1 == 2 * k1) mma_commit(dfull(acc));
+          for (int j = 0; j < 8; ++j)   // 16 columns of k: 8 of tensor memory, two 16-byte units of the descriptor's address
+            mma_f16_ts(td, ta + 8 * j, db + 2 * (j & 3) + (j >> 2) * (xb / 32), idesc, (k > k0) | (j > 0));
+          mma_commit(free(s));
+          if (k + 1 == k1) mma_commit(dfull(acc));
         }
         __syncwarp();
+        ++it;
+        if (++s == ST) s = 0, ph ^= 1;
       }
     }
   } else if (warp >= kW4Out) {   // results
