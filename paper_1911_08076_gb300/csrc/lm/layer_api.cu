@@ -80,7 +80,7 @@ bool encode_x(const W4Args& a, int box, CUtensorMap* tm) {
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr int kW4MaxSplit = 8, kW4SplitCols = 128;
+constexpr int kW4MaxSplit = 8;
 
 // One-time setup of an instance on the current device: its shared memory, and how many clusters of each size run at once
 // (in `slots`; a plain launch is size 1).
@@ -115,38 +115,93 @@ int w4_many_setup(K kern, int (&known)[kMaxDevices][kW4MaxSplit + 1], const int*
   return IFQ_OK;
 }
 
-template <bool BF, int G, bool GATED>
-int run_w4_many(const W4Args& a, cudaStream_t st) {
-  static int known[kMaxDevices][kW4MaxSplit + 1];
-  const auto kern = w4_many_kernel<BF, G, GATED>;
-  const int* slots;
-  const int rc = w4_many_setup(kern, known, &slots);
-  if (rc) return rc;
-  W4Many r;
-  r.a = a;
-  r.tiles_w = ceil_div(a.n, GATED ? 64 : 128);
-  // The columns of a tile and the split of k with the least time: blocks of k in a row, each 256 cycles of expansion or
-  // 4 a column of MMAs, and what a tile and a cluster's join cost besides.
-  double best = 1e300;
-  for (int tx = ceil_div(a.m, kW4MaxCols), n = 0; n < 3; ++n, ++tx) {
+// How a product runs: columns of a tile, a pair of CTAs a tile or one, the split of k.
+struct W4Plan {
+  int cg, bn, ks, halves;
+  double cycles;
+};
+
+// An estimate of the cycles of `turns` tiles in a row: blocks of k at 450 cycles of expansion or 4 a column of MMAs, and a
+// tile's start and end.
+double w4_cycles(double turns, int blocks, int bn) { return turns * (blocks * std::max(450.0, 4.0 * bn) + 1200); }
+
+W4Plan plan_w4_one(const W4Args& a, bool gated, const int* slots) {
+  W4Plan best = {1, 16, 1, 0, 1e300};
+  const long long tw = ceil_div(a.n, gated ? 64 : 128);
+  for (int tx = ceil_div(a.m, 128), n = 0; n < 3; ++n, ++tx) {
     const int bn = (int)round_up(ceil_div(a.m, tx), 16);
-    const long long tiles = (long long)r.tiles_w * ceil_div(a.m, bn);
-    if (tiles > INT_MAX / kW4MaxSplit) return IFQ_ERANGE;
-    const double block = std::max(350.0, 4.0 * bn);
+    const long long tiles = tw * ceil_div(a.m, bn);
     for (int ks = 1; ks <= kW4MaxSplit && ks <= a.kb; ++ks) {
-      if (slots[ks] < 1 || (ks > 1 && bn > kW4SplitCols)) continue;
-      const double turns = (double)((tiles + slots[ks] - 1) / slots[ks]);
-      const double c = turns * (ceil_div(a.kb, ks) * block + 1500 + 4 * bn) + (ks > 1 ? 2500 : 0);
-      if (c < best) best = c, r.bn = bn, r.ks = ks, r.tiles = (int)tiles;
+      if (slots[ks] < 1) continue;
+      const double c = w4_cycles((double)((tiles + slots[ks] - 1) / slots[ks]), ceil_div(a.kb, ks), bn) + (ks > 1 ? 2500 : 0);
+      if (c < best.cycles) best = {1, bn, ks, 0, c};
     }
   }
-  r.tiles_x = ceil_div(a.m, r.bn);
-  r.stages = w4_many_stages(G, r.bn, r.ks);
+  return best;
+}
+W4Plan plan_w4_two(const W4Args& a, bool gated, const int* slots) {
+  W4Plan best = {2, 0, 1, 0, 1e300};
+  if (slots[2] < 1) return best;
+  const int most = a.out_type == IFQ_F32 ? 128 : 256;
+  const long long tw = ceil_div(a.n, gated ? 128 : 256);
+  for (int tx = ceil_div(a.m, most), n = 0; n < 3; ++n, ++tx) {
+    const int bn = (int)round_up(ceil_div(a.m, tx), 64);
+    const long long tiles = tw * ceil_div(a.m, bn);
+    const int rest = (int)(tiles % slots[2]);
+    // the tiles of a last turn that fills half of the SMs or less are cut in two
+    const int halves = rest && 2 * rest <= slots[2];
+    const double c = w4_cycles((double)(tiles / slots[2]), a.kb, bn) + (rest ? w4_cycles(1, a.kb, halves ? bn / 2 : bn) : 0);
+    if (c < best.cycles) best = {2, bn, 1, halves, c};
+  }
+  return best;
+}
+
+template <bool BF, int G, bool GATED, int CG>
+int run_w4_many(const W4Args& a, const W4Plan& p, const int* slots, cudaStream_t st) {
+  const auto kern = w4_many_kernel<BF, G, GATED, CG>;
+  W4Many r;
+  r.a = a;
+  r.bn = p.bn;
+  r.ks = p.ks;
+  r.tiles_w = ceil_div(a.n, (GATED ? 64 : 128) * CG);
+  r.tiles_x = ceil_div(a.m, p.bn);
+  const long long tiles = (long long)r.tiles_w * r.tiles_x;
+  if (tiles > INT_MAX / (2 * kW4MaxSplit)) return IFQ_ERANGE;
+  r.tiles = r.whole = (int)tiles;
+  if (p.halves) {
+    const int rest = r.tiles % slots[2];
+    r.whole -= rest;
+    r.tiles += rest;
+  }
+  const auto wide = [&](const void* q, long long stride) { return aligned16(q) && stride % 8 == 0; };
+  r.vec = a.n % 8 == 0 && wide(a.out, a.out_stride) && (!a.res || wide(a.res, a.res_stride));
+  // shared memory: three or four blocks of x, then codes, then what is left for x
+  const int xb = p.bn / CG * 256, cb = 8 * w4_block_bytes(G);
+  int room = kW4ManySmem - 1024 - 512 - w4_many_recv(p.bn, p.ks) - w4_many_turn(CG, p.bn, a.out_type, GATED);
+  r.stages = 3;
+  room -= 3 * xb;
+  r.slots = std::min(12, room / cb);
+  room -= r.slots * cb;
+  r.stages += std::min(kW4Bars - 3, room / xb);
+  if (r.slots < 2) return IFQ_EUNSUPPORTED;
   CUtensorMap tx;
-  if (!encode_x(a, r.bn, &tx)) return IFQ_ECUDA;
-  if (r.ks > 1)
-    return done(launch_k_cluster(kern, r.ks, dim3((unsigned)(r.tiles * r.ks)), dim3(kW4ManyThreads), kW4ManySmem, st, tx, r));
-  return done(launch_k(kern, dim3((unsigned)std::min(r.tiles, slots[1])), dim3(kW4ManyThreads), kW4ManySmem, st, tx, r));
+  if (!encode_x(a, CG == 2 ? p.bn / 4 : p.bn, &tx)) return IFQ_ECUDA;
+  const int cluster = CG == 2 ? 2 : p.ks, most = CG == 2 ? slots[2] : p.ks > 1 ? r.tiles : slots[1];
+  const dim3 grid((unsigned)(std::min(r.tiles, most) * cluster));
+  if (cluster > 1) return done(launch_k_cluster(kern, cluster, grid, dim3(kW4ManyThreads), kW4ManySmem, st, tx, r));
+  return done(launch_k(kern, grid, dim3(kW4ManyThreads), kW4ManySmem, st, tx, r));
+}
+
+template <bool BF, int G, bool GATED>
+int run_w4_tiles(const W4Args& a, cudaStream_t st) {
+  static int known[2][kMaxDevices][kW4MaxSplit + 1];
+  const int *one, *two;
+  int rc;
+  if ((rc = w4_many_setup(w4_many_kernel<BF, G, GATED, 1>, known[0], &one))) return rc;
+  if ((rc = w4_many_setup(w4_many_kernel<BF, G, GATED, 2>, known[1], &two))) return rc;
+  const W4Plan p1 = plan_w4_one(a, GATED, one), p2 = plan_w4_two(a, GATED, two);
+  if (a.m > 128 && p2.cycles < p1.cycles) return run_w4_many<BF, G, GATED, 2>(a, p2, two, st);
+  return run_w4_many<BF, G, GATED, 1>(a, p1, one, st);
 }
 
 int run_w4(const ifq_w4_desc* d, W4Args& a, const void* x, const void* packed, void* out, const void* res, cudaStream_t st) {
@@ -161,7 +216,7 @@ int run_w4(const ifq_w4_desc* d, W4Args& a, const void* x, const void* packed, v
   return by_weights(d->weights, [&](auto bf, auto group) {
     constexpr bool BF = decltype(bf)::value;
     constexpr int G = decltype(group)::value;
-    return d->weights.gated ? run_w4_many<BF, G, true>(a, st) : run_w4_many<BF, G, false>(a, st);
+    return d->weights.gated ? run_w4_tiles<BF, G, true>(a, st) : run_w4_tiles<BF, G, false>(a, st);
   });
 }
 

@@ -1,16 +1,23 @@
 // Products with weights in 4 bits, many rows of x: tcgen05 tiles whose weights are expanded into tensor memory.
 //
-// A tile is 128 packed rows of w (tensor-memory lanes, the MMA's A operand) x bn rows of x (columns, up to 256).  The
-// weights go from 4 bits to 16 once for all of a tile's columns, in registers, and from there to tensor memory: their
-// fragments need no swizzle, no shared memory, and leave its bandwidth to x.  A block of 128 columns of 16 rows is
-// contiguous, so the codes of a tile's block are eight bulk copies; x comes by TMA in the 128-byte swizzle.
+// A tile is 128 packed rows of w (tensor-memory lanes, the MMA's A operand) x bn rows of x (columns).  The weights go
+// from 4 bits to 16 once for all of a tile's columns, in registers, and from there to tensor memory: their fragments need
+// no swizzle, no shared memory, and leave its bandwidth to x.  A block of 128 columns of 16 rows is contiguous, so the
+// codes of a tile's block are eight bulk copies; x comes by TMA in the 128-byte swizzle.
+//
+// CG = 2: two CTAs of a cluster share a tile of 256 rows (128 lanes each) x up to 256 columns, whose x they hold half
+// each: one thread issues the MMAs of both SMs, and a value of x leaves L2 half as often.
+// CG = 1, for fewer columns: up to 128, and a tile's k may be split over a cluster of ks blocks: each sends its partial
+// columns to the block that owns them through distributed shared memory, which adds them in the order of the ranks.
+//
+// Tensor memory: columns 0 to 255 are the accumulator (two that take turns where bn <= 128, so that a tile's results
+// leave beside the next tile's products), the others four blocks of expanded weights: from an MMA that frees a block to
+// one that reads its successor take 700 cycles, and more between two SMs.
+// Where bn > 128 results are of 16 bits, and leave through shared memory: the accumulator is free again after 1500 cycles
+// or so.
 //
 // Warps: sixteen that expand (a quadrant of 32 lanes, half of the columns of every other block of k each), two that load,
-// one that issues MMAs, four that take results out.  Two accumulators take turns, so that a tile's results leave tensor
-// memory beside the next tile's products.
-//
-// A tile's k may be split over a cluster of ks blocks: each sends its partial columns to the block that owns them through
-// distributed shared memory, which adds them in the order of the ranks.
+// one that issues MMAs, four that take results out.
 #pragma once
 #include <cuda.h>
 
@@ -21,21 +28,24 @@ namespace ifq {
 
 struct W4Many {
   W4Args a;
-  int bn, stages;              // columns a tile (a multiple of 16, up to 192); shared-memory stages of 128 columns of k
-  int tiles, tiles_w, tiles_x; // items; tiles of w's rows and of x's
+  int bn, stages, slots;       // columns a tile; stages of 128 columns of k of x, and of codes, in shared memory
+  int tiles, tiles_w, tiles_x; // items; tiles of w's rows (CG times 128) and of x's
+  int whole;                   // items that are whole tiles; the rest are halves (CG = 2)
   int ks;                      // blocks that a tile's k is split over
+  int vec;                     // rows of out (and of the residual) can be accessed 16 bytes at a time
 };
 
-constexpr int kW4Expand = 16, kW4Out = kW4Expand + 4, kW4ManyThreads = 32 * (kW4Out + 4);   // first warp that stores
-constexpr int kW4CodeSlots = 3, kW4AStages = 2, kW4MaxCols = 192, kW4ACol = 2 * kW4MaxCols;
+constexpr int kW4Expand = 16, kW4Out = kW4Expand + 4, kW4ManyThreads = 32 * (kW4Out + 4);   // kW4Out: first warp that stores
+constexpr int kW4Bars = 8;         // barriers in turn: no fewer than stages of x or blocks of expanded weights
+constexpr int kW4AStages = 4, kW4ACol = 256;
 constexpr int kW4ManySmem = 232448;
 
-__host__ __device__ constexpr int w4_many_codes(int group) { return kW4CodeSlots * 8 * w4_block_bytes(group); }
 // a receive slot a rank: the owner's columns, 129 floats each
 __host__ __device__ constexpr int w4_many_recv(int bn, int ks) { return ks > 1 ? (bn + 8) * 129 * 4 : 0; }
-constexpr int w4_many_stages(int group, int bn, int ks) {
-  const int n = (kW4ManySmem - 1024 - 512 - w4_many_codes(group) - w4_many_recv(bn, ks)) / (bn * 256);
-  return n < 8 ? n : 8;
+// results of 16 bits on their way out: a row a column of the tile (a gated pair's lanes write two rows at a time: apart)
+__host__ __device__ constexpr int w4_out_pitch(bool gated) { return gated ? 144 : 256; }
+__host__ __device__ constexpr int w4_many_turn(int cg, int bn, int out_type, bool gated) {
+  return cg == 2 && out_type != IFQ_F32 ? bn * w4_out_pitch(gated) : 0;
 }
 
 // A word's four pairs of codes to 16-bit values: rows g (s[0], m[0]) and g + 8 (s[1], m[1]).
@@ -62,34 +72,80 @@ __device__ __forceinline__ void w4_params(uint2 p, uint32_t (&s)[2], uint32_t (&
   m[1] = __byte_perm(p.y, 0, 0x3232);
 }
 
-template <bool BF, int G, bool GATED>
+
+// The instructions of two CTAs' MMAs.
+template <int CG>
+__device__ __forceinline__ void w4_mma(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  if constexpr (CG == 1) mma_f16_ts(d, a, b, idesc, acc);
+  else
+    asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;}" ::"r"(d),
+                 "r"(a), "l"(b), "r"(idesc), "r"(acc)
+                 : "memory");
+}
+template <int CG>   // arrives on the barrier of this CTA, or of both
+__device__ __forceinline__ void w4_commit(uint32_t bar) {
+  if constexpr (CG == 1) mma_commit(bar);
+  else
+    asm volatile(
+        "{.reg .b16 m; mov.b16 m, 3; tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
+        "[%0], m;}" ::"r"(bar)
+        : "memory");
+}
+template <int CG>   // bar: a shared::cluster address where CG = 2
+__device__ __forceinline__ void w4_load_x(uint32_t dst, const void* tmap, uint32_t bar, int x, int y) {
+  if constexpr (CG == 1) tma_load_2d(dst, tmap, bar, x, y);
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], "
+        "[%2];" ::"r"(dst),
+        "l"(tmap), "r"(bar), "r"(x), "r"(y)
+        : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void w4_alloc(uint32_t dst) {
+  if constexpr (CG == 1) {
+    tmem_alloc(dst, 512);
+    tmem_relinquish();
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(dst) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+}
+template <int CG>
+__device__ __forceinline__ void w4_dealloc(uint32_t t) {
+  if constexpr (CG == 1) tmem_dealloc(t, 512);
+  else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(t) : "memory");
+}
+
+template <bool BF, int G, bool GATED, int CG>
 __global__ void __launch_bounds__(kW4ManyThreads, 1)
     w4_many_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ W4Many r) {
-  constexpr int WB = w4_block_bytes(G), CS = kW4CodeSlots, AS = kW4AStages;
+  constexpr int WB = w4_block_bytes(G), AS = kW4AStages, NB = kW4Bars, PITCH = w4_out_pitch(GATED), NO = GATED ? 64 : 128;
   const W4Args& a = r.a;
   extern __shared__ uint8_t raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   const uint32_t base = smem_u32(smem);
-  const int ST = r.stages, xb = r.bn * 256;
+  const int ST = r.stages, CS = r.slots, half = r.bn / CG * 128, xb = 2 * half;   // bytes of 64 and 128 columns of k
   uint8_t* codes = smem + ST * xb;
-  float* recv = (float*)(codes + CS * 8 * WB);
+  uint8_t* turn = codes + CS * 8 * WB;
+  float* recv = (float*)turn;
   const uint32_t cbase = smem_u32(codes);
-  const uint32_t bars = cbase + CS * 8 * WB + w4_many_recv(r.bn, r.ks);
-  // full: a block's x has landed and its weights stand in tensor memory; free: its products are done
-  auto full = [&](int s) { return bars + 8 * s; };
-  auto free = [&](int s) { return bars + 8 * (ST + s); };
-  const uint32_t fixed = bars + 16 * ST;
-  auto cfull = [&](int s) { return fixed + 8 * s; };
-  auto cempty = [&](int s) { return fixed + 8 * (CS + s); };
-  auto dfull = [&](int b) { return fixed + 8 * (2 * CS + b); };
-  auto dempty = [&](int b) { return fixed + 8 * (2 * CS + 2 + b); };
-  uint32_t* tptr = (uint32_t*)(smem + (dempty(2) - base));
+  const uint32_t bars = smem_u32(turn) + w4_many_recv(r.bn, r.ks) + w4_many_turn(CG, r.bn, a.out_type, GATED);
+  // Block it of all that the CTA goes through: full(it % NB): its x has landed and its weights stand in tensor memory (of
+  // both CTAs, on the first one's barrier); done(it % NB): its products are there.
+  auto full = [&](int i) { return bars + 8 * i; };
+  auto done = [&](int i) { return bars + 8 * (NB + i); };
+  auto dfull = [&](int b) { return bars + 8 * (2 * NB + b); };
+  auto dempty = [&](int b) { return bars + 8 * (2 * NB + 2 + b); };
+  auto cfull = [&](int s) { return bars + 8 * (2 * NB + 4 + s); };
+  auto cempty = [&](int s) { return bars + 8 * (2 * NB + 4 + CS + s); };
+  uint32_t* tptr = (uint32_t*)(smem + (cempty(CS) - base));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int ks = r.ks, rank = ks > 1 ? (int)cluster_ctarank() : 0;
+  const int rank = CG == 2 || r.ks > 1 ? (int)cluster_ctarank() : 0, ks = r.ks;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < ST; ++i) {
-      mbar_init(full(i), 1 + kW4Expand / 2);
-      mbar_init(free(i), 1);
+    for (int i = 0; i < NB; ++i) {
+      mbar_init(full(i), 1 + CG * kW4Expand / 2);
+      mbar_init(done(i), 1);
     }
     for (int i = 0; i < CS; ++i) {
       mbar_init(cfull(i), 1);
@@ -97,45 +153,55 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(dfull(i), 1);
-      mbar_init(dempty(i), 4);
+      mbar_init(dempty(i), 4 * CG);
     }
     fence_mbar_init();
     prefetch_tmap(&tx);
   }
-  if (warp == 0) {
-    tmem_alloc(smem_u32(tptr), 512);
-    tmem_relinquish();
-  }
+  if (warp == 0) w4_alloc<CG>(smem_u32(tptr));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tptr;
-  if (ks > 1) cluster_sync_all();   // the partners' shared memory is there
+  if (CG == 2 || ks > 1) cluster_sync_all();   // the partners' shared memory is there
   grid_dep_wait();
   grid_dep_launch();
 
-  const uint32_t uks = ks;
-  const int k0 = (uint32_t)(rank * a.kb) / uks, k1 = (uint32_t)((rank + 1) * a.kb) / uks;
-  const int first = blockIdx.x / uks, step = gridDim.x / uks;
-  // Tiles in groups of 16 tiles of w, within a group along w first.
-  auto tile = [&](uint32_t t, int& iw, int& ix) {
-    const uint32_t g = t / (16u * r.tiles_x), in = t - g * 16u * r.tiles_x, wide = min(16u, r.tiles_w - 16u * g);
-    ix = in / wide;
-    iw = 16 * g + in - ix * wide;
+  const uint32_t uks = ks, uc = CG == 2 ? 2 : uks;   // CTAs of a cluster
+  const int k0 = CG == 2 ? 0 : (uint32_t)(rank * a.kb) / uks, k1 = CG == 2 ? a.kb : (uint32_t)((rank + 1) * a.kb) / uks;
+  const int first = blockIdx.x / uc, step = gridDim.x / uc, accs = r.bn <= 128 ? 2 : 1;
+  // Item t: columns m0 to m0 + wd of the rows of w in tile iw (of this CTA).  Tiles in groups of 16 tiles of w, within a
+  // group along w first.
+  auto tile = [&](uint32_t t, int& iw, int& m0, int& wd) {
+    wd = r.bn;
+    uint32_t odd = 0;
+    if (CG == 2 && t >= (uint32_t)r.whole) {
+      odd = (t - r.whole) & 1;
+      t = r.whole + (t - r.whole) / 2;
+      wd = r.bn / 2;
+    }
+    const uint32_t g = t / (16u * r.tiles_x), in = t - g * 16u * r.tiles_x, wide = min(16u, r.tiles_w - 16u * g), ix = in / wide;
+    iw = (16 * g + in - ix * wide) * CG + (CG == 2 ? rank : 0);
+    m0 = ix * r.bn + odd * (r.bn / 2);
+  };
+  // an arrival on a barrier of the CTA that issues the MMAs
+  auto tell = [&](uint32_t bar) {
+    if (CG == 2) mbar_arrive_remote(mapa_shared(bar, 0));
+    else mbar_arrive(bar);
   };
 
   if (warp < kW4Expand) {
     const int q = warp & 3, h = (warp >> 2) & 1, odd = warp >> 3;
     constexpr int NP = G == 32 ? 2 : 1;   // groups in 64 columns
-    const uint32_t tl = tmem + kW4ACol + ((uint32_t)(q * 32) << 16);
+    const uint32_t tl = tmem + kW4ACol + 32 * h + ((uint32_t)(q * 32) << 16);
     // this warp's blocks are every other one of all that the CTA goes through
     const uint32_t turns = first < r.tiles ? (r.tiles - first + step - 1) / step : 0, total = turns * (k1 - k0);
     uint4 w[2];
     uint2 p[2][NP];
     bool ok = true;
-    auto fetch = [&](uint32_t it) {
-      const uint32_t slot = it % CS;
-      if (!__all_sync(0xffffffffu, mbar_wait(cfull(slot), (it / CS) & 1))) { ok = false; return; }
+    uint32_t slot = odd % CS, ph = odd / CS & 1;
+    auto fetch = [&] {
+      if (!__all_sync(0xffffffffu, mbar_wait(cfull(slot), ph))) { ok = false; return; }
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const uint8_t* c = codes + (slot * 8 + 2 * q + b) * WB;
@@ -144,7 +210,7 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
         for (int i = 0; i < NP; ++i) p[b][i] = *(const uint2*)(c + 1024 + 64 * (h * 64 / G + i) + 8 * (lane / 4));
       }
     };
-    if (odd < total) fetch(odd);
+    if (odd < total) fetch();
     for (uint32_t it = odd; it < total && ok; it += 2) {
       uint32_t v[2][2][8];
 #pragma unroll
@@ -159,91 +225,170 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
         }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(cempty(it % CS));
-      if (it + 2 < total) fetch(it + 2);   // the next codes are on their way while these go to tensor memory
-      // (two blocks stand in tensor memory: the products of the last but one are done)
-      if (!ok || (it >= AS && !__all_sync(0xffffffffu, mbar_wait(free((it - AS) % ST), ((it - AS) / ST) & 1)))) break;
+      if (lane == 0) mbar_arrive(cempty(slot));
+      if ((slot += 2) >= CS) slot -= CS, ph ^= 1;
+      if (it + 2 < total) fetch();   // the next codes are on their way while these go to tensor memory
+      if (!ok || (it >= AS && !__all_sync(0xffffffffu, mbar_wait(done((it - AS) % NB), (it - AS) / NB & 1)))) break;
       tc_fence_after();
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) tmem_st_frag(tl + 64 * odd + 32 * h + ((uint32_t)(16 * b) << 16) + 16 * j, v[b][j]);
+        for (int j = 0; j < 2; ++j)
+          tmem_st_frag(tl + 64 * (it % AS) + ((uint32_t)(16 * b) << 16) + 16 * j, v[b][j]);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(full(it % ST));
+      if (lane == 0) tell(full(it % NB));
     }
   } else if (warp == kW4Expand) {   // x
-    int it = 0;
+    int it = 0, s = 0;
     bool ok = true;
     for (int t = first; t < r.tiles && ok; t += step) {
-      int iw, ix;
-      tile(t, iw, ix);
+      int iw, m0, wd;
+      tile(t, iw, m0, wd);
+      const int rows = wd / CG, box = r.bn / (CG == 2 ? 4 : 1);
+      m0 += rank * (CG == 2 ? rows : 0);
       for (int k = k0; k < k1; ++k, ++it) {
-        const int s = it % ST;
-        if (it >= ST && !__all_sync(0xffffffffu, mbar_wait(free(s), (it / ST - 1) & 1))) { ok = false; break; }
+        if (it >= ST && !__all_sync(0xffffffffu, mbar_wait(done((it - ST) % NB), (it - ST) / NB & 1))) { ok = false; break; }
         if (elect_one()) {
-          mbar_arrive_expect_tx(full(s), xb);
-          tma_load_2d(base + s * xb, &tx, full(s), k * 128, ix * r.bn);
-          tma_load_2d(base + s * xb + xb / 2, &tx, full(s), k * 128 + 64, ix * r.bn);
+          const uint32_t bar = CG == 2 ? mapa_shared(full(it % NB), 0) : full(it % NB);
+          if (CG == 1 || rank == 0) mbar_arrive_expect_tx(full(it % NB), wd * 256);
+          for (int u = 0; u < 2; ++u)
+            for (int c = 0; c < rows; c += box)
+              w4_load_x<CG>(base + s * xb + u * half + c * 128, &tx, bar, k * 128 + 64 * u, m0 + c);
         }
         __syncwarp();
+        if (++s == ST) s = 0;
       }
     }
     // what was loaded has landed, and in the end been read, before the block may exit
-    for (int i = it - ST < 0 ? 0 : it - ST; i < it; ++i) mbar_wait(ok ? free(i % ST) : full(i % ST), (i / ST) & 1);
+    for (int i = it - ST < 0 ? 0 : it - ST; i < it; ++i) mbar_wait(ok ? done(i % NB) : full(i % NB), i / NB & 1);
   } else if (warp == kW4Expand + 1) {   // codes and parameters
-    int it = 0;
+    int it = 0, s = 0, ph = 1;
     bool ok = true;
     for (int t = first; t < r.tiles && ok; t += step) {
-      int iw, ix;
-      tile(t, iw, ix);
-      for (int k = k0; k < k1; ++k, ++it) {
-        const int s = it % CS;
-        if (it >= CS && !__all_sync(0xffffffffu, mbar_wait(cempty(s), (it / CS - 1) & 1))) { ok = false; break; }
+      int iw, m0, wd;
+      tile(t, iw, m0, wd);
+      // (the second of two CTAs may have no rows: it goes through the last ones' again)
+      const uint8_t* from = a.w + ((8ll * min(iw, (a.n - 1) / NO) + min(lane, 7)) * a.kb + k0) * WB;
+      for (int k = k0; k < k1; ++k, ++it, from += WB) {
+        if (!__all_sync(0xffffffffu, mbar_wait(cempty(s), ph))) { ok = false; break; }
         if (lane == 0) mbar_arrive_expect_tx(cfull(s), 8 * WB);
         __syncwarp();
-        if (lane < 8)
-          bulk_copy_g2s(cbase + (s * 8 + lane) * WB, a.w + ((8ll * iw + lane) * a.kb + k) * WB, WB, cfull(s));
+        if (lane < 8) bulk_copy_g2s(cbase + (s * 8 + lane) * WB, from, WB, cfull(s));
         __syncwarp();
+        if (++s == CS) s = 0, ph ^= 1;
       }
     }
-    for (int i = it - CS < 0 ? 0 : it - CS; i < it; ++i) mbar_wait(ok ? cempty(i % CS) : cfull(i % CS), (i / CS) & 1);
-  } else if (warp == kW4Expand + 2) {   // MMAs
-    const uint32_t idesc = idesc_f16_f32(128, r.bn, BF);
-    uint32_t it = 0, nt = 0, ph = 0;
-    int s = 0;
-    bool ok = true;
-    for (int t = first; t < r.tiles && ok; t += step, ++nt) {
-      const uint32_t acc = nt & 1, td = tmem + acc * kW4MaxCols;
-      if (nt > 1 && !__all_sync(0xffffffffu, mbar_wait(dempty(acc), (nt / 2 - 1) & 1))) break;
-      for (int k = k0; k < k1; ++k) {
-        if (!__all_sync(0xffffffffu, mbar_wait(full(s), ph))) { ok = false; break; }
-        tc_fence_after();
-        if (elect_one()) {
+    for (int i = it - CS < 0 ? 0 : it - CS; i < it; ++i) mbar_wait(ok ? cempty(i % CS) : cfull(i % CS), i / CS & 1);
+  } else if (warp == kW4Expand + 2) {   // MMAs: one thread, of the first CTA where there are two
+    if ((CG == 1 || rank == 0) && elect_one()) {
+      uint32_t it = 0, nt = 0;
+      int s = 0;
+      bool ok = true;
+      for (int t = first; t < r.tiles && ok; t += step, ++nt) {
+        const uint32_t acc = accs == 2 ? nt & 1 : 0, use = nt / accs, td = tmem + acc * 128;
+        const uint32_t idesc = idesc_f16_f32(128 * CG, CG == 2 && t >= r.whole ? r.bn / 2 : r.bn, BF);
+        if (use && !(CG == 2 ? mbar_wait_cluster(dempty(acc), (use - 1) & 1) : mbar_wait(dempty(acc), (use - 1) & 1))) break;
+        for (int k = k0; k < k1; ++k, ++it) {
+          const uint32_t bar = full(it % NB), ph = it / NB & 1;
+          if (!(CG == 2 ? mbar_wait_cluster(bar, ph) : mbar_wait(bar, ph))) { ok = false; break; }
+          tc_fence_after();
           const uint64_t db = sdesc_sw128(base + s * xb);
-          const uint32_t ta = tmem + kW4ACol + 64 * (it & 1);
+          const uint32_t ta = tmem + kW4ACol + 64 * (it % AS);
 #pragma unroll
           for (int j = 0; j < 8; ++j)   // 16 columns of k: 8 of tensor memory, two 16-byte units of the descriptor's address
-            mma_f16_ts(td, ta + 8 * j, db + 2 * (j & 3) + (j >> 2) * (xb / 32), idesc, (k > k0) | (j > 0));
-          mma_commit(free(s));
-          if (k + 1 == k1) mma_commit(dfull(acc));
+            w4_mma<CG>(td, ta + 8 * j, db + 2 * (j & 3) + (j >> 2) * (half / 16), idesc, (k > k0) | (j > 0));
+          w4_commit<CG>(done(it % NB));
+          if (k + 1 == k1) w4_commit<CG>(dfull(acc));
+          if (++s == ST) s = 0;
         }
-        __syncwarp();
-        ++it;
-        if (++s == ST) s = 0, ph ^= 1;
       }
     }
+    __syncwarp();
   } else if (warp >= kW4Out) {   // results
-    const int q = warp & 3, row = q * 32 + lane;
+    const int q = warp & 3, row = q * 32 + lane, e = (lane >> 3) & 1;
+    // a lane's column of out in its tile; a gated pair's lanes with bit 3 clear hold the gate's rows, and do the even
+    // columns, the others the odd ones
+    const int nc = GATED ? q * 16 + (lane >> 4) * 8 + (lane & 7) : row;
+    auto pair = [&](const uint32_t* v, int i) {
+      const float mine = __uint_as_float(e ? v[i + 1] : v[i]);
+      const float other = __uint_as_float(__shfl_xor_sync(0xffffffffu, e ? v[i] : v[i + 1], 8));
+      return w4_act(a.act, e ? other : mine) * (e ? mine : other);
+    };
     uint32_t nt = 0;
+    bool ok = true;
     for (int t = first; t < r.tiles; t += step, ++nt) {
-      int iw, ix;
-      tile(t, iw, ix);
-      const uint32_t acc = nt & 1, tl = tmem + acc * kW4MaxCols + ((uint32_t)(q * 32) << 16);
-      if (!__all_sync(0xffffffffu, mbar_wait(dfull(acc), (nt / 2) & 1))) break;
+      int iw, m0, wd;
+      tile(t, iw, m0, wd);
+      const uint32_t acc = accs == 2 ? nt & 1 : 0, tl = tmem + acc * 128 + ((uint32_t)(q * 32) << 16);
+      const int n0 = iw * NO, n = n0 + nc;
+      auto release = [&] {   // the accumulator has been read
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tell(dempty(acc));
+      };
+      if (CG == 2 && a.out_type != IFQ_F32) {
+        // through shared memory: rows of out in pieces of 16 bytes, before (the residual) and after
+        const int id = row, wide = min(NO, a.n - n0), tall = min(wd, a.m - m0);
+        auto move = [&](bool in) {
+          if (r.vec) {
+            for (int i = id; i < tall * (NO / 8); i += 128) {
+              const int c = i / (NO / 8), j = i % (NO / 8) * 8;
+              uint4* to = (uint4*)(turn + c * PITCH + 2 * j);
+              if (j < wide) {
+                if (in) *to = *(const uint4*)((const uint16_t*)a.res + (m0 + c) * a.res_stride + n0 + j);
+                else *(uint4*)((uint16_t*)a.out + (m0 + c) * a.out_stride + n0 + j) = *to;
+              }
+            }
+          } else {
+            for (int i = id; i < tall * NO; i += 128) {
+              const int c = i / NO, j = i % NO;
+              uint16_t* to = (uint16_t*)(turn + c * PITCH + 2 * j);
+              if (j < wide) {
+                if (in) *to = ((const uint16_t*)a.res)[(m0 + c) * a.res_stride + n0 + j];
+                else ((uint16_t*)a.out)[(m0 + c) * a.out_stride + n0 + j] = *to;
+              }
+            }
+          }
+          named_bar(1, 128);
+        };
+        if (!GATED && a.res) move(true);
+        // (a wait that ran out: the four warps still meet at every named barrier)
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(dfull(acc), (nt / accs) & 1));
+        tc_fence_after();
+        for (int c0 = 0; c0 < wd; c0 += 32) {
+          uint32_t v[32];
+          tmem_ld<32>(tl + c0, v);
+          if (c0 + 32 == wd) release();
+          if constexpr (GATED) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) w4_store(BF ? IFQ_BF16 : IFQ_F16, turn + (c0 + i + e) * PITCH, nc, pair(v, i));
+          } else {
+            uint8_t* to = turn + c0 * PITCH;
+            float add[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) add[i] = a.res ? w4_load(a.out_type, to + i * PITCH, nc) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) w4_store(a.out_type, to + i * PITCH, nc, __uint_as_float(v[i]) + add[i]);
+          }
+        }
+        named_bar(1, 128);
+        move(false);
+        continue;
+      }
+      float add[16], next[16];   // the residual, loaded 16 columns ahead
+      auto residual = [&](int c0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int m = m0 + c0 + i;
+          next[i] = c0 < wd && m < a.m && n < a.n ? w4_load(a.out_type, a.res, m * a.res_stride + n) : 0.0f;
+        }
+      };
+      if (!GATED && a.res && ks == 1) residual(0);
+      if (!__all_sync(0xffffffffu, mbar_wait(dfull(acc), (nt / accs) & 1))) break;
       tc_fence_after();
-      if (ks > 1) {
+      if (CG == 1 && ks > 1) {
         const int per = (r.bn + ks - 1) / uks;
         for (int c0 = 0; c0 < r.bn; c0 += 16) {
           uint32_t v[16];
@@ -258,43 +403,24 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
         }
         break;
       }
-      const int e = (lane >> 3) & 1;
-      const int n = GATED ? iw * 64 + q * 16 + (lane >> 4) * 8 + (lane & 7) : iw * 128 + row;
-      float add[16], next[16];   // the residual, loaded 16 columns ahead
-      auto residual = [&](int c0) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int m = ix * r.bn + c0 + i;
-          next[i] = c0 < r.bn && m < a.m && n < a.n ? w4_load(a.out_type, a.res, m * a.res_stride + n) : 0.0f;
-        }
-      };
-      if (!GATED && a.res) residual(0);
-      for (int c0 = 0; c0 < r.bn; c0 += 16) {
+      for (int c0 = 0; c0 < wd; c0 += 16) {
         uint32_t v[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) add[i] = next[i];
         if (!GATED && a.res) residual(c0 + 16);
         tmem_ld<16>(tl + c0, v);
-        if (c0 + 16 == r.bn) {   // the accumulator has been read
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(dempty(acc));
-        }
-        const int m0 = ix * r.bn + c0;
+        if (c0 + 16 == wd) release();
         if constexpr (GATED) {
-          // lanes with bit 3 clear hold the gate's rows: they do the even columns, the others the odd ones
 #pragma unroll
           for (int i = 0; i < 16; i += 2) {
-            const float mine = __uint_as_float(e ? v[i + 1] : v[i]);
-            const float other = __uint_as_float(__shfl_xor_sync(0xffffffffu, e ? v[i] : v[i + 1], 8));
-            const float y = w4_act(a.act, e ? other : mine) * (e ? mine : other);
-            const int m = m0 + i + e;
+            const float y = pair(v, i);
+            const int m = m0 + c0 + i + e;
             if (m < a.m && n < a.n) w4_store(BF ? IFQ_BF16 : IFQ_F16, a.out, m * a.out_stride + n, y);
           }
         } else {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int m = m0 + i;
+            const int m = m0 + c0 + i;
             const float y = __uint_as_float(v[i]) + (a.res ? add[i] : 0.0f);
             if (m < a.m && n < a.n) w4_store(a.out_type, a.out, m * a.out_stride + n, y);
           }
@@ -302,16 +428,16 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
       }
     }
   }
-  if (ks > 1) {
+  if (CG == 1 && ks > 1) {
     __syncwarp();
     cluster_sync_all();   // every partial sum has arrived
-    int iw, ix;
-    tile(first, iw, ix);
+    int iw, m0, wd;
+    tile(first, iw, m0, wd);
     const int lo = rank * r.bn / uks, wide = (rank + 1) * r.bn / uks - lo, per = (r.bn + ks - 1) / uks;
-    const int total = (GATED ? 64 : 128) * wide;
+    const int total = NO * wide;
     for (int i = threadIdx.x; i < total; i += kW4ManyThreads) {
-      const int c = i / (GATED ? 64 : 128), j = i % (GATED ? 64 : 128), m = ix * r.bn + lo + c;
-      const int n = iw * (GATED ? 64 : 128) + j, row = GATED ? j / 8 * 16 + j % 8 : j;
+      const int c = i / NO, j = i % NO, m = m0 + lo + c;
+      const int n = iw * NO + j, row = GATED ? j / 8 * 16 + j % 8 : j;
       float v = 0.0f, u = 0.0f;
       for (int p = 0; p < ks; ++p) {
         v += recv[(p * per + c) * 129 + row];
@@ -325,7 +451,8 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 0) tmem_dealloc(tmem, 512);
+  if (CG == 2) cluster_sync_all();   // neither CTA's memory is used by the other any more
+  if (warp == 0) w4_dealloc<CG>(tmem);
 }
 
 }  // namespace ifq
