@@ -10,6 +10,7 @@
 #include "norm.cuh"
 #include "scores.cuh"
 #include "w4.cuh"
+#include "w4_few.cuh"
 #include "w4_many.cuh"
 
 namespace {
@@ -133,7 +134,9 @@ W4Plan plan_w4_one(const W4Args& a, bool gated, const int* slots) {
     const long long tiles = tw * ceil_div(a.m, bn);
     for (int ks = 1; ks <= kW4MaxSplit && ks <= a.kb; ++ks) {
       if (slots[ks] < 1) continue;
-      const double c = w4_cycles((double)((tiles + slots[ks] - 1) / slots[ks]), ceil_div(a.kb, ks), bn) + (ks > 1 ? 2500 : 0);
+      const double turns = (double)((tiles + slots[ks] - 1) / slots[ks]);
+      // (a cluster does one tile and ends)
+      const double c = w4_cycles(turns, ceil_div(a.kb, ks), bn) + (ks > 1 ? 2500 + 5000 * (turns - 1) : 0);
       if (c < best.cycles) best = {1, bn, ks, 0, c};
     }
   }
@@ -204,6 +207,29 @@ int run_w4_tiles(const W4Args& a, cudaStream_t st) {
   return run_w4_many<BF, G, GATED, 1>(a, p1, one, st);
 }
 
+constexpr int kW4FewRows = 16;
+
+template <bool BF, int G, bool GATED, int NT>
+int run_w4_few(const W4Args& a, cudaStream_t st) {
+  static bool set[kMaxDevices];
+  const auto kern = w4_few_kernel<BF, G, GATED, NT>;
+  const int rc = allow_smem(kern, kW4ManySmem, set);
+  if (rc) return rc;
+  W4Few r;
+  r.a = a;
+  r.blocks = ceil_div(a.n, GATED ? 8 : 16);
+  // Warps along k: the fewest blocks in a row a warp, and of equals the fewest warps (their sums are added).
+  const int sms = sm_count();
+  long long best = LLONG_MAX;
+  for (int wk = 1; wk <= kW4FewWarps; wk *= 2) {
+    const int wr = kW4FewWarps / wk;
+    const long long c = ((r.blocks + (long long)wr * sms - 1) / ((long long)wr * sms)) * ceil_div(a.kb, wk);
+    if (c < best) best = c, r.wk = wk, r.wr = wr;
+  }
+  const dim3 grid((unsigned)std::min(ceil_div(r.blocks, r.wr), sms));
+  return done(launch_k(kern, grid, dim3(32 * kW4FewWarps), (size_t)w4_few_smem(a.m, a.kb, NT), st, r));
+}
+
 int run_w4(const ifq_w4_desc* d, W4Args& a, const void* x, const void* packed, void* out, const void* res, cudaStream_t st) {
   if (!d->m) return IFQ_OK;
   if (!x || !packed || !out) return IFQ_EINVAL;
@@ -216,7 +242,14 @@ int run_w4(const ifq_w4_desc* d, W4Args& a, const void* x, const void* packed, v
   return by_weights(d->weights, [&](auto bf, auto group) {
     constexpr bool BF = decltype(bf)::value;
     constexpr int G = decltype(group)::value;
-    return d->weights.gated ? run_w4_tiles<BF, G, true>(a, st) : run_w4_tiles<BF, G, false>(a, st);
+    const auto run = [&](auto pair) {
+      constexpr bool GATED = decltype(pair)::value;
+      // few rows, whose x fits shared memory
+      if (a.m <= 8 && w4_few_smem(a.m, a.kb, 1) <= kW4ManySmem) return run_w4_few<BF, G, GATED, 1>(a, st);
+      if (a.m <= kW4FewRows && w4_few_smem(a.m, a.kb, 2) <= kW4ManySmem) return run_w4_few<BF, G, GATED, 2>(a, st);
+      return run_w4_tiles<BF, G, GATED>(a, st);
+    };
+    return d->weights.gated ? run(std::true_type()) : run(std::false_type());
   });
 }
 

@@ -1,0 +1,176 @@
+// Products with weights in 4 bits, few rows of x: the weights are read once, and are what bounds it.
+//
+// mma.sync with 16 rows of w on M and 8 rows of x on N (NT such tiles): a lane's 16 bytes of codes are its operands of
+// four steps of k.  A block is 16 warps, WR of them beside each other along w's rows and WK along k; the partial sums of
+// a row block's WK warps meet in shared memory and are added in order.  Row blocks go round the blocks of the grid.
+// A warp has four blocks of 128 columns under way, 70 KB an SM, whatever row block they belong to.
+//
+// x stands in shared memory as operands: of every 32 columns, the 16 bytes of lane t of a quad are its registers of two
+// steps, and rows begin 64 bytes apart modulo 128, so that eight lanes read all banks once.
+#pragma once
+#include "w4.cuh"
+
+namespace ifq {
+
+struct W4Few {
+  W4Args a;
+  int wk, wr, blocks;   // warps along k and along rows; row blocks in all
+};
+
+constexpr int kW4FewWarps = 16, kW4FewDeep = 4;
+
+__host__ __device__ constexpr long long w4_few_pitch(int kb) { return kb * 256ll + 64; }
+__host__ __device__ constexpr long long w4_few_smem(int m, int kb, int nt) {   // x, and two turns of partial sums
+  return m * w4_few_pitch(kb) + 2ll * kW4FewWarps * 16 * 8 * nt * 4;
+}
+
+template <bool BF>
+__device__ __forceinline__ void mma_16x8x16(float (&c)[4], const uint32_t* a, uint32_t b0, uint32_t b1) {
+  if constexpr (BF)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint4 load_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint2 load_once2(const void* p) {
+  uint2 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  return v;
+}
+
+template <bool BF, int G, bool GATED, int NT>
+__global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __grid_constant__ W4Few r) {
+  constexpr int WB = w4_block_bytes(G), NP = kW4Cols / G, P = kW4FewDeep, NO = GATED ? 8 : 16;
+  const W4Args& a = r.a;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane / 4, t = lane % 4;
+  const int wk = warp % r.wk, wr = warp / r.wk, id = wk * 32 + lane;   // id: the thread among its row block's
+  const long long pitch = w4_few_pitch(a.kb);
+  float* part = (float*)(smem + a.m * pitch) + wr * r.wk * (16 * 8 * NT);   // [2][WR][WK][8 NT tokens][16 rows]
+  constexpr int TURN = kW4FewWarps * 16 * 8 * NT;
+  grid_dep_wait();
+  grid_dep_launch();
+
+  // this warp's blocks: columns k0 to k1 of row blocks first, first + step, ...
+  const int k0 = wk * a.kb / r.wk, nk = (wk + 1) * a.kb / r.wk - k0;
+  const int first = blockIdx.x * r.wr + wr, step = gridDim.x * r.wr;
+  const int rows = first < r.blocks ? (r.blocks - first + step - 1) / step : 0;
+  const int total = rows * nk;
+  const uint8_t* from = a.w + ((long long)first * a.kb + k0) * WB;
+  const long long jump = ((long long)step * a.kb - nk) * WB;
+  uint4 w[P][2];
+  uint2 p[P][NP];
+  int left = nk;
+  auto load = [&](int u) {
+    w[u][0] = load_once(from + 16 * lane);
+    w[u][1] = load_once(from + 512 + 16 * lane);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) p[u][i] = load_once2(from + 1024 + 64 * i + 8 * g);
+    from += WB;
+    if (--left == 0) left = nk, from += jump;
+  };
+#pragma unroll
+  for (int u = 0; u < P; ++u)
+    if (u < total) load(u);
+
+  // x, 16 bytes at a time: four pairs of columns of one step's half, one for each lane of a quad
+  {
+    const int vecs = a.kb * 16;
+    for (int i = threadIdx.x; i < a.m * vecs; i += 32 * kW4FewWarps) {
+      const int row = i / vecs, c = i - row * vecs;
+      uint32_t v[4] = {0, 0, 0, 0};
+      if (c * 8 < a.k) load_words(v, a.x + row * a.x_stride + c * 8);
+      uint8_t* to = smem + row * pitch + (c / 4) * 64 + (c % 4) * 4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *(uint32_t*)(to + 16 * j) = v[j];
+    }
+  }
+  __syncthreads();
+
+  float acc[NT][4];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
+  const uint8_t* xs[NT];   // (rows past the last read the last: their results are not stored)
+#pragma unroll
+  for (int i = 0; i < NT; ++i) xs[i] = smem + min(8 * i + g, a.m - 1) * pitch + k0 * 256 + 16 * t;
+
+  int rb = first, turn = 0;
+  auto residual = [&](int i, int block) -> float {   // output i of a row block
+    const int n = block * NO + i % NO;
+    return !GATED && a.res && i < NO * a.m && n < a.n ? w4_load(a.out_type, a.res, (i / NO) * a.res_stride + n) : 0.0f;
+  };
+  float add = rows > 0 ? residual(id, rb) : 0.0f;
+  auto flush = [&] {   // a row block's sums
+    float* mine = part + turn * TURN + wk * (16 * 8 * NT);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        mine[(8 * i + 2 * t + (j & 1)) * 16 + g + 8 * (j >> 1)] = acc[i][j];
+        acc[i][j] = 0.0f;
+      }
+    }
+    if (r.wk == 1) __syncwarp();
+    else named_bar(1 + wr, r.wk * 32);
+    for (int i = id; i < NO * a.m; i += r.wk * 32) {
+      const float* s = part + turn * TURN + (i / NO) * 16 + i % NO;
+      float v = 0.0f, u = 0.0f;
+      for (int q = 0; q < r.wk; ++q) {
+        v += s[q * (16 * 8 * NT)];
+        if (GATED) u += s[q * (16 * 8 * NT) + 8];
+      }
+      const int n = rb * NO + i % NO;
+      if (n >= a.n) continue;
+      if (GATED) v = w4_act(a.act, v) * u;
+      else v += i == id ? add : residual(i, rb);
+      w4_store(a.out_type, a.out, (i / NO) * a.out_stride + n, v);
+    }
+    turn ^= 1;   // (the next sums go elsewhere: who writes to this place again has passed the barrier after these reads)
+    rb += step;
+    if (rb < r.blocks) add = residual(id, rb);
+  };
+
+  if (nk == 0) {   // fewer blocks of k than warps: zeros for the others' sums
+    for (int i = 0; i < rows; ++i) flush();
+    return;
+  }
+  int kk = 0;
+  for (int i = 0; i < total; i += P) {
+#pragma unroll
+    for (int u = 0; u < P; ++u) {
+      if (i + u >= total) break;
+      const uint32_t words[8] = {w[u][0].x, w[u][0].y, w[u][0].z, w[u][0].w, w[u][1].x, w[u][1].y, w[u][1].z, w[u][1].w};
+      uint32_t s[2], m[2];
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) {   // 32 columns
+        if (j * 16 % G == 0) w4_params(p[u][j * 16 / G], s, m);
+        uint32_t v[8];
+        w4_expand<BF>(words[j], s, m, v);
+        w4_expand<BF>(words[j + 1], s, m, v + 4);
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+          const uint4 b = *(const uint4*)(xs[q] + kk * 256 + j * 32);
+          mma_16x8x16<BF>(acc[q], v, b.x, b.y);
+          mma_16x8x16<BF>(acc[q], v + 4, b.z, b.w);
+        }
+      }
+      if (i + u + P < total) load(u);
+      if (++kk == nk) {
+        kk = 0;
+        flush();
+      }
+    }
+  }
+}
+
+}  // namespace ifq

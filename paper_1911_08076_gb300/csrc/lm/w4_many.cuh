@@ -48,31 +48,6 @@ __host__ __device__ constexpr int w4_many_turn(int cg, int bn, int out_type, boo
   return cg == 2 && out_type != IFQ_F32 ? bn * w4_out_pitch(gated) : 0;
 }
 
-// A word's four pairs of codes to 16-bit values: rows g (s[0], m[0]) and g + 8 (s[1], m[1]).
-template <bool BF>
-__device__ __forceinline__ void w4_expand(uint32_t w, const uint32_t (&s)[2], const uint32_t (&m)[2], uint32_t* v) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    // 128 + code as bfloat16, 1024 + code as half: exact, and so is the difference
-    uint32_t c = ((w >> (4 * i)) & 0x000f000fu) | (BF ? 0x43004300u : 0x64006400u);
-    if constexpr (BF) {
-      asm("{.reg .b32 t; mov.b32 t, 0xc300c300; add.rn.bf16x2 %0, %0, t;}" : "+r"(c));
-      asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[i]) : "r"(c), "r"(s[i & 1]), "r"(m[i & 1]));
-    } else {
-      asm("{.reg .b32 t; mov.b32 t, 0xe400e400; add.rn.f16x2 %0, %0, t;}" : "+r"(c));
-      asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(v[i]) : "r"(c), "r"(s[i & 1]), "r"(m[i & 1]));
-    }
-  }
-}
-// A lane's parameters (scale, min of row g; of row g + 8) in both halves of a register each.
-__device__ __forceinline__ void w4_params(uint2 p, uint32_t (&s)[2], uint32_t (&m)[2]) {
-  s[0] = __byte_perm(p.x, 0, 0x1010);
-  m[0] = __byte_perm(p.x, 0, 0x3232);
-  s[1] = __byte_perm(p.y, 0, 0x1010);
-  m[1] = __byte_perm(p.y, 0, 0x3232);
-}
-
-
 // The instructions of two CTAs' MMAs.
 template <int CG>
 __device__ __forceinline__ void w4_mma(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
