@@ -269,9 +269,21 @@ int run_norm(const NormArgs& a, cudaStream_t st) {
   }
 }
 
+constexpr int kScoreParts = 8;
+
 template <int TYPE>
-int run_scores(const ScoresArgs& a, cudaStream_t st) {
-  return done(launch_k(token_scores_kernel<TYPE>, dim3(a.rows), dim3(256), 0, st, a));
+int run_scores(ScoresArgs& a, cudaStream_t st) {
+  // Threads: four loads each, in earnest sizes 512.  A row is split where rows are few, while a thread has a load or more.
+  const long long pieces = (long long)a.vocab * (TYPE == IFQ_F32 ? 4 : 2) / 16 + 2;
+  int threads = 64;
+  while (threads < kScoreThreads && threads * 4 < pieces) threads *= 2;
+  int parts = 1;
+  while (parts < kScoreParts && (long long)a.rows * parts * 2 <= 2 * sm_count() && pieces >= 2ll * parts * threads) parts *= 2;
+  if ((long long)a.rows * parts > INT_MAX) return IFQ_ERANGE;
+  a.parts = parts;
+  const dim3 grid(a.rows * parts), block(threads);
+  if (parts > 1) return done(launch_k_cluster(token_scores_kernel<TYPE>, parts, grid, block, 0, st, a));
+  return done(launch_k(token_scores_kernel<TYPE>, grid, block, 0, st, a));
 }
 
 }  // namespace
@@ -394,6 +406,7 @@ int ifq_token_scores(const ifq_scores_desc* d, const void* logits, const int64_t
   a.vocab = d->vocab;
   a.top = top_ids || top_logprobs ? d->top : 0;
   a.scale = d->scale;
+  a.c = (float)(d->scale * 1.4426950408889634);
   switch (d->dtype) {
     case IFQ_F16: return run_scores<IFQ_F16>(a, S(stream));
     case IFQ_BF16: return run_scores<IFQ_BF16>(a, S(stream));

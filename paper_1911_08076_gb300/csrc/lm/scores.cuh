@@ -1,5 +1,16 @@
 // Scores of tokens: log probabilities, log-sum-exp, entropy and the likeliest tokens of rows of logits.
+//
+// One pass over a row: a thread keeps its largest logit, the sum of e^(z - that) and the sum of e^(z - that) (z - that), and
+// brings both sums to a new reference once for every four loads of 16 bytes.  Reading the row bounds it; a row may be
+// split over a cluster of blocks, whose sums and lists the first one joins, where there are few.
+//
+// The likeliest tokens: if k threads have a logit of at least T, so have the k likeliest tokens.  T is found from the threads'
+// maxima, 16 bits of it one by one; the few threads that reach it have their logits read again (from L2), a warp a
+// thread, and what is at least T is put in a list, from which the k first are taken by counting.  A row with more
+// logits at T than the list holds (many equals) is gone through once for each of the k instead.
 #pragma once
+#include <type_traits>
+
 #include "kv4.cuh"
 
 namespace ifq {
@@ -13,7 +24,8 @@ struct ScoresArgs {
   int64_t* top_ids;
   long long stride;
   int rows, vocab, top;
-  float scale;
+  int parts;            // blocks (of a cluster) a row
+  float scale, c;       // c = scale / ln 2
 };
 
 template <int TYPE>
@@ -36,77 +48,298 @@ __device__ __forceinline__ float key_logit(uint64_t k) {
   return __uint_as_float((int)u < 0 ? u & 0x7fffffffu : ~u);   // (a NaN's key gives a NaN)
 }
 
-// What a row's sums come to.  most: largest z; sum: of e^(z - most); weighted: of e^(z - most) (z - most).
-struct RowScores {
-  float most, log_sum;
-  __device__ RowScores(float m, float sum) : most(m), log_sum(logf(sum)) {}
-  __device__ float lse() const { return most == -INFINITY || most == INFINITY ? most : most + log_sum; }
-  __device__ float logprob(float z) const { return most == -INFINITY ? most : most == INFINITY ? z - most : z - most - log_sum; }
-  __device__ float entropy(float sum, float weighted) const { return most == -INFINITY ? 0.0f : log_sum - weighted / sum; }
-};
 
-__device__ __forceinline__ float block_sum(float v, float* part) {
+constexpr int kScoreThreads = 512, kScoreList = 1024, kScoreDeep = 4;
+
+// A row's sums are relative to its largest logit: of 2^d with d = (x - top) c, c = scale / ln 2, and of 2^d d.  The difference
+// is taken before the product, so that large logits cost no digits.  d is at least -1000: a masked logit's 0 times its
+// -infinity would be no number (NaN and infinities are seen in `top`).
+struct RowSums {
+  float top;        // NaN where there is one, -infinity before any
+  float sum, weighted;
+};
+__device__ __forceinline__ float exp2_of(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void move_to(RowSums& r, float top, float c) {
+  const float d = fmaxf((r.top - top) * c, -1000.0f), f = exp2_of(d);
+  r.weighted = f * fmaf(r.sum, d, r.weighted);
+  r.sum *= f;
+  r.top = top;
+}
+__device__ __forceinline__ void join(RowSums& r, RowSums o, float c) {
+  const float top = max_nan(r.top, o.top);
+  move_to(r, top, c);
+  move_to(o, top, c);
+  r.sum += o.sum;
+  r.weighted += o.weighted;
+}
+
+// Two floats in one register pair, and operations on both.
+__device__ __forceinline__ uint64_t two(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 apart(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+// 16 bytes of a row as logits.
+template <int TYPE, int N>
+__device__ __forceinline__ void unpack_logits(const uint32_t (&w)[4], float (&x)[N]) {
+  if constexpr (TYPE == IFQ_F32) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = v;
-  __syncthreads();
-  v = 0.0f;
-  for (int i = 0; i < (int)blockDim.x / 32; ++i) v += part[i];
-  return v;
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = unpack16<TYPE == IFQ_BF16>(w[i]);
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
+  }
 }
 
 template <int TYPE>
-__global__ void __launch_bounds__(256) token_scores_kernel(const __grid_constant__ ScoresArgs a) {
+__global__ void __launch_bounds__(kScoreThreads) token_scores_kernel(const __grid_constant__ ScoresArgs a) {
+  constexpr int SIZE = TYPE == IFQ_F32 ? 4 : 2, N = 16 / SIZE, U = kScoreDeep;
+  __shared__ RowSums warp_sums[kScoreThreads / 32], block_sums;
+  __shared__ uint64_t list[kScoreList], best[kTopMax];
+  __shared__ int count;
+  const int tid = threadIdx.x, T = blockDim.x, warp = tid / 32, lane = tid % 32, warps = T / 32;
+  const int parts = a.parts, rank = parts > 1 ? (int)cluster_ctarank() : 0;
+  const long long row = blockIdx.x / parts;
+  const float c = a.c;
   grid_dep_wait();
   grid_dep_launch();
-  __shared__ float part[8];
-  __shared__ uint64_t best[8];
-  const long long row = blockIdx.x, at = row * a.stride;
-  float most = -INFINITY;
-  for (int i = threadIdx.x; i < a.vocab; i += 256) most = max_nan(most, logit_at<TYPE>(a.logits, at + i) * a.scale);
+
+  // 16-byte pieces of the row, aligned, and this block's: piece i holds logits i * N - skip and on
+  const uint8_t* begin = (const uint8_t*)a.logits + row * a.stride * SIZE;
+  const int skip = (int)(((uintptr_t)begin & 15) / SIZE);
+  const uint8_t* p = begin - skip * SIZE;
+  const long long pieces = ((long long)a.vocab + skip + N - 1) / N;
+  const int lo = (int)(pieces * rank / parts), hi = (int)(pieces * (rank + 1) / parts);
+  const int whole_lo = skip ? 1 : 0, whole_hi = (int)((a.vocab + (long long)skip) / N);   // pieces that are all logits
+  auto load = [&](int i, uint32_t (&w)[4]) {
+    if (i >= whole_lo && i < whole_hi) {
+      load_words(w, p + 16ll * i);
+      return;
+    }
 #pragma unroll
-  for (int o = 16; o; o >>= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
-  if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = most;
+    for (int j = 0; j < N; ++j) {   // a row's ends
+      const long long e = (long long)i * N - skip + j;
+      const bool in = i < hi && e >= 0 && e < a.vocab;
+      if constexpr (SIZE == 4) w[j] = in ? ((const uint32_t*)begin)[e] : 0xff800000u;
+      else {
+        const uint32_t v = in ? ((const uint16_t*)begin)[e] : TYPE == IFQ_BF16 ? 0xff80u : 0xfc00u;
+        w[j / 2] = j & 1 ? w[j / 2] | v << 16 : v;
+      }
+    }
+  };
+
+  RowSums r = {-INFINITY, 0.0f, 0.0f};
+  const uint64_t c2 = two(c, c);
+  for (int i0 = lo + tid; i0 < hi; i0 += U * T) {
+    uint32_t w[U][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(i0 + u * T < hi ? i0 + u * T : 0x7fffffff, w[u]);
+    float top = r.top;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float x[N];
+      unpack_logits<TYPE>(w[u], x);
+#pragma unroll
+      for (int j = 0; j < N; ++j) top = max_nan(top, x[j]);
+    }
+    if (top != r.top) move_to(r, top, c);
+    const uint64_t down = two(-top, -top);
+    uint64_t sum = two(r.sum, 0.0f), weighted = two(r.weighted, 0.0f);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float x[N];
+      unpack_logits<TYPE>(w[u], x);
+#pragma unroll
+      for (int j = 0; j < N; j += 2) {
+        float2 d = apart(mul2(add2(two(x[j], x[j + 1]), down), c2));
+        d.x = fmaxf(d.x, -1000.0f);
+        d.y = fmaxf(d.y, -1000.0f);
+        const uint64_t e = two(exp2_of(d.x), exp2_of(d.y));
+        sum = add2(sum, e);
+        weighted = fma2(e, two(d.x, d.y), weighted);
+      }
+    }
+    const float2 s = apart(sum), v = apart(weighted);
+    r.sum = s.x + s.y;
+    r.weighted = v.x + v.y;
+  }
+  const uint32_t mine = lo + tid < hi ? (uint32_t)(top_key(r.top, 0) >> 32) : 0u;   // 0: no logits
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    RowSums q;
+    q.top = __shfl_xor_sync(0xffffffffu, r.top, o);
+    q.sum = __shfl_xor_sync(0xffffffffu, r.sum, o);
+    q.weighted = __shfl_xor_sync(0xffffffffu, r.weighted, o);
+    join(r, q, c);
+  }
+  if (lane == 0) warp_sums[warp] = r;
+  if (tid == 0) count = 0;
   __syncthreads();
-  for (int i = 0; i < 8; ++i) most = max_nan(most, part[i]);
-  const float ref = most == -INFINITY ? 0.0f : most;
-  float sum = 0.0f, weighted = 0.0f;
-  for (int i = threadIdx.x; i < a.vocab; i += 256) {
-    const float d = logit_at<TYPE>(a.logits, at + i) * a.scale - ref, e = expf(d);
-    sum += e;
-    weighted += e > 0.0f ? e * d : e;
+  if (warp == 0) {
+    r = warp_sums[0];
+    for (int i = 1; i < warps; ++i) join(r, warp_sums[i], c);
+    if (lane == 0) block_sums = r;
   }
-  sum = block_sum(sum, part);
-  weighted = block_sum(weighted, part);
-  const RowScores s(most, sum);
-  if (threadIdx.x == 0) {
-    if (a.lse) a.lse[row] = s.lse();
-    if (a.entropy) a.entropy[row] = s.entropy(sum, weighted);
-    if (a.logprobs) {
-      const long long t = a.tokens[row];
-      if (t >= a.vocab) set_status(IFQ_ERANGE);
-      a.logprobs[row] = t < 0 ? 0.0f : t >= a.vocab ? NAN : s.logprob(logit_at<TYPE>(a.logits, at + t) * a.scale);
+
+  if (a.top) {
+    // T, the first 16 bits: the largest that k threads reach (all logits where fewer have any)
+    uint32_t t = 0;
+    for (int b = 15; b >= 0; --b) {
+      const uint32_t trial = t | 1u << b;
+      const int n = __syncthreads_count(mine >> 16 >= trial);
+      if (n >= a.top) t = trial;
+      if (n >= a.top && n <= a.top + a.top / 2) break;
     }
-  }
-  uint64_t last = ~0ull;
-  for (int j = 0; j < a.top; ++j) {
-    uint64_t k = 0;
-    for (int i = threadIdx.x; i < a.vocab; i += 256) {
-      const uint64_t u = top_key(logit_at<TYPE>(a.logits, at + i), i);
-      if (u < last && u > k) k = u;
-    }
+    uint32_t take = __ballot_sync(0xffffffffu, mine != 0 && mine >> 16 >= t);
+    while (take) {
+      const int from = lo + warp * 32 + __ffs(take) - 1;
+      take &= take - 1;
+      for (long long i = from + (long long)lane * T; i < hi; i += 32ll * T) {
+        uint32_t w[4];
+        load((int)i, w);
+        float x[N];
+        unpack_logits<TYPE>(w, x);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
-    __syncthreads();
-    if (threadIdx.x % 32 == 0) best[threadIdx.x / 32] = k;
-    __syncthreads();
-    for (int i = 0; i < 8; ++i) k = max(k, best[i]);
-    last = k;
-    if (threadIdx.x == 0) {
-      if (a.top_ids) a.top_ids[row * a.top + j] = key_token(k);
-      if (a.top_logprobs) a.top_logprobs[row * a.top + j] = s.logprob(key_logit(k) * a.scale);
+        for (int j = 0; j < N; ++j) {
+          const long long e = i * N - skip + j;
+          const uint64_t k = top_key(x[j], (int)e);
+          if (k >> 48 >= t && e >= 0 && e < a.vocab) {
+            const int at = atomicAdd(&count, 1);
+            if (at < kScoreList) list[at] = k;
+          }
+        }
+      }
     }
+    if (tid < kTopMax) best[tid] = 0;
+    __syncthreads();
+    const int n = count;
+    if (n <= kScoreList) {
+      for (int i = tid; i < n; i += T) {
+        const uint64_t k = list[i];
+        int before = 0;
+        for (int j = 0; j < n; ++j) before += list[j] > k;
+        if (before < a.top) best[before] = k;
+      }
+    } else {
+      uint64_t last = ~0ull;
+      for (int j = 0; j < a.top; ++j) {
+        uint64_t k = 0;
+        for (int i = lo + tid; i < hi; i += T) {
+          uint32_t w[4];
+          load(i, w);
+          float x[N];
+          unpack_logits<TYPE>(w, x);
+#pragma unroll
+          for (int q = 0; q < N; ++q) {
+            const long long e = (long long)i * N - skip + q;
+            const uint64_t v = top_key(x[q], (int)e);
+            if (v < last && v > k && e >= 0 && e < a.vocab) k = v;
+          }
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
+        if (lane == 0) list[warp] = k;
+        __syncthreads();
+        for (int i = 0; i < warps; ++i) k = max(k, list[i]);
+        if (tid == 0) best[j] = k;
+        last = k;
+        __syncthreads();
+      }
+    }
+  }
+  __syncthreads();
+
+  // the parts' results meet in the first block
+  const uint64_t* tops = best;
+  if (parts > 1) {
+    cluster_sync_all();
+    if (rank == 0) {
+      if (warp == 0) {
+        r = block_sums;
+        for (int q = 1; q < parts; ++q) {
+          const uint32_t from = mapa_shared(smem_u32(&block_sums), q);
+          RowSums o;
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.top) : "r"(from) : "memory");
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.sum) : "r"(from + 4) : "memory");
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.weighted) : "r"(from + 8) : "memory");
+          join(r, o, c);
+        }
+      }
+      if (a.top) {
+        for (int i = tid; i < parts * a.top; i += T) {
+          const int q = i / a.top, j = i - q * a.top;
+          asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(list[i]) : "r"(mapa_shared(smem_u32(&best[j]), q)) : "memory");
+        }
+        __syncthreads();
+        uint64_t k[2] = {0, 0};
+        int before[2] = {0, 0};
+        for (int h = 0; h < 2; ++h) {
+          const int i = tid + h * T;
+          if (i >= parts * a.top) break;
+          k[h] = list[i];
+          for (int j = 0; j < parts * a.top; ++j) before[h] += list[j] > k[h] || (list[j] == k[h] && j < i);   // (zeros are alike)
+        }
+        __syncthreads();
+        for (int h = 0; h < 2; ++h)
+          if (tid + h * T < parts * a.top && before[h] < a.top) list[before[h]] = k[h];
+        tops = list;
+      }
+      if (warp == 0 && lane == 0) block_sums = r;
+    }
+    __syncthreads();
+    cluster_sync_all();   // what the first block has read may go
+    if (rank) return;
+  }
+
+  r = block_sums;
+  const float log2_sum = log2f(r.sum), log_sum = 0.69314718055994531f * log2_sum;
+  auto logprob = [&](float x) {
+    return r.top == -INFINITY ? r.top : (x - r.top) * a.scale - (r.top == INFINITY ? 0.0f : log_sum);
+  };
+  if (tid == 0) {
+    if (a.lse) a.lse[row] = fabsf(r.top) == INFINITY ? r.top : fmaf(r.top, a.scale, log_sum);
+    if (a.entropy)
+      a.entropy[row] = r.top == -INFINITY ? 0.0f : r.top == INFINITY || r.top != r.top ? NAN
+                                                     : 0.69314718055994531f * (log2_sum - r.weighted / r.sum);
+    if (a.logprobs) {
+      const long long k = a.tokens[row];
+      if (k >= a.vocab) set_status(IFQ_ERANGE);
+      a.logprobs[row] = k < 0 ? 0.0f : k >= a.vocab ? NAN : logprob(logit_at<TYPE>(begin, k));
+    }
+  }
+  if (tid < a.top) {
+    const uint64_t k = tops[tid];
+    if (a.top_ids) a.top_ids[row * a.top + tid] = key_token(k);
+    if (a.top_logprobs) a.top_logprobs[row * a.top + tid] = logprob(key_logit(k));
   }
 }
 
