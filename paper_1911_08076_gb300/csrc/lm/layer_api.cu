@@ -27,7 +27,7 @@ int check_w4(const ifq_w4_weights* w, size_t* bytes) {
   const size_t rows = (size_t)w->n * (w->gated ? 2 : 1);
   // (a gated pair's blocks hold 8 rows of each matrix)
   const size_t blocks = round_up(w->gated ? (size_t)(w->n + 7) / 8 : (rows + 15) / 16, 8);
-  *bytes = blocks * (size_t)ceil_div(w->k, kW4Cols) * w4_block_bytes(w->group);
+  *bytes = blocks * (size_t)ceil_div(w->k, kW4Cols) * w4_block_bytes(w->group) + kW4Tail;
   return IFQ_OK;
 }
 
@@ -51,10 +51,9 @@ int any_stride(int64_t given, long long width, long long* out) {
   return IFQ_OK;
 }
 
-int check_w4_desc(const ifq_w4_desc* d, int gated, W4Args* a) {
+int check_w4_desc(const ifq_w4_desc* d, int gated, W4Args* a, size_t* bytes) {
   if (!d) return IFQ_EINVAL;
-  size_t bytes;
-  int rc = check_w4(&d->weights, &bytes);
+  int rc = check_w4(&d->weights, bytes);
   if (rc) return rc;
   const ifq_w4_weights& w = d->weights;
   if (w.gated != gated || d->m < 0 || (!is16(d->out_dtype) && d->out_dtype != IFQ_F32)) return IFQ_EINVAL;
@@ -218,24 +217,25 @@ int run_w4_few(const W4Args& a, cudaStream_t st) {
   W4Few r;
   r.a = a;
   r.blocks = ceil_div(a.n, GATED ? 8 : 16);
-  // Warps along k: the fewest blocks in a row a warp, and of equals the fewest warps (their sums are added).
+  // Warps along k: a warp's blocks in a row, and a row block's sums at the cost of one more.
   const int sms = sm_count();
   long long best = LLONG_MAX;
   for (int wk = 1; wk <= kW4FewWarps; wk *= 2) {
     const int wr = kW4FewWarps / wk;
-    const long long c = ((r.blocks + (long long)wr * sms - 1) / ((long long)wr * sms)) * ceil_div(a.kb, wk);
+    const long long c = ((r.blocks + (long long)wr * sms - 1) / ((long long)wr * sms)) * (ceil_div(a.kb, wk) + 1);
     if (c < best) best = c, r.wk = wk, r.wr = wr;
   }
   const dim3 grid((unsigned)std::min(ceil_div(r.blocks, r.wr), sms));
   return done(launch_k(kern, grid, dim3(32 * kW4FewWarps), (size_t)w4_few_smem(a.m, a.kb, NT), st, r));
 }
 
-int run_w4(const ifq_w4_desc* d, W4Args& a, const void* x, const void* packed, void* out, const void* res, cudaStream_t st) {
+int run_w4(const ifq_w4_desc* d, W4Args& a, size_t bytes, const void* x, const void* packed, void* out, const void* res, cudaStream_t st) {
   if (!d->m) return IFQ_OK;
   if (!x || !packed || !out) return IFQ_EINVAL;
   if (!aligned16(x) || !aligned16(packed) || !aligned16(out) || !aligned16(res)) return IFQ_EALIGN;
   a.x = (const uint16_t*)x;
   a.w = (const uint8_t*)packed;
+  a.large = (const uint32_t*)(a.w + bytes - kW4Tail);
   a.out = out;
   a.res = res;
   if (!get_encode()) return IFQ_ECUDA;
@@ -325,29 +325,33 @@ int ifq_w4_pack(const ifq_w4_weights* w, const void* codes, const void* scales, 
   a.kb = ceil_div(w->k, kW4Cols);
   a.groups = ceil_div(w->k, w->group);
   a.gated = w->gated;
-  const size_t blocks = bytes / w4_block_bytes(w->group);
+  const size_t blocks = (bytes - kW4Tail) / w4_block_bytes(w->group);
   a.row_blocks = (int)(blocks / a.kb);
+  a.large = (uint32_t*)(a.out + bytes - kW4Tail);
+  if (cudaMemsetAsync(a.large, 0, kW4Tail, S(stream)) != cudaSuccess) return IFQ_ECUDA;
   const dim3 grid((unsigned)std::min<size_t>((blocks + kW4PackWarps - 1) / kW4PackWarps, 16 * 1024));
-  return by_weights(*w, [&](auto, auto group) {
-    return done(launch_k(w4_pack_kernel<decltype(group)::value>, grid, dim3(32 * kW4PackWarps), 0, S(stream), a));
+  return by_weights(*w, [&](auto bf, auto group) {
+    return done(launch_k(w4_pack_kernel<decltype(bf)::value, decltype(group)::value>, grid, dim3(32 * kW4PackWarps), 0, S(stream), a));
   });
 }
 
 int ifq_w4_matmul(const ifq_w4_desc* d, const void* x, const void* packed, void* out, const void* residual,
                   void* stream) {
   W4Args a = {};
-  int rc = check_w4_desc(d, 0, &a);
+  size_t bytes;
+  int rc = check_w4_desc(d, 0, &a, &bytes);
   if (rc) return rc;
   if (residual && (rc = any_stride(d->residual_stride, d->weights.n, &a.res_stride))) return rc;
   if (residual && residual == out && a.res_stride != a.out_stride) return IFQ_EINVAL;
-  return run_w4(d, a, x, packed, out, residual, S(stream));
+  return run_w4(d, a, bytes, x, packed, out, residual, S(stream));
 }
 
 int ifq_w4_gated(const ifq_w4_desc* d, const void* x, const void* packed, void* out, void* stream) {
   W4Args a = {};
-  const int rc = check_w4_desc(d, 1, &a);
+  size_t bytes;
+  const int rc = check_w4_desc(d, 1, &a, &bytes);
   if (rc) return rc;
-  return run_w4(d, a, x, packed, out, nullptr, S(stream));
+  return run_w4(d, a, bytes, x, packed, out, nullptr, S(stream));
 }
 
 int ifq_rms_norm(const ifq_norm_desc* d, const void* x, const void* residual, const void* weight, void* sum, void* out,

@@ -7,9 +7,11 @@
 // of a row block is contiguous, 1024 bytes of codes and 64 of parameters a group, and a row block's blocks follow each
 // other:
 //   codes       [2 units of 64 columns][32 lanes][4 words]; the word of step j (16 columns) in lane 4 g + t holds four
-//               pairs of neighbouring columns, pair i in bits 4 i .. 4 i + 3 and 16 + 4 i .. 16 + 4 i + 3:
-//               i = 0, 1: rows g, g + 8, columns 16 j + 2 t and the next; i = 2, 3: the same rows, 8 columns further
+//               pairs of neighbouring columns, pair i in the bits that rotating the word right by 4 i brings to
+//               w4_at .. w4_at + 3 of either half: i = 0, 1: rows g, g + 8, columns 16 j + 2 t and the next; i = 2, 3: the
+//               same rows, 8 columns further
 //   parameters  [128 / group][8][2] pairs (scale, min): of row g, of row g + 8
+// Behind the blocks stand 64 bytes whose first word says whether every scale is below 1/4 in size (0), see w4_expand.
 // A pair of codes masked out of a word and made floats is thus one register of an mma.sync operand (A, 16 x 16), and a
 // register of a tcgen05.st in 16-lane fragments.  Rows and columns past the matrix hold zeros up to whole tiles of 128.
 #pragma once
@@ -17,12 +19,14 @@
 
 namespace ifq {
 
-constexpr int kW4Rows = 16, kW4Cols = 128;
+constexpr int kW4Rows = 16, kW4Cols = 128, kW4Tail = 64;
+__host__ __device__ constexpr int w4_at(bool bf) { return bf ? 3 : 6; }   // first bit of a code: the upper ones of a mantissa
 
 __host__ __device__ constexpr int w4_block_bytes(int group) { return 1024 + 64 * (kW4Cols / group); }
 
 struct W4Args {
   const uint8_t* w;
+  const uint32_t* large;   // a word behind the blocks: 0 if no scale is 1/4 or more
   const uint16_t* x;
   const void* res;     // NULL: none
   void* out;
@@ -60,30 +64,42 @@ __device__ __forceinline__ void w4_store(int type, void* p, long long at, float 
   else ((__nv_bfloat16*)p)[at] = __float2bfloat16_rn(v);
 }
 
-// A word's four pairs of codes to 16-bit values: rows g (s[0], m[0]) and g + 8 (s[1], m[1]).
-template <bool BF>
+// A word's four pairs of codes to 16-bit values: rows g (s[0], m[0]) and g + 8 (s[1], m[1]), each code * scale + min with
+// one rounding.
+//
+// FAST: the masked code is a number as it stands, a subnormal one, code * 2^-130 in bfloat16 and code * 2^-18 in half, which
+// the fma takes as exactly as any other; the scale carries the factor that is missing, and must be below 1/4 for it to be
+// finite.  Otherwise the code is made the mantissa of 16 + code, from which 16 is taken: one operation more for each pair.
+template <bool BF, bool FAST>
 __device__ __forceinline__ void w4_expand(uint32_t w, const uint32_t (&s)[2], const uint32_t (&m)[2], uint32_t* v) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    // 128 + code as bfloat16, 1024 + code as half: exact, and so is the difference
-    uint32_t c = ((w >> (4 * i)) & 0x000f000fu) | (BF ? 0x43004300u : 0x64006400u);
+    uint32_t c = __funnelshift_r(w, w, 4 * i) & (0x000f000fu << w4_at(BF));
+    if (!FAST) c |= BF ? 0x41804180u : 0x4c004c00u;
     if constexpr (BF) {
-      asm("{.reg .b32 t; mov.b32 t, 0xc300c300; add.rn.bf16x2 %0, %0, t;}" : "+r"(c));
+      if (!FAST) asm("{.reg .b32 t; mov.b32 t, 0xc180c180; add.rn.bf16x2 %0, %0, t;}" : "+r"(c));
       asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[i]) : "r"(c), "r"(s[i & 1]), "r"(m[i & 1]));
     } else {
-      asm("{.reg .b32 t; mov.b32 t, 0xe400e400; add.rn.f16x2 %0, %0, t;}" : "+r"(c));
+      if (!FAST) asm("{.reg .b32 t; mov.b32 t, 0xcc00cc00; add.rn.f16x2 %0, %0, t;}" : "+r"(c));
       asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(v[i]) : "r"(c), "r"(s[i & 1]), "r"(m[i & 1]));
     }
   }
 }
-// A lane's parameters (scale, min of row g; of row g + 8) in both halves of a register each.
+// A lane's parameters (scale, min of row g; of row g + 8) in both halves of a register each; FAST: the scales times 2^130 or
+// 2^18, in two exact steps.
+template <bool BF, bool FAST>
 __device__ __forceinline__ void w4_params(uint2 p, uint32_t (&s)[2], uint32_t (&m)[2]) {
   s[0] = __byte_perm(p.x, 0, 0x1010);
   m[0] = __byte_perm(p.x, 0, 0x3232);
   s[1] = __byte_perm(p.y, 0, 0x1010);
   m[1] = __byte_perm(p.y, 0, 0x3232);
+  if (FAST)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (BF) asm("{.reg .b32 t; mov.b32 t, 0x60006000; mul.rn.bf16x2 %0, %0, t;}" : "+r"(s[i & 1]));   // 2^65
+      else asm("{.reg .b32 t; mov.b32 t, 0x60006000; mul.rn.f16x2 %0, %0, t;}" : "+r"(s[i & 1]));                // 2^9
+    }
 }
-
 
 // ---------------------------------------------------------------- packing
 
@@ -91,6 +107,7 @@ struct W4PackArgs {
   const uint8_t* codes;
   const uint16_t *scales, *mins;
   uint8_t* out;
+  uint32_t* large;
   int n, k, kb, groups, gated;
   int row_blocks;   // all of them, those past the matrix too
 };
@@ -99,7 +116,7 @@ constexpr int kW4PackWarps = 8;
 
 // A warp makes one block (16 rows x 128 columns): its codes go through shared memory, where a row has 17 words, so that
 // the bytes that a lane gathers (rows g and g + 8) lie in different banks.
-template <int G>
+template <bool BF, int G>
 __global__ void __launch_bounds__(32 * kW4PackWarps) w4_pack_kernel(const __grid_constant__ W4PackArgs a) {
   grid_dep_wait();
   grid_dep_launch();
@@ -132,7 +149,8 @@ __global__ void __launch_bounds__(32 * kW4PackWarps) w4_pack_kernel(const __grid
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t v = bytes[(g + 8 * (i & 1)) * 68 + (64 * u + 16 * j + 2 * t + 8 * (i >> 1)) / 2];
-          w[j] |= (v & 15u) << (4 * i) | (v >> 4) << (16 + 4 * i);
+          const uint32_t two = ((v & 15u) | (v >> 4) << 16) << w4_at(BF);
+          w[j] |= __funnelshift_l(two, two, 4 * i);
         }
       }
       *(uint4*)(out + 512 * u + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -142,6 +160,7 @@ __global__ void __launch_bounds__(32 * kW4PackWarps) w4_pack_kernel(const __grid
       const long long j = source(rb, r), at = (long long)kb * (kW4Cols / G) + q;
       uint32_t v = 0;
       if (j >= 0 && at < a.groups) v = a.scales[j * a.groups + at] | (uint32_t)a.mins[j * a.groups + at] << 16;
+      if ((v & 0x7fffu) >= (BF ? 0x3e80u : 0x3400u)) *a.large = 1;   // (1/4 or more, an infinity, a NaN; all write the same)
       *(uint32_t*)(out + 1024 + 64 * q + 8 * (r % 8) + 4 * (r / 8)) = v;
     }
     __syncwarp();

@@ -8,6 +8,8 @@
 // x stands in shared memory as operands: of every 32 columns, the 16 bytes of lane t of a quad are its registers of two
 // steps, and rows begin 64 bytes apart modulo 128, so that eight lanes read all banks once.
 #pragma once
+#include <type_traits>
+
 #include "w4.cuh"
 
 namespace ifq {
@@ -64,22 +66,29 @@ __global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __gri
   const int first = blockIdx.x * r.wr + wr, step = gridDim.x * r.wr;
   const int rows = first < r.blocks ? (r.blocks - first + step - 1) / step : 0;
   const int total = rows * nk;
-  const uint8_t* from = a.w + ((long long)first * a.kb + k0) * WB;
+  const uint8_t* codes = a.w + ((long long)first * a.kb + k0) * WB + 16 * lane;
+  const uint8_t* pars = codes - 16 * lane + 1024 + 8 * g;
   const long long jump = ((long long)step * a.kb - nk) * WB;
   uint4 w[P][2];
   uint2 p[P][NP];
   int left = nk;
   auto load = [&](int u) {
-    w[u][0] = load_once(from + 16 * lane);
-    w[u][1] = load_once(from + 512 + 16 * lane);
+    w[u][0] = load_once(codes);
+    w[u][1] = load_once(codes + 512);
 #pragma unroll
-    for (int i = 0; i < NP; ++i) p[u][i] = load_once2(from + 1024 + 64 * i + 8 * g);
-    from += WB;
-    if (--left == 0) left = nk, from += jump;
+    for (int i = 0; i < NP; ++i) p[u][i] = load_once2(pars + 64 * i);
+    codes += WB;
+    pars += WB;
+    if (--left == 0) {
+      left = nk;
+      codes += jump;
+      pars += jump;
+    }
   };
 #pragma unroll
   for (int u = 0; u < P; ++u)
     if (u < total) load(u);
+  const bool large = *a.large != 0;
 
   // x, 16 bytes at a time: four pairs of columns of one step's half, one for each lane of a quad
   {
@@ -144,33 +153,41 @@ __global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __gri
     for (int i = 0; i < rows; ++i) flush();
     return;
   }
-  int kk = 0;
-  for (int i = 0; i < total; i += P) {
+  // (the loop in two forms, of which a launch runs one)
+  auto multiply = [&](auto fast) {
+    constexpr bool FAST = decltype(fast)::value;
+    int kk = nk, xo = 0;
+    for (int i = total; i > 0; i -= P) {
 #pragma unroll
-    for (int u = 0; u < P; ++u) {
-      if (i + u >= total) break;
-      const uint32_t words[8] = {w[u][0].x, w[u][0].y, w[u][0].z, w[u][0].w, w[u][1].x, w[u][1].y, w[u][1].z, w[u][1].w};
-      uint32_t s[2], m[2];
+      for (int u = 0; u < P; ++u) {
+        if (u >= i) break;
+        const uint32_t words[8] = {w[u][0].x, w[u][0].y, w[u][0].z, w[u][0].w, w[u][1].x, w[u][1].y, w[u][1].z, w[u][1].w};
+        uint32_t s[2], m[2];
 #pragma unroll
-      for (int j = 0; j < 8; j += 2) {   // 32 columns
-        if (j * 16 % G == 0) w4_params(p[u][j * 16 / G], s, m);
-        uint32_t v[8];
-        w4_expand<BF>(words[j], s, m, v);
-        w4_expand<BF>(words[j + 1], s, m, v + 4);
+        for (int j = 0; j < 8; j += 2) {   // 32 columns
+          if (j * 16 % G == 0) w4_params<BF, FAST>(p[u][j * 16 / G], s, m);
+          uint32_t v[8];
+          w4_expand<BF, FAST>(words[j], s, m, v);
+          w4_expand<BF, FAST>(words[j + 1], s, m, v + 4);
 #pragma unroll
-        for (int q = 0; q < NT; ++q) {
-          const uint4 b = *(const uint4*)(xs[q] + kk * 256 + j * 32);
-          mma_16x8x16<BF>(acc[q], v, b.x, b.y);
-          mma_16x8x16<BF>(acc[q], v + 4, b.z, b.w);
+          for (int q = 0; q < NT; ++q) {
+            const uint4 b = *(const uint4*)(xs[q] + xo + j * 32);
+            mma_16x8x16<BF>(acc[q], v, b.x, b.y);
+            mma_16x8x16<BF>(acc[q], v + 4, b.z, b.w);
+          }
+        }
+        if (u + P < i) load(u);
+        xo += 256;
+        if (--kk == 0) {
+          kk = nk;
+          xo = 0;
+          flush();
         }
       }
-      if (i + u + P < total) load(u);
-      if (++kk == nk) {
-        kk = 0;
-        flush();
-      }
     }
-  }
+  };
+  if (large) multiply(std::false_type());
+  else multiply(std::true_type());
 }
 
 }  // namespace ifq

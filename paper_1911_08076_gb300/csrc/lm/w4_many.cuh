@@ -21,6 +21,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "tmem.cuh"
 #include "w4.cuh"
 
@@ -187,19 +189,25 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
       }
     };
     uint32_t v[2][2][8];
-    auto expand = [&] {
-      fetch();
+    auto convert = [&](auto fast) {
+      constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const uint32_t words[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
         uint32_t s[2], m[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          if (j < NP) w4_params(p[b][j], s, m);
-          w4_expand<BF>(words[2 * j], s, m, v[b][j]);
-          w4_expand<BF>(words[2 * j + 1], s, m, v[b][j] + 4);
+          if (j < NP) w4_params<BF, FAST>(p[b][j], s, m);
+          w4_expand<BF, FAST>(words[2 * j], s, m, v[b][j]);
+          w4_expand<BF, FAST>(words[2 * j + 1], s, m, v[b][j] + 4);
         }
       }
+    };
+    const bool large = *a.large != 0;
+    auto expand = [&] {
+      fetch();
+      if (large) convert(std::false_type());
+      else convert(std::true_type());
       __syncwarp();
       if (lane == 0) mbar_arrive(cempty(slot));
       if ((slot += 2) >= CS) slot -= CS, ph ^= 1;

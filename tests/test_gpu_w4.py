@@ -98,17 +98,20 @@ def test_real_values(m, n, k, group, dtype, out):
     assert (np.abs(got - y) <= tol).all(), np.max(np.abs(got - y) / tol)
 
 
+@pytest.mark.parametrize("largest", [0.2, 1.0, 300.0])
 @pytest.mark.parametrize("m", [8, 200])
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-def test_every_weight_reads_back(m, group, dtype):
+def test_every_weight_reads_back(m, group, dtype, largest):
     """Rows of x with a single 1: out is the weights, each rounded once from code * scale + min."""
     n, k = 130, 392
     rng = np.random.default_rng(group)
     w = ifq.w4_weights(n, k, group, TYPES[dtype][0])
     codes, scales, mins, values = draw(rng, n, k, group, dtype, False)
     scales[::7], mins[::5] = R.round_to(scales[::7] * 2.0 ** -9, dtype), R.round_to(mins[::5] * 2.0 ** 6, dtype)
-    scales[3], mins[4] = -scales[3], 0.0
+    scales[3], mins[4], scales[5] = -scales[3], 0.0, 0.0
+    scales[6], scales[8] = R.round_to(2.0 ** (-24 if dtype == 'f16' else -130), dtype), R.round_to(largest, dtype)
+    mins[6] = 0.0
     values = R.weights(codes, scales, mins, group, dtype)
     packed = pack(w, codes, scales, mins, dtype)
     for c0 in range(0, k, m):

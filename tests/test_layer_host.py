@@ -15,11 +15,11 @@ def _status(f, *a, **k):
 
 
 def test_packed_sizes():
-    """16 x 128 blocks of 1024 bytes and 64 a group, rows up to whole tiles of 128."""
-    assert ifq.ifq_w4_bytes(ifq.w4_weights(4096, 4096, 128)) == 256 * 32 * 1088
-    assert ifq.ifq_w4_bytes(ifq.w4_weights(1, 8, 32)) == 8 * 1280
-    assert ifq.ifq_w4_bytes(ifq.w4_weights(65, 136, 64, gated=True)) == 16 * 2 * 1152
-    assert ifq.ifq_w4_bytes(ifq.w4_weights(131072, 65536, 128)) == 8192 * 512 * 1088
+    """16 x 128 blocks of 1024 bytes and 64 a group, rows up to whole tiles of 128; 64 bytes behind them."""
+    assert ifq.ifq_w4_bytes(ifq.w4_weights(4096, 4096, 128)) == 256 * 32 * 1088 + 64
+    assert ifq.ifq_w4_bytes(ifq.w4_weights(1, 8, 32)) == 8 * 1280 + 64
+    assert ifq.ifq_w4_bytes(ifq.w4_weights(65, 136, 64, gated=True)) == 16 * 2 * 1152 + 64
+    assert ifq.ifq_w4_bytes(ifq.w4_weights(131072, 65536, 128)) == 8192 * 512 * 1088 + 64
 
 
 @pytest.mark.parametrize("change,status", [
