@@ -4,8 +4,8 @@
 //
 // A row block is 16 packed rows: 16 rows of w, or of a gated pair the gate's rows 8 b .. 8 b + 7 and the other's after
 // them, so that a lane that holds rows g and g + 8 of a block has both factors of an output.  A block of 128 columns
-// of a row block is contiguous, 1024 bytes of codes and 64 of parameters a group, and a row block's blocks follow each
-// other:
+// of a row block is contiguous, 1024 bytes of codes and 64 of parameters a group; those of eight row blocks (a tile of 128
+// rows) follow each other, and then those of the next 128 columns:
 //   codes       [2 units of 64 columns][32 lanes][4 words]; the word of step j (16 columns) in lane 4 g + t holds four
 //               pairs of neighbouring columns, pair i in the bits that rotating the word right by 4 i brings to
 //               w4_at .. w4_at + 3 of either half: i = 0, 1: rows g, g + 8, columns 16 j + 2 t and the next; i = 2, 3: the
@@ -23,6 +23,8 @@ constexpr int kW4Rows = 16, kW4Cols = 128, kW4Tail = 64;
 __host__ __device__ constexpr int w4_at(bool bf) { return bf ? 3 : 6; }   // first bit of a code: the upper ones of a mantissa
 
 __host__ __device__ constexpr int w4_block_bytes(int group) { return 1024 + 64 * (kW4Cols / group); }
+// Where block kb of row block rb stands, in blocks.
+__host__ __device__ constexpr long long w4_place(long long rb, int kb, int blocks) { return (rb / 8 * blocks + kb) * 8 + rb % 8; }
 
 struct W4Args {
   const uint8_t* w;
@@ -129,8 +131,8 @@ __global__ void __launch_bounds__(32 * kW4PackWarps) w4_pack_kernel(const __grid
     return j >= a.n ? -1 : a.gated && r >= 8 ? j + a.n : j;
   };
   for (long long b = (long long)blockIdx.x * kW4PackWarps + warp; b < blocks; b += (long long)gridDim.x * kW4PackWarps) {
-    const long long rb = b / a.kb;
-    const int kb = (int)(b - rb * a.kb);
+    const long long rb = b / (8ll * a.kb) * 8 + b % 8;
+    const int kb = (int)(b / 8 % a.kb);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int r = 2 * i + lane / 16, c = lane % 16;

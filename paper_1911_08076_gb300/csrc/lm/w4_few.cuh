@@ -66,9 +66,14 @@ __global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __gri
   const int first = blockIdx.x * r.wr + wr, step = gridDim.x * r.wr;
   const int rows = first < r.blocks ? (r.blocks - first + step - 1) / step : 0;
   const int total = rows * nk;
-  const uint8_t* codes = a.w + ((long long)first * a.kb + k0) * WB + 16 * lane;
-  const uint8_t* pars = codes - 16 * lane + 1024 + 8 * g;
-  const long long jump = ((long long)step * a.kb - nk) * WB;
+  const uint8_t *codes, *pars;
+  int at = first;
+  auto seek = [&] {
+    codes = a.w + w4_place(at, k0, a.kb) * WB + 16 * lane;
+    pars = codes - 16 * lane + 1024 + 8 * g;
+    at += step;
+  };
+  seek();
   uint4 w[P][2];
   uint2 p[P][NP];
   int left = nk;
@@ -77,12 +82,11 @@ __global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __gri
     w[u][1] = load_once(codes + 512);
 #pragma unroll
     for (int i = 0; i < NP; ++i) p[u][i] = load_once2(pars + 64 * i);
-    codes += WB;
-    pars += WB;
+    codes += 8 * WB;
+    pars += 8 * WB;
     if (--left == 0) {
       left = nk;
-      codes += jump;
-      pars += jump;
+      seek();
     }
   };
 #pragma unroll

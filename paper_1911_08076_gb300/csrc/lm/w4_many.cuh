@@ -2,8 +2,8 @@
 //
 // A tile is 128 packed rows of w (tensor-memory lanes, the MMA's A operand) x bn rows of x (columns).  The weights go
 // from 4 bits to 16 once for all of a tile's columns, in registers, and from there to tensor memory: their fragments need
-// no swizzle, no shared memory, and leave its bandwidth to x.  A block of 128 columns of 16 rows is contiguous, so the
-// codes of a tile's block are eight bulk copies; x comes by TMA in the 128-byte swizzle.
+// no swizzle, no shared memory, and leave its bandwidth to x.  The codes of a tile's 128 columns are contiguous, one bulk
+// copy (eight took 800 cycles to issue); x comes by TMA in the 128-byte swizzle.
 //
 // CG = 2: two CTAs of a cluster share a tile of 256 rows (128 lanes each) x up to 256 columns, whose x they hold half
 // each: one thread issues the MMAs of both SMs, and a value of x leaves L2 half as often.
@@ -258,12 +258,13 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
       int iw, m0, wd;
       tile(t, iw, m0, wd);
       // (the second of two CTAs may have no rows: it goes through the last ones' again)
-      const uint8_t* from = a.w + ((8ll * min(iw, (a.n - 1) / NO) + min(lane, 7)) * a.kb + k0) * WB;
-      for (int k = k0; k < k1; ++k, ++it, from += WB) {
+      const uint8_t* from = a.w + w4_place(8ll * min(iw, (a.n - 1) / NO), k0, a.kb) * WB;
+      for (int k = k0; k < k1; ++k, ++it, from += 8 * WB) {
         if (!__all_sync(0xffffffffu, mbar_wait(cempty(s), ph))) { ok = false; break; }
-        if (lane == 0) mbar_arrive_expect_tx(cfull(s), 8 * WB);
-        __syncwarp();
-        if (lane < 8) bulk_copy_g2s(cbase + (s * 8 + lane) * WB, from, WB, cfull(s));
+        if (elect_one()) {
+          mbar_arrive_expect_tx(cfull(s), 8 * WB);
+          bulk_copy_g2s(cbase + s * 8 * WB, from, 8 * WB, cfull(s));
+        }
         __syncwarp();
         if (++s == CS) s = 0, ph ^= 1;
       }
