@@ -210,6 +210,18 @@ constexpr int kW4FewRows = 16;
 
 template <bool BF, int G, bool GATED, int NT>
 int run_w4_few(const W4Args& a, cudaStream_t st) {
+  const int sms = sm_count(), tiles = ceil_div(a.n, GATED ? 64 : 128);
+  const long long room = kW4ManySmem - w4_ring_fixed(a.m, a.kb, NT);
+  const int stages = (int)std::min<long long>(kW4RingMost, room / (8 * w4_block_bytes(G)));
+  if (tiles >= sms / 2 && stages >= 4) {
+    static bool set[kMaxDevices];
+    const auto kern = w4_ring_kernel<BF, G, GATED, NT>;
+    const int rc = allow_smem(kern, kW4ManySmem, set);
+    if (rc) return rc;
+    const W4Ring r = {a, tiles, stages};
+    const size_t smem = (size_t)w4_ring_fixed(a.m, a.kb, NT) + (size_t)stages * 8 * w4_block_bytes(G);
+    return done(launch_k(kern, dim3((unsigned)std::min(tiles, sms)), dim3(32 * (8 * w4_ring_wk(NT) + 1)), smem, st, r));
+  }
   static bool set[kMaxDevices];
   const auto kern = w4_few_kernel<BF, G, GATED, NT>;
   const int rc = allow_smem(kern, kW4ManySmem, set);
@@ -218,7 +230,6 @@ int run_w4_few(const W4Args& a, cudaStream_t st) {
   r.a = a;
   r.blocks = ceil_div(a.n, GATED ? 8 : 16);
   // Warps along k: a warp's blocks in a row, and a row block's sums at the cost of one more.
-  const int sms = sm_count();
   long long best = LLONG_MAX;
   for (int wk = 1; wk <= kW4FewWarps; wk *= 2) {
     const int wr = kW4FewWarps / wk;

@@ -48,9 +48,87 @@ __device__ __forceinline__ uint2 load_once2(const void* p) {
   return v;
 }
 
+// One block of 128 columns: acc += 16 rows of w times 8 NT rows of x, whose operands stand at xs + xo.
+template <bool BF, bool FAST, int G, int NT>
+__device__ __forceinline__ void w4_block(const uint4 (&w)[2], const uint2 (&p)[kW4Cols / G], const uint8_t* const (&xs)[NT], int xo,
+                                         float (&acc)[NT][4]) {
+  const uint32_t words[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
+  uint32_t s[2], m[2];
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {   // 32 columns
+    if (j * 16 % G == 0) w4_params<BF, FAST>(p[j * 16 / G], s, m);
+    uint32_t v[8];
+    w4_expand<BF, FAST>(words[j], s, m, v);
+    w4_expand<BF, FAST>(words[j + 1], s, m, v + 4);
+#pragma unroll
+    for (int q = 0; q < NT; ++q) {
+      const uint4 b = *(const uint4*)(xs[q] + xo + j * 32);
+      mma_16x8x16<BF>(acc[q], v, b.x, b.y);
+      mma_16x8x16<BF>(acc[q], v + 4, b.z, b.w);
+    }
+  }
+}
+
+// x into shared memory, 16 bytes at a time: four pairs of columns of one step's half, one for each lane of a quad.
+__device__ __forceinline__ void w4_stage_x(const W4Args& a, uint8_t* smem, long long pitch, int id, int threads) {
+  const int vecs = a.kb * 16, total = a.m * vecs;
+  for (int i0 = id; i0 < total; i0 += 4 * threads) {
+    uint32_t v[4][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * threads, row = i / vecs, c = i - row * vecs;
+      v[u][0] = v[u][1] = v[u][2] = v[u][3] = 0;
+      if (i < total && c * 8 < a.k) load_words(v[u], a.x + row * a.x_stride + c * 8);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * threads, row = i / vecs, c = i - row * vecs;
+      if (i >= total) break;
+      uint8_t* to = smem + row * pitch + (c / 4) * 64 + (c % 4) * 4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *(uint32_t*)(to + 16 * j) = v[u][j];
+    }
+  }
+}
+
+// A row block's outputs from its partial sums, part[WK][8 NT tokens][16 rows], by threads id of `threads`.
+template <bool GATED, int NT>
+__device__ __forceinline__ void w4_few_out(const W4Args& a, const float* part, int wk, int rb, int id, int threads, float add) {
+  constexpr int NO = GATED ? 8 : 16;
+  for (int i = id; i < NO * a.m; i += threads) {
+    const float* s = part + (i / NO) * 16 + i % NO;
+    float v = 0.0f, u = 0.0f;
+    for (int q = 0; q < wk; ++q) {
+      v += s[q * (16 * 8 * NT)];
+      if (GATED) u += s[q * (16 * 8 * NT) + 8];
+    }
+    const int n = rb * NO + i % NO;
+    if (n >= a.n) continue;
+    if (GATED) v = w4_act(a.act, v) * u;
+    else if (a.res) v += i == id ? add : w4_load(a.out_type, a.res, (i / NO) * a.res_stride + n);
+    w4_store(a.out_type, a.out, (i / NO) * a.out_stride + n, v);
+  }
+}
+// The residual of output `id` of a row block, loaded before its sums are there.
+template <bool GATED>
+__device__ __forceinline__ float w4_few_residual(const W4Args& a, int rb, int id) {
+  const int n = rb * 16 + id % 16;
+  return !GATED && a.res && id < 16 * a.m && n < a.n ? w4_load(a.out_type, a.res, (id / 16) * a.res_stride + n) : 0.0f;
+}
+template <int NT>
+__device__ __forceinline__ void w4_few_put(float* part, float (&acc)[NT][4], int g, int t) {
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      part[(8 * i + 2 * t + (j & 1)) * 16 + g + 8 * (j >> 1)] = acc[i][j];
+      acc[i][j] = 0.0f;
+    }
+}
+
 template <bool BF, int G, bool GATED, int NT>
 __global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __grid_constant__ W4Few r) {
-  constexpr int WB = w4_block_bytes(G), NP = kW4Cols / G, P = kW4FewDeep, NO = GATED ? 8 : 16;
+  constexpr int WB = w4_block_bytes(G), NP = kW4Cols / G, P = kW4FewDeep;
   const W4Args& a = r.a;
   extern __shared__ __align__(16) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane / 4, t = lane % 4;
@@ -94,18 +172,7 @@ __global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __gri
     if (u < total) load(u);
   const bool large = *a.large != 0;
 
-  // x, 16 bytes at a time: four pairs of columns of one step's half, one for each lane of a quad
-  {
-    const int vecs = a.kb * 16;
-    for (int i = threadIdx.x; i < a.m * vecs; i += 32 * kW4FewWarps) {
-      const int row = i / vecs, c = i - row * vecs;
-      uint32_t v[4] = {0, 0, 0, 0};
-      if (c * 8 < a.k) load_words(v, a.x + row * a.x_stride + c * 8);
-      uint8_t* to = smem + row * pitch + (c / 4) * 64 + (c % 4) * 4;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) *(uint32_t*)(to + 16 * j) = v[j];
-    }
-  }
+  w4_stage_x(a, smem, pitch, threadIdx.x, 32 * kW4FewWarps);
   __syncthreads();
 
   float acc[NT][4];
@@ -118,39 +185,16 @@ __global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __gri
   for (int i = 0; i < NT; ++i) xs[i] = smem + min(8 * i + g, a.m - 1) * pitch + k0 * 256 + 16 * t;
 
   int rb = first, turn = 0;
-  auto residual = [&](int i, int block) -> float {   // output i of a row block
-    const int n = block * NO + i % NO;
-    return !GATED && a.res && i < NO * a.m && n < a.n ? w4_load(a.out_type, a.res, (i / NO) * a.res_stride + n) : 0.0f;
-  };
-  float add = rows > 0 ? residual(id, rb) : 0.0f;
+  float add = rows > 0 ? w4_few_residual<GATED>(a, rb, id) : 0.0f;
   auto flush = [&] {   // a row block's sums
-    float* mine = part + turn * TURN + wk * (16 * 8 * NT);
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        mine[(8 * i + 2 * t + (j & 1)) * 16 + g + 8 * (j >> 1)] = acc[i][j];
-        acc[i][j] = 0.0f;
-      }
-    }
+    float* sums = part + turn * TURN;
+    w4_few_put<NT>(sums + wk * (16 * 8 * NT), acc, g, t);
     if (r.wk == 1) __syncwarp();
     else named_bar(1 + wr, r.wk * 32);
-    for (int i = id; i < NO * a.m; i += r.wk * 32) {
-      const float* s = part + turn * TURN + (i / NO) * 16 + i % NO;
-      float v = 0.0f, u = 0.0f;
-      for (int q = 0; q < r.wk; ++q) {
-        v += s[q * (16 * 8 * NT)];
-        if (GATED) u += s[q * (16 * 8 * NT) + 8];
-      }
-      const int n = rb * NO + i % NO;
-      if (n >= a.n) continue;
-      if (GATED) v = w4_act(a.act, v) * u;
-      else v += i == id ? add : residual(i, rb);
-      w4_store(a.out_type, a.out, (i / NO) * a.out_stride + n, v);
-    }
+    w4_few_out<GATED, NT>(a, sums, r.wk, rb, id, r.wk * 32, add);
     turn ^= 1;   // (the next sums go elsewhere: who writes to this place again has passed the barrier after these reads)
     rb += step;
-    if (rb < r.blocks) add = residual(id, rb);
+    if (rb < r.blocks) add = w4_few_residual<GATED>(a, rb, id);
   };
 
   if (nk == 0) {   // fewer blocks of k than warps: zeros for the others' sums
@@ -165,21 +209,7 @@ __global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __gri
 #pragma unroll
       for (int u = 0; u < P; ++u) {
         if (u >= i) break;
-        const uint32_t words[8] = {w[u][0].x, w[u][0].y, w[u][0].z, w[u][0].w, w[u][1].x, w[u][1].y, w[u][1].z, w[u][1].w};
-        uint32_t s[2], m[2];
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {   // 32 columns
-          if (j * 16 % G == 0) w4_params<BF, FAST>(p[u][j * 16 / G], s, m);
-          uint32_t v[8];
-          w4_expand<BF, FAST>(words[j], s, m, v);
-          w4_expand<BF, FAST>(words[j + 1], s, m, v + 4);
-#pragma unroll
-          for (int q = 0; q < NT; ++q) {
-            const uint4 b = *(const uint4*)(xs[q] + xo + j * 32);
-            mma_16x8x16<BF>(acc[q], v, b.x, b.y);
-            mma_16x8x16<BF>(acc[q], v + 4, b.z, b.w);
-          }
-        }
+        w4_block<BF, FAST, G, NT>(w[u], p[u], xs, xo, acc);
         if (u + P < i) load(u);
         xo += 256;
         if (--kk == 0) {
@@ -188,6 +218,115 @@ __global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __gri
           flush();
         }
       }
+    }
+  };
+  if (large) multiply(std::false_type());
+  else multiply(std::true_type());
+}
+
+// The same for weights of many rows: a block takes tiles of eight row blocks, whose codes a warp of its own brings in by bulk
+// copies, a block of 128 columns of the tile each, as many ahead as shared memory holds; WK warps a row block take every
+// WK-th of them.
+struct W4Ring {
+  W4Args a;
+  int tiles, stages;
+};
+
+__host__ __device__ constexpr int w4_ring_wk(int nt) { return nt == 1 ? 3 : 2; }
+__host__ __device__ constexpr int w4_ring_part(int nt) { return 2 * 8 * w4_ring_wk(nt) * 16 * 8 * nt * 4; }
+__host__ __device__ constexpr long long w4_ring_fixed(int m, int kb, int nt) {   // without the stages
+  return m * w4_few_pitch(kb) + w4_ring_part(nt) + 1024;
+}
+constexpr int kW4RingMost = 32;   // stages
+
+template <bool BF, int G, bool GATED, int NT>
+__global__ void __launch_bounds__(32 * (8 * w4_ring_wk(NT) + 1), 1) w4_ring_kernel(const __grid_constant__ W4Ring r) {
+  constexpr int WB = w4_block_bytes(G), NP = kW4Cols / G, WK = w4_ring_wk(NT);
+  const W4Args& a = r.a;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ST = r.stages;
+  const long long pitch = w4_few_pitch(a.kb);
+  uint8_t* ring = smem + a.m * pitch;   // (a multiple of 64 bytes)
+  float* part = (float*)(ring + ST * 8 * WB);
+  const uint32_t bars = smem_u32(part) + w4_ring_part(NT);
+  auto full = [&](int s) { return bars + 8 * s; };
+  auto empty = [&](int s) { return bars + 8 * (ST + s); };
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < ST; ++s) {
+      mbar_init(full(s), 1);
+      mbar_init(empty(s), 8);
+    }
+    fence_mbar_init();
+  }
+  __syncthreads();
+  grid_dep_wait();
+  grid_dep_launch();
+  const int first = blockIdx.x, step = gridDim.x;
+  if (warp == 8 * WK) {
+    int it = 0, s = 0, ph = 1;
+    bool ok = true;
+    for (int t = first; t < r.tiles && ok; t += step) {
+      const uint8_t* from = a.w + w4_place(8ll * t, 0, a.kb) * WB;
+      for (int k = 0; k < a.kb; ++k, ++it, from += 8 * WB) {
+        if (!__all_sync(0xffffffffu, mbar_wait(empty(s), ph))) { ok = false; break; }
+        if (elect_one()) {
+          mbar_arrive_expect_tx(full(s), 8 * WB);
+          bulk_copy_g2s(smem_u32(ring) + s * 8 * WB, from, 8 * WB, full(s));
+        }
+        __syncwarp();
+        if (++s == ST) s = 0, ph ^= 1;
+      }
+    }
+    // what was copied has landed, and in the end been read, before the block may exit
+    for (int i = it - ST < 0 ? 0 : it - ST; i < it; ++i) mbar_wait(ok ? empty(i % ST) : full(i % ST), i / ST & 1);
+    return;
+  }
+  w4_stage_x(a, smem, pitch, threadIdx.x, 32 * 8 * WK);
+  const bool large = *a.large != 0;
+  named_bar(10, 32 * 8 * WK);
+
+  const int row = warp & 7, wk = warp >> 3, g = lane / 4, t4 = lane % 4, id = wk * 32 + lane;
+  float acc[NT][4];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
+  const uint8_t* xs[NT];   // (rows past the last read the last: their results are not stored)
+#pragma unroll
+  for (int i = 0; i < NT; ++i) xs[i] = smem + min(8 * i + g, a.m - 1) * pitch + 16 * t4;
+  const uint8_t* mine = ring + row * WB;
+  auto multiply = [&](auto fast) {
+    constexpr bool FAST = decltype(fast)::value;
+    int s = 0, ph = 0, turn = 0;   // stage and phase of block k
+    bool ok = true;
+    auto ahead = [&](int n) {
+      s += n;
+      while (s >= ST) s -= ST, ph ^= 1;
+    };
+    for (int t = first; t < r.tiles; t += step, turn ^= 1) {
+      const int rb = 8 * t + row;
+      const float add = w4_few_residual<GATED>(a, rb, id);
+      int k = wk;
+      ahead(wk);
+      for (; k < a.kb; k += WK) {
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(full(s), ph));   // (after one that ran out none waits again)
+        const uint8_t* c = mine + s * 8 * WB;
+        uint4 w[2] = {*(const uint4*)(c + 16 * lane), *(const uint4*)(c + 512 + 16 * lane)};
+        uint2 p[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) p[i] = *(const uint2*)(c + 1024 + 64 * i + 8 * g);
+        w4_block<BF, FAST, G, NT>(w, p, xs, k * 256, acc);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(s));
+        ahead(WK);
+      }
+      // (k - kb blocks past the tile's last: back to the next tile's first)
+      s -= k - a.kb;
+      if (s < 0) s += ST, ph ^= 1;
+      float* sums = part + turn * (w4_ring_part(NT) / 8) + row * WK * (16 * 8 * NT);
+      w4_few_put<NT>(sums + wk * (16 * 8 * NT), acc, g, t4);
+      named_bar(1 + row, 32 * WK);
+      w4_few_out<GATED, NT>(a, sums, WK, rb, id, 32 * WK, add);
     }
   };
   if (large) multiply(std::false_type());

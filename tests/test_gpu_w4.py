@@ -64,7 +64,8 @@ def matmul(w, x, packed, dtype, out, residual=None, pads=(0, 0, 0), extra=3):
 SIZES = [(1, 1, 8), (1, 16, 128), (1, 130, 136), (2, 48, 1024), (3, 257, 264), (5, 64, 4104), (7, 4097, 512), (8, 1000, 640),
          (9, 33, 2056), (15, 300, 384), (16, 512, 1160), (17, 129, 256), (24, 700, 72), (31, 128, 1288), (33, 1025, 520),
          (47, 160, 2560), (64, 96, 8), (65, 640, 328), (100, 2049, 136), (128, 256, 1024), (129, 127, 640), (200, 1152, 264),
-         (255, 64, 392), (257, 384, 200), (384, 130, 520), (513, 520, 648), (1000, 260, 136)]
+         (255, 64, 392), (257, 384, 200), (384, 130, 520), (513, 520, 648), (1000, 260, 136),
+         (1, 9730, 264), (3, 40007, 128), (6, 12289, 1416), (8, 19600, 8), (12, 10000, 648), (16, 20100, 136)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
@@ -122,7 +123,8 @@ def test_every_weight_reads_back(m, group, dtype, largest):
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 8, 8), (1, 100, 1032), (4, 65, 264), (8, 1032, 512), (11, 7, 648), (16, 520, 1024),
-                                   (19, 129, 264), (40, 600, 136), (64, 64, 1288), (130, 257, 392), (300, 96, 520), (600, 200, 128)])
+                                   (19, 129, 264), (40, 600, 136), (64, 64, 1288), (130, 257, 392), (300, 96, 520), (600, 200, 128),
+                                   (1, 5003, 392), (7, 10001, 136), (14, 4901, 648)])
 @pytest.mark.parametrize("group,dtype,act", [(32, "f16", "gelu_tanh"), (64, "bf16", "gelu"), (128, "bf16", "silu"), (128, "f16", "silu")])
 def test_gated(m, n, k, group, dtype, act):
     rng = np.random.default_rng([m, n, k, group, 2])
