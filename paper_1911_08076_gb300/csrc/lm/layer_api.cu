@@ -213,7 +213,7 @@ int run_w4_few(const W4Args& a, cudaStream_t st) {
   const int sms = sm_count(), tiles = ceil_div(a.n, GATED ? 64 : 128);
   const long long room = kW4ManySmem - w4_ring_fixed(a.m, a.kb, NT);
   const int stages = (int)std::min<long long>(kW4RingMost, room / (8 * w4_block_bytes(G)));
-  if (tiles >= sms / 2 && stages >= 4) {
+  if (tiles >= 2 * sms && stages >= 4) {
     static bool set[kMaxDevices];
     const auto kern = w4_ring_kernel<BF, G, GATED, NT>;
     const int rc = allow_smem(kern, kW4ManySmem, set);

@@ -140,10 +140,6 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tptr;
-  if (CG == 2 || ks > 1) cluster_sync_all();   // the partners' shared memory is there
-  grid_dep_wait();
-  grid_dep_launch();
-
   const uint32_t uks = ks, uc = CG == 2 ? 2 : uks;   // CTAs of a cluster
   const int k0 = CG == 2 ? 0 : (uint32_t)(rank * a.kb) / uks, k1 = CG == 2 ? a.kb : (uint32_t)((rank + 1) * a.kb) / uks;
   const int first = blockIdx.x / uc, step = gridDim.x / uc, accs = r.bn <= 128 ? 2 : 1;
@@ -161,6 +157,18 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
     iw = (16 * g + in - ix * wide) * CG + (CG == 2 ? rank : 0);
     m0 = ix * r.bn + odd * (r.bn / 2);
   };
+  // Where the codes of a tile begin.  (The second of two CTAs may have no rows: it goes through the last ones' again.)
+  auto source = [&](int iw) { return a.w + w4_place(8ll * min(iw, (a.n - 1) / NO), k0, a.kb) * WB; };
+  // While the kernel before this one ends, the first codes come as far as L2, which has them right whoever writes them.
+  if (threadIdx.x == 32) {
+    int iw, m0, wd;
+    tile(first, iw, m0, wd);
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(source(iw)), "r"(min(CS, k1 - k0) * 8 * WB) : "memory");
+  }
+  if (CG == 2 || ks > 1) cluster_sync_all();   // the partners' shared memory is there
+  grid_dep_wait();
+  grid_dep_launch();
+
   // An arrival on a barrier of the CTA that issues the MMAs.  What it tells of is tensor memory, which the tcgen05 fences
   // order; a release of the cluster's scope, for all other memory, took 1600 cycles beside the loads.
   auto tell = [&](uint32_t bar) {
@@ -257,8 +265,7 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
     for (int t = first; t < r.tiles && ok; t += step) {
       int iw, m0, wd;
       tile(t, iw, m0, wd);
-      // (the second of two CTAs may have no rows: it goes through the last ones' again)
-      const uint8_t* from = a.w + w4_place(8ll * min(iw, (a.n - 1) / NO), k0, a.kb) * WB;
+      const uint8_t* from = source(iw);
       for (int k = k0; k < k1; ++k, ++it, from += 8 * WB) {
         if (!__all_sync(0xffffffffu, mbar_wait(cempty(s), ph))) { ok = false; break; }
         if (elect_one()) {
