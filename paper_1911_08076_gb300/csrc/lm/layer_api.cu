@@ -280,8 +280,6 @@ int run_norm(const NormArgs& a, cudaStream_t st) {
   }
 }
 
-constexpr int kScoreParts = 8;
-
 template <int TYPE>
 int run_scores(ScoresArgs& a, cudaStream_t st) {
   // Threads: four loads each, in earnest sizes 512.  A row is split where rows are few, while a thread has a load or more.

@@ -4,10 +4,10 @@
 // brings both sums to a new reference once for every four loads of 16 bytes.  Reading the row bounds it; a row may be
 // split over a cluster of blocks, whose sums and lists the first one joins, where there are few.
 //
-// The likeliest tokens: if k threads have a logit of at least T, so have the k likeliest tokens.  T is found from the threads'
-// maxima, 16 bits of it one by one; the few threads that reach it have their logits read again (from L2), a warp a
-// thread, and what is at least T is put in a list, from which the k first are taken by counting.  A row with more
-// logits at T than the list holds (many equals) is gone through once for each of the k instead.
+// The likeliest tokens: if k of the block's 64 groups of threads have a logit of at least T, so have the k likeliest tokens.
+// T is the k-th of the groups' maxima (some 44 of random logits reach it for k = 32); the few threads that reach it have
+// their logits read again (from L2), a warp a thread, and what is at least T is put in a list, from which the k first are
+// taken by counting.  A row with more logits at T than the list holds (many equals) is gone through once for each of the k.
 #pragma once
 #include <type_traits>
 
@@ -49,7 +49,7 @@ __device__ __forceinline__ float key_logit(uint64_t k) {
 }
 
 
-constexpr int kScoreThreads = 512, kScoreList = 1024, kScoreDeep = 4;
+constexpr int kScoreThreads = 512, kScoreList = 1024, kScoreDeep = 4, kScoreBlocks = 2;
 
 // A row's sums are relative to its largest logit: of 2^d with d = (x - top) c, c = scale / ln 2, and of 2^d d.  The difference
 // is taken before the product, so that large logits cost no digits.  d is at least -1000: a masked logit's 0 times its
@@ -120,16 +120,40 @@ __device__ __forceinline__ void unpack_logits(const uint32_t (&w)[4], float (&x)
   }
 }
 
+constexpr int kScoreGroups = 64, kScoreParts = 8;
+
+// What a block of a cluster gives the first one.
+struct RowPart {
+  RowSums sums;
+  float pad;
+  uint64_t best[kTopMax];   // descending
+};
+
+__device__ __forceinline__ RowSums join_lanes(RowSums r, float c, int lanes) {   // over groups of `lanes`
+  for (int o = lanes / 2; o; o >>= 1) {
+    RowSums q;
+    q.top = __shfl_xor_sync(0xffffffffu, r.top, o);
+    q.sum = __shfl_xor_sync(0xffffffffu, r.sum, o);
+    q.weighted = __shfl_xor_sync(0xffffffffu, r.weighted, o);
+    join(r, q, c);
+  }
+  return r;
+}
+
 template <int TYPE>
-__global__ void __launch_bounds__(kScoreThreads) token_scores_kernel(const __grid_constant__ ScoresArgs a) {
+__global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) token_scores_kernel(const __grid_constant__ ScoresArgs a) {
   constexpr int SIZE = TYPE == IFQ_F32 ? 4 : 2, N = 16 / SIZE, U = kScoreDeep;
-  __shared__ RowSums warp_sums[kScoreThreads / 32], block_sums;
-  __shared__ uint64_t list[kScoreList], best[kTopMax];
+  __shared__ RowSums warp_sums[kScoreThreads / 32];
+  __shared__ RowPart part[kScoreParts];
+  __shared__ __align__(16) uint64_t list[kScoreList];
+  __shared__ __align__(16) uint32_t group_top[kScoreGroups];
+  __shared__ uint32_t reach;
   __shared__ int count;
   const int tid = threadIdx.x, T = blockDim.x, warp = tid / 32, lane = tid % 32, warps = T / 32;
   const int parts = a.parts, rank = parts > 1 ? (int)cluster_ctarank() : 0;
-  const long long row = blockIdx.x / parts;
+  const long long row = blockIdx.x / (uint32_t)parts;
   const float c = a.c;
+  if (parts > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (this block's memory is there)
   grid_dep_wait();
   grid_dep_launch();
 
@@ -157,6 +181,13 @@ __global__ void __launch_bounds__(kScoreThreads) token_scores_kernel(const __gri
     }
   };
 
+  // the given token's logit, on its way meanwhile
+  long long token = -1;
+  float given = 0.0f;
+  if (tid == 0 && rank == 0 && a.logprobs) {
+    token = a.tokens[row];
+    if (token >= 0 && token < a.vocab) given = logit_at<TYPE>(begin, token);
+  }
   RowSums r = {-INFINITY, 0.0f, 0.0f};
   const uint64_t c2 = two(c, c);
   for (int i0 = lo + tid; i0 < hi; i0 += U * T) {
@@ -193,33 +224,37 @@ __global__ void __launch_bounds__(kScoreThreads) token_scores_kernel(const __gri
     r.weighted = v.x + v.y;
   }
   const uint32_t mine = lo + tid < hi ? (uint32_t)(top_key(r.top, 0) >> 32) : 0u;   // 0: no logits
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    RowSums q;
-    q.top = __shfl_xor_sync(0xffffffffu, r.top, o);
-    q.sum = __shfl_xor_sync(0xffffffffu, r.sum, o);
-    q.weighted = __shfl_xor_sync(0xffffffffu, r.weighted, o);
-    join(r, q, c);
-  }
+  r = join_lanes(r, c, 32);
   if (lane == 0) warp_sums[warp] = r;
-  if (tid == 0) count = 0;
+  if (a.top) {
+    const int per = T / kScoreGroups;   // threads a group: 1, 2, 4 or 8
+    uint32_t most = mine;
+    for (int o = per / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if (tid % per == 0) group_top[tid / per] = most;
+    if (tid == 0) count = 0;
+    if (tid < kTopMax) part[0].best[tid] = 0;
+  }
   __syncthreads();
   if (warp == 0) {
-    r = warp_sums[0];
-    for (int i = 1; i < warps; ++i) join(r, warp_sums[i], c);
-    if (lane == 0) block_sums = r;
+    r = lane < warps ? warp_sums[lane] : RowSums{-INFINITY, 0.0f, 0.0f};
+    r = join_lanes(r, c, 16);
+    if (lane == 0) part[0].sums = r;
   }
-
   if (a.top) {
-    // T, the first 16 bits: the largest that k threads reach (all logits where fewer have any)
-    uint32_t t = 0;
-    for (int b = 15; b >= 0; --b) {
-      const uint32_t trial = t | 1u << b;
-      const int n = __syncthreads_count(mine >> 16 >= trial);
-      if (n >= a.top) t = trial;
-      if (n >= a.top && n <= a.top + a.top / 2) break;
+    if (tid < kScoreGroups) {
+      const uint32_t v = group_top[tid];
+      int before = 0;
+#pragma unroll 4
+      for (int j = 0; j < kScoreGroups; j += 4) {
+        const uint4 q = *(const uint4*)&group_top[j];
+        before += (q.x > v || (q.x == v && j < tid)) + (q.y > v || (q.y == v && j + 1 < tid)) +
+                  (q.z > v || (q.z == v && j + 2 < tid)) + (q.w > v || (q.w == v && j + 3 < tid));
+      }
+      if (before == a.top - 1) reach = v;
     }
-    uint32_t take = __ballot_sync(0xffffffffu, mine != 0 && mine >> 16 >= t);
+    __syncthreads();
+    const uint32_t t = reach;   // 0 (all logits) where fewer than k groups have any
+    uint32_t take = __ballot_sync(0xffffffffu, mine != 0 && mine >= t);
     while (take) {
       const int from = lo + warp * 32 + __ffs(take) - 1;
       take &= take - 1;
@@ -232,14 +267,13 @@ __global__ void __launch_bounds__(kScoreThreads) token_scores_kernel(const __gri
         for (int j = 0; j < N; ++j) {
           const long long e = i * N - skip + j;
           const uint64_t k = top_key(x[j], (int)e);
-          if (k >> 48 >= t && e >= 0 && e < a.vocab) {
+          if ((uint32_t)(k >> 32) >= t && e >= 0 && e < a.vocab) {
             const int at = atomicAdd(&count, 1);
             if (at < kScoreList) list[at] = k;
           }
         }
       }
     }
-    if (tid < kTopMax) best[tid] = 0;
     __syncthreads();
     const int n = count;
     if (n <= kScoreList) {
@@ -247,7 +281,7 @@ __global__ void __launch_bounds__(kScoreThreads) token_scores_kernel(const __gri
         const uint64_t k = list[i];
         int before = 0;
         for (int j = 0; j < n; ++j) before += list[j] > k;
-        if (before < a.top) best[before] = k;
+        if (before < a.top) part[0].best[before] = k;
       }
     } else {
       uint64_t last = ~0ull;
@@ -270,7 +304,7 @@ __global__ void __launch_bounds__(kScoreThreads) token_scores_kernel(const __gri
         if (lane == 0) list[warp] = k;
         __syncthreads();
         for (int i = 0; i < warps; ++i) k = max(k, list[i]);
-        if (tid == 0) best[j] = k;
+        if (tid == 0) part[0].best[j] = k;
         last = k;
         __syncthreads();
       }
@@ -279,48 +313,43 @@ __global__ void __launch_bounds__(kScoreThreads) token_scores_kernel(const __gri
   __syncthreads();
 
   // the parts' results meet in the first block
-  const uint64_t* tops = best;
+  const uint64_t* tops = part[0].best;
   if (parts > 1) {
-    cluster_sync_all();
-    if (rank == 0) {
-      if (warp == 0) {
-        r = block_sums;
-        for (int q = 1; q < parts; ++q) {
-          const uint32_t from = mapa_shared(smem_u32(&block_sums), q);
-          RowSums o;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.top) : "r"(from) : "memory");
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.sum) : "r"(from + 4) : "memory");
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.weighted) : "r"(from + 8) : "memory");
-          join(r, o, c);
-        }
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (rank) {
+      const uint32_t to = mapa_shared(smem_u32(&part[rank]), 0), from = smem_u32(&part[0]);
+      for (int i = tid; i < (int)sizeof(RowPart) / 8; i += T) {
+        uint64_t v;
+        asm volatile("ld.shared.u64 %0, [%1];" : "=l"(v) : "r"(from + 8 * i) : "memory");
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to + 8 * i), "l"(v) : "memory");
       }
-      if (a.top) {
-        for (int i = tid; i < parts * a.top; i += T) {
-          const int q = i / a.top, j = i - q * a.top;
-          asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(list[i]) : "r"(mapa_shared(smem_u32(&best[j]), q)) : "memory");
-        }
-        __syncthreads();
-        uint64_t k[2] = {0, 0};
-        int before[2] = {0, 0};
-        for (int h = 0; h < 2; ++h) {
-          const int i = tid + h * T;
-          if (i >= parts * a.top) break;
-          k[h] = list[i];
-          for (int j = 0; j < parts * a.top; ++j) before[h] += list[j] > k[h] || (list[j] == k[h] && j < i);   // (zeros are alike)
-        }
-        __syncthreads();
-        for (int h = 0; h < 2; ++h)
-          if (tid + h * T < parts * a.top && before[h] < a.top) list[before[h]] = k[h];
-        tops = list;
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (rank) return;
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (warp == 0) {
+      r = lane < parts ? part[lane].sums : RowSums{-INFINITY, 0.0f, 0.0f};
+      r = join_lanes(r, c, kScoreParts);
+    }
+    for (int i = tid; i < parts * a.top; i += T) {
+      const int q = i / a.top, j = i - q * a.top;
+      const uint64_t k = part[q].best[j];
+      int before = j;
+      for (int o = 0; o < parts; ++o) {   // how many of each other list come before it
+        int n = 0;
+        for (int b = kTopMax; b; b >>= 1)
+          if (n + b <= a.top && part[o].best[n + b - 1] > k) n += b;
+        before += o == q ? 0 : n;
       }
-      if (warp == 0 && lane == 0) block_sums = r;
+      if (k && before < a.top) list[before] = k;
     }
     __syncthreads();
-    cluster_sync_all();   // what the first block has read may go
-    if (rank) return;
+    if (warp == 0 && lane == 0) part[0].sums = r;
+    __syncthreads();
+    tops = list;
   }
 
-  r = block_sums;
+  r = part[0].sums;
   const float log2_sum = log2f(r.sum), log_sum = 0.69314718055994531f * log2_sum;
   auto logprob = [&](float x) {
     return r.top == -INFINITY ? r.top : (x - r.top) * a.scale - (r.top == INFINITY ? 0.0f : log_sum);
@@ -331,9 +360,8 @@ __global__ void __launch_bounds__(kScoreThreads) token_scores_kernel(const __gri
       a.entropy[row] = r.top == -INFINITY ? 0.0f : r.top == INFINITY || r.top != r.top ? NAN
                                                      : 0.69314718055994531f * (log2_sum - r.weighted / r.sum);
     if (a.logprobs) {
-      const long long k = a.tokens[row];
-      if (k >= a.vocab) set_status(IFQ_ERANGE);
-      a.logprobs[row] = k < 0 ? 0.0f : k >= a.vocab ? NAN : logprob(logit_at<TYPE>(begin, k));
+      if (token >= a.vocab) set_status(IFQ_ERANGE);
+      a.logprobs[row] = token < 0 ? 0.0f : token >= a.vocab ? NAN : logprob(given);
     }
   }
   if (tid < a.top) {
