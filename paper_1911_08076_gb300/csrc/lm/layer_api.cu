@@ -291,8 +291,9 @@ int run_scores(ScoresArgs& a, cudaStream_t st) {
   if ((long long)a.rows * parts > INT_MAX) return IFQ_ERANGE;
   a.parts = parts;
   const dim3 grid(a.rows * parts), block(threads);
-  if (parts > 1) return done(launch_k_cluster(token_scores_kernel<TYPE>, parts, grid, block, 0, st, a));
-  return done(launch_k(token_scores_kernel<TYPE>, grid, block, 0, st, a));
+  if (parts > 1) return done(launch_k_cluster(token_scores_kernel<TYPE, 2>, parts, grid, block, 0, st, a));
+  if (a.rows <= 2 * sm_count()) return done(launch_k(token_scores_kernel<TYPE, 2>, grid, block, 0, st, a));
+  return done(launch_k(token_scores_kernel<TYPE, 3>, grid, block, 0, st, a));
 }
 
 }  // namespace

@@ -6,7 +6,7 @@
 //
 // The likeliest tokens: if k of the block's 64 groups of threads have a logit of at least T, so have the k likeliest tokens.
 // T is the k-th of the groups' maxima (some 44 of random logits reach it for k = 32); the few threads that reach it have
-// their logits read again (from L2), a warp a thread, and what is at least T is put in a list, from which the k first are
+// their logits read again (from L2), by all threads, and what is at least T is put in a list, from which the k first are
 // taken by counting.  A row with more logits at T than the list holds (many equals) is gone through once for each of the k.
 #pragma once
 #include <type_traits>
@@ -49,11 +49,10 @@ __device__ __forceinline__ float key_logit(uint64_t k) {
 }
 
 
-constexpr int kScoreThreads = 512, kScoreList = 1024, kScoreDeep = 4, kScoreBlocks = 2;
+constexpr int kScoreThreads = 512, kScoreList = 1024, kScoreDeep = 4;
 
 // A row's sums are relative to its largest logit: of 2^d with d = (x - top) c, c = scale / ln 2, and of 2^d d.  The difference
-// is taken before the product, so that large logits cost no digits.  d is at least -1000: a masked logit's 0 times its
-// -infinity would be no number (NaN and infinities are seen in `top`).
+// is taken before the product, so that large logits cost no digits.
 struct RowSums {
   float top;        // NaN where there is one, -infinity before any
   float sum, weighted;
@@ -104,6 +103,22 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return r;
 }
 
+// The larger of two logits each of a word; _nan: a NaN where there is one, otherwise the number.
+template <bool BF>
+__device__ __forceinline__ uint32_t max16_nan(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if constexpr (BF) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <bool BF>
+__device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if constexpr (BF) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
 // 16 bytes of a row as logits.
 template <int TYPE, int N>
 __device__ __forceinline__ void unpack_logits(const uint32_t (&w)[4], float (&x)[N]) {
@@ -140,15 +155,18 @@ __device__ __forceinline__ RowSums join_lanes(RowSums r, float c, int lanes) {  
   return r;
 }
 
-template <int TYPE>
-__global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) token_scores_kernel(const __grid_constant__ ScoresArgs a) {
+// BLOCKS an SM: three hide each other's selections where rows are many (2048 x 131072: 115 -> 103 us), two leave more
+// registers where few blocks run.
+template <int TYPE, int BLOCKS>
+__global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(const __grid_constant__ ScoresArgs a) {
   constexpr int SIZE = TYPE == IFQ_F32 ? 4 : 2, N = 16 / SIZE, U = kScoreDeep;
   __shared__ RowSums warp_sums[kScoreThreads / 32];
   __shared__ RowPart part[kScoreParts];
-  __shared__ __align__(16) uint64_t list[kScoreList];
+  __shared__ __align__(16) uint64_t list[kScoreList + 2];
+  __shared__ uint16_t who[kScoreThreads];
   __shared__ __align__(16) uint32_t group_top[kScoreGroups];
   __shared__ uint32_t reach;
-  __shared__ int count;
+  __shared__ int count, threads;
   const int tid = threadIdx.x, T = blockDim.x, warp = tid / 32, lane = tid % 32, warps = T / 32;
   const int parts = a.parts, rank = parts > 1 ? (int)cluster_ctarank() : 0;
   const long long row = blockIdx.x / (uint32_t)parts;
@@ -190,38 +208,87 @@ __global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) token_scores_kern
   }
   RowSums r = {-INFINITY, 0.0f, 0.0f};
   const uint64_t c2 = two(c, c);
-  for (int i0 = lo + tid; i0 < hi; i0 += U * T) {
-    uint32_t w[U][4];
-#pragma unroll
-    for (int u = 0; u < U; ++u) load(i0 + u * T < hi ? i0 + u * T : 0x7fffffff, w[u]);
+  const float reach_down = 1000.0f / c;
+  auto add = [&](auto& w) {   // [pieces][4 words]
+    constexpr int V = sizeof(w) / 16;
     float top = r.top;
+    if constexpr (SIZE == 4) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float x[N];
-      unpack_logits<TYPE>(w[u], x);
+      for (int u = 0; u < V; ++u)
 #pragma unroll
-      for (int j = 0; j < N; ++j) top = max_nan(top, x[j]);
+        for (int j = 0; j < 4; ++j) top = max_nan(top, __uint_as_float(w[u][j]));
+    } else {   // two at a time
+      uint32_t m = w[0][0];
+#pragma unroll
+      for (int u = 0; u < V; ++u)
+#pragma unroll
+        for (int j = u == 0; j < 4; ++j) m = max16_nan<TYPE == IFQ_BF16>(m, w[u][j]);
+      const float2 f = unpack16<TYPE == IFQ_BF16>(m);
+      top = max_nan(top, max_nan(f.x, f.y));
     }
     if (top != r.top) move_to(r, top, c);
+    if (top == -INFINITY) return;
+    // A logit below `low` counts as one of its value, 2^-1000 or less: it has a share of 0, and 0 times its distance is 0,
+    // which -infinity's would not be.
+    const float low = top - fmaxf(reach_down, fabsf(top) * (1.0f / 64.0f));
+    uint32_t low2 = 0;
+    if constexpr (TYPE == IFQ_BF16) low2 = 0x10001u * __bfloat16_as_ushort(__float2bfloat16_rd(fmaxf(low, -3.38e38f)));
+    else if constexpr (TYPE == IFQ_F16) low2 = 0x10001u * __half_as_ushort(__float2half_rd(fmaxf(low, -65504.0f)));
     const uint64_t down = two(-top, -top);
     uint64_t sum = two(r.sum, 0.0f), weighted = two(r.weighted, 0.0f);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < V; ++u) {
+      if constexpr (SIZE == 2)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[u][j] = max16<TYPE == IFQ_BF16>(w[u][j], low2);
       float x[N];
       unpack_logits<TYPE>(w[u], x);
 #pragma unroll
       for (int j = 0; j < N; j += 2) {
-        float2 d = apart(mul2(add2(two(x[j], x[j + 1]), down), c2));
-        d.x = fmaxf(d.x, -1000.0f);
-        d.y = fmaxf(d.y, -1000.0f);
-        const uint64_t e = two(exp2_of(d.x), exp2_of(d.y));
+        const uint64_t y = SIZE == 4 ? two(fmaxf(x[j], low), fmaxf(x[j + 1], low)) : two(x[j], x[j + 1]);
+        const uint64_t d = mul2(add2(y, down), c2);
+        const float2 f = apart(d);
+        const uint64_t e = two(exp2_of(f.x), exp2_of(f.y));
         sum = add2(sum, e);
-        weighted = fma2(e, two(d.x, d.y), weighted);
+        weighted = fma2(e, d, weighted);
       }
     }
     const float2 s = apart(sum), v = apart(weighted);
     r.sum = s.x + s.y;
     r.weighted = v.x + v.y;
+  };
+  {
+    // pieces lo + tid, lo + tid + T, ...: those that are all logits four at a time, a row's ends by themselves
+    int i = lo + tid;
+    const int full = min(hi, whole_hi);
+    uint32_t one[1][4];
+    if (i < whole_lo) {
+      load(i, one[0]);
+      add(one);
+      i += T;
+    }
+    const uint8_t* q = p + 16ll * i;
+    const long long ahead = 16ll * T;
+    for (; i < full - (U - 1) * T; i += U * T, q += U * ahead) {
+      uint32_t w[U][4];
+#pragma unroll
+      for (int u = 0; u < U; ++u) load_words(w[u], q + u * ahead);
+      add(w);
+    }
+    if (i < full) {   // the last ones, under way together too
+      uint32_t w[U][4];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        w[u][0] = w[u][1] = w[u][2] = w[u][3] = TYPE == IFQ_F32 ? 0xff800000u : TYPE == IFQ_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+        if (i + u * T < full) load_words(w[u], q + u * ahead);
+      }
+      add(w);
+      i += (full - i + T - 1) / T * T;
+    }
+    if (i < hi) {
+      load(i, one[0]);
+      add(one);
+    }
   }
   const uint32_t mine = lo + tid < hi ? (uint32_t)(top_key(r.top, 0) >> 32) : 0u;   // 0: no logits
   r = join_lanes(r, c, 32);
@@ -231,7 +298,7 @@ __global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) token_scores_kern
     uint32_t most = mine;
     for (int o = per / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
     if (tid % per == 0) group_top[tid / per] = most;
-    if (tid == 0) count = 0;
+    if (tid == 0) count = threads = 0;
     if (tid < kTopMax) part[0].best[tid] = 0;
   }
   __syncthreads();
@@ -254,33 +321,40 @@ __global__ void __launch_bounds__(kScoreThreads, kScoreBlocks) token_scores_kern
     }
     __syncthreads();
     const uint32_t t = reach;   // 0 (all logits) where fewer than k groups have any
-    uint32_t take = __ballot_sync(0xffffffffu, mine != 0 && mine >= t);
-    while (take) {
-      const int from = lo + warp * 32 + __ffs(take) - 1;
-      take &= take - 1;
-      for (long long i = from + (long long)lane * T; i < hi; i += 32ll * T) {
-        uint32_t w[4];
-        load((int)i, w);
-        float x[N];
-        unpack_logits<TYPE>(w, x);
+    if (mine != 0 && mine >= t) who[atomicAdd(&threads, 1)] = (uint16_t)tid;
+    __syncthreads();
+    // their pieces, spread over all threads
+    const int each = (hi - lo + T - 1) / T, all = threads * each;
+    for (int i = tid; i < all; i += T) {
+      const int q = i / each, at = lo + who[q] + (i - q * each) * T;
+      if (at >= hi) continue;
+      uint32_t w[4];
+      load(at, w);
+      float x[N];
+      unpack_logits<TYPE>(w, x);
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const long long e = i * N - skip + j;
-          const uint64_t k = top_key(x[j], (int)e);
-          if ((uint32_t)(k >> 32) >= t && e >= 0 && e < a.vocab) {
-            const int at = atomicAdd(&count, 1);
-            if (at < kScoreList) list[at] = k;
-          }
+      for (int j = 0; j < N; ++j) {
+        const long long e = (long long)at * N - skip + j;
+        const uint64_t k = top_key(x[j], (int)e);
+        if ((uint32_t)(k >> 32) >= t && e >= 0 && e < a.vocab) {
+          const int to = atomicAdd(&count, 1);
+          if (to < kScoreList) list[to] = k;
         }
       }
     }
     __syncthreads();
     const int n = count;
     if (n <= kScoreList) {
+      if (tid == 0 && n % 2) list[n] = 0;   // (below all; the list has a place more)
+      __syncthreads();
       for (int i = tid; i < n; i += T) {
         const uint64_t k = list[i];
         int before = 0;
-        for (int j = 0; j < n; ++j) before += list[j] > k;
+#pragma unroll 4
+        for (int j = 0; j < n; j += 2) {
+          const ulonglong2 o = *(const ulonglong2*)&list[j];
+          before += (o.x > k) + (o.y > k);
+        }
         if (before < a.top) part[0].best[before] = k;
       }
     } else {
