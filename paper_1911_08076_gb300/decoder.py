@@ -1,4 +1,5 @@
-"""The attention block of a quantised decoder layer: e4m3 projections around attention over a 4-bit paged cache.
+"""A quantised decoder layer: attention with e4m3 projections over a 4-bit paged cache, a gated feed-forward block with
+4-bit weights, the norms between them, and the scores of its answers.
 
 PagedSequences keeps, on the host, which pages belong to which sequence and gives a step's index tensors;
 DecoderAttention holds the quantised weights and the cache, and runs a step (a batch of sequences with
@@ -6,12 +7,14 @@ one or several new tokens each) as six calls on the current stream:
 
     quantise x, x Wqkv^T, rotate + quantise + append, attend, quantise the context, context Wo^T
 
-All compute is in libifq.so.
+FeedForward is act(x Wg^T) * (x Wu^T) and the product with Wd, DecoderLayer puts a norm before each block and adds its result
+to the stream, and Head turns the stream into logits and token_scores those into log probabilities and the likeliest
+tokens.  All compute is in libifq.so.
 """
 from __future__ import annotations
 
 import math
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -157,3 +160,132 @@ class DecoderAttention:
         size = ifq.ifq_kv4_attention_workspace_bytes(t)
         ifq.ifq_kv4_attention(t, q, self.cache, step.table, step.lens, step.starts, context, None, self._room(size), size)
         return self._product(context, self.w_out, self.s_out)
+
+
+ACTS = {"silu": ifq.IFQ_ACT_SILU, "gelu": ifq.IFQ_ACT_GELU, "gelu_tanh": ifq.IFQ_ACT_GELU_TANH}
+
+
+def quantise_weights4(w: torch.Tensor, group: int = 128, dtype: torch.dtype = torch.bfloat16):
+    """Weights [n][k] (k a multiple of 8) to 4 bits with a scale and a minimum of `dtype` per row and group of columns, once:
+    (codes [n][k / 2], scales [n][groups], mins [n][groups])."""
+    n, k = w.shape
+    groups = -(-k // group)
+    pad = groups * group - k
+    f = w.float()
+    low = torch.nn.functional.pad(f, (0, pad), value=math.inf).view(n, groups, group).amin(-1)
+    high = torch.nn.functional.pad(f, (0, pad), value=-math.inf).view(n, groups, group).amax(-1)
+    scales, mins = ((high - low) / 15.0).to(dtype), low.to(dtype)
+    s, m = (t.float().repeat_interleave(group, 1)[:, :k] for t in (scales, mins))
+    codes = torch.where(s > 0, ((f - m) / s).round().clamp(0, 15), torch.zeros_like(f)).to(torch.uint8)
+    return codes[:, 0::2] | (codes[:, 1::2] << 4), scales, mins
+
+
+class Weights4:
+    """A matrix [n][k] in 4 bits, or a gated pair of them (the gate's, the other's), packed for the products."""
+
+    def __init__(self, *matrices: torch.Tensor, group: int = 128, dtype: torch.dtype = torch.bfloat16):
+        if len(matrices) not in (1, 2) or any(m.shape != matrices[0].shape for m in matrices):
+            raise ValueError("one matrix [n][k], or a gated pair of the same shape")
+        self.n, self.k = matrices[0].shape
+        self.dtype, self.gated = dtype, len(matrices) == 2
+        self.desc = ifq.w4_weights(self.n, self.k, group, TYPES[dtype], self.gated)
+        size = ifq.ifq_w4_bytes(self.desc)
+        parts = [quantise_weights4(m, group, dtype) for m in matrices]
+        codes, scales, mins = (torch.cat(p).contiguous() for p in zip(*parts))
+        self.packed = torch.empty(size, dtype=torch.uint8, device=codes.device)
+        ifq.ifq_w4_pack(self.desc, codes, scales, mins, self.packed)
+
+    def _rows(self, x):
+        if x.dim() != 2 or x.dtype != self.dtype or x.shape[1] != self.k or x.stride(1) != 1 or x.stride(0) % 8:
+            raise ValueError(f"x is a [rows][{self.k}] tensor of {self.dtype}, rows a multiple of 8 elements apart")
+        return x.shape[0], x.stride(0) if x.shape[0] > 1 else 0
+
+    def matmul(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+        """x w^T (+ residual), x [rows][k] -> [rows][n] of out_dtype (the weights' where none is given)."""
+        rows, stride = self._rows(x)
+        out_dtype = out_dtype or self.dtype
+        if residual is not None and (residual.shape != (rows, self.n) or residual.dtype != out_dtype or not residual.is_contiguous()):
+            raise ValueError("residual is a dense tensor of the result's shape and type")
+        out = torch.empty(rows, self.n, dtype=out_dtype, device=x.device)
+        d = ifq.w4_desc(self.desc, rows, ifq.IFQ_F32 if out_dtype == torch.float32 else TYPES[out_dtype], 0, stride)
+        ifq.ifq_w4_matmul(d, x, self.packed, out, residual)
+        return out
+
+    def gate(self, x: torch.Tensor, act: str = "silu") -> torch.Tensor:
+        """act(x wg^T) * (x wu^T) of a gated pair."""
+        rows, stride = self._rows(x)
+        out = torch.empty(rows, self.n, dtype=self.dtype, device=x.device)
+        ifq.ifq_w4_gated(ifq.w4_desc(self.desc, rows, TYPES[self.dtype], ACTS[act], stride), x, self.packed, out)
+        return out
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual: Optional[torch.Tensor] = None):
+    """Norm of the rows of x [rows][dim]; with a residual (norm of x + residual, x + residual)."""
+    if x.dim() != 2 or not x.is_contiguous() or weight.shape != x.shape[1:] or weight.dtype != x.dtype or not weight.is_contiguous() or \
+            (residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype or not residual.is_contiguous())):
+        raise ValueError("x and residual are dense [rows][dim] tensors, weight [dim], all of one type")
+    out, total = torch.empty_like(x), None if residual is None else torch.empty_like(x)
+    ifq.ifq_rms_norm(ifq.norm_desc(x.shape[0], x.shape[1], TYPES[x.dtype], eps), x, residual, weight, total, out)
+    return out if residual is None else (out, total)
+
+
+class FeedForward:
+    """x -> act(x w_gate^T) * (x w_up^T), times w_down^T.  w_gate, w_up [inner][hidden], w_down [hidden][inner]."""
+
+    def __init__(self, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, act: str = "silu", group: int = 128,
+                 dtype: torch.dtype = torch.bfloat16):
+        if w_down.shape != w_gate.shape[::-1]:
+            raise ValueError("w_gate and w_up are [inner][hidden], w_down [hidden][inner]")
+        self.act = act
+        self.first, self.second = Weights4(w_gate, w_up, group=group, dtype=dtype), Weights4(w_down, group=group, dtype=dtype)
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+        return self.second.matmul(self.first.gate(x, self.act), residual)
+
+
+class DecoderLayer:
+    """stream -> stream: stream + attention(norm(stream)), then that + feed_forward(norm(that))."""
+
+    def __init__(self, attention: DecoderAttention, feed_forward: FeedForward, attention_norm: torch.Tensor,
+                 feed_forward_norm: torch.Tensor, eps: float = 1e-5):
+        self.attention, self.feed_forward, self.eps = attention, feed_forward, eps
+        self.attention_norm, self.feed_forward_norm = (w.to(attention.dtype).contiguous() for w in (attention_norm, feed_forward_norm))
+
+    def forward(self, x: torch.Tensor, step: Step) -> torch.Tensor:
+        a = self.attention.forward(rms_norm(x, self.attention_norm, self.eps), step)
+        h, x = rms_norm(a, self.feed_forward_norm, self.eps, x)
+        return self.feed_forward.forward(h, x)
+
+
+class Scores(NamedTuple):
+    logprobs: Optional[torch.Tensor]       # of the given tokens (0 where that is negative), [rows]
+    lse: torch.Tensor                      # [rows]
+    entropy: torch.Tensor                  # [rows]
+    top_ids: Optional[torch.Tensor]        # [rows][top], the likeliest first
+    top_logprobs: Optional[torch.Tensor]   # [rows][top]
+
+
+def token_scores(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0) -> Scores:
+    """Scores of rows of logits [rows][vocab] at a temperature; tokens: int64 [rows]."""
+    if logits.dim() != 2 or logits.stride(1) != 1 or (tokens is not None and (
+            tokens.shape != logits.shape[:1] or tokens.dtype != torch.int64 or not tokens.is_contiguous())):
+        raise ValueError("logits are rows [rows][vocab], tokens a dense int64 tensor [rows]")
+    rows, vocab = logits.shape
+    new = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device=logits.device)   # noqa: E731
+    s = Scores(None if tokens is None else new(rows), new(rows), new(rows), new(rows, top, t=torch.int64) if top else None,
+               new(rows, top) if top else None)
+    code = ifq.IFQ_F32 if logits.dtype == torch.float32 else TYPES[logits.dtype]
+    d = ifq.scores_desc(rows, vocab, code, top, 1.0 / temperature, logits.stride(0) if rows > 1 else 0)
+    ifq.ifq_token_scores(d, logits, tokens, *s)
+    return s
+
+
+class Head:
+    """The stream's last norm and the product with the vocabulary's rows [vocab][hidden]."""
+
+    def __init__(self, w: torch.Tensor, norm: torch.Tensor, group: int = 128, dtype: torch.dtype = torch.bfloat16, eps: float = 1e-5):
+        self.weights, self.norm, self.eps = Weights4(w, group=group, dtype=dtype), norm.to(dtype).contiguous(), eps
+
+    def logits(self, x: torch.Tensor) -> torch.Tensor:
+        """float32 [rows][vocab]"""
+        return self.weights.matmul(rms_norm(x, self.norm, self.eps), out_dtype=torch.float32)
