@@ -282,12 +282,17 @@ int run_norm(const NormArgs& a, cudaStream_t st) {
 
 template <int TYPE>
 int run_scores(ScoresArgs& a, cudaStream_t st) {
-  // Threads: four loads each, in earnest sizes 512.  A row is split where rows are few, while a thread has a load or more.
+  // Threads: four loads each, in earnest sizes 512.  A row is split where rows are few, while a thread has a load.
   const long long pieces = (long long)a.vocab * (TYPE == IFQ_F32 ? 4 : 2) / 16 + 2;
   int threads = 64;
   while (threads < kScoreThreads && threads * 4 < pieces) threads *= 2;
+  // The part of a row that the fullest SM reads, and a little for each block whose results are joined.
   int parts = 1;
-  while (parts < kScoreParts && (long long)a.rows * parts * 2 <= 2 * sm_count() && pieces >= 2ll * parts * threads) parts *= 2;
+  double best = 1e300;
+  for (int n = 1; n <= kScoreParts && (n == 1 || ((long long)a.rows * n <= 2 * sm_count() && pieces >= n * threads)); ++n) {
+    const double c = (double)(((long long)a.rows * n + sm_count() - 1) / sm_count()) / n + 0.01 * n;
+    if (c < best) best = c, parts = n;
+  }
   if ((long long)a.rows * parts > INT_MAX) return IFQ_ERANGE;
   a.parts = parts;
   const dim3 grid(a.rows * parts), block(threads);

@@ -68,14 +68,6 @@ __device__ __forceinline__ void move_to(RowSums& r, float top, float c) {
   r.sum *= f;
   r.top = top;
 }
-__device__ __forceinline__ void join(RowSums& r, RowSums o, float c) {
-  const float top = max_nan(r.top, o.top);
-  move_to(r, top, c);
-  move_to(o, top, c);
-  r.sum += o.sum;
-  r.weighted += o.weighted;
-}
-
 // Two floats in one register pair, and operations on both.
 __device__ __forceinline__ uint64_t two(float a, float b) {
   uint64_t r;
@@ -137,22 +129,22 @@ __device__ __forceinline__ void unpack_logits(const uint32_t (&w)[4], float (&x)
 
 constexpr int kScoreGroups = 64, kScoreParts = 8;
 
-// What a block of a cluster gives the first one.
-struct RowPart {
-  RowSums sums;
-  float pad;
-  uint64_t best[kTopMax];   // descending
-};
-
 __device__ __forceinline__ RowSums join_lanes(RowSums r, float c, int lanes) {   // over groups of `lanes`
+  float top = r.top;
+  for (int o = lanes / 2; o; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+  move_to(r, top, c);
   for (int o = lanes / 2; o; o >>= 1) {
-    RowSums q;
-    q.top = __shfl_xor_sync(0xffffffffu, r.top, o);
-    q.sum = __shfl_xor_sync(0xffffffffu, r.sum, o);
-    q.weighted = __shfl_xor_sync(0xffffffffu, r.weighted, o);
-    join(r, q, c);
+    r.sum += __shfl_xor_sync(0xffffffffu, r.sum, o);
+    r.weighted += __shfl_xor_sync(0xffffffffu, r.weighted, o);
   }
   return r;
+}
+// How many of n keys are above k.
+__device__ __forceinline__ int keys_above(const uint64_t* keys, int n, uint64_t k) {
+  int above = 0;
+#pragma unroll 8
+  for (int j = 0; j < n; ++j) above += keys[j] > k;
+  return above;
 }
 
 // BLOCKS an SM: three hide each other's selections where rows are many (2048 x 131072: 115 -> 103 us), two leave more
@@ -160,9 +152,9 @@ __device__ __forceinline__ RowSums join_lanes(RowSums r, float c, int lanes) {  
 template <int TYPE, int BLOCKS>
 __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(const __grid_constant__ ScoresArgs a) {
   constexpr int SIZE = TYPE == IFQ_F32 ? 4 : 2, N = 16 / SIZE, U = kScoreDeep;
-  __shared__ RowSums warp_sums[kScoreThreads / 32];
-  __shared__ RowPart part[kScoreParts];
-  __shared__ __align__(16) uint64_t list[kScoreList + 2];
+  __shared__ RowSums warp_sums[kScoreThreads / 32], part_sums[kScoreParts];   // (of the first block: all parts')
+  __shared__ uint64_t part_best[kScoreParts * kTopMax], best[kTopMax];        // the parts' first ones, and what comes of them
+  __shared__ __align__(16) uint64_t list[kScoreList];
   __shared__ uint16_t who[kScoreThreads];
   __shared__ __align__(16) uint32_t group_top[kScoreGroups];
   __shared__ uint32_t reach;
@@ -299,23 +291,24 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
     for (int o = per / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
     if (tid % per == 0) group_top[tid / per] = most;
     if (tid == 0) count = threads = 0;
-    if (tid < kTopMax) part[0].best[tid] = 0;
+    if (tid < kTopMax) part_best[tid] = 0;
   }
   __syncthreads();
   if (warp == 0) {
     r = lane < warps ? warp_sums[lane] : RowSums{-INFINITY, 0.0f, 0.0f};
     r = join_lanes(r, c, 16);
-    if (lane == 0) part[0].sums = r;
+    if (lane == 0) part_sums[0] = r;
   }
   if (a.top) {
-    if (tid < kScoreGroups) {
-      const uint32_t v = group_top[tid];
+    const int id = tid - (T - kScoreGroups);   // (the last two warps')
+    if (id >= 0) {
+      const uint32_t v = group_top[id];
       int before = 0;
-#pragma unroll 4
+#pragma unroll
       for (int j = 0; j < kScoreGroups; j += 4) {
         const uint4 q = *(const uint4*)&group_top[j];
-        before += (q.x > v || (q.x == v && j < tid)) + (q.y > v || (q.y == v && j + 1 < tid)) +
-                  (q.z > v || (q.z == v && j + 2 < tid)) + (q.w > v || (q.w == v && j + 3 < tid));
+        before += (q.x > v || (q.x == v && j < id)) + (q.y > v || (q.y == v && j + 1 < id)) +
+                  (q.z > v || (q.z == v && j + 2 < id)) + (q.w > v || (q.w == v && j + 3 < id));
       }
       if (before == a.top - 1) reach = v;
     }
@@ -345,17 +338,10 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
     __syncthreads();
     const int n = count;
     if (n <= kScoreList) {
-      if (tid == 0 && n % 2) list[n] = 0;   // (below all; the list has a place more)
-      __syncthreads();
       for (int i = tid; i < n; i += T) {
         const uint64_t k = list[i];
-        int before = 0;
-#pragma unroll 4
-        for (int j = 0; j < n; j += 2) {
-          const ulonglong2 o = *(const ulonglong2*)&list[j];
-          before += (o.x > k) + (o.y > k);
-        }
-        if (before < a.top) part[0].best[before] = k;
+        const int before = keys_above(list, n, k);
+        if (before < a.top) part_best[before] = k;
       }
     } else {
       uint64_t last = ~0ull;
@@ -378,7 +364,7 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
         if (lane == 0) list[warp] = k;
         __syncthreads();
         for (int i = 0; i < warps; ++i) k = max(k, list[i]);
-        if (tid == 0) part[0].best[j] = k;
+        if (tid == 0) part_best[j] = k;
         last = k;
         __syncthreads();
       }
@@ -387,43 +373,37 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
   __syncthreads();
 
   // the parts' results meet in the first block
-  const uint64_t* tops = part[0].best;
+  const uint64_t* tops = part_best;
   if (parts > 1) {
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (rank) {
-      const uint32_t to = mapa_shared(smem_u32(&part[rank]), 0), from = smem_u32(&part[0]);
-      for (int i = tid; i < (int)sizeof(RowPart) / 8; i += T) {
-        uint64_t v;
-        asm volatile("ld.shared.u64 %0, [%1];" : "=l"(v) : "r"(from + 8 * i) : "memory");
-        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to + 8 * i), "l"(v) : "memory");
-      }
+      if (tid < a.top)
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(mapa_shared(smem_u32(&part_best[rank * a.top + tid]), 0)), "l"(part_best[tid])
+                     : "memory");
+      if (tid < 3)
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_shared(smem_u32(&part_sums[rank]) + 4 * tid, 0)),
+                     "f"(((const float*)&part_sums[0])[tid])
+                     : "memory");
     }
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     if (rank) return;
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (warp == 0) {
-      r = lane < parts ? part[lane].sums : RowSums{-INFINITY, 0.0f, 0.0f};
+      r = lane < parts ? part_sums[lane] : RowSums{-INFINITY, 0.0f, 0.0f};
       r = join_lanes(r, c, kScoreParts);
+      __syncwarp();
+      if (lane == 0) part_sums[0] = r;
     }
     for (int i = tid; i < parts * a.top; i += T) {
-      const int q = i / a.top, j = i - q * a.top;
-      const uint64_t k = part[q].best[j];
-      int before = j;
-      for (int o = 0; o < parts; ++o) {   // how many of each other list come before it
-        int n = 0;
-        for (int b = kTopMax; b; b >>= 1)
-          if (n + b <= a.top && part[o].best[n + b - 1] > k) n += b;
-        before += o == q ? 0 : n;
-      }
-      if (k && before < a.top) list[before] = k;
+      const uint64_t k = part_best[i];
+      const int before = keys_above(part_best, parts * a.top, k);
+      if (k && before < a.top) best[before] = k;
     }
     __syncthreads();
-    if (warp == 0 && lane == 0) part[0].sums = r;
-    __syncthreads();
-    tops = list;
+    tops = best;
   }
 
-  r = part[0].sums;
+  r = part_sums[0];
   const float log2_sum = log2f(r.sum), log_sum = 0.69314718055994531f * log2_sum;
   auto logprob = [&](float x) {
     return r.top == -INFINITY ? r.top : (x - r.top) * a.scale - (r.top == INFINITY ? 0.0f : log_sum);
@@ -432,7 +412,7 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
     if (a.lse) a.lse[row] = fabsf(r.top) == INFINITY ? r.top : fmaf(r.top, a.scale, log_sum);
     if (a.entropy)
       a.entropy[row] = r.top == -INFINITY ? 0.0f : r.top == INFINITY || r.top != r.top ? NAN
-                                                     : 0.69314718055994531f * (log2_sum - r.weighted / r.sum);
+                                                     : 0.69314718055994531f * (log2_sum - __fdividef(r.weighted, r.sum));
     if (a.logprobs) {
       if (token >= a.vocab) set_status(IFQ_ERANGE);
       a.logprobs[row] = token < 0 ? 0.0f : token >= a.vocab ? NAN : logprob(given);
