@@ -775,11 +775,12 @@ typedef struct {
 /*
  * ifq_w4_matmul -- out[i][j] = sum over c of x[i][c] * w[j][c] (+ residual[i][j]).
  * x (device): [m][k] of the weights' dtype; residual (device): [m][n], may be
- * NULL, and may be out where the strides agree.  Products are exact, sums in
- * single precision (which the tensor cores may truncate), rounded once to
- * out_dtype.  Results do not depend on timing; they may on m, which chooses the
- * kernel and so the order of the sums.  What is not finite in a row of x or of
- * the weights stays in that row of out, or column.  weights.gated is 0.
+ * NULL, and may be out where the strides agree; out overlaps nothing else.
+ * Products are exact, sums in single precision (which the tensor cores may
+ * truncate), rounded once to out_dtype.  Results do not depend on timing; they
+ * may on m, which chooses the kernel and so the order of the sums.  What is not
+ * finite in a row of x or of the weights stays in that row of out, or column.
+ * weights.gated is 0.
  */
 int ifq_w4_matmul(const ifq_w4_desc* d, const void* x, const void* packed, void* out, const void* residual,
                   void* stream);

@@ -95,7 +95,7 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return r;
 }
 
-// The larger of two logits each of a word; _nan: a NaN where there is one, otherwise the number.
+// The larger of two logits each of a word, a NaN where there is one.
 template <bool BF>
 __device__ __forceinline__ uint32_t max16_nan(uint32_t a, uint32_t b) {
   uint32_t r;
@@ -103,14 +103,6 @@ __device__ __forceinline__ uint32_t max16_nan(uint32_t a, uint32_t b) {
   else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-template <bool BF>
-__device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {
-  uint32_t r;
-  if constexpr (BF) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-
 // 16 bytes of a row as logits.
 template <int TYPE, int N>
 __device__ __forceinline__ void unpack_logits(const uint32_t (&w)[4], float (&x)[N]) {
@@ -200,7 +192,6 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
   }
   RowSums r = {-INFINITY, 0.0f, 0.0f};
   const uint64_t c2 = two(c, c);
-  const float reach_down = 1000.0f / c;
   auto add = [&](auto& w) {   // [pieces][4 words]
     constexpr int V = sizeof(w) / 16;
     float top = r.top;
@@ -220,29 +211,21 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
     }
     if (top != r.top) move_to(r, top, c);
     if (top == -INFINITY) return;
-    // A logit below `low` counts as one of its value, 2^-1000 or less: it has a share of 0, and 0 times its distance is 0,
-    // which -infinity's would not be.
-    const float low = top - fmaxf(reach_down, fabsf(top) * (1.0f / 64.0f));
-    uint32_t low2 = 0;
-    if constexpr (TYPE == IFQ_BF16) low2 = 0x10001u * __bfloat16_as_ushort(__float2bfloat16_rd(fmaxf(low, -3.38e38f)));
-    else if constexpr (TYPE == IFQ_F16) low2 = 0x10001u * __half_as_ushort(__float2half_rd(fmaxf(low, -65504.0f)));
     const uint64_t down = two(-top, -top);
     uint64_t sum = two(r.sum, 0.0f), weighted = two(r.weighted, 0.0f);
 #pragma unroll
     for (int u = 0; u < V; ++u) {
-      if constexpr (SIZE == 2)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[u][j] = max16<TYPE == IFQ_BF16>(w[u][j], low2);
       float x[N];
       unpack_logits<TYPE>(w[u], x);
 #pragma unroll
       for (int j = 0; j < N; j += 2) {
-        const uint64_t y = SIZE == 4 ? two(fmaxf(x[j], low), fmaxf(x[j + 1], low)) : two(x[j], x[j + 1]);
-        const uint64_t d = mul2(add2(y, down), c2);
-        const float2 f = apart(d);
-        const uint64_t e = two(exp2_of(f.x), exp2_of(f.y));
+        // (at least -1000: a masked logit's share of 0 times its distance, -infinity, would be no number)
+        float2 d = apart(mul2(add2(two(x[j], x[j + 1]), down), c2));
+        d.x = fmaxf(d.x, -1000.0f);
+        d.y = fmaxf(d.y, -1000.0f);
+        const uint64_t e = two(exp2_of(d.x), exp2_of(d.y));
         sum = add2(sum, e);
-        weighted = fma2(e, d, weighted);
+        weighted = fma2(e, two(d.x, d.y), weighted);
       }
     }
     const float2 s = apart(sum), v = apart(weighted);

@@ -82,7 +82,7 @@ def scores(logits, tokens, scale, top):
             else:
                 e = np.exp(z - m)
                 lse = m + np.log(e.sum()) if np.isfinite(m) else m
-                lp = z - lse
+                lp = z - m - np.log(e.sum()) if np.isfinite(m) else z - m   # (not z - lse: a large m swallows the logarithm)
                 ent = -np.sum(np.where(e > 0, e / e.sum() * lp, e))
         key = np.where(np.isnan(row), np.inf, row)
         order = np.lexsort((np.arange(len(z)), -key, ~np.isnan(row)))[:top]

@@ -107,6 +107,35 @@ def test_masked_and_infinite_logits(vocab, dtype):
     assert got["entropy"][2] == 0 and got["lse"][1] == -np.inf
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("scale", [1.0, 1e-4, 1e-6, 30.0])
+@pytest.mark.parametrize("vocab", [300, 20011])
+def test_masks_of_the_lowest_value_beside_infinities(vocab, dtype, scale):
+    """A finite mask counts by its value, however hot the temperature; -infinity never does."""
+    rng = np.random.default_rng(vocab)
+    lowest = {"f32": -3.4028234663852886e38, "bf16": -3.3895313892515355e38, "f16": -65504.0}[dtype]
+    logits = draw(rng, 7, vocab, dtype)
+    logits[0, rng.random(vocab) < 0.7] = lowest
+    logits[1] = lowest
+    logits[2, rng.random(vocab) < 0.7] = -np.inf
+    logits[3] = lowest
+    logits[3, ::3] = -np.inf
+    logits[4] = -np.inf
+    logits[4, vocab - 1] = lowest
+    logits[5, ::2], logits[5, 1::4] = -np.inf, lowest
+    logits[6] = -lowest
+    tokens = rng.integers(0, vocab, 7)
+    got = run(logits, tokens, dtype, 3, scale)
+    want = R.scores(logits, tokens, float(np.float32(scale)), 3)
+    tol = R.scores_tolerance(np.where(logits < lowest / 2, 0, logits), scale)
+    assert np.array_equal(got["top_ids"], want["top_ids"])
+    for k in ("entropy", "logprobs", "lse"):
+        with np.errstate(invalid="ignore", over="ignore"):
+            w = want[k].astype(np.float32).astype(np.float64)     # (what a float cannot hold is infinite)
+            close = np.abs(got[k] - w) <= 16 * tol + np.abs(w) * 2.0 ** -22
+        assert (close | (got[k] == w)).all(), (k, got[k], w)
+
+
 def test_tokens_outside_the_vocabulary():
     rng = np.random.default_rng(3)
     logits, tokens = draw(rng, 5, 700, "f32"), [-1, 699, 700, 0, 2 ** 40]

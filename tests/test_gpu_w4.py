@@ -64,7 +64,7 @@ def matmul(w, x, packed, dtype, out, residual=None, pads=(0, 0, 0), extra=3):
 SIZES = [(1, 1, 8), (1, 16, 128), (1, 130, 136), (2, 48, 1024), (3, 257, 264), (5, 64, 4104), (7, 4097, 512), (8, 1000, 640),
          (9, 33, 2056), (15, 300, 384), (16, 512, 1160), (17, 129, 256), (24, 700, 72), (31, 128, 1288), (33, 1025, 520),
          (47, 160, 2560), (64, 96, 8), (65, 640, 328), (100, 2049, 136), (128, 256, 1024), (129, 127, 640), (200, 1152, 264),
-         (255, 64, 392), (257, 384, 200), (384, 130, 520), (513, 520, 648), (1000, 260, 136),
+         (255, 64, 392), (257, 384, 200), (384, 130, 520), (513, 520, 648), (1000, 260, 136), (4, 40, 33024), (14, 24, 20008),
          (1, 9730, 264), (3, 40007, 128), (6, 12289, 1416), (8, 19600, 8), (12, 10000, 648), (16, 20100, 136)]
 
 
@@ -237,6 +237,29 @@ def test_same_bits_in_every_call_on_any_stream_and_in_graphs(m):
         got.append([t.clone() for t in y])
     assert all(torch.equal(p, q) for one in got for p, q in zip(one, want))
     assert ifq.ifq_device_status() == ifq.IFQ_OK
+
+
+def test_packing_in_a_graph_before_its_product():
+    n, k = 200, 392
+    rng = np.random.default_rng(8)
+    w = ifq.w4_weights(n, k, 64, ifq.IFQ_BF16)
+    first, second = draw(rng, n, k, 64, "bf16", True), draw(rng, n, k, 64, "bf16", False)
+    dev = [[torch.from_numpy(d[0]).to(DEV), to_dev(d[1], "bf16"), to_dev(d[2], "bf16")] for d in (first, second)]
+    held = [t.clone() for t in dev[0]]
+    x = activations(rng, 3, k, "bf16", True)
+    xd, out = to_dev(x, "bf16"), torch.empty(3, n, device=DEV)
+    packed = torch.empty(ifq.ifq_w4_bytes(w), dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ifq.ifq_w4_pack(w, *held, packed)
+        ifq.ifq_w4_matmul(ifq.w4_desc(w, 3, ifq.IFQ_F32), xd, packed, out)
+    for i, d in ((0, first), (1, second), (0, first)):     # scales of 1/4 and more, then smaller ones: the flag follows
+        for a, b in zip(held, dev[i]):
+            a.copy_(b)
+        graph.replay()
+        y, tol = R.products(x, d[3])
+        assert (np.abs(out.double().cpu().numpy() - y) <= tol).all()
+    assert np.array_equal(out.double().cpu().numpy(), x @ first[3].T)
 
 
 def test_offsets_past_32_bits():
