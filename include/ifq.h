@@ -823,7 +823,8 @@ int ifq_rms_norm(const ifq_norm_desc* d, const void* x, const void* residual, co
  * Rows of vocab logits of dtype (IFQ_F16, IFQ_BF16 or IFQ_F32), stride elements
  * from row to row (0: dense; any number of them).  top: how many of the
  * likeliest tokens are wanted, 0 to 32 (IFQ_EUNSUPPORTED) and at most vocab
- * (IFQ_ESHAPE).  scale: finite, > 0 (one over a temperature).
+ * (IFQ_ESHAPE).  scale: one over a temperature, > 0 and at most 2^100
+ * (IFQ_ERANGE).
  */
 typedef struct {
   int rows, vocab;

@@ -405,7 +405,7 @@ int ifq_token_scores(const ifq_scores_desc* d, const void* logits, const int64_t
     return IFQ_EINVAL;
   if (d->top > kTopMax) return IFQ_EUNSUPPORTED;
   if (d->top > d->vocab) return IFQ_ESHAPE;
-  if (d->rows > kMaxSize || d->vocab > kMaxSize) return IFQ_ERANGE;
+  if (d->rows > kMaxSize || d->vocab > kMaxSize || d->scale > 0x1p100f) return IFQ_ERANGE;
   ScoresArgs a = {};
   const int rc = any_stride(d->stride, d->vocab, &a.stride);
   if (rc) return rc;

@@ -299,11 +299,8 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
     const uint32_t t = reach;   // 0 (all logits) where fewer than k groups have any
     if (mine != 0 && mine >= t) who[atomicAdd(&threads, 1)] = (uint16_t)tid;
     __syncthreads();
-    // their pieces, spread over all threads
-    const int each = (hi - lo + T - 1) / T, all = threads * each;
-    for (int i = tid; i < all; i += T) {
-      const int q = i / each, at = lo + who[q] + (i - q * each) * T;
-      if (at >= hi) continue;
+    // what pass() takes of piece `at` goes to the list
+    auto gather = [&](int at, auto&& pass) {
       uint32_t w[4];
       load(at, w);
       float x[N];
@@ -312,11 +309,43 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
       for (int j = 0; j < N; ++j) {
         const long long e = (long long)at * N - skip + j;
         const uint64_t k = top_key(x[j], (int)e);
-        if ((uint32_t)(k >> 32) >= t && e >= 0 && e < a.vocab) {
+        if (pass((uint32_t)(k >> 32)) && e >= 0 && e < a.vocab) {
           const int to = atomicAdd(&count, 1);
           if (to < kScoreList) list[to] = k;
         }
       }
+    };
+    // those threads' pieces, spread over all threads
+    auto gather_all = [&](auto&& pass) {
+      const int each = (hi - lo + T - 1) / T, all = threads * each;
+      for (int i = tid; i < all; i += T) {
+        const int q = i / each, at = lo + who[q] + (i - q * each) * T;
+        if (*(volatile int*)&count > kScoreList) break;   // (too many)
+        if (at < hi) gather(at, pass);
+      }
+    };
+    gather_all([&](uint32_t k) { return k >= t; });
+    __syncthreads();
+    if (count > kScoreList) {
+      // Many equals (a mask that leaves fewer than k, a constant row): those above them, and of the equals the first that
+      // are found going through the row from its start, 512 logits or fewer at a time.
+      __syncthreads();
+      if (tid == 0) count = threads = 0;
+      __syncthreads();
+      if (mine > t) who[atomicAdd(&threads, 1)] = (uint16_t)tid;
+      __syncthreads();
+      gather_all([&](uint32_t k) { return k > t; });
+      __syncthreads();
+      const int above = count;
+      int now = above;
+      __syncthreads();
+      for (int i = lo; i < hi && now < above + a.top && now <= kScoreList - 512; i += 64) {
+        if (tid < 64 && i + tid < hi) gather(i + tid, [&](uint32_t k) { return k == t; });
+        __syncthreads();
+        now = count;
+        __syncthreads();
+      }
+      if (now > kScoreList - 512 && now < above + a.top && tid == 0) count = kScoreList + 1;   // (too many above them)
     }
     __syncthreads();
     const int n = count;

@@ -79,8 +79,17 @@ def test_ties_go_to_the_lowest_token(vocab, dtype):
     logits[5] = np.minimum(np.arange(vocab), vocab // 2)    # rounds to many equals in bfloat16
     logits[6] = -np.arange(vocab)
     logits[7] = np.where(np.arange(vocab) == vocab - 1, 3.0, -1.0)
+    more = np.zeros((6, vocab))
+    more[0, rng.integers(0, vocab, 9)] = np.arange(9) + 1.0          # fewer above the many equals than wanted
+    more[1] = -np.inf
+    more[1, rng.integers(0, vocab, 5)] = 2.0
+    more[2] = np.where(np.arange(vocab) >= vocab - vocab // 3, 2.0, np.arange(vocab) / vocab)   # equals at the end
+    more[3] = np.where(np.arange(vocab) % 64 == 63, 4.0, -4.0)
+    more[4, : vocab // 2] = np.linspace(1, 2, vocab // 2)            # many above, and equals
+    more[5, rng.random(vocab) < 0.3] = np.nan
+    logits = np.concatenate([logits, more])
     logits = R.round_to(logits, dtype)
-    tokens = rng.integers(0, vocab, 8)
+    tokens = rng.integers(0, vocab, 14)
     for top in (1, 7, 32):
         check(logits, tokens, dtype, top, 0.01, run(logits, tokens, dtype, top, 0.01))
 

@@ -118,7 +118,7 @@ def test_scores_refuse():
         assert st(**kw) == E.IFQ_EINVAL, kw
     assert st(top=33) == E.IFQ_EUNSUPPORTED
     assert st(vocab=3) == E.IFQ_ESHAPE
-    assert st(rows=BIG) == st(vocab=BIG) == E.IFQ_ERANGE
+    assert st(rows=BIG) == st(vocab=BIG) == st(scale=2e30) == E.IFQ_ERANGE
 
 
 def test_calls_without_rows_take_null_pointers():
