@@ -115,6 +115,8 @@ int w4_many_setup(K kern, int (&known)[kMaxDevices][kW4MaxSplit + 1], const int*
   return IFQ_OK;
 }
 
+constexpr int kW4Chain = 8;
+
 // How a product runs: columns of a tile, a pair of CTAs a tile or one, the split of k.
 struct W4Plan {
   int cg, bn, ks, halves;
@@ -176,16 +178,19 @@ int run_w4_many(const W4Args& a, const W4Plan& p, const int* slots, cudaStream_t
     r.tiles += rest;
   }
   const auto wide = [&](const void* q, long long stride) { return aligned16(q) && stride % 8 == 0; };
+  r.chain = a.out_type == IFQ_F32 ? kW4Chain : a.kb;
   r.vec = a.n % 8 == 0 && wide(a.out, a.out_stride) && (!a.res || wide(a.res, a.res_stride));
-  // shared memory: three or four blocks of x, then codes, then what is left for x
+  if (a.out_type == IFQ_F32) r.turn = ceil_div(a.kb, p.ks) > r.chain ? p.bn * 512 : 0;
+  else r.turn = CG == 2 ? p.bn * w4_out_pitch(GATED) : 0;
+  // shared memory: three blocks of x (two where they do not fit beside two of codes), then codes, then what is left for x
   const int xb = p.bn / CG * 256, cb = 8 * w4_block_bytes(G);
-  int room = kW4ManySmem - 1024 - 512 - w4_many_recv(p.bn, p.ks) - w4_many_turn(CG, p.bn, a.out_type, GATED);
-  r.stages = 3;
-  room -= 3 * xb;
+  int room = kW4ManySmem - 1024 - 512 - w4_many_recv(p.bn, p.ks) - r.turn;
+  r.stages = 3 * xb + 2 * cb <= room ? 3 : 2;
+  room -= r.stages * xb;
   r.slots = std::min(12, room / cb);
   room -= r.slots * cb;
-  r.stages += std::min(kW4Bars - 3, room / xb);
-  if (r.slots < 2) return IFQ_EUNSUPPORTED;
+  r.stages += std::min(kW4Bars - r.stages, room / xb);
+  if (r.slots < 2) return IFQ_EUNSUPPORTED;   // (128 columns in floats over a cluster: two of each)
   CUtensorMap tx;
   if (!encode_x(a, CG == 2 ? p.bn / 4 : p.bn, &tx)) return IFQ_ECUDA;
   const int cluster = CG == 2 ? 2 : p.ks, most = CG == 2 ? slots[2] : p.ks > 1 ? r.tiles : slots[1];

@@ -48,12 +48,15 @@ __device__ __forceinline__ uint2 load_once2(const void* p) {
   return v;
 }
 
-// One block of 128 columns: acc += 16 rows of w times 8 NT rows of x, whose operands stand at xs + xo.
+// One block of 128 columns: acc += 16 rows of w times 8 NT rows of x, whose operands stand at xs + xo.  The tensor cores
+// truncate what they add: a block's sums begin at 0, and are added to the others' in single precision (8 x 131072 x 4096 to
+// floats: off by 1.1e-6 of the result in one chain, 3e-7 so).
 template <bool BF, bool FAST, int G, int NT>
 __device__ __forceinline__ void w4_block(const uint4 (&w)[2], const uint2 (&p)[kW4Cols / G], const uint8_t* const (&xs)[NT], int xo,
                                          float (&acc)[NT][4]) {
   const uint32_t words[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
   uint32_t s[2], m[2];
+  float sum[NT][4] = {};
 #pragma unroll
   for (int j = 0; j < 8; j += 2) {   // 32 columns
     if (j * 16 % G == 0) w4_params<BF, FAST>(p[j * 16 / G], s, m);
@@ -63,10 +66,14 @@ __device__ __forceinline__ void w4_block(const uint4 (&w)[2], const uint2 (&p)[k
 #pragma unroll
     for (int q = 0; q < NT; ++q) {
       const uint4 b = *(const uint4*)(xs[q] + xo + j * 32);
-      mma_16x8x16<BF>(acc[q], v, b.x, b.y);
-      mma_16x8x16<BF>(acc[q], v + 4, b.z, b.w);
+      mma_16x8x16<BF>(sum[q], v, b.x, b.y);
+      mma_16x8x16<BF>(sum[q], v + 4, b.z, b.w);
     }
   }
+#pragma unroll
+  for (int q = 0; q < NT; ++q)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[q][j] += sum[q][j];
 }
 
 // x into shared memory, 16 bytes at a time: four pairs of columns of one step's half, one for each lane of a quad.

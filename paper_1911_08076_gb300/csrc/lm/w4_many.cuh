@@ -13,6 +13,9 @@
 // Tensor memory: columns 0 to 255 are the accumulator (two that take turns where bn <= 128, so that a tile's results
 // leave beside the next tile's products), the others four blocks of expanded weights: from an MMA that frees a block to
 // one that reads its successor take 700 cycles, and more between two SMs.
+// The tensor cores truncate what they add, which shows in results of 32 bits (1000 x 2048 x 16384: off by 1.4e-5 of the
+// result).  Those (bn <= 128) are added in tensor memory over 1024 columns of k at most; the sums of such chains meet in shared
+// memory, in single precision, beside the next chain's products.
 // Where bn > 128 results are of 16 bits, and leave through shared memory: the accumulator is free again after 1500 cycles
 // or so.
 //
@@ -34,6 +37,8 @@ struct W4Many {
   int tiles, tiles_w, tiles_x; // items; tiles of w's rows (CG times 128) and of x's
   int whole;                   // items that are whole tiles; the rest are halves (CG = 2)
   int ks;                      // blocks that a tile's k is split over
+  int chain;                   // blocks of 128 columns of k that are added in tensor memory
+  int turn;                    // bytes of shared memory for results on their way out, or sums of several chains
   int vec;                     // rows of out (and of the residual) can be accessed 16 bytes at a time
 };
 
@@ -46,9 +51,6 @@ constexpr int kW4ManySmem = 232448;
 __host__ __device__ constexpr int w4_many_recv(int bn, int ks) { return ks > 1 ? (bn + 8) * 129 * 4 : 0; }
 // results of 16 bits on their way out: a row a column of the tile (a gated pair's lanes write two rows at a time: apart)
 __host__ __device__ constexpr int w4_out_pitch(bool gated) { return gated ? 144 : 256; }
-__host__ __device__ constexpr int w4_many_turn(int cg, int bn, int out_type, bool gated) {
-  return cg == 2 && out_type != IFQ_F32 ? bn * w4_out_pitch(gated) : 0;
-}
 
 // The instructions of two CTAs' MMAs.
 template <int CG>
@@ -107,7 +109,7 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
   uint8_t* turn = codes + CS * 8 * WB;
   float* recv = (float*)turn;
   const uint32_t cbase = smem_u32(codes);
-  const uint32_t bars = smem_u32(turn) + w4_many_recv(r.bn, r.ks) + w4_many_turn(CG, r.bn, a.out_type, GATED);
+  const uint32_t bars = smem_u32(turn) + w4_many_recv(r.bn, r.ks) + r.turn;
   // Block it of all that the CTA goes through: full(it % NB): its x has landed and its weights stand in tensor memory (of
   // both CTAs, on the first one's barrier); done(it % NB): its products are there.
   auto full = [&](int i) { return bars + 8 * i; };
@@ -282,22 +284,28 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
       uint32_t it = 0, nt = 0;
       int s = 0;
       bool ok = true;
-      for (int t = first; t < r.tiles && ok; t += step, ++nt) {
-        const uint32_t acc = accs == 2 ? nt & 1 : 0, use = nt / accs, td = tmem + acc * 128;
+      for (int t = first; t < r.tiles && ok; t += step) {
         const uint32_t idesc = idesc_f16_f32(128 * CG, CG == 2 && t >= r.whole ? r.bn / 2 : r.bn, BF);
-        if (use && !(CG == 2 ? mbar_wait_cluster(dempty(acc), (use - 1) & 1) : mbar_wait(dempty(acc), (use - 1) & 1))) break;
-        for (int k = k0; k < k1; ++k, ++it) {
-          const uint32_t bar = full(it % NB), ph = it / NB & 1;
-          if (!(CG == 2 ? mbar_wait_cluster(bar, ph) : mbar_wait(bar, ph))) { ok = false; break; }
-          tc_fence_after();
-          const uint64_t db = sdesc_sw128(base + s * xb);
-          const uint32_t ta = tmem + kW4ACol + 64 * (it % AS);
+        for (int kc = k0; kc < k1 && ok; kc += r.chain, ++nt) {   // a chain an accumulator
+          const uint32_t acc = accs == 2 ? nt & 1 : 0, use = nt / accs, td = tmem + acc * 128;
+          if (use && !(CG == 2 ? mbar_wait_cluster(dempty(acc), (use - 1) & 1) : mbar_wait(dempty(acc), (use - 1) & 1))) {
+            ok = false;
+            break;
+          }
+          const int end = min(kc + r.chain, k1);
+          for (int k = kc; k < end; ++k, ++it) {
+            const uint32_t bar = full(it % NB), ph = it / NB & 1;
+            if (!(CG == 2 ? mbar_wait_cluster(bar, ph) : mbar_wait(bar, ph))) { ok = false; break; }
+            tc_fence_after();
+            const uint64_t db = sdesc_sw128(base + s * xb);
+            const uint32_t ta = tmem + kW4ACol + 64 * (it % AS);
 #pragma unroll
-          for (int j = 0; j < 8; ++j)   // 16 columns of k: 8 of tensor memory, two 16-byte units of the descriptor's address
-            w4_mma<CG>(td, ta + 8 * j, db + 2 * (j & 3) + (j >> 2) * (half / 16), idesc, (k > k0) | (j > 0));
-          w4_commit<CG>(done(it % NB));
-          if (k + 1 == k1) w4_commit<CG>(dfull(acc));
-          if (++s == ST) s = 0;
+            for (int j = 0; j < 8; ++j)   // 16 columns of k: 8 of tensor memory, two 16-byte units of the descriptor's address
+              w4_mma<CG>(td, ta + 8 * j, db + 2 * (j & 3) + (j >> 2) * (half / 16), idesc, (k > kc) | (j > 0));
+            w4_commit<CG>(done(it % NB));
+            if (k + 1 == end) w4_commit<CG>(dfull(acc));
+            if (++s == ST) s = 0;
+          }
         }
       }
     }
@@ -317,6 +325,25 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
     for (int t = first; t < r.tiles; t += step, ++nt) {
       int iw, m0, wd;
       tile(t, iw, m0, wd);
+      // the sums of all chains but the last: a thread's own row, so nothing waits for others
+      float* sums = (float*)(turn + (ks > 1 ? w4_many_recv(r.bn, ks) : 0)) + row;
+      bool some = false;
+      for (int kc = k0 + r.chain; kc < k1 && ok; kc += r.chain, ++nt, some = true) {
+        const uint32_t acc = accs == 2 ? nt & 1 : 0, tl = tmem + acc * 128 + ((uint32_t)(q * 32) << 16);
+        ok = __all_sync(0xffffffffu, mbar_wait(dfull(acc), (nt / accs) & 1));
+        tc_fence_after();
+        for (int c0 = 0; c0 < wd; c0 += 16) {
+          uint32_t v[16];
+          tmem_ld<16>(tl + c0, v);
+          if (c0 + 16 == wd) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tell(dempty(acc));
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sums[(c0 + i) * 128] = __uint_as_float(v[i]) + (some ? sums[(c0 + i) * 128] : 0.0f);
+        }
+      }
       const uint32_t acc = accs == 2 ? nt & 1 : 0, tl = tmem + acc * 128 + ((uint32_t)(q * 32) << 16);
       const int n0 = iw * NO, n = n0 + nc;
       auto release = [&] {   // the accumulator has been read
@@ -385,16 +412,24 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
       if (!__all_sync(0xffffffffu, mbar_wait(dfull(acc), (nt / accs) & 1))) break;
       tc_fence_after();
       if (CG == 1 && ks > 1) {
+        // owner of column c: own bn / ks <= c < end
         const int per = (r.bn + ks - 1) / uks;
+        int own = 0, end = r.bn / uks;
+        uint32_t to = mapa_shared(smem_u32(recv + rank * per * 129 + row), 0);
         for (int c0 = 0; c0 < r.bn; c0 += 16) {
           uint32_t v[16];
           tmem_ld<16>(tl + c0, v);
+          if (some)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + sums[(c0 + i) * 128]);
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int c = c0 + i, own = ((c + 1) * uks - 1) / r.bn, lo = own * r.bn / uks;   // own bn / ks <= c
-            asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(mapa_shared(smem_u32(recv + (rank * per + c - lo) * 129 + row), own)),
-                         "r"(v[i])
-                         : "memory");
+            const int c = c0 + i;
+            if (c == end) {
+              to = mapa_shared(smem_u32(recv + (rank * per - end) * 129 + row), ++own);
+              end = (own + 1) * r.bn / uks;
+            }
+            asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(to + c * 129 * 4), "r"(v[i]) : "memory");
           }
         }
         break;
@@ -406,6 +441,9 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
         if (!GATED && a.res) residual(c0 + 16);
         tmem_ld<16>(tl + c0, v);
         if (c0 + 16 == wd) release();
+        if (!GATED && some)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + sums[(c0 + i) * 128]);
         if constexpr (GATED) {
 #pragma unroll
           for (int i = 0; i < 16; i += 2) {

@@ -99,6 +99,25 @@ def test_real_values(m, n, k, group, dtype, out):
     assert (np.abs(got - y) <= tol).all(), np.max(np.abs(got - y) / tol)
 
 
+@pytest.mark.parametrize("m,n,k", [(5, 200, 12000), (16, 9730, 4096), (40, 300, 16384), (120, 130, 16384), (128, 100, 4096), (100, 2000, 5000),
+                                   (300, 300, 16384), (1000, 256, 9216), (1100, 2560, 2048)])
+@pytest.mark.parametrize("group", [32, 128])
+def test_floats_of_long_sums(m, n, k, group):
+    """Sums of one sign, where truncated additions add up: tensor memory adds 64 times 16 products (chains of 1024 columns) at
+    most before single precision takes over.  An addition there truncates, by 2^-23 of the sum at most, and on average of
+    a growing sum by a quarter of that: 64 / 4 additions' worth for a chain, and for each of the k / 1024 chains' additions,
+    k / 128 where a block is one, half a step."""
+    rng = np.random.default_rng([m, n, k])
+    w = ifq.w4_weights(n, k, group, ifq.IFQ_BF16)
+    codes, scales, mins, values = draw(rng, n, k, group, "bf16", False)
+    mins = np.abs(mins)
+    values = R.weights(codes, scales, mins, group, "bf16")
+    packed = pack(w, codes, scales, mins, "bf16")
+    x = np.abs(activations(rng, m, k, "bf16", False))
+    got, y = matmul(w, x, packed, "bf16", "f32"), x @ values.T
+    assert (np.abs(got - y) <= y * (64 + k / 128) * 2.0 ** -24).all(), np.max(np.abs(got - y) / y) * 2 ** 24
+
+
 @pytest.mark.parametrize("largest", [0.2, 1.0, 300.0])
 @pytest.mark.parametrize("m", [8, 200])
 @pytest.mark.parametrize("group", [32, 64, 128])
