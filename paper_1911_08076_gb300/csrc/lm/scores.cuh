@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
   __shared__ int count, threads;
   const int tid = threadIdx.x, T = blockDim.x, warp = tid / 32, lane = tid % 32, warps = T / 32;
   const int parts = a.parts, rank = parts > 1 ? (int)cluster_ctarank() : 0;
-  const long long row = blockIdx.x / (uint32_t)parts;
+  const long long row = parts == 1 ? blockIdx.x : blockIdx.x / (uint32_t)parts;
   const float c = a.c;
   if (parts > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (this block's memory is there)
   grid_dep_wait();
@@ -163,9 +163,10 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
   const uint8_t* begin = (const uint8_t*)a.logits + row * a.stride * SIZE;
   const int skip = (int)(((uintptr_t)begin & 15) / SIZE);
   const uint8_t* p = begin - skip * SIZE;
-  const long long pieces = ((long long)a.vocab + skip + N - 1) / N;
-  const int lo = (int)(pieces * rank / parts), hi = (int)(pieces * (rank + 1) / parts);
-  const int whole_lo = skip ? 1 : 0, whole_hi = (int)((a.vocab + (long long)skip) / N);   // pieces that are all logits
+  // (32-bit divisions, and none where a row is whole: pieces are below 2^29 and parts 8 at most)
+  const uint32_t pieces = ((uint32_t)a.vocab + skip + N - 1) / N;
+  const int lo = parts == 1 ? 0 : pieces * rank / (uint32_t)parts, hi = parts == 1 ? pieces : pieces * (rank + 1) / (uint32_t)parts;
+  const int whole_lo = skip ? 1 : 0, whole_hi = (int)(((uint32_t)a.vocab + skip) / N);   // pieces that are all logits
   auto load = [&](int i, uint32_t (&w)[4]) {
     if (i >= whole_lo && i < whole_hi) {
       load_words(w, p + 16ll * i);
@@ -258,7 +259,7 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
         if (i + u * T < full) load_words(w[u], q + u * ahead);
       }
       add(w);
-      i += (full - i + T - 1) / T * T;
+      i += (full - i + T - 1) & -T;
     }
     if (i < hi) {
       load(i, one[0]);
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
     };
     // those threads' pieces, spread over all threads
     auto gather_all = [&](auto&& pass) {
-      const int each = (hi - lo + T - 1) / T, all = threads * each;
+      const int each = (hi - lo + T - 1) >> (31 - __clz(T)), all = threads * each;   // (T is a power of two)
       for (int i = tid; i < all; i += T) {
         const int q = i / each, at = lo + who[q] + (i - q * each) * T;
         if (*(volatile int*)&count > kScoreList) break;   // (too many)
