@@ -272,16 +272,20 @@ int run_w4(const ifq_w4_desc* d, W4Args& a, size_t bytes, const void* x, const v
 // ---------------------------------------------------------------- rows
 
 template <bool BF>
-int run_norm(const NormArgs& a, cudaStream_t st) {
+int run_norm(NormArgs& a, cudaStream_t st) {
   const int vecs = a.dim / 8;
   // few rows: as many threads as there are; many: four times 16 bytes a thread, so that blocks are small
-  const int v = vecs > 4096 ? 8 : a.rows >= 2 * sm_count() || vecs > 2048 ? 4 : vecs > 1024 ? 2 : 1;
-  const dim3 grid(a.rows), block(round_up(ceil_div(vecs, v), 32));
+  const int v = vecs > 2048 ? 8 : a.rows >= 2 * sm_count() ? 4 : vecs > 1024 ? 2 : 1;
+  a.threads = (int)round_up(ceil_div(vecs, v), 32);
+  const int rows = a.threads == 32 ? 8 : 1;   // a block
+  const dim3 grid(ceil_div(a.rows, rows)), block(a.threads * rows);
   switch (v) {
-    case 1: return done(launch_k(rms_norm_kernel<BF, 1>, grid, block, 0, st, a));
-    case 2: return done(launch_k(rms_norm_kernel<BF, 2>, grid, block, 0, st, a));
-    case 4: return done(launch_k(rms_norm_kernel<BF, 4>, grid, block, 0, st, a));
-    default: return done(launch_k(rms_norm_kernel<BF, 8>, grid, block, 0, st, a));
+    case 1: return done(launch_k(rms_norm_kernel<BF, 1, 1024>, grid, block, 0, st, a));
+    case 2: return done(launch_k(rms_norm_kernel<BF, 2, 1024>, grid, block, 0, st, a));
+    case 4: return done(launch_k(rms_norm_kernel<BF, 4, 512>, grid, block, 0, st, a));
+    default:
+      if (a.threads <= 512) return done(launch_k(rms_norm_kernel<BF, 8, 512>, grid, block, 0, st, a));
+      return done(launch_k(rms_norm_kernel<BF, 8, 1024>, grid, block, 0, st, a));
   }
 }
 

@@ -19,7 +19,7 @@
 
 namespace ifq {
 
-constexpr int kW4Rows = 16, kW4Cols = 128, kW4Tail = 64;
+constexpr int kW4Cols = 128, kW4Tail = 64;
 __host__ __device__ constexpr int w4_at(bool bf) { return bf ? 3 : 6; }   // first bit of a code: the upper ones of a mantissa
 
 __host__ __device__ constexpr int w4_block_bytes(int group) { return 1024 + 64 * (kW4Cols / group); }
@@ -36,13 +36,6 @@ struct W4Args {
   int m, n, k, kb;     // kb: blocks of 128 columns
   int out_type, act;
 };
-
-// code * scale + min in the weights' type.
-template <bool BF>
-__device__ __forceinline__ float w4_value(int code, uint16_t scale, uint16_t min) {
-  if constexpr (BF) return __bfloat162float(__hfma(__int2bfloat16_rn(code), __ushort_as_bfloat16(scale), __ushort_as_bfloat16(min)));
-  else return __half2float(__hfma(__int2half_rn(code), __ushort_as_half(scale), __ushort_as_half(min)));
-}
 
 // act(a) of a gated pair.  The exponentials are of -|.|, so that none overflows.
 __device__ __forceinline__ float w4_sigmoid(float a) {

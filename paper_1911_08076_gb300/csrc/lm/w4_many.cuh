@@ -380,20 +380,20 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
         // (a wait that ran out: the four warps still meet at every named barrier)
         ok = ok && __all_sync(0xffffffffu, mbar_wait(dfull(acc), (nt / accs) & 1));
         tc_fence_after();
-        for (int c0 = 0; c0 < wd; c0 += 32) {
-          uint32_t v[32];
-          tmem_ld<32>(tl + c0, v);
-          if (c0 + 32 == wd) release();
+        for (int c0 = 0; c0 < wd; c0 += 16) {
+          uint32_t v[16];
+          tmem_ld<16>(tl + c0, v);
+          if (c0 + 16 == wd) release();
           if constexpr (GATED) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) w4_store(BF ? IFQ_BF16 : IFQ_F16, turn + (c0 + i + e) * PITCH, nc, pair(v, i));
+            for (int i = 0; i < 16; i += 2) w4_store(BF ? IFQ_BF16 : IFQ_F16, turn + (c0 + i + e) * PITCH, nc, pair(v, i));
           } else {
             uint8_t* to = turn + c0 * PITCH;
-            float add[32];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) add[i] = a.res ? w4_load(a.out_type, to + i * PITCH, nc) : 0.0f;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) w4_store(a.out_type, to + i * PITCH, nc, __uint_as_float(v[i]) + add[i]);
+            for (int i = 0; i < 16; ++i) {
+              const float add = a.res ? w4_load(a.out_type, to + i * PITCH, nc) : 0.0f;
+              w4_store(a.out_type, to + i * PITCH, nc, __uint_as_float(v[i]) + add);
+            }
           }
         }
         named_bar(1, 128);

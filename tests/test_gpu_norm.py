@@ -44,7 +44,7 @@ def check(x, r, w, eps, dtype, pads=(0, 0, 0, 0), seed=0):
 
 
 @pytest.mark.parametrize("rows,dim", [(1, 8), (1, 4096), (1, 8200), (3, 248), (2, 32768), (1, 65536), (5, 40000), (7, 1032),
-                                      (400, 2048), (1000, 136), (333, 5000), (310, 65536)])
+                                      (400, 2048), (1000, 136), (333, 5000), (310, 65536), (2, 16384), (3, 16392), (400, 16384), (305, 32768), (2, 32776), (1003, 8), (2001, 1024), (17, 256), (3000, 1032)])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("residual", [True, False])
 def test_values(rows, dim, dtype, residual):
