@@ -20,7 +20,7 @@
 // or so.
 //
 // Warps: sixteen that expand (a quadrant of 32 lanes, half of the columns of every other block of k each), two that load,
-// one that issues MMAs, four that take results out.
+// one that issues MMAs, eight that take results out.
 #pragma once
 #include <cuda.h>
 
@@ -42,7 +42,7 @@ struct W4Many {
   int vec;                     // rows of out (and of the residual) can be accessed 16 bytes at a time
 };
 
-constexpr int kW4Expand = 16, kW4Out = kW4Expand + 4, kW4ManyThreads = 32 * (kW4Out + 4);   // kW4Out: first warp that stores
+constexpr int kW4Expand = 16, kW4Out = kW4Expand + 4, kW4Outs = 8, kW4ManyThreads = 32 * (kW4Out + kW4Outs);   // kW4Out: first warp that stores
 constexpr int kW4Bars = 8;         // barriers in turn: no fewer than stages of x or blocks of expanded weights
 constexpr int kW4AStages = 4, kW4ACol = 256;
 constexpr int kW4ManySmem = 232448;
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(dfull(i), 1);
-      mbar_init(dempty(i), 4 * CG);
+      mbar_init(dempty(i), kW4Outs * CG);
     }
     fence_mbar_init();
     prefetch_tmap(&tx);
@@ -311,7 +311,8 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
     }
     __syncwarp();
   } else if (warp >= kW4Out) {   // results
-    const int q = warp & 3, row = q * 32 + lane, e = (lane >> 3) & 1;
+    // a quadrant of 32 lanes and every other 16 columns a warp
+    const int q = warp & 3, row = q * 32 + lane, e = (lane >> 3) & 1, first_col = 16 * ((warp - kW4Out) >> 2);
     // a lane's column of out in its tile; a gated pair's lanes with bit 3 clear hold the gate's rows, and do the even
     // columns, the others the odd ones
     const int nc = GATED ? q * 16 + (lane >> 4) * 8 + (lane & 7) : row;
@@ -332,17 +333,15 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
         const uint32_t acc = accs == 2 ? nt & 1 : 0, tl = tmem + acc * 128 + ((uint32_t)(q * 32) << 16);
         ok = __all_sync(0xffffffffu, mbar_wait(dfull(acc), (nt / accs) & 1));
         tc_fence_after();
-        for (int c0 = 0; c0 < wd; c0 += 16) {
+        for (int c0 = first_col; c0 < wd; c0 += 32) {
           uint32_t v[16];
           tmem_ld<16>(tl + c0, v);
-          if (c0 + 16 == wd) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) tell(dempty(acc));
-          }
 #pragma unroll
           for (int i = 0; i < 16; ++i) sums[(c0 + i) * 128] = __uint_as_float(v[i]) + (some ? sums[(c0 + i) * 128] : 0.0f);
         }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tell(dempty(acc));
       }
       const uint32_t acc = accs == 2 ? nt & 1 : 0, tl = tmem + acc * 128 + ((uint32_t)(q * 32) << 16);
       const int n0 = iw * NO, n = n0 + nc;
@@ -353,10 +352,10 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
       };
       if (CG == 2 && a.out_type != IFQ_F32) {
         // through shared memory: rows of out in pieces of 16 bytes, before (the residual) and after
-        const int id = row, wide = min(NO, a.n - n0), tall = min(wd, a.m - m0);
+        const int id = threadIdx.x - 32 * kW4Out, wide = min(NO, a.n - n0), tall = min(wd, a.m - m0);
         auto move = [&](bool in) {
           if (r.vec) {
-            for (int i = id; i < tall * (NO / 8); i += 128) {
+            for (int i = id; i < tall * (NO / 8); i += 32 * kW4Outs) {
               const int c = i / (NO / 8), j = i % (NO / 8) * 8;
               uint4* to = (uint4*)(turn + c * PITCH + 2 * j);
               if (j < wide) {
@@ -365,7 +364,7 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
               }
             }
           } else {
-            for (int i = id; i < tall * NO; i += 128) {
+            for (int i = id; i < tall * NO; i += 32 * kW4Outs) {
               const int c = i / NO, j = i % NO;
               uint16_t* to = (uint16_t*)(turn + c * PITCH + 2 * j);
               if (j < wide) {
@@ -374,16 +373,17 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
               }
             }
           }
-          named_bar(1, 128);
+          named_bar(1, 32 * kW4Outs);
         };
         if (!GATED && a.res) move(true);
-        // (a wait that ran out: the four warps still meet at every named barrier)
+        // (a wait that ran out: the warps still meet at every named barrier)
         ok = ok && __all_sync(0xffffffffu, mbar_wait(dfull(acc), (nt / accs) & 1));
         tc_fence_after();
-        for (int c0 = 0; c0 < wd; c0 += 16) {
+        if (first_col >= wd) release();
+        for (int c0 = first_col; c0 < wd; c0 += 32) {
           uint32_t v[16];
           tmem_ld<16>(tl + c0, v);
-          if (c0 + 16 == wd) release();
+          if (c0 + 32 >= wd) release();
           if constexpr (GATED) {
 #pragma unroll
             for (int i = 0; i < 16; i += 2) w4_store(BF ? IFQ_BF16 : IFQ_F16, turn + (c0 + i + e) * PITCH, nc, pair(v, i));
@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
             }
           }
         }
-        named_bar(1, 128);
+        named_bar(1, 32 * kW4Outs);
         move(false);
         continue;
       }
@@ -408,20 +408,20 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
           next[i] = c0 < wd && m < a.m && n < a.n ? w4_load(a.out_type, a.res, m * a.res_stride + n) : 0.0f;
         }
       };
-      if (!GATED && a.res && ks == 1) residual(0);
+      if (!GATED && a.res && ks == 1) residual(first_col);
       if (!__all_sync(0xffffffffu, mbar_wait(dfull(acc), (nt / accs) & 1))) break;
       tc_fence_after();
       if (CG == 1 && ks > 1) {
-        // owner of column c: own bn / ks <= c < end
         const int per = (r.bn + ks - 1) / uks;
-        int own = 0, end = r.bn / uks;
-        uint32_t to = mapa_shared(smem_u32(recv + rank * per * 129 + row), 0);
-        for (int c0 = 0; c0 < r.bn; c0 += 16) {
+        for (int c0 = first_col; c0 < r.bn; c0 += 32) {
           uint32_t v[16];
           tmem_ld<16>(tl + c0, v);
           if (some)
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + sums[(c0 + i) * 128]);
+          // owner of column c: own bn / ks <= c < end
+          int own = ((c0 + 1) * uks - 1) / r.bn, end = (own + 1) * r.bn / uks;
+          uint32_t to = mapa_shared(smem_u32(recv + (int)(rank * per - own * r.bn / uks) * 129 + row), own);
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int c = c0 + i;
@@ -434,13 +434,14 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
         }
         break;
       }
-      for (int c0 = 0; c0 < wd; c0 += 16) {
+      if (first_col >= wd) release();
+      for (int c0 = first_col; c0 < wd; c0 += 32) {
         uint32_t v[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) add[i] = next[i];
-        if (!GATED && a.res) residual(c0 + 16);
+        if (!GATED && a.res) residual(c0 + 32);
         tmem_ld<16>(tl + c0, v);
-        if (c0 + 16 == wd) release();
+        if (c0 + 32 >= wd) release();
         if (!GATED && some)
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + sums[(c0 + i) * 128]);
