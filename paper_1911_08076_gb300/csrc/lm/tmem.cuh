@@ -32,6 +32,18 @@ __device__ __forceinline__ void tmem_ld(uint32_t t, uint32_t (&v)[X]) {
         : "r"(t)
         : "memory");
 }
+// 32 lanes x 16 columns as matrix fragments: thread 4 g + t has v[h][4 k + 2 e + i] = column 8 k + 2 t + i of lane
+// 16 h + g + 8 e.
+__device__ __forceinline__ void tmem_ld_frag(uint32_t t, uint32_t (&v)[2][8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%16];\n\t"
+      "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%8,%9,%10,%11,%12,%13,%14,%15}, [%17];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0][0]), "=r"(v[0][1]), "=r"(v[0][2]), "=r"(v[0][3]), "=r"(v[0][4]), "=r"(v[0][5]), "=r"(v[0][6]), "=r"(v[0][7]),
+        "=r"(v[1][0]), "=r"(v[1][1]), "=r"(v[1][2]), "=r"(v[1][3]), "=r"(v[1][4]), "=r"(v[1][5]), "=r"(v[1][6]), "=r"(v[1][7])
+      : "r"(t), "r"(t + (16u << 16))
+      : "memory");
+}
 // Instruction descriptor, kind::f16, operands of half or bfloat16, fp32 accumulator, both K-major.
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool bf = false) {
   return (1u << 4) | (bf ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);

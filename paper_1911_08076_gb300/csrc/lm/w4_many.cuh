@@ -49,7 +49,7 @@ constexpr int kW4ManySmem = 232448;
 
 // a receive slot a rank: the owner's columns, 129 floats each
 __host__ __device__ constexpr int w4_many_recv(int bn, int ks) { return ks > 1 ? (bn + 8) * 129 * 4 : 0; }
-// results of 16 bits on their way out: a row a column of the tile (a gated pair's lanes write two rows at a time: apart)
+// results of 16 bits on their way out: a row a column of the tile (a gated pair's fragments write four at a time: apart)
 __host__ __device__ constexpr int w4_out_pitch(bool gated) { return gated ? 144 : 256; }
 
 // The instructions of two CTAs' MMAs.
@@ -381,13 +381,21 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
         tc_fence_after();
         if (first_col >= wd) release();
         for (int c0 = first_col; c0 < wd; c0 += 32) {
-          uint32_t v[16];
-          tmem_ld<16>(tl + c0, v);
-          if (c0 + 32 >= wd) release();
-          if constexpr (GATED) {
+          if constexpr (GATED) {   // as fragments: rows g and g + 8, a gate's and its other's, are in one thread
+            uint32_t v[2][8];
+            tmem_ld_frag(tl + c0, v);
+            if (c0 + 32 >= wd) release();
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) w4_store(BF ? IFQ_BF16 : IFQ_F16, turn + (c0 + i + e) * PITCH, nc, pair(v, i));
+            for (int j = 0; j < 16; ++j) {
+              const int h = j >> 3, k = (j >> 2) & 1, i = j & 1;
+              if (j & 2) continue;
+              const float y = w4_act(a.act, __uint_as_float(v[h][4 * k + i])) * __uint_as_float(v[h][4 * k + 2 + i]);
+              w4_store(BF ? IFQ_BF16 : IFQ_F16, turn + (c0 + 8 * k + 2 * (lane & 3) + i) * PITCH, q * 16 + 8 * h + lane / 4, y);
+            }
           } else {
+            uint32_t v[16];
+            tmem_ld<16>(tl + c0, v);
+            if (c0 + 32 >= wd) release();
             uint8_t* to = turn + c0 * PITCH;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
