@@ -123,9 +123,10 @@ struct W4Plan {
   double cycles;
 };
 
-// An estimate of the cycles of `turns` tiles in a row: blocks of k at 450 cycles of expansion or 4 a column of MMAs, and a
-// tile's start and end.
-double w4_cycles(double turns, int blocks, int bn) { return turns * (blocks * std::max(450.0, 4.0 * bn) + 1200); }
+// An estimate of the cycles of `turns` tiles in a row: blocks of k at 650 cycles of expansion and waits (as measured) or 4 a
+// column of MMAs, and a tile's start and end.  (With 450 tiles came out too narrow: 1000 x 4096 x 9216 60 us instead of 46,
+// gated 448 x 9216 x 4096 53 instead of 44.)
+double w4_cycles(double turns, int blocks, int bn) { return turns * (blocks * std::max(650.0, 4.0 * bn) + 1200); }
 
 W4Plan plan_w4_one(const W4Args& a, bool gated, const int* slots) {
   W4Plan best = {1, 16, 1, 0, 1e300};
