@@ -354,6 +354,11 @@ int ifq_w4_pack(const ifq_w4_weights* w, const void* codes, const void* scales, 
   a.row_blocks = (int)(blocks / a.kb);
   a.large = (uint32_t*)(a.out + bytes - kW4Tail);
   if (cudaMemsetAsync(a.large, 0, kW4Tail, S(stream)) != cudaSuccess) return IFQ_ECUDA;
+  const long long count = (long long)w->n * (w->gated ? 2 : 1) * a.groups;
+  const dim3 scan((unsigned)std::min<long long>((count + 2047) / 2048, 4 * sm_count()));
+  const cudaError_t e = w->dtype == IFQ_BF16 ? launch_k(w4_scan_kernel<true>, scan, dim3(256), 0, S(stream), a)
+                                             : launch_k(w4_scan_kernel<false>, scan, dim3(256), 0, S(stream), a);
+  if (e != cudaSuccess) return IFQ_ECUDA;
   const dim3 grid((unsigned)std::min<size_t>((blocks + kW4PackWarps - 1) / kW4PackWarps, 16 * 1024));
   return by_weights(*w, [&](auto bf, auto group) {
     return done(launch_k(w4_pack_kernel<decltype(bf)::value, decltype(group)::value>, grid, dim3(32 * kW4PackWarps), 0, S(stream), a));

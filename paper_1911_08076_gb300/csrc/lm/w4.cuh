@@ -11,7 +11,8 @@
 //               w4_at .. w4_at + 3 of either half: i = 0, 1: rows g, g + 8, columns 16 j + 2 t and the next; i = 2, 3: the
 //               same rows, 8 columns further
 //   parameters  [128 / group][8][2] pairs (scale, min): of row g, of row g + 8
-// Behind the blocks stand 64 bytes whose first word says whether every scale is below 1/4 in size (0), see w4_expand.
+// Behind the blocks stand 64 bytes whose first word says whether every scale is below 1/4 in size (0), see w4_expand: the
+// scales stand there times 2^130 (bfloat16) or 2^18 (half) then.
 // A pair of codes masked out of a word and made floats is thus one register of an mma.sync operand (A, 16 x 16), and a
 // register of a tcgen05.st in 16-lane fragments.  Rows and columns past the matrix hold zeros up to whole tiles of 128.
 #pragma once
@@ -63,8 +64,8 @@ __device__ __forceinline__ void w4_store(int type, void* p, long long at, float 
 // one rounding.
 //
 // FAST: the masked code is a number as it stands, a subnormal one, code * 2^-130 in bfloat16 and code * 2^-18 in half, which
-// the fma takes as exactly as any other; the scale carries the factor that is missing, and must be below 1/4 for it to be
-// finite.  Otherwise the code is made the mantissa of 16 + code, from which 16 is taken: one operation more for each pair.
+// the fma takes as exactly as any other; the packed scale carries the factor that is missing, and must be below 1/4 for it
+// to be finite.  Otherwise the code is made the mantissa of 16 + code, from which 16 is taken: one operation more for each pair.
 template <bool BF, bool FAST>
 __device__ __forceinline__ void w4_expand(uint32_t w, const uint32_t (&s)[2], const uint32_t (&m)[2], uint32_t* v) {
 #pragma unroll
@@ -80,20 +81,12 @@ __device__ __forceinline__ void w4_expand(uint32_t w, const uint32_t (&s)[2], co
     }
   }
 }
-// A lane's parameters (scale, min of row g; of row g + 8) in both halves of a register each; FAST: the scales times 2^130 or
-// 2^18, in two exact steps.
-template <bool BF, bool FAST>
+// A lane's parameters (scale, min of row g; of row g + 8) in both halves of a register each.
 __device__ __forceinline__ void w4_params(uint2 p, uint32_t (&s)[2], uint32_t (&m)[2]) {
   s[0] = __byte_perm(p.x, 0, 0x1010);
   m[0] = __byte_perm(p.x, 0, 0x3232);
   s[1] = __byte_perm(p.y, 0, 0x1010);
   m[1] = __byte_perm(p.y, 0, 0x3232);
-  if (FAST)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (BF) asm("{.reg .b32 t; mov.b32 t, 0x60006000; mul.rn.bf16x2 %0, %0, t;}" : "+r"(s[i & 1]));   // 2^65
-      else asm("{.reg .b32 t; mov.b32 t, 0x60006000; mul.rn.f16x2 %0, %0, t;}" : "+r"(s[i & 1]));                // 2^9
-    }
 }
 
 // ---------------------------------------------------------------- packing
@@ -109,7 +102,19 @@ struct W4PackArgs {
 
 constexpr int kW4PackWarps = 8;
 
-// Run once a matrix (131072 x 4096 in 260 us).  A warp makes one block (16 rows x 128 columns): its codes go through shared
+// Whether a scale is 1/4 or more, an infinity or a NaN (a.large begins at 0; all that write write the same).
+template <bool BF>
+__global__ void __launch_bounds__(256) w4_scan_kernel(const __grid_constant__ W4PackArgs a) {
+  grid_dep_wait();
+  grid_dep_launch();
+  const long long total = (long long)a.n * (a.gated ? 2 : 1) * a.groups;
+  bool any = false;
+  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < total; i += 256ll * gridDim.x)
+    any |= (a.scales[i] & 0x7fffu) >= (BF ? 0x3e80u : 0x3400u);
+  if (__any_sync(0xffffffffu, any) && threadIdx.x % 32 == 0) *a.large = 1;
+}
+
+// Run once a matrix (131072 x 4096 in 138 us with the scan).  A warp makes one block (16 rows x 128 columns): its codes go through shared
 // memory, where a row has 17 words, so that the bytes that a lane gathers (rows g and g + 8) lie in different banks.
 template <bool BF, int G>
 __global__ void __launch_bounds__(32 * kW4PackWarps) w4_pack_kernel(const __grid_constant__ W4PackArgs a) {
@@ -119,6 +124,7 @@ __global__ void __launch_bounds__(32 * kW4PackWarps) w4_pack_kernel(const __grid
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane / 4, t = lane % 4;
   uint32_t* in = turn[warp];
   const long long blocks = (long long)a.row_blocks * a.kb, words = a.k / 8;
+  const bool large = *a.large != 0;
   const auto source = [&](long long rb, int r) -> long long {   // the row of the matrix, or -1
     const long long j = a.gated ? rb * 8 + r % 8 : rb * 16 + r;
     return j >= a.n ? -1 : a.gated && r >= 8 ? j + a.n : j;
@@ -154,8 +160,11 @@ __global__ void __launch_bounds__(32 * kW4PackWarps) w4_pack_kernel(const __grid
       const int q = i / 16, r = i % 16;
       const long long j = source(rb, r), at = (long long)kb * (kW4Cols / G) + q;
       uint32_t v = 0;
-      if (j >= 0 && at < a.groups) v = a.scales[j * a.groups + at] | (uint32_t)a.mins[j * a.groups + at] << 16;
-      if ((v & 0x7fffu) >= (BF ? 0x3e80u : 0x3400u)) *a.large = 1;   // (1/4 or more, an infinity, a NaN; all write the same)
+      if (j >= 0 && at < a.groups) {
+        float scale = unpack16<BF>(a.scales[j * a.groups + at]).x;
+        if (!large) scale *= BF ? 0x1p65f : 0x1p9f, scale *= BF ? 0x1p65f : 0x1p9f;   // (exact)
+        v = (pack16<BF>(scale, 0.0f) & 0xffffu) | (uint32_t)a.mins[j * a.groups + at] << 16;
+      }
       *(uint32_t*)(out + 1024 + 64 * q + 8 * (r % 8) + 4 * (r / 8)) = v;
     }
     __syncwarp();

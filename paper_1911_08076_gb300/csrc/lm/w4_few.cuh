@@ -7,7 +7,7 @@
 //
 // What bounds it is the expansion: 88 of some 170 warp instructions for a block of 16 x 128, half of them on the integer pipe
 // (58 % busy over all, issue slots 65 %).  1 x 4096 x 4096 takes 4.2 us in a row of calls, where a call alone is 4; 8 x 131072 x 4096 in
-// the second form 63 us, 4.9 TB/s (72 % of a copy).
+// the second form 61 us, 5.0 TB/s (74 % of a copy).
 //
 // x stands in shared memory as operands: of every 32 columns, the 16 bytes of lane t of a quad are its registers of two
 // steps, and rows begin 64 bytes apart modulo 128, so that eight lanes read all banks once.
@@ -63,7 +63,7 @@ __device__ __forceinline__ void w4_block(const uint4 (&w)[2], const uint2 (&p)[k
   float sum[NT][4] = {};
 #pragma unroll
   for (int j = 0; j < 8; j += 2) {   // 32 columns
-    if (j * 16 % G == 0) w4_params<BF, FAST>(p[j * 16 / G], s, m);
+    if (j * 16 % G == 0) w4_params(p[j * 16 / G], s, m);
     uint32_t v[8];
     w4_expand<BF, FAST>(words[j], s, m, v);
     w4_expand<BF, FAST>(words[j + 1], s, m, v + 4);

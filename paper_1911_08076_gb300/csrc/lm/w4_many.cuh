@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kW4ManyThreads, 1)
         uint32_t s[2], m[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          if (j < NP) w4_params<BF, FAST>(p[b][j], s, m);
+          if (j < NP) w4_params(p[b][j], s, m);
           w4_expand<BF, FAST>(words[2 * j], s, m, v[b][j]);
           w4_expand<BF, FAST>(words[2 * j + 1], s, m, v[b][j] + 4);
         }
