@@ -38,7 +38,7 @@ bool get_encode() {
 
 // Programmatic dependent launch (on unless IFQ_PDL=0): a kernel may start its
 // prologue while the previous kernel in the stream finishes; every kernel here
-// waits (griddepcontrol.wait) before it touches global memory.
+// waits (griddepcontrol.wait) before it reads or writes global memory (some bring weights into L2 before).
 bool pdl_enabled() {
   static const bool on = [] {
     const char* v = getenv("IFQ_PDL");
