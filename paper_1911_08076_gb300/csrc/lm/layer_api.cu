@@ -219,6 +219,8 @@ int run_w4_few(const W4Args& a, cudaStream_t st) {
   const int sms = sm_count(), tiles = ceil_div(a.n, GATED ? 64 : 128);
   const long long room = kW4ManySmem - w4_ring_fixed(a.m, a.kb, NT);
   const int stages = (int)std::min<long long>(kW4RingMost, room / (8 * w4_block_bytes(G)));
+  // The ring takes whole tiles of 128 rows, so it waits for two or more an SM (one row of x: 192 tiles of 4096 columns 19.5 us
+  // against 15.9 without it, 288 tiles 21.0 against 19.7; 1024 tiles and 8 rows 61.5 against 67.6).
   if (tiles >= 2 * sms && stages >= 4) {
     static bool set[kMaxDevices];
     const auto kern = w4_ring_kernel<BF, G, GATED, NT>;
@@ -261,7 +263,8 @@ int run_w4(const ifq_w4_desc* d, W4Args& a, size_t bytes, const void* x, const v
     constexpr int G = decltype(group)::value;
     const auto run = [&](auto pair) {
       constexpr bool GATED = decltype(pair)::value;
-      // few rows, whose x fits shared memory
+      // Few rows, whose x fits shared memory.  (16 against 17 rows, the first of the tiles: 4096 x 4096 7.4 and 9.5 us,
+      // 6144 x 4096 10.3 and 12.0, gated 9216 x 4096 15.7 and 15.4; four tiles of 8 rows would take 20 there.)
       if (a.m <= 8 && w4_few_smem(a.m, a.kb, 1) <= kW4ManySmem) return run_w4_few<BF, G, GATED, 1>(a, st);
       if (a.m <= kW4FewRows && w4_few_smem(a.m, a.kb, 2) <= kW4ManySmem) return run_w4_few<BF, G, GATED, 2>(a, st);
       return run_w4_tiles<BF, G, GATED>(a, st);
@@ -275,7 +278,8 @@ int run_w4(const ifq_w4_desc* d, W4Args& a, size_t bytes, const void* x, const v
 template <bool BF>
 int run_norm(NormArgs& a, cudaStream_t st) {
   const int vecs = a.dim / 8;
-  // few rows: as many threads as there are; many: four times 16 bytes a thread, so that blocks are small
+  // Few rows: as many threads as there are, so that one load is waited for; many: four times 16 bytes a thread, and many
+  // small blocks an SM (8191 x 4096 in 40 us, 98 % of a copy; eight times 16 bytes where a row is longer).
   const int v = vecs > 2048 ? 8 : a.rows >= 2 * sm_count() ? 4 : vecs > 1024 ? 2 : 1;
   a.threads = (int)round_up(ceil_div(vecs, v), 32);
   const int rows = a.threads == 32 ? 8 : 1;   // a block
