@@ -148,7 +148,9 @@ template <int TYPE, int BLOCKS>
 __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(const __grid_constant__ ScoresArgs a) {
   constexpr int SIZE = TYPE == IFQ_F32 ? 4 : 2, N = 16 / SIZE, U = kScoreDeep;
   __shared__ RowSums warp_sums[kScoreThreads / 32], part_sums[kScoreParts];   // (of the first block: all parts')
-  __shared__ uint64_t part_best[kScoreParts * kTopMax], best[kTopMax];        // the parts' first ones, and what comes of them
+  // The parts' first ones, and what comes of them.  From the moment this block has started the other blocks may write to the first
+  // one's part_sums[1] and part_best[top] and on: a block itself writes below those only.
+  __shared__ uint64_t part_best[kScoreParts * kTopMax], best[kTopMax];
   __shared__ __align__(16) uint64_t list[kScoreList];
   __shared__ uint16_t who[kScoreThreads];
   __shared__ __align__(16) uint32_t group_top[kScoreGroups];
@@ -278,7 +280,7 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
     for (int o = per / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
     if (tid % per == 0) group_top[tid / per] = most;
     if (tid == 0) count = threads = 0;
-    if (tid < kTopMax) part_best[tid] = 0;
+    if (tid < a.top) part_best[tid] = best[tid] = 0;
   }
   __syncthreads();
   if (warp == 0) {
