@@ -218,16 +218,19 @@ template <bool BF, int G, bool GATED, int NT>
 int run_w4_few(const W4Args& a, cudaStream_t st) {
   const int sms = sm_count(), tiles = ceil_div(a.n, GATED ? 64 : 128);
   const long long room = kW4ManySmem - w4_ring_fixed(a.m, a.kb, NT);
-  const int stages = (int)std::min<long long>(kW4RingMost, room / (8 * w4_block_bytes(G)));
-  // The ring takes whole tiles of 128 rows, so it waits for two or more an SM (one row of x: 192 tiles of 4096 columns 19.5 us
-  // against 15.9 without it, 288 tiles 21.0 against 19.7; 1024 tiles and 8 rows 61.5 against 67.6).
-  if (tiles >= 2 * sms && stages >= 4) {
+  const int deep = w4_ring_deep((int)(room / (8 * w4_block_bytes(G))), NT);
+  // The ring takes whole tiles of 128 rows, a block an SM, so it waits for turns that are full, or nearly, and for more than four rows
+  // of x (131072 x 4096, ring against none: 1 row 61.6 against 60.2 us, 4 rows 61.4 and 60.6, 8 rows 61.8 and 62.6, 12 rows
+  // 71.4 and 75.5; 16 x 131072 x 1024 23.2 and 26.7; 3.4 turns, 12 x 65536 x 6144: 68.6 and 59.1).  Less than two stages a ring
+  // is no ring: 8 x 65536 x 10240 118 and 79.
+  const int turns = ceil_div(tiles, sms);
+  if (a.m > 4 && tiles >= 2 * sms && 10ll * tiles >= 9ll * turns * sms && deep >= 2) {
     static bool set[kMaxDevices];
     const auto kern = w4_ring_kernel<BF, G, GATED, NT>;
     const int rc = allow_smem(kern, kW4ManySmem, set);
     if (rc) return rc;
-    const W4Ring r = {a, tiles, stages};
-    const size_t smem = (size_t)w4_ring_fixed(a.m, a.kb, NT) + (size_t)stages * 8 * w4_block_bytes(G);
+    const W4Ring r = {a, tiles, deep};
+    const size_t smem = (size_t)w4_ring_fixed(a.m, a.kb, NT) + (size_t)deep * w4_ring_wk(NT) * 8 * w4_block_bytes(G);
     return done(launch_k(kern, dim3((unsigned)std::min(tiles, sms)), dim3(32 * (8 * w4_ring_wk(NT) + 1)), smem, st, r));
   }
   static bool set[kMaxDevices];

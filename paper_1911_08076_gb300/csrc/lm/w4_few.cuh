@@ -240,10 +240,11 @@ __global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __gri
 
 // The same for weights of many rows: a block takes tiles of eight row blocks, whose codes a warp of its own brings in by bulk
 // copies, a block of 128 columns of the tile each, as many ahead as shared memory holds; WK warps a row block take every
-// WK-th of them.
+// WK-th of them.  Those go through a ring of their own, `deep` stages each: copies may land in any order, and a wait for a
+// phase of a barrier holds only for who has seen the one before it.
 struct W4Ring {
   W4Args a;
-  int tiles, stages;
+  int tiles, deep;
 };
 
 __host__ __device__ constexpr int w4_ring_wk(int nt) { return nt == 1 ? 3 : 2; }
@@ -251,14 +252,16 @@ __host__ __device__ constexpr int w4_ring_part(int nt) { return 2 * 8 * w4_ring_
 __host__ __device__ constexpr long long w4_ring_fixed(int m, int kb, int nt) {   // without the stages
   return m * w4_few_pitch(kb) + w4_ring_part(nt) + 1024;
 }
-constexpr int kW4RingMost = 32;   // stages
+constexpr int kW4RingMost = 32;   // stages, all rings'
+// Stages of a ring where shared memory has room for `fit` in all.
+__host__ __device__ constexpr int w4_ring_deep(int fit, int nt) { return (fit < kW4RingMost ? fit : kW4RingMost) / w4_ring_wk(nt); }
 
 template <bool BF, int G, bool GATED, int NT>
 __global__ void __launch_bounds__(32 * (8 * w4_ring_wk(NT) + 1), 1) w4_ring_kernel(const __grid_constant__ W4Ring r) {
   constexpr int WB = w4_block_bytes(G), NP = kW4Cols / G, WK = w4_ring_wk(NT);
   const W4Args& a = r.a;
   extern __shared__ __align__(16) uint8_t smem[];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ST = r.stages;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = r.deep, ST = D * WK;
   const long long pitch = w4_few_pitch(a.kb);
   uint8_t* ring = smem + a.m * pitch;   // (a multiple of 64 bytes)
   float* part = (float*)(ring + ST * 8 * WB);
@@ -281,22 +284,38 @@ __global__ void __launch_bounds__(32 * (8 * w4_ring_wk(NT) + 1), 1) w4_ring_kern
   grid_dep_wait();
   grid_dep_launch();
   if (warp == 8 * WK) {
-    int it = 0, s = 0, ph = 1;
+    int at[WK] = {}, ph[WK];   // of each ring: the stage that is filled next, and the phase that frees it
+#pragma unroll
+    for (int w = 0; w < WK; ++w) ph[w] = 1;
+    auto ahead = [&](int w) {
+      if (++at[w] == D) at[w] = 0, ph[w] ^= 1;
+    };
     bool ok = true;
     for (int t = first; t < r.tiles && ok; t += step) {
       const uint8_t* from = a.w + w4_place(8ll * t, 0, a.kb) * WB;
-      for (int k = 0; k < a.kb; ++k, ++it, from += 8 * WB) {
-        if (!__all_sync(0xffffffffu, mbar_wait(empty(s), ph))) { ok = false; break; }
-        if (elect_one()) {
-          mbar_arrive_expect_tx(full(s), 8 * WB);
-          bulk_copy_g2s(smem_u32(ring) + s * 8 * WB, from, 8 * WB, full(s));
+      for (int k = 0; k < a.kb && ok; k += WK) {
+#pragma unroll
+        for (int w = 0; w < WK; ++w, from += 8 * WB) {
+          if (k + w >= a.kb) break;
+          const int s = w * D + at[w];
+          if (!__all_sync(0xffffffffu, mbar_wait(empty(s), ph[w]))) { ok = false; break; }
+          if (elect_one()) {
+            mbar_arrive_expect_tx(full(s), 8 * WB);
+            bulk_copy_g2s(smem_u32(ring) + s * 8 * WB, from, 8 * WB, full(s));
+          }
+          __syncwarp();
+          ahead(w);
         }
-        __syncwarp();
-        if (++s == ST) s = 0, ph ^= 1;
       }
     }
-    // what was copied has landed, and in the end been read, before the block may exit
-    for (int i = it - ST < 0 ? 0 : it - ST; i < it; ++i) mbar_wait(ok ? empty(i % ST) : full(i % ST), i / ST & 1);
+    // What was copied has landed, and in the end been read, before the block may exit.  (A stage's last copy completes the phase of
+    // full that its release completes of empty; one that was never filled waits for nothing.)
+#pragma unroll
+    for (int w = 0; w < WK; ++w)
+      for (int i = 0; i < D; ++i) {
+        mbar_wait(ok ? empty(w * D + at[w]) : full(w * D + at[w]), ph[w]);
+        ahead(w);
+      }
     return;
   }
   w4_stage_x(a, smem, pitch, threadIdx.x, 32 * 8 * WK);
@@ -315,18 +334,13 @@ __global__ void __launch_bounds__(32 * (8 * w4_ring_wk(NT) + 1), 1) w4_ring_kern
   const uint8_t* mine = ring + row * WB;
   auto multiply = [&](auto fast) {
     constexpr bool FAST = decltype(fast)::value;
-    int s = 0, ph = 0, turn = 0;   // stage and phase of block k
+    int at = 0, ph = 0, turn = 0;   // the next stage of these warps' ring, and its phase
     bool ok = true;
-    auto ahead = [&](int n) {
-      s += n;
-      while (s >= ST) s -= ST, ph ^= 1;
-    };
     for (int t = first; t < r.tiles; t += step, turn ^= 1) {
       const int rb = 8 * t + row;
       const float add = w4_few_residual<GATED>(a, rb, id);
-      int k = wk;
-      ahead(wk);
-      for (; k < a.kb; k += WK) {
+      for (int k = wk; k < a.kb; k += WK) {
+        const int s = wk * D + at;
         ok = ok && __all_sync(0xffffffffu, mbar_wait(full(s), ph));   // (after one that ran out none waits again)
         const uint8_t* c = mine + s * 8 * WB;
         uint4 w[2] = {*(const uint4*)(c + 16 * lane), *(const uint4*)(c + 512 + 16 * lane)};
@@ -336,11 +350,8 @@ __global__ void __launch_bounds__(32 * (8 * w4_ring_wk(NT) + 1), 1) w4_ring_kern
         w4_block<BF, FAST, G, NT>(w, p, xs, k * 256, acc);
         __syncwarp();
         if (lane == 0) mbar_arrive(empty(s));
-        ahead(WK);
+        if (++at == D) at = 0, ph ^= 1;
       }
-      // (k - kb blocks past the tile's last: back to the next tile's first)
-      s -= k - a.kb;
-      if (s < 0) s += ST, ph ^= 1;
       float* sums = part + turn * (w4_ring_part(NT) / 8) + row * WK * (16 * 8 * NT);
       w4_few_put<NT>(sums + wk * (16 * 8 * NT), acc, g, t4);
       named_bar(1 + row, 32 * WK);
