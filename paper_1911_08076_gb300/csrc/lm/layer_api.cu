@@ -188,7 +188,7 @@ int run_w4_many(const W4Args& a, const W4Plan& p, const int* slots, cudaStream_t
   int room = kW4ManySmem - 1024 - 512 - w4_many_recv(p.bn, p.ks) - r.turn;
   r.stages = 3 * xb + 2 * cb <= room ? 3 : 2;
   room -= r.stages * xb;
-  r.slots = std::min(12, room / cb);
+  r.slots = w4_code_slots(room / cb);
   room -= r.slots * cb;
   r.stages += std::min(kW4Bars - r.stages, room / xb);
   if (r.slots < 2) return IFQ_EUNSUPPORTED;   // (128 columns in floats over a cluster: two of each)

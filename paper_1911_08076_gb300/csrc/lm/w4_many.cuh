@@ -48,6 +48,15 @@ constexpr int kW4Expand = 16, kW4Out = kW4Expand + 4, kW4Outs = 8, kW4ManyThread
 constexpr int kW4Bars = 8;         // barriers in turn: no fewer than stages of x or blocks of expanded weights
 constexpr int kW4AStages = 4, kW4ACol = 256;
 constexpr int kW4ManySmem = 232448;
+// Slots for blocks of codes where shared memory has room for `fit`.  The two sets of expanding warps take alternate blocks, and a
+// wait for a phase of a slot's barrier holds only where the block that had the slot before is known to have landed: it was the same
+// set's (an even number), or it is behind the block whose products the set has waited for, kW4AStages + 2 before.
+__host__ __device__ constexpr int w4_code_slots(int fit) {
+  const int n = fit < 12 ? fit : 12;
+  return n % 2 == 0 || n > kW4AStages + 2 ? n : n - 1;
+}
+static_assert(w4_code_slots(3) == 2 && w4_code_slots(5) == 4 && w4_code_slots(6) == 6 && w4_code_slots(7) == 7 && w4_code_slots(30) == 12,
+              "slots that alternate blocks may share");
 
 // a receive slot a rank: the owner's columns, 129 floats each
 __host__ __device__ constexpr int w4_many_recv(int bn, int ks) { return ks > 1 ? (bn + 8) * 129 * 4 : 0; }

@@ -73,3 +73,13 @@ def test_many_rows_of_a_gated_pair(m, k, group, dtype, act):
         assert first is None or torch.equal(out, first)
         first = out
     assert ifq.ifq_device_status() == ifq.IFQ_OK
+
+
+# Floats whose k is split, in parts of more than one chain: the fewest slots for codes beside the sums (two to six).  And the sizes
+# with seven and more.
+@pytest.mark.parametrize("m,n,k,group,out", [(128, 130, 16384, 128, "f32"), (128, 130, 16384, 64, "f32"), (128, 100, 16392, 32, "f32"),
+                                             (96, 130, 16384, 64, "f32"), (96, 250, 16384, 32, "f32"), (96, 130, 12296, 128, "f32"),
+                                             (80, 130, 16384, 128, "f32"), (112, 130, 16384, 64, "f32"), (120, 130, 13000, 128, "bf16"),
+                                             (128, 4000, 4096, 128, "f32"), (600, 2000, 9216, 128, "bf16"), (700, 2000, 4096, 64, "f32")])
+def test_many_rows_of_x(m, n, k, group, out):
+    exact_products(m, n, k, group, "bf16", out)
