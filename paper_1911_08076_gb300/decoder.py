@@ -196,8 +196,10 @@ class Weights4:
         ifq.ifq_w4_pack(self.desc, codes, scales, mins, self.packed)
 
     def _rows(self, x):
-        if x.dim() != 2 or x.dtype != self.dtype or x.shape[1] != self.k or x.stride(1) != 1 or x.stride(0) % 8:
-            raise ValueError(f"x is a [rows][{self.k}] tensor of {self.dtype}, rows a multiple of 8 elements apart")
+        # (rows that share their storage, as an expanded tensor's: a stride of 0 would mean dense)
+        if x.dim() != 2 or x.dtype != self.dtype or x.shape[1] != self.k or x.stride(1) != 1 or x.stride(0) % 8 or \
+                (x.shape[0] > 1 and x.stride(0) < self.k):
+            raise ValueError(f"x is a [rows][{self.k}] tensor of {self.dtype}, rows a multiple of 8 elements apart and of its own")
         return x.shape[0], x.stride(0) if x.shape[0] > 1 else 0
 
     def matmul(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
@@ -267,9 +269,9 @@ class Scores(NamedTuple):
 
 def token_scores(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0) -> Scores:
     """Scores of rows of logits [rows][vocab] at a temperature; tokens: int64 [rows]."""
-    if logits.dim() != 2 or logits.stride(1) != 1 or (tokens is not None and (
+    if logits.dim() != 2 or logits.stride(1) != 1 or (logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]) or (tokens is not None and (
             tokens.shape != logits.shape[:1] or tokens.dtype != torch.int64 or not tokens.is_contiguous())):
-        raise ValueError("logits are rows [rows][vocab], tokens a dense int64 tensor [rows]")
+        raise ValueError("logits are rows [rows][vocab] that share nothing, tokens a dense int64 tensor [rows]")
     rows, vocab = logits.shape
     new = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device=logits.device)   # noqa: E731
     s = Scores(None if tokens is None else new(rows), new(rows), new(rows), new(rows, top, t=torch.int64) if top else None,
