@@ -197,8 +197,8 @@ class Weights4:
 
     def _rows(self, x):
         # (rows that share their storage, as an expanded tensor's: a stride of 0 would mean dense)
-        if x.dim() != 2 or x.dtype != self.dtype or x.shape[1] != self.k or x.stride(1) != 1 or x.stride(0) % 8 or \
-                (x.shape[0] > 1 and x.stride(0) < self.k):
+        if x.dim() != 2 or x.dtype != self.dtype or x.shape[1] != self.k or x.stride(1) != 1 or \
+                (x.shape[0] > 1 and (x.stride(0) % 8 or x.stride(0) < self.k)):
             raise ValueError(f"x is a [rows][{self.k}] tensor of {self.dtype}, rows a multiple of 8 elements apart and of its own")
         return x.shape[0], x.stride(0) if x.shape[0] > 1 else 0
 

@@ -30,3 +30,12 @@ def test_expanded_rows_are_refused(calls):   # noqa: F811
     decoder.token_scores(torch.zeros(1, 50).expand(1, 50))
     w.matmul(x.expand(0, 40))
     assert [a[0].x_stride for n, a in calls if n == "ifq_w4_matmul"] == [0, 0] and calls[1][1][0].stride == 0
+
+
+def test_the_stride_of_one_row_does_not_matter(calls):   # noqa: F811
+    w = decoder.Weights4(torch.randn(24, 40), group=32)
+    wide = torch.zeros(6, 44, dtype=torch.bfloat16)
+    w.matmul(wide[:1, :40])
+    assert calls[-1][0] == "ifq_w4_matmul" and calls[-1][1][0].m == 1 and calls[-1][1][0].x_stride == 0
+    with pytest.raises(ValueError):
+        w.matmul(wide[:2, :40])
