@@ -162,6 +162,14 @@ class DecoderAttention:
         return self._product(context, self.w_out, self.s_out)
 
 
+def _check_devices(first, *others):
+    """ValueError unless all tensors (or None) are on one device, the current one: the calls take their addresses."""
+    device = first.device
+    if any(t is not None and t.device != device for t in others) or \
+            (device.type == "cuda" and device.index != torch.cuda.current_device()):
+        raise ValueError("all tensors are on one device, the current one")
+
+
 ACTS = {"silu": ifq.IFQ_ACT_SILU, "gelu": ifq.IFQ_ACT_GELU, "gelu_tanh": ifq.IFQ_ACT_GELU_TANH}
 
 
@@ -192,6 +200,7 @@ class Weights4:
         size = ifq.ifq_w4_bytes(self.desc)
         parts = [quantise_weights4(m, group, dtype) for m in matrices]
         codes, scales, mins = (torch.cat(p).contiguous() for p in zip(*parts))
+        _check_devices(codes)
         self.packed = torch.empty(size, dtype=torch.uint8, device=codes.device)
         ifq.ifq_w4_pack(self.desc, codes, scales, mins, self.packed)
 
@@ -200,6 +209,7 @@ class Weights4:
         if x.dim() != 2 or x.dtype != self.dtype or x.shape[1] != self.k or x.stride(1) != 1 or \
                 (x.shape[0] > 1 and (x.stride(0) % 8 or x.stride(0) < self.k)):
             raise ValueError(f"x is a [rows][{self.k}] tensor of {self.dtype}, rows a multiple of 8 elements apart and of its own")
+        _check_devices(x, self.packed)
         return x.shape[0], x.stride(0) if x.shape[0] > 1 else 0
 
     def matmul(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
@@ -208,6 +218,8 @@ class Weights4:
         out_dtype = out_dtype or self.dtype
         if residual is not None and (residual.shape != (rows, self.n) or residual.dtype != out_dtype or not residual.is_contiguous()):
             raise ValueError("residual is a dense tensor of the result's shape and type")
+        if residual is not None:
+            _check_devices(x, residual)
         out = torch.empty(rows, self.n, dtype=out_dtype, device=x.device)
         d = ifq.w4_desc(self.desc, rows, ifq.IFQ_F32 if out_dtype == torch.float32 else TYPES[out_dtype], 0, stride)
         ifq.ifq_w4_matmul(d, x, self.packed, out, residual)
@@ -226,6 +238,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual:
     if x.dim() != 2 or not x.is_contiguous() or weight.shape != x.shape[1:] or weight.dtype != x.dtype or not weight.is_contiguous() or \
             (residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype or not residual.is_contiguous())):
         raise ValueError("x and residual are dense [rows][dim] tensors, weight [dim], all of one type")
+    _check_devices(x, weight, residual)
     out, total = torch.empty_like(x), None if residual is None else torch.empty_like(x)
     ifq.ifq_rms_norm(ifq.norm_desc(x.shape[0], x.shape[1], TYPES[x.dtype], eps), x, residual, weight, total, out)
     return out if residual is None else (out, total)
@@ -272,6 +285,7 @@ def token_scores(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, to
     if logits.dim() != 2 or logits.stride(1) != 1 or (logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]) or (tokens is not None and (
             tokens.shape != logits.shape[:1] or tokens.dtype != torch.int64 or not tokens.is_contiguous())):
         raise ValueError("logits are rows [rows][vocab] that share nothing, tokens a dense int64 tensor [rows]")
+    _check_devices(logits, tokens)
     rows, vocab = logits.shape
     new = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device=logits.device)   # noqa: E731
     s = Scores(None if tokens is None else new(rows), new(rows), new(rows), new(rows, top, t=torch.int64) if top else None,

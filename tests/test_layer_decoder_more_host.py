@@ -39,3 +39,27 @@ def test_the_stride_of_one_row_does_not_matter(calls):   # noqa: F811
     assert calls[-1][0] == "ifq_w4_matmul" and calls[-1][1][0].m == 1 and calls[-1][1][0].x_stride == 0
     with pytest.raises(ValueError):
         w.matmul(wide[:2, :40])
+
+
+def test_tensors_of_other_devices_are_refused(calls, monkeypatch):   # noqa: F811
+    """The calls take addresses: one of another device than the current one, or of the host, is not the kernels' to read."""
+    w, pair = decoder.Weights4(torch.randn(24, 40), group=32), decoder.Weights4(torch.randn(24, 40), torch.randn(24, 40), group=32)
+    del calls[:]
+    x, weight, logits = torch.zeros(6, 40, dtype=torch.bfloat16), torch.ones(40, dtype=torch.bfloat16), torch.zeros(6, 50)
+    for call in (lambda: w.matmul(x.to("meta")), lambda: pair.gate(x.to("meta")),
+                 lambda: w.matmul(x, torch.zeros(6, 24, dtype=torch.bfloat16, device="meta")),
+                 lambda: decoder.rms_norm(x, weight.to("meta")), lambda: decoder.rms_norm(x, weight, 1e-5, x.to("meta")),
+                 lambda: decoder.token_scores(logits, torch.zeros(6, dtype=torch.int64, device="meta"))):
+        with pytest.raises(ValueError):
+            call()
+    assert calls == []
+
+    class On:
+        def __init__(self, device):
+            self.device = torch.device(device)
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    decoder._check_devices(On("cuda:1"), None, On("cuda:1"))
+    for bad in (("cuda:0", "cuda:0"), ("cuda:1", "cuda:0"), ("cuda:1", "cpu")):
+        with pytest.raises(ValueError):
+            decoder._check_devices(*map(On, bad))
