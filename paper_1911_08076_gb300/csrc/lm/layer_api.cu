@@ -447,7 +447,7 @@ int ifq_token_scores(const ifq_scores_desc* d, const void* logits, const int64_t
   a.vocab = d->vocab;
   a.top = top_ids || top_logprobs ? d->top : 0;
   a.scale = d->scale;
-  a.c = (float)(d->scale * 1.4426950408889634);
+  a.c = (float)(d->scale * 2.8853900817779268);
   switch (d->dtype) {
     case IFQ_F16: return run_scores<IFQ_F16>(a, S(stream));
     case IFQ_BF16: return run_scores<IFQ_BF16>(a, S(stream));

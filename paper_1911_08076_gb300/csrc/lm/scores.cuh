@@ -28,7 +28,7 @@ struct ScoresArgs {
   long long stride;
   int rows, vocab, top;
   int parts;            // blocks (of a cluster) a row
-  float scale, c;       // c = scale / ln 2
+  float scale, c;       // c = 2 scale / ln 2
 };
 
 template <int TYPE>
@@ -54,8 +54,9 @@ __device__ __forceinline__ float key_logit(uint64_t k) {
 
 constexpr int kScoreThreads = 512, kScoreList = 1024, kScoreDeep = 4;
 
-// A row's sums are relative to its largest logit: of 2^d with d = (x - top) c, c = scale / ln 2, and of 2^d d.  The difference
-// is taken before the product, so that large logits cost no digits.
+// A row's sums are relative to its largest logit: of 2^d with d = (x - top) scale / ln 2, and of 2^d d.  The difference
+// is taken before the product, so that large logits cost no digits, and of halves, x / 2 - top / 2 with one rounding, which no
+// two floats take past the type's end; c = 2 scale / ln 2.
 struct RowSums {
   float top;        // NaN where there is one, -infinity before any
   float sum, weighted;
@@ -66,7 +67,7 @@ __device__ __forceinline__ float exp2_of(float x) {
   return y;
 }
 __device__ __forceinline__ void move_to(RowSums& r, float top, float c) {
-  const float d = fmaxf((r.top - top) * c, -1000.0f), f = exp2_of(d);
+  const float d = fmaxf(fmaf(r.top, 0.5f, -0.5f * top) * c, -1000.0f), f = exp2_of(d);
   r.weighted = f * fmaf(r.sum, d, r.weighted);
   r.sum *= f;
   r.top = top;
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
     }
     if (top != r.top) move_to(r, top, c);
     if (top == -INFINITY) return;
-    const uint64_t down = two(-top, -top);
+    const uint64_t half = two(0.5f, 0.5f), down = two(-0.5f * top, -0.5f * top);
     uint64_t sum = two(r.sum, 0.0f), weighted = two(r.weighted, 0.0f);
 #pragma unroll
     for (int u = 0; u < V; ++u) {
@@ -226,7 +227,7 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
 #pragma unroll
       for (int j = 0; j < N; j += 2) {
         // (at least -1000: a masked logit's share of 0 times its distance, -infinity, would be no number)
-        float2 d = apart(mul2(add2(two(x[j], x[j + 1]), down), c2));
+        float2 d = apart(mul2(fma2(two(x[j], x[j + 1]), half, down), c2));
         d.x = fmaxf(d.x, -1000.0f);
         d.y = fmaxf(d.y, -1000.0f);
         const uint64_t e = two(exp2_of(d.x), exp2_of(d.y));
@@ -424,7 +425,7 @@ __global__ void __launch_bounds__(kScoreThreads, BLOCKS) token_scores_kernel(con
   r = part_sums[0];
   const float log2_sum = log2f(r.sum), log_sum = 0.69314718055994531f * log2_sum;
   auto logprob = [&](float x) {
-    return r.top == -INFINITY ? r.top : (x - r.top) * a.scale - (r.top == INFINITY ? 0.0f : log_sum);
+    return r.top == -INFINITY ? r.top : fmaf(x, 0.5f, -0.5f * r.top) * (2.0f * a.scale) - (r.top == INFINITY ? 0.0f : log_sum);
   };
   if (tid == 0) {
     if (a.lse) a.lse[row] = fabsf(r.top) == INFINITY ? r.top : fmaf(r.top, a.scale, log_sum);

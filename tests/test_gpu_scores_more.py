@@ -5,7 +5,7 @@ import torch
 
 import layer_reference as R
 from paper_1911_08076_gb300 import ifq
-from test_gpu_scores import TYPES, draw
+from test_gpu_scores import TYPES, check, draw, run
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,19 @@ def test_split_rows_beside_another_stream(rows, vocab, dtype, top):
         assert all(torch.equal(a, b) for a, b in zip(o, got[0]))
     assert (np.abs(got[0][1].cpu().numpy() - want["lse"]) <= tol).all()
     assert (np.abs(got[0][4].cpu().numpy() - want["top_logprobs"]) <= tol[:, None]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,top", [(300, 5), (70001, 8)])
+@pytest.mark.parametrize("scale", [1e-38, 2.0 ** -127, 1e-37])
+def test_logits_farther_apart_than_a_float_holds(vocab, top, dtype, scale):
+    """Differences of logits past 2^128, which a small scale brings back into range."""
+    rng = np.random.default_rng(vocab)
+    logits = rng.uniform(-3.38e38, 3.38e38, (5, vocab))
+    logits[1] = np.where(rng.random(vocab) < 0.9, -3.38e38, 3e38)
+    logits[2], logits[2, vocab // 2] = -3.38e38, 3.38e38
+    logits[3, ::3] = -np.inf
+    logits[4] = rng.normal(size=vocab) * 1e37
+    logits = R.round_to(logits, dtype)
+    tokens = rng.integers(0, vocab, 5)
+    check(logits, tokens, dtype, top, scale, run(logits, tokens, dtype, top, scale))
