@@ -788,7 +788,8 @@ int ifq_w4_matmul(const ifq_w4_desc* d, const void* x, const void* packed, void*
 /*
  * ifq_w4_gated -- out[i][j] = act(sum x[i][c] * w[j][c]) * sum x[i][c] * w[n+j][c]:
  * both projections of a gated feed-forward block, the activation and the product
- * in one launch, with sums as above, act in single precision, and one rounding.
+ * in one launch, with sums as above, act in single precision (what is below
+ * 2^-126 there may be 0), and one rounding.
  *   IFQ_ACT_SILU: a / (1 + e^-a);  IFQ_ACT_GELU: a * (1 + erf(a / sqrt 2)) / 2;
  *   IFQ_ACT_GELU_TANH: a * (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2.
  * weights.gated is 1, out_dtype the weights' dtype.  residual_stride is not read.
@@ -809,9 +810,11 @@ typedef struct {
 
 /*
  * ifq_rms_norm -- out = h * weight / sqrt(mean(h * h) + eps), with h = x, or with
- * a residual h = x + residual rounded to dtype, which is written to sum (may be
- * NULL).  Squares and their sum in single precision (in double where they leave
- * its range), out rounded once.  weight (device): dtype [dim].  sum and out may
+ * a residual h = x + residual, added in single precision and rounded to dtype,
+ * which is written to sum (may be NULL).  Squares and their sum in single
+ * precision (in double where they leave its range), h / sqrt(...) and its product
+ * with weight in single precision too (where the first is below 2^-126 it has
+ * fewer digits), out rounded to dtype.  weight (device): dtype [dim].  sum and out may
  * each be x or residual, where the strides agree, but not the same buffer.
  * Without a residual sum is NULL.
  * rows may be 0.  Pointers are 16-byte aligned.

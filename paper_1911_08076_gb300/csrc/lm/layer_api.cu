@@ -267,7 +267,9 @@ int run_w4(const ifq_w4_desc* d, W4Args& a, size_t bytes, const void* x, const v
     const auto run = [&](auto pair) {
       constexpr bool GATED = decltype(pair)::value;
       // Few rows, whose x fits shared memory.  (16 against 17 rows, the first of the tiles: 4096 x 4096 7.4 and 9.5 us,
-      // 6144 x 4096 10.3 and 12.0, gated 9216 x 4096 15.7 and 15.4; four tiles of 8 rows would take 20 there.)
+      // 6144 x 4096 10.3 and 12.0, gated 9216 x 4096 15.7 and 15.4; four tiles of 8 rows would take 20 there.  On either side of
+      // what fits, 4096 rows of w: 16 rows of x with k = 6144 10.9 us, with 6272 10.8; 8 rows with 13312 14.6, with 13568 15.8; 3 rows
+      // with 32768 24.2, with 36864 31.8.)
       if (a.m <= 8 && w4_few_smem(a.m, a.kb, 1) <= kW4ManySmem) return run_w4_few<BF, G, GATED, 1>(a, st);
       if (a.m <= kW4FewRows && w4_few_smem(a.m, a.kb, 2) <= kW4ManySmem) return run_w4_few<BF, G, GATED, 2>(a, st);
       return run_w4_tiles<BF, G, GATED>(a, st);

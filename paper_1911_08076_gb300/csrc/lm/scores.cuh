@@ -1,6 +1,6 @@
 // Scores of tokens: log probabilities, log-sum-exp, entropy and the likeliest tokens of rows of logits.
 //
-// 98 us, 5.5 TB/s (81 % of a copy) for 2048 x 131072 in bfloat16 with 8 tokens, 88 without; one row takes 6.7 us, 13 000 cycles of steps that
+// 97 us, 5.5 TB/s (82 % of a copy) for 2048 x 131072 in bfloat16 with 8 tokens, 88 without; one row takes 6.7 us, 13 000 cycles of steps that
 // wait for each other.
 //
 // One pass over a row: a thread keeps its largest logit, the sum of e^(z - that) and the sum of e^(z - that) (z - that), and

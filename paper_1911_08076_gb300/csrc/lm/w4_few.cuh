@@ -5,9 +5,9 @@
 // a row block's WK warps meet in shared memory and are added in order.  Row blocks go round the blocks of the grid.
 // A warp has four blocks of 128 columns under way, 70 KB an SM, whatever row block they belong to.
 //
-// What bounds it is the expansion: 88 of some 170 warp instructions for a block of 16 x 128, half of them on the integer pipe
-// (58 % busy over all, issue slots 65 %).  1 x 4096 x 4096 takes 4.2 us in a row of calls, where a call alone is 4; 8 x 131072 x 4096 in
-// the second form 61 us, 5.0 TB/s (74 % of a copy).
+// The expansion is 88 of some 167 warp instructions for a block of 16 x 128, half of them on the integer pipe (59 % busy
+// over all, issue slots 60 %; the rest are waits).  1 x 4096 x 4096 takes 4.2 us in a row of calls, where a call alone is 4;
+// 8 x 131072 x 4096 in the second form 63 us, 4.85 TB/s (71 % of a copy).
 //
 // x stands in shared memory as operands: of every 32 columns, the 16 bytes of lane t of a quad are its registers of two
 // steps, and rows begin 64 bytes apart modulo 128, so that eight lanes read all banks once.
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(32 * kW4FewWarps, 1) w4_few_kernel(const __gri
   const int rows = first < r.blocks ? (r.blocks - first + step - 1) / step : 0;
   const int total = rows * nk;
   // While the kernel before this one ends, the first blocks come as far as L2, which has them right whoever writes them
-  // (1 x 4096 x 4096 in a row of calls: 5.1 -> 4.4 us).
+  // (1 x 4096 x 4096 in a row of calls: 5.1 -> 4.2 us).
   if (rows && lane < (WB + 127) / 128)
     for (int u = 0; u < min(nk, P); ++u)
       asm volatile("prefetch.global.L2 [%0];" ::"l"(a.w + w4_place(first, k0 + u, a.kb) * WB + min(128 * lane, WB - 16)));

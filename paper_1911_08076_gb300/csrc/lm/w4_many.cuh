@@ -18,8 +18,8 @@
 // memory, in single precision, beside the next chain's products.
 // Where bn > 128 results are of 16 bits, and leave through shared memory: the accumulator is free again after some 4000 cycles.
 //
-// Measured: 4096 x 4096 x 9216 in 187 us, 1.66 PFLOP/s, gated 2048 x 9216 x 4096 in 181, 1.71 (a library product of bfloat16: 1.86 in a
-// burst, 1.70 for long); one SM a tile took 277.  With few columns a block of 128 of k takes 600 cycles whatever bn is.
+// Measured: 4096 x 4096 x 9216 in 186 to 193 us from card to card, 1.66 to 1.60 PFLOP/s, gated 2048 x 9216 x 4096 in 178 to 187, 1.74 to 1.65
+// (a library product of bfloat16: 1.86 in a burst, 1.70 for long); one SM a tile took 277.  With few columns a block of 128 of k takes 600 cycles whatever bn is.
 //
 // Warps: sixteen that expand (a quadrant of 32 lanes, half of the columns of every other block of k each), two that load,
 // one that issues MMAs, eight that take results out.
